@@ -244,8 +244,8 @@ gpo_status gpo_compute_host(gpo_ctx* ctx, const gpo_batch* host, const gpo_batch
                             void* stream);
 
 /* Waits for `stream` and returns the first error the kernels of the last
- * gpo_compute (or of the gpo_compute_groups calls since the last clearing one)
- * on this context reported (GPO_OK if none). */
+ * gpo_compute (or of the gpo_compute_groups calls since the last clearing one), or of
+ * the last other call that enqueues work, on this context reported (GPO_OK if none). */
 gpo_status gpo_sync_status(gpo_ctx* ctx, void* stream);
 
 /* Static description of a status code. */
@@ -335,8 +335,8 @@ gpo_status gpo_layer_budget(gpo_ctx* ctx, const gpo_batch* batch, int32_t layer,
  * G' = groups with at least one state, |E_g| = the states of group g (one direct
  * edge enters each state), |e| = step_len of the edge's state, e the edge holding
  * token t in the batch's token layout (that of gpo_compute's per-token outputs).
- * The entropy bonus of Algorithm S.1 needs the whole vocabulary distribution and
- * is left to the caller.
+ * The entropy bonus of Algorithm S.1 needs the whole vocabulary distribution: its terms and
+ * their gradient come from gpo_vocab_logp and gpo_vocab_grad, its weight from the caller.
  */
 typedef enum { GPO_LOSS_DUAL = 0, GPO_LOSS_SPLIT = 1 } gpo_loss_form;
 typedef enum { GPO_LOSS_NORM_EDGE = 0, GPO_LOSS_NORM_TOKEN = 1 } gpo_loss_norm;
@@ -388,6 +388,106 @@ gpo_status gpo_loss_plan(gpo_ctx* ctx, const gpo_batch* batch, void* plan, size_
  * (GPO_ERR_UNSUPPORTED), plan size. */
 gpo_status gpo_token_loss(gpo_ctx* ctx, const gpo_batch* batch, void* plan, const gpo_loss_params* params,
                           const gpo_loss_inputs* in, const gpo_loss_outputs* out, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The vocabulary ends of the policy model (GraphPO trains a language model with the loss
+ * above; the paper has no counterpart of these calls): per-token log-probabilities and
+ * entropies from hidden states and the vocabulary matrix, the gradients of both, the token
+ * embedding and the gradient of its table.
+ *
+ *   z[t][v] = scale <hidden_t, weight_v>          lse_t = log sum_v exp z[t][v]
+ *   logp_t = z[t][target_t] - lse_t               (gpo_loss_inputs.logp, old_logp, ref_logp)
+ *   entropy_t = lse_t - sum_v p[t][v] z[t][v]     p[t][v] = exp(z[t][v] - lse_t)
+ *   dz[t][v] = grad_logp_t (1[v = target_t] - p[t][v])
+ *              - grad_entropy_t p[t][v] (z[t][v] - lse_t + entropy_t)
+ *   d_hidden_t = scale sum_v dz[t][v] weight_v    d_weight_v = scale sum_t dz[t][v] hidden_t
+ *
+ * The [T x V] logits are never stored: the forward pass keeps a running maximum and sum per
+ * tile of the vocabulary, the gradient computes them again, a piece of the vocabulary at a
+ * time.  Products of bf16 or fp16 operands, accumulated in fp32; maxima, sums and entropies in
+ * fp32; dz is rounded to the operands' type before its products, as the gradients are after
+ * them.  Results do not depend on the launch and are the same on every run.
+ *
+ * A target below 0 means no token (a prompt, tool output, padding): its outputs are 0, it has no
+ * gradient, and its hidden row (NaN, say) reaches no other result.  Nor does the row of a token
+ * whose incoming gradients are all 0: it counts as a token without a gradient.  A target >= vocab is
+ * reported by gpo_sync_status (GPO_ERR_SHAPE); the outputs are then undefined.
+ */
+typedef enum { GPO_DT_BF16 = 0, GPO_DT_F32 = 1, GPO_DT_F16 = 2 } gpo_dtype;
+
+typedef struct {
+  int64_t num_tokens;    /* T >= 0 */
+  int64_t vocab;         /* V >= 1 */
+  int64_t d;             /* width >= 1 */
+  int64_t hidden_stride; /* elements between rows, >= d; row bytes must be a multiple of 16 */
+  int64_t weight_stride; /* the same of the vocabulary matrix */
+  const void* hidden;    /* [T x hidden_stride], 16-byte aligned */
+  const void* weight;    /* [V x weight_stride], 16-byte aligned */
+  const void* target;    /* [T] int32 or int64 */
+  int32_t dtype;         /* of hidden, weight and their gradients: GPO_DT_BF16 or GPO_DT_F16 */
+  int32_t id_bytes;      /* bytes of one target: 4 or 8 */
+  double scale;          /* in [1e-4, 1e4]: 1 / temperature */
+} gpo_vocab;
+
+typedef struct {
+  float* logp;     /* [T] required */
+  float* lse;      /* [T] optional (the gradient needs it) */
+  float* entropy;  /* [T] optional */
+} gpo_vocab_outputs;
+
+typedef struct {
+  const float* lse;          /* [T] of the forward pass */
+  const float* grad_logp;    /* [T] d loss / d logp (gpo_loss_outputs.grad_logp) */
+  const float* entropy;      /* [T] of the forward pass; read only with grad_entropy */
+  const float* grad_entropy; /* [T] optional: d loss / d entropy */
+} gpo_vocab_grad_inputs;
+
+typedef struct {
+  void* d_hidden;          /* [T x d_hidden_stride] optional, overwritten */
+  void* d_weight;          /* [V x d_weight_stride] optional */
+  int64_t d_hidden_stride; /* >= d */
+  int64_t d_weight_stride; /* >= d */
+  int32_t accumulate;      /* d_weight: 0 overwritten, else the gradient is added to what it holds
+                              (one rounding to its type per call) */
+} gpo_vocab_grads;
+
+/* Workspace bytes of gpo_vocab_logp (gradient = 0) or gpo_vocab_grad (gradient != 0) for these sizes;
+ * reads sizes only and needs no device. */
+gpo_status gpo_vocab_workspace_size(const gpo_vocab* v, int gradient, size_t* bytes);
+
+/* Enqueues the forward pass on `stream`.  Host-checked as for gpo_compute: sizes, NULL
+ * pointers, alignment (GPO_ERR_UNSUPPORTED), the workspace (256-byte aligned). */
+gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outputs* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Enqueues the gradients on `stream`.  At least one of d_hidden and d_weight must be given (for
+ * T = 0: d_weight alone has anything to write). */
+gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const gpo_vocab_grads* out,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
+/* Token embedding: out_t = scale table[id_t], rounded once to the table's type; a row of zeros for
+ * an id below 0 (no token); an id >= vocab is reported as for targets.
+ * Its gradient: d_table_v = scale sum_{t: id_t = v} grad_t, the tokens of a row added in their
+ * order in fp32 (in pieces of 32 of the tokens sorted by id, so that a frequent token's sum is
+ * spread over the GPU): the same result on every run.  Rows without tokens are zeros, or keep
+ * what they hold with accumulate (a table tied to the vocabulary matrix: gpo_vocab_grads.d_weight). */
+typedef struct {
+  int64_t num_tokens;   /* T >= 0 */
+  int64_t vocab;        /* V >= 1 */
+  int64_t d;            /* width >= 1 */
+  int64_t table_stride; /* elements between rows of the table (gradient: of d_table), >= d */
+  int64_t row_stride;   /* elements between rows of the output (gradient: of grad), >= d */
+  const void* ids;      /* [T] int32 or int64 */
+  int32_t dtype;        /* gpo_dtype of table and rows */
+  int32_t id_bytes;     /* bytes of one id: 4 or 8 */
+  double scale;         /* finite */
+} gpo_embedding;
+
+gpo_status gpo_embed_workspace_size(const gpo_embedding* e, int gradient, size_t* bytes);
+gpo_status gpo_embed(gpo_ctx* ctx, const gpo_embedding* e, const void* table, void* out, void* workspace,
+                     size_t workspace_bytes, void* stream);
+gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad, void* d_table, int accumulate,
+                          void* workspace, size_t workspace_bytes, void* stream);
 
 /* Library version string. */
 const char* gpo_version(void);

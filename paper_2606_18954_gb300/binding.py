@@ -77,6 +77,32 @@ class LossOutputs(ctypes.Structure):
     _fields_ = [("loss", ctypes.c_void_p), ("grad_logp", ctypes.c_void_p), ("stats", ctypes.c_void_p)]
 
 
+class CVocab(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("hidden_stride", ctypes.c_int64), ("weight_stride", ctypes.c_int64), ("hidden", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("target", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("id_bytes", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class VocabOutputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("logp", "lse", "entropy")]
+
+
+class VocabGradInputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "grad_logp", "entropy", "grad_entropy")]
+
+
+class VocabGrads(ctypes.Structure):
+    _fields_ = [("d_hidden", ctypes.c_void_p), ("d_weight", ctypes.c_void_p), ("d_hidden_stride", ctypes.c_int64),
+                ("d_weight_stride", ctypes.c_int64), ("accumulate", ctypes.c_int32)]
+
+
+class CEmbedding(ctypes.Structure):
+    _fields_ = [("num_tokens", ctypes.c_int64), ("vocab", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("table_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64), ("ids", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
 LOSS_FORMS = {"dual": 0, "split": 1}
 LOSS_NORMS = {"edge": 0, "token": 1}
 LOSS_NSTATS = 4
@@ -84,7 +110,8 @@ LOSS_NSTATS = 4
 EXPORTS = ["gpo_create", "gpo_workspace_size", "gpo_compute", "gpo_sync_status", "gpo_status_string",
            "gpo_last_error", "gpo_version", "gpo_destroy", "gpo_enable_timing", "gpo_stage_times", "gpo_compute_noalloc",
            "gpo_compute_groups", "gpo_compute_host", "gpo_loss_plan_size", "gpo_loss_plan", "gpo_token_loss",
-           "gpo_layer_budget"]
+           "gpo_layer_budget", "gpo_vocab_workspace_size", "gpo_vocab_logp", "gpo_vocab_grad",
+           "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad"]
 
 FUSED_MAX_STATES = 384  # largest group the group-resident path (and gpo_compute_groups) serves
 
@@ -156,6 +183,20 @@ def load(build_if_missing: bool = False):
                                      ctypes.POINTER(LossParams), ctypes.POINTER(LossInputs),
                                      ctypes.POINTER(LossOutputs), ctypes.c_void_p]
         L.gpo_token_loss.restype = ctypes.c_int
+        vp, sz = ctypes.c_void_p, ctypes.c_size_t
+        L.gpo_vocab_workspace_size.argtypes = [ctypes.POINTER(CVocab), ctypes.c_int, ctypes.POINTER(sz)]
+        L.gpo_vocab_workspace_size.restype = ctypes.c_int
+        L.gpo_vocab_logp.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(VocabOutputs), vp, sz, vp]
+        L.gpo_vocab_logp.restype = ctypes.c_int
+        L.gpo_vocab_grad.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(VocabGradInputs),
+                                     ctypes.POINTER(VocabGrads), vp, sz, vp]
+        L.gpo_vocab_grad.restype = ctypes.c_int
+        L.gpo_embed_workspace_size.argtypes = [ctypes.POINTER(CEmbedding), ctypes.c_int, ctypes.POINTER(sz)]
+        L.gpo_embed_workspace_size.restype = ctypes.c_int
+        L.gpo_embed.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, vp, sz, vp]
+        L.gpo_embed.restype = ctypes.c_int
+        L.gpo_embed_grad.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, ctypes.c_int, vp, sz, vp]
+        L.gpo_embed_grad.restype = ctypes.c_int
         _lib = L
         return L
 
@@ -182,6 +223,60 @@ def loss_plan_size(batch) -> int:
     if code != GPO_OK:
         raise GraphPOError(code, "gpo_loss_plan_size")
     return n.value
+
+
+def vocab_workspace_size(v: CVocab, gradient: bool = False) -> int:
+    """Device workspace bytes of gpo_vocab_logp, or with `gradient` of gpo_vocab_grad, for these
+    sizes (no device needed)."""
+    n = ctypes.c_size_t()
+    code = load().gpo_vocab_workspace_size(ctypes.byref(v), int(gradient), ctypes.byref(n))
+    if code != GPO_OK:
+        raise GraphPOError(code, "gpo_vocab_workspace_size")
+    return n.value
+
+
+def embed_workspace_size(e: CEmbedding, gradient: bool = False) -> int:
+    """Device workspace bytes of gpo_embed, or with `gradient` of gpo_embed_grad, for these sizes
+    (no device needed)."""
+    n = ctypes.c_size_t()
+    code = load().gpo_embed_workspace_size(ctypes.byref(e), int(gradient), ctypes.byref(n))
+    if code != GPO_OK:
+        raise GraphPOError(code, "gpo_embed_workspace_size")
+    return n.value
+
+
+def _dtype_code(t, what: str) -> int:
+    import torch
+    code = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what} must be bfloat16, float16 or float32, not {t.dtype}")
+    return code
+
+
+def _matrix(t, what: str, dev, rows=None, cols=None, dtype=None) -> int:
+    """Checks a [rows, cols] device matrix with unit inner stride; returns its row stride."""
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{what} must be [{'rows' if rows is None else rows}, {'d' if cols is None else cols}], "
+                         f"not {tuple(t.shape)}")
+    if t.device != dev:
+        raise ValueError(f"{what} is on {t.device}, not {dev}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    st, one = t.stride()
+    if one != 1 and t.shape[1] > 1 and t.shape[0] > 0:
+        raise ValueError(f"{what} must have unit inner stride")
+    return st if t.shape[0] > 1 else max(st, t.shape[1])
+
+
+def _vector(t, what: str, dev, n: int, dtypes) -> int:
+    """Checks a contiguous device vector of n elements; returns its address (None if empty)."""
+    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what} must be a contiguous vector of {n} elements")
+    if t.device != dev:
+        raise ValueError(f"{what} is on {t.device}, not {dev}")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    return t.data_ptr() or None
 
 
 def _ptr(t) -> Optional[int]:
@@ -478,6 +573,131 @@ class GraphPO:
         cb = batch.c_struct()
         code = self._lib.gpo_token_loss(self._h, ctypes.byref(cb), plan.data_ptr(), ctypes.byref(lp),
                                         ctypes.byref(li), ctypes.byref(lo), _raw_stream(stream, dev))
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    # ---- the model's vocabulary ends (gpo_vocab_logp / gpo_vocab_grad, gpo_embed / gpo_embed_grad)
+
+    def _room(self, need: int, dev):
+        """The context's workspace, at least `need` bytes on `dev`."""
+        import torch
+        if self._ws is None or self._ws.numel() < need or self._ws.device != dev:
+            self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        return self._ws
+
+    @staticmethod
+    def _vocab(hidden, weight, target, scale) -> CVocab:
+        import torch
+        dev = hidden.device
+        hs = _matrix(hidden, "hidden", dev)
+        ws = _matrix(weight, "weight", dev, cols=hidden.shape[1], dtype=hidden.dtype)
+        tp = _vector(target, "target", dev, hidden.shape[0], (torch.int32, torch.int64))
+        return CVocab(hidden.shape[0], weight.shape[0], weight.shape[1], hs, ws, hidden.data_ptr() or None,
+                      weight.data_ptr() or None, tp, _dtype_code(hidden, "hidden"), target.element_size(), float(scale))
+
+    def vocab_logp(self, hidden, weight, target, scale=1.0, lse=True, entropy=False, out=None, workspace=None,
+                   stream=None) -> dict:
+        """Log-probabilities of `target` (int32 or int64 [T]; below 0: no token, outputs 0) under
+        softmax(scale * hidden weight^T), hidden [T, d] and weight [V, d] both bfloat16 or both
+        float16: {"logp": [T] float32, "lse": the log-sum-exp (if lse; vocab_grad takes it),
+        "entropy" (if entropy)}, or fills `out`.  The logits are never stored.  Enqueued on the
+        current stream; `check()` raises on a target outside the vocabulary."""
+        import torch
+        v = self._vocab(hidden, weight, target, scale)
+        dev, T = hidden.device, hidden.shape[0]
+        if out is None:
+            out = {"logp": _empty(T, torch.float32, dev)}
+            if lse:
+                out["lse"] = _empty(T, torch.float32, dev)
+            if entropy:
+                out["entropy"] = _empty(T, torch.float32, dev)
+        f32 = (torch.float32,)
+        vo = VocabOutputs(*[None if out.get(k) is None else _vector(out[k], k, dev, T, f32)
+                            for k in ("logp", "lse", "entropy")])
+        ws = self._room(vocab_workspace_size(v), dev) if workspace is None else workspace
+        code = self._lib.gpo_vocab_logp(self._h, ctypes.byref(v), ctypes.byref(vo), ws.data_ptr(), ws.numel(),
+                                        _raw_stream(stream, dev))
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def vocab_grad(self, hidden, weight, target, lse, grad_logp, scale=1.0, entropy=None, grad_entropy=None,
+                   accumulate=False, d_hidden=True, d_weight=True, out=None, workspace=None, stream=None) -> dict:
+        """Gradients {"d_hidden": [T, d], "d_weight": [V, d]} (each if asked for) of a loss with the
+        gradients grad_logp (e.g. token_loss's) and optionally grad_entropy [T] float32 with respect to
+        vocab_logp's outputs, whose lse (and entropy) are given; or fills `out`, with `accumulate`
+        adding to out["d_weight"].  Enqueued on the current stream."""
+        import torch
+        v = self._vocab(hidden, weight, target, scale)
+        dev, T = hidden.device, hidden.shape[0]
+        if out is None:
+            if accumulate and d_weight:
+                raise ValueError("accumulate needs the d_weight to add to in `out`")
+            out = {}
+            if d_hidden:
+                out["d_hidden"] = torch.empty(T, hidden.shape[1], dtype=hidden.dtype, device=dev)
+            if d_weight:
+                out["d_weight"] = torch.empty(weight.shape, dtype=weight.dtype, device=dev)
+        f32 = (torch.float32,)
+        if grad_entropy is not None and entropy is None:
+            raise ValueError("grad_entropy needs vocab_logp's entropy")
+        gi = VocabGradInputs(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
+                             None if grad_entropy is None else _vector(entropy, "entropy", dev, T, f32),
+                             None if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32))
+        dh, dw = out.get("d_hidden"), out.get("d_weight")
+        go = VocabGrads(None, None, 0, 0, int(bool(accumulate)))
+        if dh is not None:
+            go.d_hidden_stride = _matrix(dh, "d_hidden", dev, T, v.d, hidden.dtype)
+            go.d_hidden = dh.data_ptr() or None
+        if dw is not None:
+            go.d_weight_stride = _matrix(dw, "d_weight", dev, v.vocab, v.d, hidden.dtype)
+            go.d_weight = dw.data_ptr() or None
+        if T == 0 and dw is None:
+            return out
+        ws = self._room(vocab_workspace_size(v, True), dev) if workspace is None else workspace
+        code = self._lib.gpo_vocab_grad(self._h, ctypes.byref(v), ctypes.byref(gi), ctypes.byref(go), ws.data_ptr(),
+                                        ws.numel(), _raw_stream(stream, dev))
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def embed(self, table, ids, scale=1.0, out=None, workspace=None, stream=None):
+        """Rows of `table` ([V, d] bfloat16, float16 or float32) by token id (int32 or int64 [T]; below
+        0: a row of zeros), times `scale`: [T, d] of the table's type.  Enqueued on the current stream."""
+        import torch
+        dev, T = table.device, ids.shape[0]
+        ts = _matrix(table, "table", dev)
+        if out is None:
+            out = torch.empty(T, table.shape[1], dtype=table.dtype, device=dev)
+        rs = _matrix(out, "out", dev, T, table.shape[1], table.dtype)
+        e = CEmbedding(T, table.shape[0], table.shape[1], ts, rs, _vector(ids, "ids", dev, T, (torch.int32, torch.int64)),
+                       _dtype_code(table, "table"), ids.element_size(), float(scale))
+        ws = self._room(embed_workspace_size(e), dev) if workspace is None else workspace
+        code = self._lib.gpo_embed(self._h, ctypes.byref(e), table.data_ptr() or None, out.data_ptr() or None,
+                                   ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def embed_grad(self, grad, ids, vocab, scale=1.0, out=None, accumulate=False, workspace=None, stream=None):
+        """Gradient [vocab, d] of embed's table from the gradient of its output (grad [T, d]): rows of
+        one token added in token order in fp32, rows without tokens 0; or, with `accumulate`, added
+        to `out` (a table tied to the vocabulary matrix: vocab_grad's d_weight).  Enqueued on the
+        current stream."""
+        import torch
+        dev, T = grad.device, grad.shape[0]
+        rs = _matrix(grad, "grad", dev)
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs the gradient to add to in `out`")
+            out = torch.empty(int(vocab), grad.shape[1], dtype=grad.dtype, device=dev)
+        ts = _matrix(out, "out", dev, int(vocab), grad.shape[1], grad.dtype)
+        e = CEmbedding(T, int(vocab), grad.shape[1], ts, rs, _vector(ids, "ids", dev, T, (torch.int32, torch.int64)),
+                       _dtype_code(grad, "grad"), ids.element_size(), float(scale))
+        ws = self._room(embed_workspace_size(e, True), dev) if workspace is None else workspace
+        code = self._lib.gpo_embed_grad(self._h, ctypes.byref(e), grad.data_ptr() or None, out.data_ptr() or None,
+                                        int(bool(accumulate)), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out

@@ -14,38 +14,12 @@
 #include <mutex>
 
 #include <algorithm>
-#include <vector>
-
 #include <nvtx3/nvToolsExt.h>
 
-#include "gpo_internal.cuh"
+#include "gpo_ctx.cuh"
 #include "gpo_tag.cuh"
 
-struct gpo_ctx {
-  gpo_params params;
-  int device;
-  int num_sms;
-  uint32_t* host_status;      // pinned copy of the workspace status words
-  const uint32_t* last_status; // device status words of the last gpo_compute
-  char msg[512];
-  bool timing;
-  int nstages;                 // stages recorded by the last gpo_compute
-  cudaEvent_t ev[gpo::kMaxStages + 1];
-  const char* stage_name[gpo::kMaxStages];
-  // gpo_compute_host: helper streams and events (created by its first pipelined call) and
-  // the per-group state and token offsets of the last host batch
-  bool pipe_ready;
-  cudaStream_t pipe_in, pipe_out, pipe_comp[gpo::kPipeComputeStreams];
-  cudaEvent_t pipe_ev[2 * gpo::kPipeMaxChunks + 2];
-  std::vector<int64_t> pipe_s, pipe_t;
-};
-
 namespace gpo {
-namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 EncodeTiledFn encode_fn() {
   static EncodeTiledFn fn = nullptr;
@@ -69,8 +43,19 @@ void set_msg(gpo_ctx* c, const char* fmt, ...) {
   va_end(ap);
 }
 
-constexpr size_t kAlign = 256;
-inline size_t up(size_t x) { return (x + kAlign - 1) & ~(kAlign - 1); }
+// A tag that no other call of this process has.
+uint64_t fresh_tag() {
+  static std::atomic<uint64_t> calls{0};
+  while (true) {
+    const uint64_t t = tag_of(calls.fetch_add(1, std::memory_order_relaxed));
+    if (t != 0) return t;
+  }
+}
+
+namespace {
+
+constexpr size_t kAlign = kWorkspaceAlign;
+inline size_t up(size_t x) { return workspace_up(x); }
 
 int64_t max_blocks_for(int64_t N, int64_t G) { return N / 128 + G + 8; }  // sum of ceil(n/128)
 
@@ -166,8 +151,6 @@ gpo_status check_params(const gpo_params& p) {
     return GPO_ERR_INVALID_ARG;
   return GPO_OK;
 }
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 gpo_status check_batch(gpo_ctx* c, const gpo_batch* b) {
   if (!b) return set_msg(c, "batch is NULL"), GPO_ERR_INVALID_ARG;
@@ -276,7 +259,8 @@ gpo_status gpo_create(gpo_ctx** out, const gpo_params* params) {
   }
   if (setup_sim_tc() != cudaSuccess || setup_sim_simt() != cudaSuccess || setup_groups() != cudaSuccess || setup_fused() != cudaSuccess ||
       setup_fused_f32() != cudaSuccess ||
-      setup_tree_prep() != cudaSuccess || setup_loss() != cudaSuccess ||
+      setup_tree_prep() != cudaSuccess || setup_loss() != cudaSuccess || setup_vocab() != cudaSuccess ||
+      setup_embed() != cudaSuccess ||
       cudaMallocHost(&c->host_status, sizeof(uint32_t) * kStatusWords) != cudaSuccess) {
     cudaGetLastError();
     delete c;
@@ -313,15 +297,6 @@ gpo_status gpo_workspace_size(const gpo_ctx* ctx, const gpo_batch* batch, size_t
 }  // extern "C"
 
 namespace {
-
-// A tag that no other call of this process has.
-uint64_t fresh_tag() {
-  static std::atomic<uint64_t> calls{0};
-  while (true) {
-    const uint64_t t = tag_of(calls.fetch_add(1, std::memory_order_relaxed));
-    if (t != 0) return t;
-  }
-}
 
 // Fused path: whether the compensated statistics of the groups after each CTA's first come from a
 // launch on the whole GPU first (exact_stats, every row) or from the kernel, once a group's

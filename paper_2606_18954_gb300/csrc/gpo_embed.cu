@@ -1,0 +1,413 @@
+// Token embedding and the gradient of its table (formulas in include/graphpo.h).
+//
+//   embed      embed_kernel: a warp per token and 2 KB (fp32: 2 KB) of its row, 16-byte accesses,
+//              four in flight per lane
+//   gradient   embed_sort_kernel: a stable counting sort of the tokens by id without any exchange
+//              between CTAs.  Each CTA owns up to 1024 rows of the table and reads all ids twice
+//              from L2 (4 bytes a token, against the thousands of bytes of a token's gradient row): first
+//              it counts those of its rows, per warp and row, and those of the rows before its own, which
+//              gives its place in the sorted list; then every warp places its tokens in their order.
+//              embed_sum_kernel: the sorted tokens in pieces of equal length, a warp per piece and
+//              512 bytes of the rows: runs of one id are summed in order in fp32, a run inside the
+//              piece is a finished row, a run that the piece's ends cut leaves its sum in the
+//              workspace.  So the work does not depend on how often a token occurs.  Rows
+//              without tokens are zeroed by the same launch.
+//              embed_join_kernel: the sums of cut runs, added in order.
+// Every sum has a fixed order: the results are the same on every run.
+#define GPO_REPORT __noinline__
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gpo_internal.cuh"
+
+namespace gpo {
+
+namespace {
+
+template <int kType>
+struct Elem;
+template <>
+struct Elem<GPO_DT_F32> {
+  using T = float;
+  static constexpr int kPer = 4;  // per 16 bytes
+  static __device__ __forceinline__ float get(T x) { return x; }
+  static __device__ __forceinline__ T put(float x) { return x; }
+};
+template <>
+struct Elem<GPO_DT_BF16> {
+  using T = __nv_bfloat16;
+  static constexpr int kPer = 8;
+  static __device__ __forceinline__ float get(T x) { return __bfloat162float(x); }
+  static __device__ __forceinline__ T put(float x) { return __float2bfloat16_rn(x); }
+};
+template <>
+struct Elem<GPO_DT_F16> {
+  using T = __half;
+  static constexpr int kPer = 8;
+  static __device__ __forceinline__ float get(T x) { return __half2float(x); }
+  static __device__ __forceinline__ T put(float x) { return __float2half_rn(x); }
+};
+
+__device__ __forceinline__ int64_t id_of(const void* ids, int id8, int64_t t) {
+  return id8 ? static_cast<const int64_t*>(ids)[t] : (int64_t)static_cast<const int32_t*>(ids)[t];
+}
+
+// A lane's kPer columns of a block of 32 kPer: with 16-byte accesses (kVec) side by side, else 32 apart.
+template <int kType, bool kVec>
+struct Cols {
+  using E = Elem<kType>;
+  using T = typename E::T;
+  static constexpr int kPer = E::kPer;
+  static __device__ __forceinline__ int64_t at(int64_t block, int lane, int i) {
+    return block * 32 * kPer + (kVec ? lane * kPer + i : i * 32 + lane);
+  }
+  struct Raw {
+    uint4 v;
+  };
+  // (a row's last block may end inside a lane's 16 bytes: those columns one by one)
+  static __device__ __forceinline__ Raw load(const T* row, int64_t block, int lane, int64_t d) {
+    Raw r;
+    r.v = make_uint4(0u, 0u, 0u, 0u);
+    if (kVec && at(block, lane, kPer) <= d) {
+      r.v = __ldg(reinterpret_cast<const uint4*>(row + at(block, lane, 0)));
+    } else {
+      T* e = reinterpret_cast<T*>(&r.v);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (at(block, lane, i) < d) e[i] = row[at(block, lane, i)];
+    }
+    return r;
+  }
+  static __device__ __forceinline__ void add(const Raw& r, float (&s)[kPer]) {
+    const T* e = reinterpret_cast<const T*>(&r.v);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) s[i] += E::get(e[i]);
+  }
+  // row = scale s (+ what it holds)
+  static __device__ __forceinline__ void store(T* row, int64_t block, int lane, int64_t d, const float (&s)[kPer],
+                                               float scale, bool add) {
+    Raw r;
+    T* e = reinterpret_cast<T*>(&r.v);
+    const bool whole = kVec && at(block, lane, kPer) <= d;
+    if (add && whole) r.v = *reinterpret_cast<const uint4*>(row + at(block, lane, 0));
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int64_t c = at(block, lane, i);
+      if (add && !whole && c < d) e[i] = row[c];
+      e[i] = E::put(add ? fmaf(scale, s[i], E::get(e[i])) : scale * s[i]);
+    }
+    if (whole) *reinterpret_cast<uint4*>(row + at(block, lane, 0)) = r.v;
+    else
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (at(block, lane, i) < d) row[at(block, lane, i)] = e[i];
+  }
+};
+
+// ------------------------------------------------------------------ lookup
+
+constexpr int kLookBlocks = 4;  // column blocks (512 bytes each) of one step of a warp
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
+  using C = Cols<kType, kVec>;
+  using T = typename C::T;
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int64_t nwarps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  const int64_t blocks = (a.D + 32 * C::kPer - 1) / (32 * C::kPer);
+  const int64_t steps = (blocks + kLookBlocks - 1) / kLookBlocks;
+  for (int64_t it = warp; it < a.T * steps; it += nwarps) {
+    const int64_t t = it / steps, b0 = (it - t * steps) * kLookBlocks;
+    const int64_t id = id_of(a.ids, a.id8, t);
+    if (id >= a.V && lane == 0) report(st, GPO_ERR_SHAPE, 30, (int)t);
+    const bool in = id >= 0 && id < a.V;
+    const T* src = static_cast<const T*>(a.src) + (in ? id : 0) * a.src_stride;
+    T* dst = static_cast<T*>(a.dst) + t * a.dst_stride;
+    typename C::Raw r[kLookBlocks];
+#pragma unroll
+    for (int b = 0; b < kLookBlocks; ++b) {
+      if (in && b0 + b < blocks) r[b] = C::load(src, b0 + b, lane, a.D);
+      else r[b].v = make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int b = 0; b < kLookBlocks; ++b) {
+      if (b0 + b >= blocks) break;
+      float s[C::kPer];
+#pragma unroll
+      for (int i = 0; i < C::kPer; ++i) s[i] = 0.f;
+      C::add(r[b], s);
+      C::store(dst, b0 + b, lane, a.D, s, a.scale, false);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ sort
+
+constexpr int kSortThreads = 1024;
+constexpr int kSortWarps = kSortThreads / 32;
+
+size_t sort_smem(int rows) { return sizeof(int) * (size_t)(kSortWarps + 1) * rows; }
+
+// CTA b owns the rows [b * per, (b + 1) * per) of the table.
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedArgs a, int per, Status st) {
+  extern __shared__ int hist[];  // [kSortWarps][per] counts, then places; [per] first place of a row
+  __shared__ int wsum[kSortWarps];
+  __shared__ int s_base;
+  int* first = hist + kSortWarps * per;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t r0 = (int64_t)blockIdx.x * per, r1 = min(r0 + per, a.V);
+  const int nr = (int)(r1 - r0);
+  for (int i = threadIdx.x; i < kSortWarps * per; i += kSortThreads) hist[i] = 0;
+  if (threadIdx.x == 0) s_base = 0;
+  __syncthreads();
+  const int64_t seg = ((a.T + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
+  const int64_t ta = min(a.T, warp * seg), tb = min(a.T, ta + seg);
+  int below = 0;
+#pragma unroll 4
+  for (int64_t t = ta + lane; t < tb; t += 32) {
+    const int64_t id = id_of(a.ids, a.id8, t);
+    if (id >= r0 && id < r1) atomicAdd(&hist[warp * per + (int)(id - r0)], 1);
+    below += id >= 0 && id < r0;
+    if (id >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 31, (int)t);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) below += __shfl_xor_sync(0xffffffffu, below, o);
+  if (lane == 0) atomicAdd(&s_base, below);
+  __syncthreads();
+  // thread i: row r0 + i (per <= kSortThreads)
+  const int i = threadIdx.x;
+  int total = 0;
+  if (i < nr) {
+    for (int w = 0; w < kSortWarps; ++w) {
+      const int c = hist[w * per + i];
+      hist[w * per + i] = total;
+      total += c;
+    }
+  }
+  int incl = total;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) wsum[warp] = incl;
+  __syncthreads();
+  int before = s_base;
+  for (int w = 0; w < warp; ++w) before += wsum[w];
+  if (i < nr) {
+    const int s = before + incl - total;
+    first[i] = s;
+    a.start[r0 + i] = s;
+    if (r0 + i == a.V - 1) a.start[a.V] = s + total;
+  }
+  __syncthreads();
+  for (int64_t t0 = ta; t0 < tb; t0 += 32) {
+    const int64_t t = t0 + lane;
+    const int64_t id = t < tb ? id_of(a.ids, a.id8, t) : -1;
+    const bool in = id >= r0 && id < r1;
+    if (!__any_sync(0xffffffffu, in)) continue;
+    const int row = in ? (int)(id - r0) : -1 - lane;
+    const uint32_t same = __match_any_sync(0xffffffffu, row);
+    int at = 0;
+    if (in) at = hist[warp * per + row];
+    __syncwarp();
+    if (in) {
+      const int place = first[row] + at + __popc(same & ((1u << lane) - 1u));
+      a.perm[place] = (int)t;
+      a.sid[place] = (int)id;
+      if (lane == __ffs(same) - 1) hist[warp * per + row] = at + __popc(same);
+    }
+    __syncwarp();
+  }
+}
+
+// ------------------------------------------------------------------ sums of runs
+
+constexpr int kSumThreads = 256;
+constexpr int kSumAhead = 8;  // rows in flight per lane
+
+template <int kType, bool kVec>
+__global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int piece, Status st) {
+  using C = Cols<kType, kVec>;
+  using T = typename C::T;
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
+  const int64_t nwarps = (int64_t)gridDim.x * (kSumThreads / 32);
+  const int64_t blocks = (a.D + 32 * C::kPer - 1) / (32 * C::kPer);
+  const int n = a.start[a.V];
+  const int64_t pieces = ((int64_t)n + piece - 1) / piece;
+  const int64_t empties = a.accumulate ? 0 : (a.V + 31) / 32;  // groups of 32 rows that may have no token
+  T* out = static_cast<T*>(a.dst);
+  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  for (int64_t it = warp; it < (pieces + empties) * blocks; it += nwarps) {
+    const int64_t unit = it / blocks, b = it - unit * blocks;
+    float s[C::kPer];
+#pragma unroll
+    for (int i = 0; i < C::kPer; ++i) s[i] = 0.f;
+    if (unit >= pieces) {
+      const int64_t v = (unit - pieces) * 32 + lane;
+      uint32_t m = __ballot_sync(0xffffffffu, v < a.V && a.start[min(v, a.V - 1)] == a.start[min(v, a.V - 1) + 1]);
+      for (; m; m &= m - 1u)
+        C::store(out + ((unit - pieces) * 32 + __ffs(m) - 1) * a.dst_stride, b, lane, a.D, s, 1.f, false);
+      continue;
+    }
+    const int64_t p0 = unit * piece, p1 = min(p0 + piece, (int64_t)n);
+    int run = a.sid[p0];                                      // the id being summed
+    bool cut = p0 > 0 && a.sid[p0 - 1] == run;                // its run began before the piece
+    const int after = p1 < n ? a.sid[p1] : -1;
+    auto leave = [&](bool cut_after) {
+      if (cut || cut_after) {
+        float* part = a.part + (unit * 2 + (cut ? 0 : 1)) * a.part_stride;
+#pragma unroll
+        for (int i = 0; i < C::kPer; ++i)
+          if (C::at(b, lane, i) < a.D) part[C::at(b, lane, i)] = s[i];
+      } else {
+        C::store(out + (int64_t)run * a.dst_stride, b, lane, a.D, s, a.scale, a.accumulate != 0);
+      }
+#pragma unroll
+      for (int i = 0; i < C::kPer; ++i) s[i] = 0.f;
+    };
+    for (int64_t q = p0; q < p1; q += 32) {
+      const int64_t pos = q + lane;
+      const int tok = pos < p1 ? a.perm[pos] : 0, id = pos < p1 ? a.sid[pos] : -1;
+      const int cnt = (int)min((int64_t)32, p1 - q);
+#pragma unroll 1
+      for (int j0 = 0; j0 < cnt; j0 += kSumAhead) {
+        typename C::Raw r[kSumAhead];
+#pragma unroll
+        for (int j = 0; j < kSumAhead; ++j) {
+          const int tk = __shfl_sync(0xffffffffu, tok, (j0 + j) & 31);
+          if (j0 + j < cnt) r[j] = C::load(static_cast<const T*>(a.src) + (int64_t)tk * a.src_stride, b, lane, a.D);
+        }
+#pragma unroll
+        for (int j = 0; j < kSumAhead; ++j) {
+          const int v = __shfl_sync(0xffffffffu, id, (j0 + j) & 31);
+          if (j0 + j < cnt) {
+            if (v != run) {
+              leave(false);
+              run = v;
+              cut = false;
+            }
+            C::add(r[j], s);
+          }
+        }
+      }
+    }
+    leave(after == run);
+  }
+}
+
+// Cut runs: a warp takes kJoinPieces pieces and 32 x 4 columns; a run belongs to the piece it starts in.
+constexpr int kJoinPieces = 8;
+constexpr int kJoinAhead = 8;
+
+template <int kType>
+__global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a, int piece) {
+  using E = Elem<kType>;
+  using T = typename E::T;
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int64_t nwarps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  const int n = a.start[a.V];
+  const int64_t pieces = ((int64_t)n + piece - 1) / piece;
+  const int64_t blocks = (a.D + 127) / 128, groups = (pieces + kJoinPieces - 1) / kJoinPieces;
+  for (int64_t it = warp; it < groups * blocks; it += nwarps) {
+    const int64_t g = it / blocks, b = it - g * blocks;
+    // lane k: the run that the end of piece g * kJoinPieces + k cuts, if it starts in that piece
+    const int64_t p = g * kJoinPieces + (lane & (kJoinPieces - 1));
+    int row = -1;
+    if (lane < kJoinPieces && (p + 1) * piece < n) {
+      const int x = a.sid[(p + 1) * piece - 1];
+      if (x == a.sid[(p + 1) * piece] && a.start[x] >= p * piece) row = x;
+    }
+    for (uint32_t m = __ballot_sync(0xffffffffu, row >= 0); m; m &= m - 1u) {
+      const int k = __ffs(m) - 1;
+      const int v = __shfl_sync(0xffffffffu, row, k);
+      const int64_t pa = g * kJoinPieces + k, pz = ((int64_t)a.start[v + 1] - 1) / piece;
+      const int64_t c = b * 128 + lane * 4;
+      if (c >= a.D) continue;
+      const float* part = a.part + c;  // (rows of the workspace have room for whole float4)
+      float4 s = *reinterpret_cast<const float4*>(part + (pa * 2 + 1) * a.part_stride);
+#pragma unroll 1
+      for (int64_t q = pa + 1; q <= pz; q += kJoinAhead) {
+        float4 x[kJoinAhead];
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j)
+          if (q + j <= pz) x[j] = *reinterpret_cast<const float4*>(part + (q + j) * 2 * a.part_stride);
+#pragma unroll
+        for (int j = 0; j < kJoinAhead; ++j)
+          if (q + j <= pz) s.x += x[j].x, s.y += x[j].y, s.z += x[j].z, s.w += x[j].w;
+      }
+      T* dst = static_cast<T*>(a.dst) + (int64_t)v * a.dst_stride + c;
+      const float y[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + i < a.D) dst[i] = E::put(a.accumulate ? fmaf(a.scale, y[i], E::get(dst[i])) : a.scale * y[i]);
+    }
+  }
+}
+
+// Tokens of one piece: longer pieces leave fewer sums of a frequent token to join, shorter ones give
+// more warps something to do.
+int piece_of(int64_t T) { return T <= 16384 ? kEmbedPiece : T <= 65536 ? 2 * kEmbedPiece : 4 * kEmbedPiece; }
+
+inline bool vec_rows(const void* p, int64_t stride, int esz) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * esz % 16 == 0;
+}
+
+template <int kType>
+cudaError_t look(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
+  const int esz = kType == GPO_DT_F32 ? 4 : 2;
+  const int64_t per = (int64_t)kLookBlocks * 512 / esz;
+  const int64_t warps = a.T * ((a.D + per - 1) / per);
+  const int grid = (int)min((warps + 7) / 8, (int64_t)lc.num_sms * 8);
+  if (vec_rows(a.src, a.src_stride, esz) && vec_rows(a.dst, a.dst_stride, esz))
+    embed_kernel<kType, true><<<grid, 256, 0, lc.stream>>>(a, st);
+  else embed_kernel<kType, false><<<grid, 256, 0, lc.stream>>>(a, st);
+  return cudaGetLastError();
+}
+
+template <int kType>
+cudaError_t sums(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
+  const int esz = kType == GPO_DT_F32 ? 4 : 2;
+  const int piece = piece_of(a.T);
+  const int64_t blocks = (a.D * esz + 511) / 512, pieces = (a.T + piece - 1) / piece;
+  const int64_t units = (pieces + (a.accumulate ? 0 : (a.V + 31) / 32)) * blocks;
+  const int grid = (int)max((int64_t)1, min((units + 7) / 8, (int64_t)lc.num_sms * 4));
+  if (vec_rows(a.src, a.src_stride, esz) && vec_rows(a.dst, a.dst_stride, esz))
+    embed_sum_kernel<kType, true><<<grid, kSumThreads, 0, lc.stream>>>(a, piece, st);
+  else embed_sum_kernel<kType, false><<<grid, kSumThreads, 0, lc.stream>>>(a, piece, st);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || pieces < 2) return e;
+  const int64_t jobs = (pieces + kJoinPieces - 1) / kJoinPieces * ((a.D + 127) / 128);
+  embed_join_kernel<kType><<<(int)min((jobs + 7) / 8, (int64_t)lc.num_sms * 8), 256, 0, lc.stream>>>(a, piece);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t setup_embed() {
+  return cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              (int)sort_smem(kEmbedMaxRows));
+}
+
+cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
+  if (a.dtype == GPO_DT_F32) return look<GPO_DT_F32>(lc, a, st);
+  if (a.dtype == GPO_DT_F16) return look<GPO_DT_F16>(lc, a, st);
+  return look<GPO_DT_BF16>(lc, a, st);
+}
+
+cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
+  const int64_t want = (a.V + lc.num_sms - 1) / lc.num_sms;
+  const int per = (int)min(max(want, (int64_t)32), (int64_t)kEmbedMaxRows);
+  embed_sort_kernel<<<(unsigned)((a.V + per - 1) / per), kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  if (a.dtype == GPO_DT_F32) return sums<GPO_DT_F32>(lc, a, st);
+  if (a.dtype == GPO_DT_F16) return sums<GPO_DT_F16>(lc, a, st);
+  return sums<GPO_DT_BF16>(lc, a, st);
+}
+
+}  // namespace gpo

@@ -380,6 +380,16 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)
       : "r"(taddr));
 }
 
+// The same with 16 columns.
+__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+}
+
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory matrix descriptor for a K-major operand stored as rows of 128
@@ -943,5 +953,92 @@ struct LossArgs {
 cudaError_t launch_loss_plan(const LaunchCtx& lc, const gpo_batch& b, const Sizes& sz, const LossPlan& lp);
 cudaError_t launch_token_loss(const LaunchCtx& lc, const LossPlan& lp, const LossArgs& a);
 cudaError_t setup_loss();
+
+// ------------------------------------------------------------------ vocabulary ends
+
+constexpr int kPairM = 256;      // rows of one tile of a CTA pair (tcgen05 M, both CTAs)
+constexpr int kPairN = 256;      // columns of one tile
+constexpr int kVocabOneTile = kPairM;  // tokens up to which the forward pass takes them as they are
+constexpr int64_t kVocabPieceBytes = (int64_t)512 << 20;  // dz of one piece of the vocabulary at most
+// parts of a forward row: the maxima and sums of the two column halves of every tile
+inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
+
+struct VocabHead {  // in the workspace, written by the index kernel
+  int rows;         // tokens that take part
+  float dz_scale;   // power of two that brings dz into fp16's range (1 for bf16)
+};
+
+struct VocabArgs {
+  int64_t T, V;
+  int D;
+  const void* target;
+  int id8;               // targets are int64
+  int f16;               // operands are fp16 (else bf16)
+  float scale, sl2;      // scale, scale log2(e)
+  const void* hidden;
+  int64_t hidden_stride;
+  // rows that take part: row r is token idx[r], head->rows of them (idx null: every token, r itself)
+  VocabHead* head;
+  int* idx;
+  uint16_t* hc;          // their hidden rows, gathered (unless all tokens take part)
+  int64_t hc_stride;
+  // forward: maxima (of scaled logits in units of log 2), sums and entropy sums of every part,
+  // the target left out, at row * part_row + part * part_col, and the targets' logits
+  float *pm, *ps, *pu, *tz;
+  int64_t part_row, part_col;
+  float *logp, *lse_out, *ent_out;
+  // gradient
+  const float *lse, *g, *ent, *ge;
+  uint16_t* dz;          // [rows up to a tile x dz_stride] of the piece [v0, v0 + vn) of the vocabulary
+  int64_t dz_stride;
+  int64_t v0, vn;
+  float* acc;            // [rows x acc_stride] d_hidden of the pieces so far (several pieces)
+  int64_t acc_stride;
+  int first, last;       // the first, the last piece
+  void* dh;
+  int64_t dh_stride;
+  void* dw;
+  int64_t dw_stride;
+  int accumulate;
+  int debug_timeout;
+};
+
+// Tensor maps of one call: hidden rows as given and gathered, the vocabulary matrix, dz; boxes of 64 x 64.
+struct VocabMaps {
+  CUtensorMap h, hc, w, dz;
+};
+
+cudaError_t setup_vocab();
+// The tokens that take part (grad: those with a gradient), their hidden rows, and the zeros of the others.
+cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad);
+cudaError_t launch_vocab_lse(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent);
+cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool ent);
+cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);
+cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);
+
+struct EmbedArgs {
+  int64_t T, V;
+  int64_t D;
+  const void* ids;
+  int id8;
+  int dtype;             // gpo_dtype
+  float scale;
+  const void* src;       // table, or grad rows
+  int64_t src_stride;
+  void* dst;             // output rows, or d_table
+  int64_t dst_stride;
+  int accumulate;
+  // gradient: tokens sorted by id (stable), their ids, the first of every row of the table,
+  // and the sums of runs that pieces of kEmbedPiece tokens cut
+  int *perm, *sid, *start;
+  float* part;           // [pieces x 2 x part_stride]
+  int64_t part_stride;
+};
+constexpr int kEmbedPiece = 32;
+constexpr int kEmbedMaxRows = 1024;  // rows of the table that one CTA of the sort owns, at most
+
+cudaError_t setup_embed();
+cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
+cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
 
 }  // namespace gpo
