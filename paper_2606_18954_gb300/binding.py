@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 import threading
 from typing import Optional
 
@@ -116,7 +117,16 @@ EXPORTS = ["gpo_create", "gpo_workspace_size", "gpo_compute", "gpo_sync_status",
 FUSED_MAX_STATES = 384  # largest group the group-resident path (and gpo_compute_groups) serves
 
 _lib = None
+_fast = {}  # the calls of every step once more, with their structs as packed bytes (see _pack)
 _lock = threading.Lock()
+
+# Packed images of gpo_vocab, gpo_vocab_outputs, gpo_vocab_grad_inputs, gpo_vocab_grads and gpo_embedding:
+# building a ctypes structure costs 2 us a call, packing one 0.5.
+_PACK_VOCAB = struct.Struct("@5q3Q2id").pack
+_PACK_3 = struct.Struct("@3Q").pack
+_PACK_4 = struct.Struct("@4Q").pack
+_PACK_GRADS = struct.Struct("@2Q2qi4x").pack
+_PACK_EMBED = struct.Struct("@5qQ2id").pack
 
 
 def lib_path() -> str:
@@ -197,6 +207,12 @@ def load(build_if_missing: bool = False):
         L.gpo_embed.restype = ctypes.c_int
         L.gpo_embed_grad.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, ctypes.c_int, vp, sz, vp]
         L.gpo_embed_grad.restype = ctypes.c_int
+        raw = ctypes.c_char_p
+        for name, args in (("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad", [vp, raw, raw, raw, vp, sz, vp]),
+                           ("gpo_embed", [vp, raw, vp, vp, vp, sz, vp]), ("gpo_embed_grad", [vp, raw, vp, vp, ctypes.c_int, vp, sz, vp])):
+            f = L[name]  # (a function object of its own)
+            f.argtypes, f.restype = args, ctypes.c_int
+            _fast[name] = f
         _lib = L
         return L
 
@@ -245,38 +261,69 @@ def embed_workspace_size(e: CEmbedding, gradient: bool = False) -> int:
     return n.value
 
 
+_dtypes = {}  # torch dtype -> gpo_dtype (filled on first use: torch is imported late)
+_id_dtypes = {}  # torch dtype -> bytes of an id
+
+
 def _dtype_code(t, what: str) -> int:
-    import torch
-    code = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}.get(t.dtype)
+    if not _dtypes:
+        import torch
+        _dtypes.update({torch.bfloat16: 0, torch.float32: 1, torch.float16: 2})
+    code = _dtypes.get(t.dtype)
     if code is None:
         raise TypeError(f"{what} must be bfloat16, float16 or float32, not {t.dtype}")
     return code
 
 
-def _matrix(t, what: str, dev, rows=None, cols=None, dtype=None) -> int:
-    """Checks a [rows, cols] device matrix with unit inner stride; returns its row stride."""
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{what} must be [{'rows' if rows is None else rows}, {'d' if cols is None else cols}], "
-                         f"not {tuple(t.shape)}")
-    if t.device != dev:
-        raise ValueError(f"{what} is on {t.device}, not {dev}")
-    if dtype is not None and t.dtype != dtype:
+def _id_bytes(t, what: str) -> int:
+    if not _id_dtypes:
+        import torch
+        _id_dtypes.update({torch.int32: 4, torch.int64: 8})
+    n = _id_dtypes.get(t.dtype)
+    if n is None:
+        raise TypeError(f"{what} must be int32 or int64, not {t.dtype}")
+    return n
+
+
+def _matrix(t, what: str, dev: int, rows, cols, dtype) -> int:
+    """Checks a [rows, cols] matrix on device `dev` with unit inner stride; returns its row stride."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or shape[1] != cols:
+        raise ValueError(f"{what} must be [{rows}, {cols}], not {tuple(shape)}")
+    if t.get_device() != dev or dev < 0:
+        raise ValueError(f"{what} is on {t.device}: the arrays must be on one CUDA device")
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
-    st, one = t.stride()
-    if one != 1 and t.shape[1] > 1 and t.shape[0] > 0:
+    if stride[1] != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{what} must have unit inner stride")
-    return st if t.shape[0] > 1 else max(st, t.shape[1])
+    return stride[0] if rows > 1 else max(stride[0], cols)
 
 
-def _vector(t, what: str, dev, n: int, dtypes) -> int:
-    """Checks a contiguous device vector of n elements; returns its address (None if empty)."""
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+def _vector(t, what: str, dev: int, n: int, dtype=None) -> int:
+    """Checks a contiguous vector of n elements on device `dev`; returns its address."""
+    shape = t.shape
+    if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous vector of {n} elements")
-    if t.device != dev:
-        raise ValueError(f"{what} is on {t.device}, not {dev}")
-    if t.dtype not in dtypes:
-        raise TypeError(f"{what} must be {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    return t.data_ptr() or None
+    if t.get_device() != dev:
+        raise ValueError(f"{what} is on {t.device}: the arrays must be on one CUDA device")
+    if dtype is not None and t.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, not {t.dtype}")
+    return t.data_ptr()
+
+
+_current_stream = None  # device index -> handle of its current stream
+
+
+def _stream_handle(stream, dev: int):
+    """The CUDA stream handle of `stream`, or of the current stream on device `dev`."""
+    global _current_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _current_stream is None:
+        import torch
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (  # (see _raw_stream)
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _current_stream(dev)
 
 
 def _ptr(t) -> Optional[int]:
@@ -427,6 +474,7 @@ class GraphPO:
             raise GraphPOError(code, "gpo_create")
         self._h = h
         self._ws = None
+        self._sizes = {}  # workspace bytes by sizes (vocabulary ends)
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -579,22 +627,32 @@ class GraphPO:
 
     # ---- the model's vocabulary ends (gpo_vocab_logp / gpo_vocab_grad, gpo_embed / gpo_embed_grad)
 
-    def _room(self, need: int, dev):
-        """The context's workspace, at least `need` bytes on `dev`."""
-        import torch
-        if self._ws is None or self._ws.numel() < need or self._ws.device != dev:
-            self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        return self._ws
+    def _room(self, key, size, dev, workspace):
+        """Address and bytes of the workspace: the caller's, or the context's, which holds at least
+        size() bytes (asked once for the sizes that `key` stands for)."""
+        if workspace is not None:
+            return workspace.data_ptr(), workspace.numel()
+        need = self._sizes.get(key)
+        if need is None:
+            if len(self._sizes) > 1024:
+                self._sizes.clear()
+            need = self._sizes[key] = size()
+        ws = self._ws
+        if ws is None or ws.numel() < need or ws.device != dev:
+            import torch
+            ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        return ws.data_ptr(), ws.numel()
 
     @staticmethod
-    def _vocab(hidden, weight, target, scale) -> CVocab:
-        import torch
-        dev = hidden.device
-        hs = _matrix(hidden, "hidden", dev)
-        ws = _matrix(weight, "weight", dev, cols=hidden.shape[1], dtype=hidden.dtype)
-        tp = _vector(target, "target", dev, hidden.shape[0], (torch.int32, torch.int64))
-        return CVocab(hidden.shape[0], weight.shape[0], weight.shape[1], hs, ws, hidden.data_ptr() or None,
-                      weight.data_ptr() or None, tp, _dtype_code(hidden, "hidden"), target.element_size(), float(scale))
+    def _head(hidden, weight, target):
+        """The checks that both directions share: device, sizes, strides, codes, the target's address."""
+        if len(hidden.shape) != 2 or len(weight.shape) != 2:
+            raise ValueError("hidden must be [T, d] and weight [V, d]")
+        dev, (T, d), V = hidden.get_device(), hidden.shape, weight.shape[0]
+        code = _dtype_code(hidden, "hidden")
+        hs = _matrix(hidden, "hidden", dev, T, d, hidden.dtype)
+        ws = _matrix(weight, "weight", dev, V, d, hidden.dtype)
+        return dev, T, V, d, hs, ws, code, _id_bytes(target, "target"), _vector(target, "target", dev, T)
 
     def vocab_logp(self, hidden, weight, target, scale=1.0, lse=True, entropy=False, out=None, workspace=None,
                    stream=None) -> dict:
@@ -604,20 +662,24 @@ class GraphPO:
         "entropy" (if entropy)}, or fills `out`.  The logits are never stored.  Enqueued on the
         current stream; `check()` raises on a target outside the vocabulary."""
         import torch
-        v = self._vocab(hidden, weight, target, scale)
-        dev, T = hidden.device, hidden.shape[0]
+        dev, T, V, d, hs, ws, code, idb, tp = self._head(hidden, weight, target)
+        f32 = torch.float32
         if out is None:
-            out = {"logp": _empty(T, torch.float32, dev)}
+            lp = torch.empty(T, dtype=f32, device=hidden.device)
+            out = {"logp": lp}
             if lse:
-                out["lse"] = _empty(T, torch.float32, dev)
+                out["lse"] = torch.empty_like(lp)
             if entropy:
-                out["entropy"] = _empty(T, torch.float32, dev)
-        f32 = (torch.float32,)
-        vo = VocabOutputs(*[None if out.get(k) is None else _vector(out[k], k, dev, T, f32)
-                            for k in ("logp", "lse", "entropy")])
-        ws = self._room(vocab_workspace_size(v), dev) if workspace is None else workspace
-        code = self._lib.gpo_vocab_logp(self._h, ctypes.byref(v), ctypes.byref(vo), ws.data_ptr(), ws.numel(),
-                                        _raw_stream(stream, dev))
+                out["entropy"] = torch.empty_like(lp)
+            po = [t.data_ptr() for t in out.values()]
+            ptrs = (po[0], po[1] if lse else 0, po[-1] if entropy else 0)
+        else:
+            ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("logp", "lse", "entropy")]
+        wp, wn = self._room((0, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0)),
+                            hidden.device, workspace)
+        code = _fast["gpo_vocab_logp"](
+            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale),
+            _PACK_3(*ptrs), wp, wn, _stream_handle(stream, dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -629,35 +691,32 @@ class GraphPO:
         vocab_logp's outputs, whose lse (and entropy) are given; or fills `out`, with `accumulate`
         adding to out["d_weight"].  Enqueued on the current stream."""
         import torch
-        v = self._vocab(hidden, weight, target, scale)
-        dev, T = hidden.device, hidden.shape[0]
+        dev, T, V, d, hs, ws, code, idb, tp = self._head(hidden, weight, target)
+        f32, dt = torch.float32, hidden.dtype
+        if grad_entropy is not None and entropy is None:
+            raise ValueError("grad_entropy needs vocab_logp's entropy")
         if out is None:
             if accumulate and d_weight:
                 raise ValueError("accumulate needs the d_weight to add to in `out`")
             out = {}
             if d_hidden:
-                out["d_hidden"] = torch.empty(T, hidden.shape[1], dtype=hidden.dtype, device=dev)
+                out["d_hidden"] = torch.empty(T, d, dtype=dt, device=hidden.device)
             if d_weight:
-                out["d_weight"] = torch.empty(weight.shape, dtype=weight.dtype, device=dev)
-        f32 = (torch.float32,)
-        if grad_entropy is not None and entropy is None:
-            raise ValueError("grad_entropy needs vocab_logp's entropy")
-        gi = VocabGradInputs(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
-                             None if grad_entropy is None else _vector(entropy, "entropy", dev, T, f32),
-                             None if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32))
+                out["d_weight"] = torch.empty(V, d, dtype=dt, device=hidden.device)
+        ins = _PACK_4(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
+                      0 if grad_entropy is None else _vector(entropy, "entropy", dev, T, f32),
+                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32))
         dh, dw = out.get("d_hidden"), out.get("d_weight")
-        go = VocabGrads(None, None, 0, 0, int(bool(accumulate)))
-        if dh is not None:
-            go.d_hidden_stride = _matrix(dh, "d_hidden", dev, T, v.d, hidden.dtype)
-            go.d_hidden = dh.data_ptr() or None
-        if dw is not None:
-            go.d_weight_stride = _matrix(dw, "d_weight", dev, v.vocab, v.d, hidden.dtype)
-            go.d_weight = dw.data_ptr() or None
+        sh = 0 if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
+        sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
         if T == 0 and dw is None:
             return out
-        ws = self._room(vocab_workspace_size(v, True), dev) if workspace is None else workspace
-        code = self._lib.gpo_vocab_grad(self._h, ctypes.byref(v), ctypes.byref(gi), ctypes.byref(go), ws.data_ptr(),
-                                        ws.numel(), _raw_stream(stream, dev))
+        wp, wn = self._room((1, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), True),
+                            hidden.device, workspace)
+        code = _fast["gpo_vocab_grad"](
+            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins,
+            _PACK_GRADS(0 if dh is None else dh.data_ptr(), 0 if dw is None else dw.data_ptr(), sh, sw, bool(accumulate)),
+            wp, wn, _stream_handle(stream, dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -666,16 +725,19 @@ class GraphPO:
         """Rows of `table` ([V, d] bfloat16, float16 or float32) by token id (int32 or int64 [T]; below
         0: a row of zeros), times `scale`: [T, d] of the table's type.  Enqueued on the current stream."""
         import torch
-        dev, T = table.device, ids.shape[0]
-        ts = _matrix(table, "table", dev)
+        if len(table.shape) != 2 or len(ids.shape) != 1:
+            raise ValueError("table must be [V, d] and ids [T]")
+        dev, (V, d), T, dt = table.get_device(), table.shape, ids.shape[0], table.dtype
+        code, idb = _dtype_code(table, "table"), _id_bytes(ids, "ids")
+        ts, ip = _matrix(table, "table", dev, V, d, dt), _vector(ids, "ids", dev, T)
         if out is None:
-            out = torch.empty(T, table.shape[1], dtype=table.dtype, device=dev)
-        rs = _matrix(out, "out", dev, T, table.shape[1], table.dtype)
-        e = CEmbedding(T, table.shape[0], table.shape[1], ts, rs, _vector(ids, "ids", dev, T, (torch.int32, torch.int64)),
-                       _dtype_code(table, "table"), ids.element_size(), float(scale))
-        ws = self._room(embed_workspace_size(e), dev) if workspace is None else workspace
-        code = self._lib.gpo_embed(self._h, ctypes.byref(e), table.data_ptr() or None, out.data_ptr() or None,
-                                   ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+            out, rs = torch.empty(T, d, dtype=dt, device=table.device), d
+        else:
+            rs = _matrix(out, "out", dev, T, d, dt)
+        wp, wn = self._room((2,), lambda: embed_workspace_size(CEmbedding(T, 1, 1, 1, 1, None, code, idb, 1.0)), table.device,
+                            workspace)
+        code = _fast["gpo_embed"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), table.data_ptr(),
+                                  out.data_ptr(), wp, wn, _stream_handle(stream, dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -686,18 +748,21 @@ class GraphPO:
         to `out` (a table tied to the vocabulary matrix: vocab_grad's d_weight).  Enqueued on the
         current stream."""
         import torch
-        dev, T = grad.device, grad.shape[0]
-        rs = _matrix(grad, "grad", dev)
+        if len(grad.shape) != 2:
+            raise ValueError("grad must be [T, d]")
+        dev, (T, d), V, dt = grad.get_device(), grad.shape, int(vocab), grad.dtype
+        code, idb = _dtype_code(grad, "grad"), _id_bytes(ids, "ids")
+        rs, ip = _matrix(grad, "grad", dev, T, d, dt), _vector(ids, "ids", dev, T)
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs the gradient to add to in `out`")
-            out = torch.empty(int(vocab), grad.shape[1], dtype=grad.dtype, device=dev)
-        ts = _matrix(out, "out", dev, int(vocab), grad.shape[1], grad.dtype)
-        e = CEmbedding(T, int(vocab), grad.shape[1], ts, rs, _vector(ids, "ids", dev, T, (torch.int32, torch.int64)),
-                       _dtype_code(grad, "grad"), ids.element_size(), float(scale))
-        ws = self._room(embed_workspace_size(e, True), dev) if workspace is None else workspace
-        code = self._lib.gpo_embed_grad(self._h, ctypes.byref(e), grad.data_ptr() or None, out.data_ptr() or None,
-                                        int(bool(accumulate)), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev))
+            out, ts = torch.empty(V, d, dtype=dt, device=grad.device), d
+        else:
+            ts = _matrix(out, "out", dev, V, d, dt)
+        wp, wn = self._room((3, T, V, d), lambda: embed_workspace_size(CEmbedding(T, V, d, d, d, None, code, idb, 1.0), True),
+                            grad.device, workspace)
+        code = _fast["gpo_embed_grad"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), grad.data_ptr(),
+                                       out.data_ptr(), bool(accumulate), wp, wn, _stream_handle(stream, dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out

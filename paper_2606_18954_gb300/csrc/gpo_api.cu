@@ -260,7 +260,7 @@ gpo_status gpo_create(gpo_ctx** out, const gpo_params* params) {
   if (setup_sim_tc() != cudaSuccess || setup_sim_simt() != cudaSuccess || setup_groups() != cudaSuccess || setup_fused() != cudaSuccess ||
       setup_fused_f32() != cudaSuccess ||
       setup_tree_prep() != cudaSuccess || setup_loss() != cudaSuccess || setup_vocab() != cudaSuccess ||
-      setup_embed() != cudaSuccess ||
+      setup_vocab_few() != cudaSuccess || setup_embed() != cudaSuccess ||
       cudaMallocHost(&c->host_status, sizeof(uint32_t) * kStatusWords) != cudaSuccess) {
     cudaGetLastError();
     delete c;

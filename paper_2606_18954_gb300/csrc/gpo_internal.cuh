@@ -380,16 +380,6 @@ __device__ __forceinline__ void tmem_ld_32x32b_x32(uint32_t taddr, uint32_t (&r)
       : "r"(taddr));
 }
 
-// The same with 16 columns.
-__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr));
-}
-
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory matrix descriptor for a K-major operand stored as rows of 128
@@ -959,7 +949,12 @@ cudaError_t setup_loss();
 constexpr int kPairM = 256;      // rows of one tile of a CTA pair (tcgen05 M, both CTAs)
 constexpr int kPairN = 256;      // columns of one tile
 constexpr int kVocabOneTile = kPairM;  // tokens up to which the forward pass takes them as they are
+constexpr int kVocabPairs = 76;      // CTA pairs that the split of d_hidden's k reckons with (GB300: 152 SMs)
+constexpr int kVocabMaxSplits = 32;
+int vocab_splits(int64_t T, int64_t vn, int64_t D);
 constexpr int64_t kVocabPieceBytes = (int64_t)512 << 20;  // dz of one piece of the vocabulary at most
+constexpr int kVocabFew = 64;        // tokens up to which the forward pass is one launch (gpo_vocab_few.cu)
+constexpr int kVocabFewCtas = 256;   // CTAs of that launch at most
 // parts of a forward row: the maxima and sums of the two column halves of every tile
 inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
 
@@ -992,8 +987,9 @@ struct VocabArgs {
   uint16_t* dz;          // [rows up to a tile x dz_stride] of the piece [v0, v0 + vn) of the vocabulary
   int64_t dz_stride;
   int64_t v0, vn;
-  float* acc;            // [rows x acc_stride] d_hidden of the pieces so far (several pieces)
-  int64_t acc_stride;
+  float* acc;            // [splits x acc_rows x acc_stride] d_hidden of the pieces so far, per part of k
+  int64_t acc_rows, acc_stride;
+  int splits;            // parts of the k of d_hidden
   int first, last;       // the first, the last piece
   void* dh;
   int64_t dh_stride;
@@ -1003,7 +999,8 @@ struct VocabArgs {
   int debug_timeout;
 };
 
-// Tensor maps of one call: hidden rows as given and gathered, the vocabulary matrix, dz; boxes of 64 x 64.
+// Tensor maps of one call: hidden rows as given and gathered, the vocabulary matrix, dz; boxes of 64 x 64
+// (few tokens: 64 x vocab_few_columns of hidden, 64 x 32 of the matrix).
 struct VocabMaps {
   CUtensorMap h, hc, w, dz;
 };
@@ -1011,6 +1008,11 @@ struct VocabMaps {
 cudaError_t setup_vocab();
 // The tokens that take part (grad: those with a gradient), their hidden rows, and the zeros of the others.
 cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad);
+// Up to kVocabFew tokens; marks: [kVocabFewCtas] in the workspace, mark: a value that no other call leaves there.
+cudaError_t setup_vocab_few();
+int vocab_few_columns(int64_t T);
+cudaError_t launch_vocab_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent,
+                             uint64_t* marks, uint64_t mark);
 cudaError_t launch_vocab_lse(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent);
 cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool ent);
 cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);

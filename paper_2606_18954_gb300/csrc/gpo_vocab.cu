@@ -1,10 +1,11 @@
 // Per-token log-probabilities from hidden states and the vocabulary matrix, and their gradients,
 // on the tcgen05 tensor cores (the formulas are in include/graphpo.h).
 //
-// Forward, two launches and for more than 256 tokens two more before them:
-//   rows     vocab_index_kernel lists the tokens with a target, vocab_gather_kernel copies their
-//            hidden rows together (skipped where every token has one): tokens without a target cost no
-//            product, and what their rows hold reaches nothing
+// Forward, two launches and for more than 256 tokens one more before them (up to 64 tokens:
+// gpo_vocab_few.cu):
+//   rows     vocab_rows_kernel lists the tokens with a target and copies their hidden rows together
+//            (not where every token has one): tokens without a target cost no product, and
+//            what their rows hold reaches nothing
 //   lse      vocab_pair_kernel<kLse>: logits tiles of 256 tokens x 256 vocabulary rows that stay in tensor
 //            memory; the epilogue reduces each row's 128 columns to a maximum and a sum (and the entropy's
 //            sum), the target's logit kept apart
@@ -12,7 +13,8 @@
 // Gradient, piece by piece of the vocabulary (dz of a piece takes at most 512 MiB):
 //   rows     as above, for the tokens with a gradient that is not 0
 //   dz       vocab_pair_kernel<kDz>: the logits again, dz in the epilogue, written in 16 bits
-//   products vocab_pair_kernel<kProducts>: d_hidden += dz W and d_weight = dz^T hidden in one launch
+//   products vocab_pair_kernel<kProducts>: d_hidden += dz W and d_weight = dz^T hidden in one launch;
+//            with few tokens the k of d_hidden in parts (vocab_splits) that vocab_parts_kernel adds
 // Keeping the sum over the other tokens of the vocabulary apart from the target's term keeps the
 // digits of a nearly certain token's log-probability -log(1 + sum), which is a small number.
 #define GPO_REPORT __noinline__
@@ -20,6 +22,7 @@
 #include <cuda_fp16.h>
 
 #include "gpo_pair.cuh"
+#include "gpo_vocab_math.cuh"
 
 namespace gpo {
 
@@ -29,21 +32,26 @@ enum Mode { kLse, kLseEnt, kDz, kDzEnt, kProducts };
 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
 constexpr int kVStages = 6;
-constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 tensor memory, 4..11 epilogue
-constexpr int kVEpiWarps = 8;
+constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 4..11 epilogue
+constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
+// The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
+// give back.  The shares add up to no more than the launch brings (setup_mode checks that).
+constexpr int kRegsLaunch = 168, kRegsFew = 72, kRegsMany = 216;
+static_assert(128 * kRegsFew + 256 * kRegsMany <= kVThreads * kRegsLaunch, "register split");
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
 constexpr int kVStage = 4 * kVBox;                 // A and B halves of one k-step, per CTA
 constexpr int kVCols = 512;                        // two accumulators of 256 columns
-// Logits: steps of k after which the tensor cores' sum is taken over into registers.  Their fp32
+// Logits: steps of 64 k after which the tensor cores' sum is taken over into registers.  Their fp32
 // additions drop the bits below the sum's last one, always towards zero, so that a sum of d products
 // shrinks by about d / 16 half ulps: 7e-6 of a logit at d = 4096, too much for the log-probability of
-// a nearly certain token.  Sums of 256 products, added in registers with rounding, stay at fp32's own
-// error.  (The gradients' sums are rounded to 16 bits, 1e3 times as much.)
-constexpr int kSegment = 4;
+// a nearly certain token.  Shorter sums, added in registers with rounding, keep that down, but reading
+// tensor memory holds up the MMAs.
+constexpr int kSegLse = 8, kSegDz = 32;
+template <int kMode>
+__device__ __forceinline__ constexpr int segment_of() {
+  return kMode == kProducts ? 1 << 30 : kMode == kDz || kMode == kDzEnt ? kSegDz : kSegLse;
+}
 constexpr int kRaster = 32;                        // row tiles that share one pass over the columns
-// A logit that is left out (a column past the vocabulary, the target) and the maximum of a part without
-// logits: for every scale in [1e-4, 1e4] the first, scaled, is finite and far below the second
-constexpr float kNone = -1e33f, kLow = -1e28f;
 
 struct __align__(8) VocabCtl {
   uint64_t full[kVStages];
@@ -55,16 +63,6 @@ struct __align__(8) VocabCtl {
 };
 
 constexpr size_t kVSmem = ((sizeof(VocabCtl) + 15) & ~size_t(15)) + 1023 + (size_t)kVStages * kVStage;
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-__device__ __forceinline__ int64_t load_id(const void* ids, int id8, int64_t t) {
-  return id8 ? static_cast<const int64_t*>(ids)[t] : (int64_t)static_cast<const int32_t*>(ids)[t];
-}
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int f16) {
   if (f16) {
@@ -79,10 +77,11 @@ __device__ __forceinline__ float widen16(uint16_t x, int f16) {
   return f16 ? __half2float(__ushort_as_half(x)) : __uint_as_float((uint32_t)x << 16);
 }
 
-// One tile of a pair: the rows of A from m0, the columns (rows of B) from n0, kb steps of 64 of k.
+// One tile of a pair: the rows of A from m0, the columns (rows of B) from n0, steps [ka, ka + kb) of 64 of k.
 struct Tile {
-  int job;  // kProducts: 0 d_hidden, 1 d_weight
-  int m0, n0, kb;
+  int job;    // kProducts: 0 d_hidden, 1 d_weight
+  int split;  // d_hidden: which part of k
+  int m0, n0, ka, kb;
 };
 
 // The tiles of one launch and which pair takes which, in what order.
@@ -90,7 +89,7 @@ struct Plan {
   int p, np;           // this pair of np
   int mt, nt, kb;      // kLse, kDz: row tiles, column tiles, k-steps
   int dt;              // kProducts: column tiles of d
-  int n_dh, kb_dh, own_dh, n_dw, kb_dw;
+  int n_dh, kb_dh, splits, own_dh, n_dw, kb_dw;
   int light0, nlight, extra;  // pairs from light0 on take `extra` d_weight tiles more, for the d_hidden tile they lack
 };
 
@@ -106,14 +105,15 @@ __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   q.dt = (a.D + kPairN - 1) / kPairN;
   // the longer d_hidden tiles first, round robin; the pairs that get one less take as much work in
   // d_weight tiles, the rest of which go round robin too
-  q.n_dh = a.dh ? q.mt * q.dt : 0;
+  q.splits = a.splits;
+  q.n_dh = a.dh ? q.mt * q.dt * q.splits : 0;
   q.n_dw = a.dw ? q.nt * q.dt : 0;
   q.kb_dh = (int)((a.vn + kTile16 - 1) / kTile16);
   q.kb_dw = (rows + kTile16 - 1) / kTile16;
   q.own_dh = q.n_dh / q.np + (q.p < q.n_dh % q.np ? 1 : 0);
   q.light0 = q.n_dh % q.np;
   q.nlight = q.np - q.light0;
-  q.extra = q.light0 > 0 && q.kb_dw > 0 ? min(q.kb_dh / q.kb_dw, q.n_dw / q.nlight) : 0;
+  q.extra = q.light0 > 0 && q.kb_dw > 0 ? min(q.kb_dh / q.splits / q.kb_dw, q.n_dw / q.nlight) : 0;
   return q;
 }
 
@@ -129,18 +129,20 @@ __device__ __forceinline__ bool next_tile(const Plan& q, int s, Tile& t) {
     const int g = (int)(i / per);
     const int r = (int)(i - g * per);
     const int gm = min(kRaster, q.mt - g * kRaster);
-    t.job = 0;
+    t.job = t.split = t.ka = 0;
     t.m0 = (g * kRaster + r % gm) * kPairM;
     t.n0 = r / gm * kPairN;
     t.kb = q.kb;
     return true;
   }
   if (s < q.own_dh) {
-    const int i = q.p + s * q.np;
+    const int i = q.p + s * q.np, mn = q.mt * q.dt, o = i % mn;
     t.job = 0;
-    t.m0 = i / q.dt * kPairM;
-    t.n0 = i % q.dt * kPairN;
-    t.kb = q.kb_dh;
+    t.split = i / mn;
+    t.m0 = o / q.dt * kPairM;
+    t.n0 = o % q.dt * kPairN;
+    t.ka = (int)((int64_t)q.kb_dh * t.split / q.splits);
+    t.kb = (int)((int64_t)q.kb_dh * (t.split + 1) / q.splits) - t.ka;
     return true;
   }
   s -= q.own_dh;
@@ -153,6 +155,7 @@ __device__ __forceinline__ bool next_tile(const Plan& q, int s, Tile& t) {
   }
   if (j >= q.n_dw) return false;
   t.job = 1;
+  t.split = t.ka = 0;
   t.m0 = j / q.dt * kPairM;
   t.n0 = j % q.dt * kPairN;
   t.kb = q.kb_dw;
@@ -200,6 +203,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   const uint32_t rank = cluster_rank();
   const int rows = a.idx ? a.head->rows : (int)a.T;
   const Plan plan = make_plan<kMode>(a, rows);
+  constexpr int seg = segment_of<kMode>();
   const CUtensorMap* hmap = a.idx && rows < a.T ? &maps.hc : &maps.h;
 
   if (threadIdx.x == 0) {
@@ -214,7 +218,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     mbar_init(&ctl->drain, 1);
     fence_mbar_init();
   }
-  if (warp == 2) {
+  if (warp == kMmaWarp) {
     tmem_alloc_pair(&ctl->tmem_base, kVCols);
     tmem_relinquish_pair();
   }
@@ -224,7 +228,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;
 
-  if (warp == 0) {
+  if (warp < 4) {
+  if (kMode != kProducts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+  if (warp == kLoadWarp) {
     // ------------------------------------------------------------ loads (lane 0 of either CTA: its halves)
     if (lane == 0) {
       int stage = 0;
@@ -246,7 +252,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           const uint32_t bar = leader_addr(&ctl->full[stage]);
           if (rank == 0) mbar_arrive_expect_tx(&ctl->full[stage], 2 * kVStage);
           ++issued;
-          const int kx = k * kTile16;
+          const int kx = (t.ka + k) * kTile16;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (a_mn) tma_load_2d_pair(sa + h * kVBox, ma, bar, am + h * kTile16, kx);
@@ -269,7 +275,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           if (s < issued) mbar_wait(&ctl->full[s], (issued - 1 - s) / kVStages & 1u, st, 21, 200000000ull, false);
     }
     __syncwarp();
-  } else if (warp == 1) {
+  } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ MMAs (lane 0 of the leader)
     if (lane == 0 && rank == 0) {
       int stage = 0;
@@ -284,7 +290,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
       for (int s = 0; ok && next_tile<kMode>(plan, s, t); ++s) {
         const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
         const uint32_t idesc = idesc_16_f32(kPairM, kPairN, a.f16 != 0, a_mn, b_mn);
-        for (int k0 = 0; ok && (k0 < t.kb || k0 == 0); k0 += kMode == kProducts ? t.kb + 1 : kSegment, ++sum) {
+        for (int64_t k0 = 0; ok && (k0 < t.kb || k0 == 0); k0 += seg, ++sum) {
         const int buf = sum & 1;
         if (!mbar_wait_cluster(&ctl->tempty[buf], ((uint32_t)(sum >> 1) & 1u) ^ 1u, st, 22)) {
           ok = false;
@@ -292,8 +298,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
         }
         tc_fence_after();
         const uint32_t dt = tmem + (uint32_t)(buf * kPairN);
-        const int k1 = kMode == kProducts ? t.kb : min(t.kb, k0 + kSegment);
-        for (int k = k0; k < k1; ++k) {
+        const int k1 = (int)min((int64_t)t.kb, k0 + seg);
+        for (int k = (int)k0; k < k1; ++k) {
           if (!mbar_wait(&ctl->full[stage], phase, st, 23)) {
             ok = false;
             break;
@@ -306,7 +312,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           const uint32_t as = a_mn ? 128u : 2u, bs = b_mn ? 128u : 2u;
 #pragma unroll
           for (uint32_t kk = 0; kk < kTile16 / 16; ++kk)
-            mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, ((k - k0) | (int)kk) != 0);
+            mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, (k - (int)k0 | (int)kk) != 0);
           mma_commit_pair(&ctl->empty[stage]);
           if (++stage == kVStages) {
             stage = 0;
@@ -321,8 +327,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
       mbar_wait(&ctl->drain, 0, st, 24, 200000000ull, false);
     }
     __syncwarp();
-  } else if (warp >= 4) {
+  }
+  } else {
     // ------------------------------------------------------------ epilogue
+    if (kMode != kProducts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
     const int q = warp & 3, half = (warp - 4) >> 2;  // tensor memory lanes 32 q .., columns 128 half ..
     const int r = (int)rank * (kPairM / 2) + q * 32 + lane;  // row in the tile
     const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (kPairN / 2));
@@ -364,23 +372,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
             }
           }
         }
-        float z[kPairN / 2];
+        uint64_t zz[kPairN / 4];  // two logits each
+#pragma unroll
+        for (int c = 0; c < kPairN / 4; ++c) zz[c] = 0ull;
         bool ok = true;
-        for (int k0 = 0; k0 < t.kb; k0 += kSegment, ++sum) {
+        const bool any = __any_sync(0xffffffffu, live);
+        for (int k0 = 0; k0 < t.kb; k0 += seg, ++sum) {
           ok = ready(sum);
           if (!ok) break;
           const uint32_t src = lanes + (uint32_t)((sum & 1) * kPairN);
+          if (any) {
 #pragma unroll
-          for (int c = 0; c < kPairN / 2; c += 16) {
-            uint32_t x[16];
-            tmem_ld_32x32b_x16(src + (uint32_t)c, x);
+          for (int c = 0; c < kPairN / 2; c += 32) {
+            uint32_t x[32];
+            tmem_ld_32x32b_x32(src + (uint32_t)c, x);
             tmem_wait_ld();
 #pragma unroll
-            for (int j = 0; j < 16; ++j) z[c + j] = k0 == 0 ? __uint_as_float(x[j]) : z[c + j] + __uint_as_float(x[j]);
+            for (int j = 0; j < 32; j += 2) zz[(c + j) / 2] = f2add(zz[(c + j) / 2], pack_f2(x[j], x[j + 1]));
+          }
           }
           release(sum);
         }
         if (!ok) break;
+        if (kLogits && !any) continue;  // no row of this warp is a token's
+        float z[kPairN / 2];
+#pragma unroll
+        for (int c = 0; c < kPairN / 4; ++c) {
+          uint32_t lo, hi;
+          unpack_f2(zz[c], lo, hi);
+          z[2 * c] = __uint_as_float(lo);
+          z[2 * c + 1] = __uint_as_float(hi);
+        }
         if constexpr (kLogits) {
           const int cols = (int)a.V - n0;
           if (cols < kPairN / 2) {
@@ -454,8 +476,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) * f : 0.f;  // (no tokens: no product ran)
           const int cols = a.D - c0;
           if (live && cols > 0 && t.job == 0) {
-            if (!(a.first && a.last)) {  // several pieces: sums so far in fp32
-              float4* acc = reinterpret_cast<float4*>(a.acc + (int64_t)row * a.acc_stride + c0);
+            const bool out = a.last && a.splits == 1;  // the whole sum
+            if (!(a.first && out)) {  // several pieces or parts of k: the sums so far in fp32
+              float4* acc = reinterpret_cast<float4*>(a.acc + ((int64_t)t.split * a.acc_rows + row) * a.acc_stride + c0);
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 if (4 * i < cols) {
@@ -466,11 +489,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
                     y[4 * i + 2] += o.z;
                     y[4 * i + 3] += o.w;
                   }
-                  if (!a.last) acc[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+                  if (!out) acc[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
                 }
               }
             }
-            if (a.last) {
+            if (out) {
               uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)a.idx[row] * a.dh_stride + c0;
               store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
             }
@@ -490,12 +513,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     const uint64_t t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 1000000ull) __nanosleep(1000);
   }
-  if (kMode == kProducts && a.last && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  if (kMode == kProducts && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   tc_fence_before();
   __syncthreads();
   cluster_sync();
   tc_fence_after();
-  if (warp == 2) tmem_dealloc_pair(tmem, kVCols);
+  if (warp == kMmaWarp) tmem_dealloc_pair(tmem, kVCols);
 }
 
 // ------------------------------------------------------------------ tokens that take part
@@ -506,114 +529,143 @@ __device__ __forceinline__ bool takes_part(const VocabArgs& a, int64_t t, bool g
   return !grad || a.g[t] != 0.f || (a.ge && a.ge[t] != 0.f);
 }
 
-constexpr int kIndexThreads = 1024;
+constexpr int kRowThreads = 512;
 
-// One CTA: the list of the tokens that take part, in order, their number, the forward outputs of
-// the others and the scale of an fp16 dz.
+// The list of the tokens that take part, in order, their number, the scale of an fp16 dz, their hidden
+// rows copied together (where some token is left out) with zeros up to the next k-step of the
+// d_weight product, and the zeros of the others' results.  Every CTA looks at all tokens (a few
+// bytes each) to know how many take part, and how many before its own share of them: one launch
+// and no exchange.
 template <bool kGrad>
-__global__ void __launch_bounds__(kIndexThreads) vocab_index_kernel(VocabArgs a, Status st) {
-  __shared__ int cnt[kIndexThreads / 32];
-  __shared__ float big[kIndexThreads / 32];
+__global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, Status st) {
+  constexpr int kW = kRowThreads / 32;
+  __shared__ int s_before[kW], s_all[kW], s_cnt[kW];
+  __shared__ float s_big[kW];
+  __shared__ int s_list[kRowThreads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int base = 0;
+  const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
+  int before = 0, all = 0;
   float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
-  for (int64_t t0 = 0; t0 < a.T; t0 += kIndexThreads) {
-    const int64_t t = t0 + threadIdx.x;
-    bool in = false;
-    if (t < a.T) {
-      const int64_t id = load_id(a.target, a.id8, t);
-      if (id >= a.V) report(st, GPO_ERR_SHAPE, 26, (int)t);
-      in = takes_part(a, t, kGrad);
-      if (kGrad && in) bound = fmaxf(bound, fabsf(a.g[t]) + (a.ge ? 24.f * fabsf(a.ge[t]) : 0.f));
-      if (!kGrad && !in) {
-        a.logp[t] = 0.f;
-        if (a.lse_out) a.lse_out[t] = 0.f;
-        if (a.ent_out) a.ent_out[t] = 0.f;
-      }
+#pragma unroll 4
+  for (int64_t t = threadIdx.x; t < a.T; t += kRowThreads) {
+    const int64_t id = load_id(a.target, a.id8, t);
+    bool in = id >= 0 && id < a.V;
+    if (kGrad) {
+      const float g = a.g[t], e = a.ge ? a.ge[t] : 0.f;
+      in = in && (g != 0.f || e != 0.f);
+      if (in) bound = fmaxf(bound, fabsf(g) + 24.f * fabsf(e));
     }
-    const uint32_t m = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) cnt[warp] = __popc(m);
-    __syncthreads();
-    int before = 0, all = 0;
-    for (int w = 0; w < kIndexThreads / 32; ++w) {
-      if (w < warp) before += cnt[w];
-      all += cnt[w];
-    }
-    if (in) a.idx[base + before + __popc(m & ((1u << lane) - 1u))] = (int)t;
-    base += all;
-    __syncthreads();
+    if (id >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)t);
+    all += in;
+    before += in && t < ta;
   }
-  if (kGrad && a.f16) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
-    if (lane == 0) big[warp] = bound;
-    __syncthreads();
-    for (int w = 0; w < kIndexThreads / 32; ++w) bound = fmaxf(bound, big[w]);
+  for (int o = 16; o > 0; o >>= 1) {
+    all += __shfl_xor_sync(0xffffffffu, all, o);
+    before += __shfl_xor_sync(0xffffffffu, before, o);
+    bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
   }
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
+    s_all[warp] = all;
+    s_before[warp] = before;
+    s_big[warp] = bound;
+  }
+  __syncthreads();
+  all = before = 0;
+  for (int w = 0; w < kW; ++w) {
+    all += s_all[w];
+    before += s_before[w];
+    bound = fmaxf(bound, s_big[w]);
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     float s = 1.f;
     if (kGrad && a.f16 && bound > 0.f && isfinite(bound)) {
       int ex;
       frexpf(bound, &ex);  // bound <= 2^ex: |dz| up to 2^14, within fp16's 65504
       s = ldexpf(1.f, min(max(14 - ex, -100), 100));
     }
-    a.head->rows = base;
+    a.head->rows = all;
     a.head->dz_scale = s;
+  }
+  const bool gather = all < a.T;
+  const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
+  int base = before;
+  for (int64_t t0 = ta; t0 < tb; t0 += kRowThreads) {
+    const int64_t t = t0 + threadIdx.x;
+    const bool in = t < tb && takes_part(a, t, kGrad);
+    const uint32_t m = __ballot_sync(0xffffffffu, in);
+    if (lane == 0) s_cnt[warp] = __popc(m);
+    __syncthreads();
+    int lower = 0, n = 0;
+    for (int w = 0; w < kW; ++w) {
+      if (w < warp) lower += s_cnt[w];
+      n += s_cnt[w];
+    }
+    if (in) {
+      const int r = lower + __popc(m & ((1u << lane) - 1u));
+      s_list[r] = (int)t;
+      a.idx[base + r] = (int)t;
+    } else if (!kGrad && t < tb) {
+      a.logp[t] = 0.f;
+      if (a.lse_out) a.lse_out[t] = 0.f;
+      if (a.ent_out) a.ent_out[t] = 0.f;
+    }
+    if (kGrad && a.dh) {  // rows without a gradient
+      for (uint32_t z = __ballot_sync(0xffffffffu, t < tb && !in); z; z &= z - 1u) {
+        uint16_t* dst = static_cast<uint16_t*>(a.dh) + (t0 + warp * 32 + __ffs(z) - 1) * a.dh_stride;
+        if (((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0) {
+          for (int c = lane; c < a.D / 8; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+          for (int c = a.D / 8 * 8 + lane; c < a.D; c += 32) dst[c] = 0;
+        } else {
+          for (int c = lane; c < a.D; c += 32) dst[c] = 0;
+        }
+      }
+    }
+    __syncthreads();
+    if (gather) {
+      for (int r = warp; r < n; r += kW) {
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + (int64_t)s_list[r] * a.hidden_stride);
+        uint4* dst = reinterpret_cast<uint4*>(a.hc + (int64_t)(base + r) * a.hc_stride);
+#pragma unroll 4
+        for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+      }
+    }
+    base += n;
+    __syncthreads();
+  }
+  if (gather && blockIdx.x == gridDim.x - 1) {
+    const int pad = (all + kTile16 - 1) / kTile16 * kTile16;
+    for (int r = all + warp; r < pad; r += kW)
+      for (int c = lane; c < chunks; c += 32) reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride)[c] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
-// Copies the listed rows together (where some token is left out), zeros up to the next k-step of the
-// d_weight product, and zeros the d_hidden rows of the others.
-template <bool kGrad>
-__global__ void __launch_bounds__(256) vocab_gather_kernel(VocabArgs a) {
-  const int rows = a.head->rows;
-  const bool gather = rows < a.T;
-  const int64_t pad = ((int64_t)rows + kTile16 - 1) / kTile16 * kTile16;
-  const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
-  for (int64_t r = blockIdx.x; r < max(pad, a.T); r += gridDim.x) {
-    if (gather && r < pad) {
-      uint4* dst = reinterpret_cast<uint4*>(a.hc + r * a.hc_stride);
-      if (r < rows) {
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + (int64_t)a.idx[r] * a.hidden_stride);
-        for (int c = threadIdx.x; c < chunks; c += blockDim.x) dst[c] = src[c];
-      } else {
-        for (int c = threadIdx.x; c < chunks; c += blockDim.x) dst[c] = make_uint4(0u, 0u, 0u, 0u);
-      }
+// d_hidden from the sums of its parts of k, added in order.
+__global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  const int rows = a.head->rows, quads = (a.D + 3) / 4;
+  const bool vec = ((a.dh_stride & 3) | (reinterpret_cast<uintptr_t>(a.dh) & 7)) == 0;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)rows * quads; i += (int64_t)gridDim.x * blockDim.x) {
+    const int row = (int)(i / quads), c = (int)(i - (int64_t)row * quads) * 4;
+    const float* p = a.acc + (int64_t)row * a.acc_stride + c;
+    float4 s = *reinterpret_cast<const float4*>(p);
+#pragma unroll 4
+    for (int k = 1; k < a.splits; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(p + k * a.acc_rows * a.acc_stride);
+      s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
     }
-    if (kGrad && a.dh && r < a.T && !takes_part(a, r, true)) {
-      uint16_t* dst = static_cast<uint16_t*>(a.dh) + r * a.dh_stride;
-      for (int c = threadIdx.x; c < a.D; c += blockDim.x) dst[c] = 0;
+    uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)a.idx[row] * a.dh_stride + c;
+    const uint2 o = make_uint2(pack16(s.x, s.y, a.f16), pack16(s.z, s.w, a.f16));
+    if (vec && c + 4 <= a.D) {
+      *reinterpret_cast<uint2*>(dst) = o;
+    } else {
+      const uint16_t h[4] = {(uint16_t)o.x, (uint16_t)(o.x >> 16), (uint16_t)o.y, (uint16_t)(o.y >> 16)};
+      for (int j = 0; j < 4 && c + j < a.D; ++j) dst[j] = h[j];
     }
   }
 }
 
 // ------------------------------------------------------------------ joining the parts of a row
-
-struct Part {
-  float m, s, u;
-};
-// Two parts of a row as one: sums relative to the larger maximum.
-template <bool kEnt>
-__device__ __forceinline__ Part join(const Part& x, const Part& y) {
-  const float m = fmaxf(x.m, y.m);
-  const float a = x.m - m, b = y.m - m, ca = exp2f(a), cb = exp2f(b);
-  Part r;
-  r.m = m;
-  r.s = ca * x.s + cb * y.s;
-  r.u = kEnt ? ca * (x.u + a * x.s) + cb * (y.u + b * y.s) : 0.f;
-  return r;
-}
-
-template <bool kEnt>
-__device__ __forceinline__ void finish(const VocabArgs& a, int64_t tok, float zy, const Part& p) {
-  const float top = fmaxf(p.m, zy), y = zy - top, c = p.m - top, ec = exp2f(c);
-  const float others = ec * p.s, total = others + exp2f(y);
-  const float ln2 = 0.6931471805599453f;
-  const float lt = y == 0.f ? log1pf(others) : logf(total);
-  a.logp[tok] = fmaf(y, ln2, -lt);
-  if (a.lse_out) a.lse_out[tok] = fmaf(top, ln2, lt);
-  if (kEnt) a.ent_out[tok] = lt - ln2 * (ec * (p.u + c * p.s) + exp2f(y) * y) / total;
-}
 
 constexpr int kJoinThreads = 256;
 
@@ -679,6 +731,11 @@ int g_pairs = 0;  // CTA pairs resident at one time
 
 template <int kMode>
 cudaError_t setup_mode() {
+  cudaFuncAttributes at;
+  const cudaError_t e = cudaFuncGetAttributes(&at, vocab_pair_kernel<kMode>);
+  if (e != cudaSuccess) return e;
+  // (a split that asks for more registers than the launch brings would wait for ever)
+  if (kMode != kProducts && at.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
   return cudaFuncSetAttribute(vocab_pair_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kVSmem);
 }
 
@@ -717,13 +774,9 @@ cudaError_t setup_vocab() {
 }
 
 cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad) {
-  if (grad) vocab_index_kernel<true><<<1, kIndexThreads, 0, lc.stream>>>(a, st);
-  else vocab_index_kernel<false><<<1, kIndexThreads, 0, lc.stream>>>(a, st);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess) return e;
-  const int grid = (int)min(a.T, (int64_t)lc.num_sms * 8);
-  if (grad) vocab_gather_kernel<true><<<grid, 256, 0, lc.stream>>>(a);
-  else vocab_gather_kernel<false><<<grid, 256, 0, lc.stream>>>(a);
+  const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
+  if (grad) vocab_rows_kernel<true><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else vocab_rows_kernel<false><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();
 }
 
@@ -748,8 +801,21 @@ cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const Vocab
   return a.ge ? launch_pair<kDzEnt>(lc, m, a, st, tiles_of(a.T, a.vn)) : launch_pair<kDz>(lc, m, a, st, tiles_of(a.T, a.vn));
 }
 
+// With few row tiles the k of d_hidden, the vocabulary, is cut into parts for as many pairs as its share of
+// the work is worth (300 tokens, 8191 x 512: one pair's sum over 8191 rows took 35 of the call's 67 us).
+int vocab_splits(int64_t T, int64_t vn, int64_t D) {
+  const int64_t dt = (D + kPairN - 1) / kPairN, mt = (T + kPairM - 1) / kPairM, kb = (vn + kTile16 - 1) / kTile16;
+  const int64_t work = mt * dt * kb + (vn + kPairN - 1) / kPairN * dt * ((T + kTile16 - 1) / kTile16);
+  const int64_t share = max(work / kVocabPairs, (int64_t)8);  // k-steps of one pair
+  return (int)max((int64_t)1, min(kb / share, (int64_t)kVocabMaxSplits));
+}
+
 cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {
-  return launch_pair<kProducts>(lc, m, a, st, (a.dh ? tiles_of(a.T, a.D) : 0) + (a.dw ? tiles_of(a.vn, a.D) : 0));
+  const cudaError_t e = launch_pair<kProducts>(lc, m, a, st, (a.dh ? tiles_of(a.T, a.D) * a.splits : 0) + (a.dw ? tiles_of(a.vn, a.D) : 0));
+  if (e != cudaSuccess || !a.last || a.splits == 1) return e;
+  const int64_t quads = a.T * ((a.D + 3) / 4);
+  vocab_parts_kernel<<<(unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream>>>(a, st);
+  return cudaGetLastError();
 }
 
 }  // namespace gpo

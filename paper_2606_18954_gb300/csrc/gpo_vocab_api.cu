@@ -17,9 +17,11 @@ constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 1024;  // tokens, vocabulary 
 constexpr int64_t kMaxMatrix = (int64_t)1 << 40;          // elements of a matrix
 
 struct VocabLayout {
-  size_t status, head, idx, hc, pm, ps, pu, tz, dz, acc, total;
+  size_t status, marks, head, idx, hc, pm, ps, pu, tz, dz, acc, total;
+  bool few;           // forward in one launch
   bool listed;        // only the tokens that take part are multiplied
   int64_t tp, hc_stride, piece, acc_stride;
+  int splits;
 };
 
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
@@ -36,15 +38,17 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L = VocabLayout();
   L.tp = up_to(T, kPairM);
   L.hc_stride = up_to(v.d, 8);
+  L.few = !grad && T <= kVocabFew;
   L.listed = grad || T > kVocabOneTile;
   L.status = take(sizeof(uint32_t) * kStatusWords);
+  if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);  // (next to the status words: cleared with them)
   L.head = take(sizeof(VocabHead));
   if (T > 0 && L.listed) {
     L.idx = take(sizeof(int) * (size_t)T);
     L.hc = take(2 * (size_t)(up_to(T, 64) * L.hc_stride));
   }
   if (T > 0 && !grad) {
-    const size_t parts = sizeof(float) * (size_t)(vocab_parts(v.vocab) * L.tp);
+    const size_t parts = sizeof(float) * (size_t)(L.few ? kVocabFewCtas * kVocabFew : vocab_parts(v.vocab) * L.tp);
     L.pm = take(parts);
     L.ps = take(parts);
     L.pu = take(parts);
@@ -57,7 +61,8 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
     L.piece = up_to((v.vocab + n - 1) / n, kPairN);
     L.acc_stride = up_to(v.d, 32);
     L.dz = take(2 * (size_t)(L.tp * L.piece));
-    if (L.piece < v.vocab) L.acc = take(sizeof(float) * (size_t)(L.tp * L.acc_stride));
+    L.splits = vocab_splits(T, std::min(L.piece, v.vocab), v.d);
+    if (L.piece < v.vocab || L.splits > 1) L.acc = take(sizeof(float) * (size_t)(L.splits * L.tp * L.acc_stride));
   }
   L.total = o;
 }
@@ -102,10 +107,11 @@ gpo_status check_call(gpo_ctx* c, const void* workspace, size_t have, size_t nee
   return GPO_OK;
 }
 
-bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16) {
+bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16,
+                int box_rows = 64) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)(stride * 2)};
-  const cuuint32_t box[2] = {64, 64}, estr[2] = {1, 1};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   return enc(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -120,8 +126,8 @@ struct Stages {
   Status st;
 
   // Signs the status words with a tag of the call's own; in a graph, whose replays would share it,
-  // the words are cleared instead.
-  Stages(gpo_ctx* c, void* stream, void* status) : ctx(c), n(0), e(cudaSuccess) {
+  // the words, and what else has to differ between calls (`bytes` in all), are cleared instead.
+  Stages(gpo_ctx* c, void* stream, void* status, size_t bytes = sizeof(uint32_t) * kStatusWords) : ctx(c), n(0), e(cudaSuccess) {
     lc.stream = static_cast<cudaStream_t>(stream);
     lc.num_sms = c->num_sms;
     st.p = static_cast<uint32_t*>(status);
@@ -130,7 +136,7 @@ struct Stages {
     if (cudaStreamIsCapturing(lc.stream, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone) {
       cudaGetLastError();
       st.tag = 0;
-      if (e == cudaSuccess) e = cudaMemsetAsync(st.p, 0, sizeof(uint32_t) * kStatusWords, lc.stream);
+      if (e == cudaSuccess) e = cudaMemsetAsync(st.p, 0, bytes, lc.stream);
     } else {
       st.tag = fresh_tag();
     }
@@ -178,8 +184,9 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
   a.debug_timeout = (ctx->params.flags & GPO_FLAG_DEBUG_TIMEOUT) != 0;
   EncodeTiledFn enc = encode_fn();
   if (!enc) return set_msg(ctx, "cuTensorMapEncodeTiled unavailable"), GPO_ERR_CUDA;
-  bool ok = encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16) &&
-            encode_map(&m.w, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16);
+  bool ok = encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16,
+                       L.few ? vocab_few_columns(a.T) : 64) &&
+            encode_map(&m.w, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, L.few ? 32 : 64);
   if (L.listed) ok = ok && encode_map(&m.hc, enc, a.hc, v.d, up_to(v.num_tokens, 64), L.hc_stride, a.f16);
   if (L.dz) ok = ok && encode_map(&m.dz, enc, at<void>(ws, L.dz), L.piece, L.tp, L.piece, a.f16);
   if (!ok) return set_msg(ctx, "cuTensorMapEncodeTiled failed"), GPO_ERR_UNSUPPORTED;
@@ -226,6 +233,13 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
   a.lse_out = out->lse;
   a.ent_out = out->entropy;
   const bool ent = out->entropy != nullptr;
+  if (L.few) {
+    Stages stage(ctx, stream, at<void>(workspace, L.status), L.marks - L.status + sizeof(uint64_t) * kVocabFewCtas);
+    stage("vocab_few", [&] {
+      return launch_vocab_few(stage.lc, m, a, stage.st, ent, at<uint64_t>(workspace, L.marks), stage.st.tag + 1);
+    });
+    return stage.done();
+  }
   Stages stage(ctx, stream, at<void>(workspace, L.status));
   if (L.listed) stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st, false); });
   stage("vocab_lse", [&] { return launch_vocab_lse(stage.lc, m, a, stage.st, ent); });
@@ -272,7 +286,9 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.dz = at<uint16_t>(workspace, L.dz);
   a.dz_stride = L.piece;
   a.acc = L.acc ? at<float>(workspace, L.acc) : nullptr;
+  a.acc_rows = L.tp;
   a.acc_stride = L.acc_stride;
+  a.splits = out->d_hidden ? L.splits : 1;
   a.dh = out->d_hidden;
   a.dh_stride = out->d_hidden_stride;
   a.dw = out->d_weight;

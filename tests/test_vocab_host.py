@@ -36,14 +36,17 @@ def embedding(B, **kw):
 
 def test_vocab_workspace(B):
     size = lambda grad=False, **kw: B.vocab_workspace_size(vocab(B, **kw), grad)  # noqa: E731
-    assert 0 < size(num_tokens=0) <= size(num_tokens=1) <= size(num_tokens=256) < size(num_tokens=257) < size(num_tokens=5000)
+    assert 0 < size(num_tokens=0) < size(num_tokens=1) == size(num_tokens=64)  # up to 64 tokens: one launch's own parts
+    assert size(num_tokens=65) <= size(num_tokens=256) < size(num_tokens=257) < size(num_tokens=5000)
     # never a whole [T x V] matrix: the gradient's largest part is a piece of 512 MiB at most
     big = dict(num_tokens=1 << 17, vocab=1 << 18, d=1024, hidden_stride=1024, weight_stride=1024)
     hidden = (1 << 17) * 1024
     assert size(True, **big) < (512 << 20) + 4 * hidden + 2 * hidden + (8 << 20)
     assert size(**big) < 2 * (1 << 17) * (1 << 18) // 4
-    # one piece needs no fp32 sums of d_hidden
-    assert size(True, num_tokens=4096, vocab=4096) < 2 * 4096 * 4096 + 3 * 4096 * 64 * 2
+    # fp32 sums of d_hidden: none with one piece and enough row tiles for the GPU, else at most 32 of them
+    wide = dict(num_tokens=4096, d=4096, hidden_stride=4096, weight_stride=4096)
+    assert size(True, vocab=8192, **wide) < 2 * 4096 * 8192 + 2 * 4096 * 4096 + (1 << 20)
+    assert size(True, num_tokens=300, vocab=100000) < 2 * 512 * 100352 + 32 * 4 * 512 * 64 + (1 << 20)
 
 
 @pytest.mark.parametrize("bad, code", [
