@@ -468,8 +468,8 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
 /* Token embedding: out_t = scale table[id_t], rounded once to the table's type; a row of zeros for
  * an id below 0 (no token); an id >= vocab is reported as for targets.
  * Its gradient: d_table_v = scale sum_{t: id_t = v} grad_t, the tokens of a row added in their
- * order in fp32 (in pieces of 32 of the tokens sorted by id, so that a frequent token's sum is
- * spread over the GPU): the same result on every run.  Rows without tokens are zeros, or keep
+ * order in fp32 (in pieces of the tokens sorted by id, of a length that depends on T alone, so
+ * that a frequent token's sum is spread over the GPU): the same result on every run.  Rows without tokens are zeros, or keep
  * what they hold with accumulate (a table tied to the vocabulary matrix: gpo_vocab_grads.d_weight). */
 typedef struct {
   int64_t num_tokens;   /* T >= 0 */

@@ -147,30 +147,39 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
+constexpr int kSortAhead = 8;  // ids of a lane in flight
 
 size_t sort_smem(int rows) { return sizeof(int) * (size_t)(kSortWarps + 1) * rows; }
 
-// CTA b owns the rows [b * per, (b + 1) * per) of the table.
-__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedArgs a, int per, Status st) {
+// CTA b owns the rows [b * per, (b + 1) * per) of the table.  (Id: a template, so that the loads of
+// one thread need no branch between them and are in flight together.)
+template <class Id>
+__global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(EmbedArgs a, int per, Status st) {
   extern __shared__ int hist[];  // [kSortWarps][per] counts, then places; [per] first place of a row
   __shared__ int wsum[kSortWarps];
   __shared__ int s_base;
   int* first = hist + kSortWarps * per;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t r0 = (int64_t)blockIdx.x * per, r1 = min(r0 + per, a.V);
+  const Id r0 = (Id)blockIdx.x * per, r1 = (Id)min((int64_t)r0 + per, a.V);
   const int nr = (int)(r1 - r0);
+  let_next_start();
+  const Id* ids = static_cast<const Id*>(a.ids);
   for (int i = threadIdx.x; i < kSortWarps * per; i += kSortThreads) hist[i] = 0;
   if (threadIdx.x == 0) s_base = 0;
   __syncthreads();
   const int64_t seg = ((a.T + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
   const int64_t ta = min(a.T, warp * seg), tb = min(a.T, ta + seg);
   int below = 0;
-#pragma unroll 4
-  for (int64_t t = ta + lane; t < tb; t += 32) {
-    const int64_t id = id_of(a.ids, a.id8, t);
-    if (id >= r0 && id < r1) atomicAdd(&hist[warp * per + (int)(id - r0)], 1);
-    below += id >= 0 && id < r0;
-    if (id >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 31, (int)t);
+  for (int64_t t0 = ta + lane; t0 < tb; t0 += 32 * kSortAhead) {
+    Id id[kSortAhead];
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) id[k] = t0 + 32 * k < tb ? ids[t0 + 32 * k] : (Id)-1;
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      if (id[k] >= r0 && id[k] < r1) atomicAdd(&hist[warp * per + (int)(id[k] - r0)], 1);
+      below += id[k] >= 0 && id[k] < r0;
+      if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 31, (int)(t0 + 32 * k));
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) below += __shfl_xor_sync(0xffffffffu, below, o);
@@ -200,26 +209,30 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(EmbedArgs a, i
     const int s = before + incl - total;
     first[i] = s;
     a.start[r0 + i] = s;
-    if (r0 + i == a.V - 1) a.start[a.V] = s + total;
+    if ((int64_t)r0 + i == a.V - 1) a.start[a.V] = s + total;
   }
   __syncthreads();
-  for (int64_t t0 = ta; t0 < tb; t0 += 32) {
-    const int64_t t = t0 + lane;
-    const int64_t id = t < tb ? id_of(a.ids, a.id8, t) : -1;
-    const bool in = id >= r0 && id < r1;
-    if (!__any_sync(0xffffffffu, in)) continue;
-    const int row = in ? (int)(id - r0) : -1 - lane;
-    const uint32_t same = __match_any_sync(0xffffffffu, row);
-    int at = 0;
-    if (in) at = hist[warp * per + row];
-    __syncwarp();
-    if (in) {
-      const int place = first[row] + at + __popc(same & ((1u << lane) - 1u));
-      a.perm[place] = (int)t;
-      a.sid[place] = (int)id;
-      if (lane == __ffs(same) - 1) hist[warp * per + row] = at + __popc(same);
+  for (int64_t t0 = ta + lane; t0 - lane < tb; t0 += 32 * kSortAhead) {
+    Id id[kSortAhead];
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) id[k] = t0 + 32 * k < tb ? ids[t0 + 32 * k] : (Id)-1;
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      const bool in = id[k] >= r0 && id[k] < r1;
+      if (!__any_sync(0xffffffffu, in)) continue;
+      const int row = in ? (int)(id[k] - r0) : -1;  // (few different values: match takes them one after another)
+      const uint32_t same = __match_any_sync(0xffffffffu, row);
+      int at = 0;
+      if (in) at = hist[warp * per + row];
+      __syncwarp();
+      if (in) {
+        const int place = first[row] + at + __popc(same & ((1u << lane) - 1u));
+        a.perm[place] = (int)(t0 + 32 * k);
+        a.sid[place] = (int)id[k];
+        if (lane == __ffs(same) - 1) hist[warp * per + row] = at + __popc(same);
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
@@ -236,6 +249,8 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
   const int64_t warp = (int64_t)blockIdx.x * (kSumThreads / 32) + (threadIdx.x >> 5);
   const int64_t nwarps = (int64_t)gridDim.x * (kSumThreads / 32);
   const int64_t blocks = (a.D + 32 * C::kPer - 1) / (32 * C::kPer);
+  let_next_start();
+  after_previous();
   const int n = a.start[a.V];
   const int64_t pieces = ((int64_t)n + piece - 1) / piece;
   const int64_t empties = a.accumulate ? 0 : (a.V + 31) / 32;  // groups of 32 rows that may have no token
@@ -300,7 +315,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
 }
 
 // Cut runs: a warp takes kJoinPieces pieces and 32 x 4 columns; a run belongs to the piece it starts in.
-constexpr int kJoinPieces = 8;
+constexpr int kJoinPieces = 2;
 constexpr int kJoinAhead = 8;
 
 template <int kType>
@@ -310,6 +325,7 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a, int piece)
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int64_t nwarps = (int64_t)gridDim.x * (blockDim.x >> 5);
+  after_previous();
   const int n = a.start[a.V];
   const int64_t pieces = ((int64_t)n + piece - 1) / piece;
   const int64_t blocks = (a.D + 127) / 128, groups = (pieces + kJoinPieces - 1) / kJoinPieces;
@@ -349,10 +365,6 @@ __global__ void __launch_bounds__(256) embed_join_kernel(EmbedArgs a, int piece)
   }
 }
 
-// Tokens of one piece: longer pieces leave fewer sums of a frequent token to join, shorter ones give
-// more warps something to do.
-int piece_of(int64_t T) { return T <= 16384 ? kEmbedPiece : T <= 65536 ? 2 * kEmbedPiece : 4 * kEmbedPiece; }
-
 inline bool vec_rows(const void* p, int64_t stride, int esz) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride * esz % 16 == 0;
 }
@@ -372,25 +384,28 @@ cudaError_t look(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
 template <int kType>
 cudaError_t sums(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
   const int esz = kType == GPO_DT_F32 ? 4 : 2;
-  const int piece = piece_of(a.T);
+  const int piece = embed_piece(a.T);
   const int64_t blocks = (a.D * esz + 511) / 512, pieces = (a.T + piece - 1) / piece;
   const int64_t units = (pieces + (a.accumulate ? 0 : (a.V + 31) / 32)) * blocks;
-  const int grid = (int)max((int64_t)1, min((units + 7) / 8, (int64_t)lc.num_sms * 4));
-  if (vec_rows(a.src, a.src_stride, esz) && vec_rows(a.dst, a.dst_stride, esz))
-    embed_sum_kernel<kType, true><<<grid, kSumThreads, 0, lc.stream>>>(a, piece, st);
-  else embed_sum_kernel<kType, false><<<grid, kSumThreads, 0, lc.stream>>>(a, piece, st);
-  cudaError_t e = cudaGetLastError();
+  const unsigned grid = (unsigned)max((int64_t)1, min((units + 7) / 8, (int64_t)lc.num_sms * 4));
+  const bool vec = vec_rows(a.src, a.src_stride, esz) && vec_rows(a.dst, a.dst_stride, esz);
+  const cudaError_t e = launch_after(vec ? embed_sum_kernel<kType, true> : embed_sum_kernel<kType, false>, grid, kSumThreads,
+                                     0, lc.stream, a, piece, st);
   if (e != cudaSuccess || pieces < 2) return e;
   const int64_t jobs = (pieces + kJoinPieces - 1) / kJoinPieces * ((a.D + 127) / 128);
-  embed_join_kernel<kType><<<(int)min((jobs + 7) / 8, (int64_t)lc.num_sms * 8), 256, 0, lc.stream>>>(a, piece);
-  return cudaGetLastError();
+  return launch_after(embed_join_kernel<kType>, (unsigned)min((jobs + 7) / 8, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a, piece);
 }
 
 }  // namespace
 
+// Longer pieces leave fewer sums of a frequent token to join, shorter ones give more warps something to do.
+int embed_piece(int64_t T) { return T <= 4096 ? 8 : T <= 16384 ? 32 : T <= 65536 ? 64 : 128; }
+
 cudaError_t setup_embed() {
-  return cudaFuncSetAttribute(embed_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)sort_smem(kEmbedMaxRows));
+  const int bytes = (int)sort_smem(kEmbedMaxRows);
+  const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(embed_sort_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
 cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
@@ -402,7 +417,9 @@ cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& 
 cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
   const int64_t want = (a.V + lc.num_sms - 1) / lc.num_sms;
   const int per = (int)min(max(want, (int64_t)32), (int64_t)kEmbedMaxRows);
-  embed_sort_kernel<<<(unsigned)((a.V + per - 1) / per), kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
+  const unsigned grid = (unsigned)((a.V + per - 1) / per);
+  if (a.id8) embed_sort_kernel<int64_t><<<grid, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
+  else embed_sort_kernel<int32_t><<<grid, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   if (a.dtype == GPO_DT_F32) return sums<GPO_DT_F32>(lc, a, st);

@@ -944,11 +944,38 @@ cudaError_t launch_loss_plan(const LaunchCtx& lc, const gpo_batch& b, const Size
 cudaError_t launch_token_loss(const LaunchCtx& lc, const LossPlan& lp, const LossArgs& a);
 cudaError_t setup_loss();
 
+// ------------------------------------------------------------------ kernels in a row
+
+// A kernel that launch_after starts while the one before it on the stream still runs: everything
+// that depends on that one comes after after_previous().  (Without a kernel before it, or started
+// otherwise, the wait is over at once.)
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The next kernel, if started by launch_after, may be brought onto the SMs from here on.
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <class... P, class... A>
+cudaError_t launch_after(void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, cudaStream_t stream,
+                         A&&... args) {
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(block);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // ------------------------------------------------------------------ vocabulary ends
 
 constexpr int kPairM = 256;      // rows of one tile of a CTA pair (tcgen05 M, both CTAs)
 constexpr int kPairN = 256;      // columns of one tile
-constexpr int kVocabOneTile = kPairM;  // tokens up to which the forward pass takes them as they are
+// Products (tokens x vocabulary x width) from which on the forward pass first lists the tokens with a target:
+// all of them take 145 us or more then, the list 10
+constexpr int64_t kVocabListed = (int64_t)1 << 37;
 constexpr int kVocabPairs = 76;      // CTA pairs that the split of d_hidden's k reckons with (GB300: 152 SMs)
 constexpr int kVocabMaxSplits = 32;
 int vocab_splits(int64_t T, int64_t vn, int64_t D);
@@ -1031,12 +1058,12 @@ struct EmbedArgs {
   int64_t dst_stride;
   int accumulate;
   // gradient: tokens sorted by id (stable), their ids, the first of every row of the table,
-  // and the sums of runs that pieces of kEmbedPiece tokens cut
+  // and the sums of runs that pieces of embed_piece tokens cut
   int *perm, *sid, *start;
   float* part;           // [pieces x 2 x part_stride]
   int64_t part_stride;
 };
-constexpr int kEmbedPiece = 32;
+int embed_piece(int64_t T);  // sorted tokens of one piece, for T tokens
 constexpr int kEmbedMaxRows = 1024;  // rows of the table that one CTA of the sort owns, at most
 
 cudaError_t setup_embed();

@@ -28,8 +28,10 @@ __device__ __forceinline__ uint32_t leader_addr(const void* p) {
   return r;
 }
 
+// Arrives on a barrier of the cluster without ordering this thread's memory accesses (a release would
+// wait for its stores): for accumulators that have been read, whose tcgen05.ld are complete.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {

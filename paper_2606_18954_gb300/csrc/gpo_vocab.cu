@@ -36,8 +36,13 @@ constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 4.
 constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
 // give back.  The shares add up to no more than the launch brings (setup_mode checks that).
-constexpr int kRegsLaunch = 168, kRegsFew = 72, kRegsMany = 216;
-static_assert(128 * kRegsFew + 256 * kRegsMany <= kVThreads * kRegsLaunch, "register split");
+// The split of each mode is one without spills: the loads' and the MMAs' lane would find theirs in an L1
+// that the epilogue's stores sweep, and fall behind the tensor cores.
+constexpr int kRegsLaunch = 168;
+__host__ __device__ constexpr int regs_few(int mode) { return mode == kDz || mode == kDzEnt ? 120 : 88; }
+__host__ __device__ constexpr int regs_many(int mode) { return mode == kDz || mode == kDzEnt ? 192 : 208; }
+static_assert(128 * regs_few(kDz) + 256 * regs_many(kDz) <= kVThreads * kRegsLaunch &&
+              128 * regs_few(kLse) + 256 * regs_many(kLse) <= kVThreads * kRegsLaunch, "register split");
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
 constexpr int kVStage = 4 * kVBox;                 // A and B halves of one k-step, per CTA
 constexpr int kVCols = 512;                        // two accumulators of 256 columns
@@ -162,6 +167,13 @@ __device__ __forceinline__ bool next_tile(const Plan& q, int s, Tile& t) {
   return true;
 }
 
+// 32 bytes, 32-byte aligned: one whole sector.
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]),
+               "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7])
+               : "memory");
+}
+
 // 16 bits of 32 consecutive columns of a row to memory, those below `cols`.
 __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int cols, bool vec, int f16, bool add) {
   if (vec && cols >= 32) {
@@ -201,11 +213,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  const int rows = a.idx ? a.head->rows : (int)a.T;
-  const Plan plan = make_plan<kMode>(a, rows);
   constexpr int seg = segment_of<kMode>();
-  const CUtensorMap* hmap = a.idx && rows < a.T ? &maps.hc : &maps.h;
 
+  let_next_start();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kVStages; ++s) {
       mbar_init(&ctl->full[s], 1);
@@ -227,9 +237,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;
+  after_previous();
+  const int rows = a.idx ? a.head->rows : (int)a.T;
+  const Plan plan = make_plan<kMode>(a, rows);
+  const CUtensorMap* hmap = a.idx && rows < a.T ? &maps.hc : &maps.h;
 
   if (warp < 4) {
-  if (kMode != kProducts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+  if (kMode != kProducts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(regs_few(kMode)));
   if (warp == kLoadWarp) {
     // ------------------------------------------------------------ loads (lane 0 of either CTA: its halves)
     if (lane == 0) {
@@ -330,7 +344,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   }
   } else {
     // ------------------------------------------------------------ epilogue
-    if (kMode != kProducts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsMany));
+    if (kMode != kProducts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
     const int q = warp & 3, half = (warp - 4) >> 2;  // tensor memory lanes 32 q .., columns 128 half ..
     const int r = (int)rank * (kPairM / 2) + q * 32 + lane;  // row in the tile
     const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (kPairN / 2));
@@ -440,23 +454,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
             if (kMode == kLseEnt) a.pu[at] = (u4[0] + u4[1]) + (u4[2] + u4[3]);
           }
         } else {
-          uint4* dst = reinterpret_cast<uint4*>(a.dz + (int64_t)row * a.dz_stride + n0);
+          uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
           const int cols = live ? (int)a.vn - n0 : 0;
 #pragma unroll
-          for (int c = 0; c < kPairN / 2; c += 8) {
-            float y[8];
+          for (int c = 0; c < kPairN / 2; c += 16) {
+            uint32_t o[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int j = c + i;
-              const float d = fmaf(z[j], a.sl2, -l2);  // log2 p
-              const float p = ex2(d);
-              float v = (j == tgt ? g : 0.f) - g * p;
-              if (kMode == kDzEnt) v = fmaf(-e * p, fmaf(d, 0.6931471805599453f, ent), v);
-              // (p of a padding row or column is no probability, and its row may hold anything)
-              y[i] = j < cols ? v : 0.f;
+            for (int i = 0; i < 16; i += 2) {
+              float y[2];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const int j = c + i + h;
+                const float d = fmaf(z[j], a.sl2, -l2);  // log2 p
+                const float p = ex2(d);
+                float v = (j == tgt ? g : 0.f) - g * p;
+                if (kMode == kDzEnt) v = fmaf(-e * p, fmaf(d, 0.6931471805599453f, ent), v);
+                // (p of a padding row or column is no probability, and its row may hold anything)
+                y[h] = j < cols ? v : 0.f;
+              }
+              o[i / 2] = pack16(y[0], y[1], a.f16);
             }
-            dst[c / 8] = make_uint4(pack16(y[0], y[1], a.f16), pack16(y[2], y[3], a.f16), pack16(y[4], y[5], a.f16),
-                                    pack16(y[6], y[7], a.f16));
+            st_global_32(dst + c, o);
           }
         }
       } else {
@@ -529,35 +547,47 @@ __device__ __forceinline__ bool takes_part(const VocabArgs& a, int64_t t, bool g
   return !grad || a.g[t] != 0.f || (a.ge && a.ge[t] != 0.f);
 }
 
-constexpr int kRowThreads = 512;
+constexpr int kRowThreads = 1024;
+constexpr int kRowAhead = 8;  // tokens of a thread in flight
 
 // The list of the tokens that take part, in order, their number, the scale of an fp16 dz, their hidden
 // rows copied together (where some token is left out) with zeros up to the next k-step of the
 // d_weight product, and the zeros of the others' results.  Every CTA looks at all tokens (a few
 // bytes each) to know how many take part, and how many before its own share of them: one launch
 // and no exchange.
-template <bool kGrad>
+// (Id: a template, so that the loads of one thread need no branch between them.)
+template <bool kGrad, class Id>
 __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, Status st) {
   constexpr int kW = kRowThreads / 32;
   __shared__ int s_before[kW], s_all[kW], s_cnt[kW];
   __shared__ float s_big[kW];
   __shared__ int s_list[kRowThreads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  let_next_start();
   const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
+  const Id* target = static_cast<const Id*>(a.target);
+  const int64_t te = kGrad && a.ge ? a.T : 0;  // (entropy gradients that there are)
   int before = 0, all = 0;
   float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
-#pragma unroll 4
-  for (int64_t t = threadIdx.x; t < a.T; t += kRowThreads) {
-    const int64_t id = load_id(a.target, a.id8, t);
-    bool in = id >= 0 && id < a.V;
-    if (kGrad) {
-      const float g = a.g[t], e = a.ge ? a.ge[t] : 0.f;
-      in = in && (g != 0.f || e != 0.f);
-      if (in) bound = fmaxf(bound, fabsf(g) + 24.f * fabsf(e));
+  for (int64_t t0 = threadIdx.x; t0 < a.T; t0 += kRowAhead * kRowThreads) {
+    Id id[kRowAhead];
+    float g[kRowAhead], e[kRowAhead];
+#pragma unroll
+    for (int k = 0; k < kRowAhead; ++k) {
+      const int64_t t = t0 + k * kRowThreads;
+      id[k] = t < a.T ? target[t] : (Id)-1;
+      g[k] = kGrad && t < a.T ? a.g[t] : 1.f;
+      e[k] = kGrad && t < te ? a.ge[t] : 0.f;
     }
-    if (id >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)t);
-    all += in;
-    before += in && t < ta;
+#pragma unroll
+    for (int k = 0; k < kRowAhead; ++k) {
+      const int64_t t = t0 + k * kRowThreads;
+      const bool in = id[k] >= 0 && id[k] < a.V && (!kGrad || g[k] != 0.f || e[k] != 0.f);
+      if (kGrad && in) bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
+      if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)t);
+      all += in;
+      before += in && t < ta;
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -626,7 +656,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
       for (int r = warp; r < n; r += kW) {
         const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + (int64_t)s_list[r] * a.hidden_stride);
         uint4* dst = reinterpret_cast<uint4*>(a.hc + (int64_t)(base + r) * a.hc_stride);
-#pragma unroll 4
+#pragma unroll 8
         for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
       }
     }
@@ -642,6 +672,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
 
 // d_hidden from the sums of its parts of k, added in order.
 __global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st) {
+  after_previous();
   if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   const int rows = a.head->rows, quads = (a.D + 3) / 4;
   const bool vec = ((a.dh_stride & 3) | (reinterpret_cast<uintptr_t>(a.dh) & 7)) == 0;
@@ -674,6 +705,7 @@ template <bool kEnt>
 __global__ void __launch_bounds__(kJoinThreads) vocab_join_row_kernel(VocabArgs a, int parts, Status st) {
   __shared__ Part red[kJoinThreads / 32];
   const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  after_previous();
   const int64_t id = load_id(a.target, a.id8, row);
   if (row == 0 && threadIdx.x == 0) sign_status(st);
   if (id < 0 || id >= a.V) {
@@ -708,7 +740,8 @@ template <bool kEnt>
 __global__ void __launch_bounds__(1024) vocab_join_kernel(VocabArgs a, int parts, Status st) {
   __shared__ Part red[32][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int row = blockIdx.x * 32 + lane, rows = a.head->rows;
+  after_previous();
+  const int row = blockIdx.x * 32 + lane, rows = a.idx ? a.head->rows : (int)a.T;
   if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   if (blockIdx.x * 32 >= rows) return;
   Part p = {kLow, 0.f, 0.f};
@@ -722,8 +755,17 @@ __global__ void __launch_bounds__(1024) vocab_join_kernel(VocabArgs a, int parts
   red[warp][lane] = p;
   __syncthreads();
   if (warp == 0 && row < rows) {
-    for (int w = 1; w < 32; ++w) p = join<kEnt>(p, red[w][lane]);
-    finish<kEnt>(a, a.idx[row], a.tz[row], p);
+    const int64_t tok = a.idx ? a.idx[row] : row;
+    const int64_t id = load_id(a.target, a.id8, tok);
+    if (id >= 0 && id < a.V) {
+      for (int w = 1; w < 32; ++w) p = join<kEnt>(p, red[w][lane]);
+      finish<kEnt>(a, tok, a.tz[row], p);
+    } else {  // (every token is multiplied)
+      if (id >= a.V) report(st, GPO_ERR_SHAPE, 26, row);
+      a.logp[tok] = 0.f;
+      if (a.lse_out) a.lse_out[tok] = 0.f;
+      if (kEnt) a.ent_out[tok] = 0.f;
+    }
   }
 }
 
@@ -742,8 +784,7 @@ cudaError_t setup_mode() {
 template <int kMode>
 cudaError_t launch_pair(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, int64_t tiles) {
   const int64_t pairs = min((int64_t)g_pairs, max(tiles, (int64_t)1));
-  vocab_pair_kernel<kMode><<<(unsigned)(2 * pairs), kVThreads, kVSmem, lc.stream>>>(m, a, st);
-  return cudaGetLastError();
+  return launch_after(vocab_pair_kernel<kMode>, (unsigned)(2 * pairs), kVThreads, kVSmem, lc.stream, m, a, st);
 }
 
 int64_t tiles_of(int64_t rows, int64_t cols) { return ((rows + kPairM - 1) / kPairM) * ((cols + kPairN - 1) / kPairN); }
@@ -775,8 +816,10 @@ cudaError_t setup_vocab() {
 
 cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad) {
   const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
-  if (grad) vocab_rows_kernel<true><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
-  else vocab_rows_kernel<false><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  if (grad && a.id8) vocab_rows_kernel<true, int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else if (grad) vocab_rows_kernel<true, int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else if (a.id8) vocab_rows_kernel<false, int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else vocab_rows_kernel<false, int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();
 }
 
@@ -786,15 +829,11 @@ cudaError_t launch_vocab_lse(const LaunchCtx& lc, const VocabMaps& m, const Voca
 
 cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool ent) {
   const int parts = (int)vocab_parts(a.V);
-  if (!a.idx) {
-    if (ent) vocab_join_row_kernel<true><<<(unsigned)a.T, kJoinThreads, 0, lc.stream>>>(a, parts, st);
-    else vocab_join_row_kernel<false><<<(unsigned)a.T, kJoinThreads, 0, lc.stream>>>(a, parts, st);
-  } else {
-    const unsigned grid = (unsigned)((a.T + 31) / 32);
-    if (ent) vocab_join_kernel<true><<<grid, 1024, 0, lc.stream>>>(a, parts, st);
-    else vocab_join_kernel<false><<<grid, 1024, 0, lc.stream>>>(a, parts, st);
-  }
-  return cudaGetLastError();
+  if (a.part_col == 1)
+    return launch_after(ent ? vocab_join_row_kernel<true> : vocab_join_row_kernel<false>, (unsigned)a.T, kJoinThreads, 0,
+                        lc.stream, a, parts, st);
+  return launch_after(ent ? vocab_join_kernel<true> : vocab_join_kernel<false>, (unsigned)((a.T + 31) / 32), 1024, 0,
+                      lc.stream, a, parts, st);
 }
 
 cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {
@@ -814,8 +853,7 @@ cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const
   const cudaError_t e = launch_pair<kProducts>(lc, m, a, st, (a.dh ? tiles_of(a.T, a.D) * a.splits : 0) + (a.dw ? tiles_of(a.vn, a.D) : 0));
   if (e != cudaSuccess || !a.last || a.splits == 1) return e;
   const int64_t quads = a.T * ((a.D + 3) / 4);
-  vocab_parts_kernel<<<(unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream>>>(a, st);
-  return cudaGetLastError();
+  return launch_after(vocab_parts_kernel, (unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a, st);
 }
 
 }  // namespace gpo

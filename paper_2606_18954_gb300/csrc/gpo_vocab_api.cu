@@ -39,7 +39,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L.tp = up_to(T, kPairM);
   L.hc_stride = up_to(v.d, 8);
   L.few = !grad && T <= kVocabFew;
-  L.listed = grad || T > kVocabOneTile;
+  L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
   L.status = take(sizeof(uint32_t) * kStatusWords);
   if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);  // (next to the status words: cleared with them)
   L.head = take(sizeof(VocabHead));
@@ -227,8 +227,9 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
   a.ps = at<float>(workspace, L.ps);
   a.pu = at<float>(workspace, L.pu);
   a.tz = at<float>(workspace, L.tz);
-  a.part_row = L.listed ? 1 : vocab_parts(v->vocab);
-  a.part_col = L.listed ? L.tp : 1;
+  const bool by_row = v->num_tokens <= kPairM;  // the parts of a row side by side: one CTA joins them
+  a.part_row = by_row ? vocab_parts(v->vocab) : 1;
+  a.part_col = by_row ? 1 : L.tp;
   a.logp = out->logp;
   a.lse_out = out->lse;
   a.ent_out = out->entropy;
@@ -330,7 +331,8 @@ void embed_layout(const gpo_embedding& e, bool grad, EmbedLayout& L) {
     L.perm = take(sizeof(int) * (size_t)e.num_tokens);
     L.sid = take(sizeof(int) * (size_t)e.num_tokens);
     L.start = take(sizeof(int) * (size_t)(e.vocab + 1));
-    L.part = take(sizeof(float) * 2 * (size_t)((e.num_tokens + kEmbedPiece - 1) / kEmbedPiece * L.part_stride));
+    const int piece = embed_piece(e.num_tokens);
+    L.part = take(sizeof(float) * 2 * (size_t)((e.num_tokens + piece - 1) / piece * L.part_stride));
   }
   L.total = o;
 }
