@@ -1011,6 +1011,10 @@ struct VocabArgs {
   float *logp, *lse_out, *ent_out;
   // gradient
   const float *lse, *g, *ent, *ge;
+  const void* weight;
+  int64_t weight_stride;
+  int* by_target;        // the rows' targets, ascending (the gradient's rows are in that order)
+  float* rest;           // [rows] what rounding took from the row's dz at its target
   uint16_t* dz;          // [rows up to a tile x dz_stride] of the piece [v0, v0 + vn) of the vocabulary
   int64_t dz_stride;
   int64_t v0, vn;
@@ -1033,8 +1037,10 @@ struct VocabMaps {
 };
 
 cudaError_t setup_vocab();
-// The tokens that take part (grad: those with a gradient), their hidden rows, and the zeros of the others.
-cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad);
+// The tokens with a target, their hidden rows, and the zeros of the others.
+cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
+// The same of the tokens with a gradient, in the order of their targets.
+cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
 // Up to kVocabFew tokens; marks: [kVocabFewCtas] in the workspace, mark: a value that no other call leaves there.
 cudaError_t setup_vocab_few();
 int vocab_few_columns(int64_t T);

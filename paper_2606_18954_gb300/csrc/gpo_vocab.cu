@@ -31,7 +31,8 @@ namespace {
 enum Mode { kLse, kLseEnt, kDz, kDzEnt, kProducts };
 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
-constexpr int kVStages = 6;
+constexpr int kVStages = 6;                        // of the logits
+constexpr int kPStages = 5;                        // of the products, beside their epilogue's sums
 constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 4..11 epilogue
 constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
@@ -56,6 +57,7 @@ template <int kMode>
 __device__ __forceinline__ constexpr int segment_of() {
   return kMode == kProducts ? 1 << 30 : kMode == kDz || kMode == kDzEnt ? kSegDz : kSegLse;
 }
+constexpr int kNoKey = 0x7fffffff;                 // above every target: a token without a gradient
 constexpr int kRaster = 32;                        // row tiles that share one pass over the columns
 
 struct __align__(8) VocabCtl {
@@ -67,7 +69,12 @@ struct __align__(8) VocabCtl {
   uint32_t tmem_base;
 };
 
-constexpr size_t kVSmem = ((sizeof(VocabCtl) + 15) & ~size_t(15)) + 1023 + (size_t)kVStages * kVStage;
+// Per epilogue warp of the products: sums of 32 rows x 32 columns (see add_rests).
+constexpr int kRestRow = 33;
+constexpr size_t kRestBytes = sizeof(float) * 32 * kRestRow * kVEpiWarps;
+constexpr size_t kVSmem = ((sizeof(VocabCtl) + 15) & ~size_t(15)) + 1023 +
+                          ((size_t)kVStages * kVStage > (size_t)kPStages * kVStage + kRestBytes
+                               ? (size_t)kVStages * kVStage : (size_t)kPStages * kVStage + kRestBytes);
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int f16) {
   if (f16) {
@@ -201,6 +208,79 @@ __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int
     if (c < cols) dst[c] = round16(add ? x[c] + widen16(dst[c], f16) : x[c], f16);
 }
 
+// The first of n ascending numbers that is not below v, by one warp.
+__device__ __forceinline__ int first_not_below(const int* x, int n, int v, int lane) {
+  int lo = 0, hi = n;
+  while (hi - lo > 32) {
+    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
+    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && x[at] < v));
+    lo += below * step;
+    hi = min(hi, lo + step);
+  }
+  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && x[lo + lane] < v));
+}
+
+// y[j] += w x[j] for 32 columns of a row of hidden or weight, those below `cols` rounded up to 8 (the
+// row has them; what lies past its width is not used).
+__device__ __forceinline__ void add_row(const uint16_t* x, float w, int cols, int f16, float (&y)[32]) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 8) {
+    if (c < cols) {
+      const uint4 u = *reinterpret_cast<const uint4*>(x + c);
+      const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[c + 2 * i] = fmaf(w, widen16((uint16_t)(h[i] & 0xFFFFu), f16), y[c + 2 * i]);
+        y[c + 2 * i + 1] = fmaf(w, widen16((uint16_t)(h[i] >> 16), f16), y[c + 2 * i + 1]);
+      }
+    }
+  }
+}
+
+// Of a token's dz the target's entry is by far the largest part.  Its rounding to 16 bits would add 40 % to
+// the error that the gradients' own rounding leaves (the other entries' adds 1 %), so what that rounding takes away
+// (a.rest) is kept in fp32 and added in the products' epilogues: for d_hidden a row of the vocabulary
+// matrix per token (add_row), for d_weight the hidden rows of the tokens whose targets a warp's 32 rows are,
+// [ra, rb) in the order of their targets.  Where one row has more than kFewRests of them, by this:
+// a lane takes a column, the tokens one after another, eight in flight, each row's sum in a register until its
+// last token; then through shared memory to the rows' lanes.
+constexpr int kFewRests = 3;
+__device__ __forceinline__ void add_rests(const VocabArgs& a, float* sums, int ra, int rb, int v, int c0, int lane,
+                                          float (&y)[32]) {
+#pragma unroll
+  for (int j = 0; j < 32; ++j) sums[j * kRestRow + lane] = 0.f;
+  const bool in = c0 + lane < a.D;
+  const uint16_t* h = a.hc + (in ? c0 + lane : 0);
+  float s = 0.f;
+  int row = a.by_target[ra];
+  for (int r = ra; r < rb; r += 8) {
+    uint16_t x[8];
+    float w[8];
+    int at[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int rk = min(r + k, rb - 1);
+      x[k] = h[(int64_t)rk * a.hc_stride];
+      w[k] = r + k < rb ? a.rest[rk] : 0.f;
+      at[k] = a.by_target[rk];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (at[k] != row) {
+        sums[(row - v) * kRestRow + lane] = s;
+        s = 0.f;
+        row = at[k];
+      }
+      s = fmaf(w[k], widen16(x[k], a.f16), s);
+    }
+  }
+  sums[(row - v) * kRestRow + lane] = s;
+  __syncwarp();
+#pragma unroll
+  for (int j = 0; j < 32; ++j) y[j] += sums[lane * kRestRow + j];
+  __syncwarp();
+}
+
 template <int kMode>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     vocab_pair_kernel(const __grid_constant__ VocabMaps maps, VocabArgs a, Status st) {
@@ -210,6 +290,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   constexpr uint32_t kCtlBytes = (sizeof(VocabCtl) + 15) & ~15u;
   const uint32_t tiles = (sbase + kCtlBytes + 1023u) & ~1023u;  // the same offset in both CTAs
   constexpr bool kLogits = kMode == kLse || kMode == kLseEnt;
+  constexpr int kStages = kMode == kProducts ? kPStages : kVStages;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
@@ -217,7 +298,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
 
   let_next_start();
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kVStages; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctl->full[s], 1);
       mbar_init(&ctl->empty[s], 1);
     }
@@ -240,7 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   after_previous();
   const int rows = a.idx ? a.head->rows : (int)a.T;
   const Plan plan = make_plan<kMode>(a, rows);
-  const CUtensorMap* hmap = a.idx && rows < a.T ? &maps.hc : &maps.h;
+  const CUtensorMap* hmap = a.idx && (!kLogits || rows < a.T) ? &maps.hc : &maps.h;
 
   if (warp < 4) {
   if (kMode != kProducts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(regs_few(kMode)));
@@ -277,7 +358,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
             if (!b_mn) tma_load_2d_pair(sb + h * kVBox, mb, bar, kx, v0 + bn + h * kTile16);
             else tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, (t.job == 0 ? v0 : 0) + kx);
           }
-          if (++stage == kVStages) {
+          if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
@@ -285,8 +366,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
       }
       // wind-down: the copies land before the CTAs may exit
       if (rank == 0)
-        for (uint32_t s = 0; s < kVStages; ++s)
-          if (s < issued) mbar_wait(&ctl->full[s], (issued - 1 - s) / kVStages & 1u, st, 21, 200000000ull, false);
+        for (uint32_t s = 0; s < kStages; ++s)
+          if (s < issued) mbar_wait(&ctl->full[s], (issued - 1 - s) / kStages & 1u, st, 21, 200000000ull, false);
     }
     __syncwarp();
   } else if (warp == kMmaWarp) {
@@ -328,7 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           for (uint32_t kk = 0; kk < kTile16 / 16; ++kk)
             mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, (k - (int)k0 | (int)kk) != 0);
           mma_commit_pair(&ctl->empty[stage]);
-          if (++stage == kVStages) {
+          if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
@@ -456,6 +537,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
         } else {
           uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
           const int cols = live ? (int)a.vn - n0 : 0;
+          float vt = 0.f;
 #pragma unroll
           for (int c = 0; c < kPairN / 2; c += 16) {
             uint32_t o[8];
@@ -469,6 +551,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
                 const float p = ex2(d);
                 float v = (j == tgt ? g : 0.f) - g * p;
                 if (kMode == kDzEnt) v = fmaf(-e * p, fmaf(d, 0.6931471805599453f, ent), v);
+                if (j == tgt) vt = v;
                 // (p of a padding row or column is no probability, and its row may hold anything)
                 y[h] = j < cols ? v : 0.f;
               }
@@ -476,9 +559,42 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
             }
             st_global_32(dst + c, o);
           }
+          // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
+          if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
         }
       } else {
         const bool live = row < (t.job == 1 ? (int)a.vn : rows);
+        float* rests = reinterpret_cast<float*>(smem_raw + (tiles - sbase) + kPStages * kVStage) + (warp - 4) * 32 * kRestRow;
+        int ra = 0, rb = 0, na = 0, nb = 0;  // d_weight: the tokens whose targets are rows of this warp, of this lane
+        float rest = 0.f;                    // d_hidden: the row's own
+        const uint16_t* wrow = nullptr;
+        if (t.job == 1) {
+          const int v = (int)a.v0 + t.m0 + (int)rank * (kPairM / 2) + q * 32;
+          ra = first_not_below(a.by_target, rows, v, lane);
+          for (rb = ra; rb < rows; rb += 32) {  // (few tokens' targets are near each other)
+            const int y = rb + lane < rows ? a.by_target[rb + lane] : kNoKey;
+            const int in = __popc(__ballot_sync(0xffffffffu, y < v + 32));
+            for (int k = 0; k < in; ++k) {
+              const int yk = __shfl_sync(0xffffffffu, y, k);
+              if (yk < v + lane) ++na;
+              if (yk <= v + lane) ++nb;
+            }
+            if (in < 32) {
+              rb += in;
+              break;
+            }
+          }
+          rb = min(rb, rows);
+          na += ra;
+          nb += ra;
+        } else if (live && t.split == 0) {
+          const int y = a.by_target[row];
+          if (y >= a.v0 && y < a.v0 + a.vn) {
+            rest = a.rest[row];
+            wrow = static_cast<const uint16_t*>(a.weight) + (int64_t)y * a.weight_stride;
+          }
+        }
+        const bool few = __all_sync(0xffffffffu, nb - na <= kFewRests);
         if (!ready(sum)) break;
         const float f = t.kb > 0 ? a.scale / a.head->dz_scale : 0.f;
 #pragma unroll 1
@@ -489,10 +605,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
           tmem_wait_ld();
           if (ch == kPairN / 2 / 32 - 1) release(sum);
           const int c0 = n0 + ch * 32;
+          const int cols = a.D - c0;
           float y[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) * f : 0.f;  // (no tokens: no product ran)
-          const int cols = a.D - c0;
+          for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
+          if (!few) add_rests(a, rests, ra, rb, (int)a.v0 + t.m0 + (int)rank * (kPairM / 2) + q * 32, c0, lane, y);
+          else
+            for (int r = na; r < nb; ++r) add_row(a.hc + (int64_t)r * a.hc_stride + c0, a.rest[r], cols, a.f16, y);
+          if (rest != 0.f) add_row(wrow + c0, rest, cols, a.f16, y);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) y[j] *= f;
           if (live && cols > 0 && t.job == 0) {
             const bool out = a.last && a.splits == 1;  // the whole sum
             if (!(a.first && out)) {  // several pieces or parts of k: the sums so far in fp32
@@ -541,115 +663,69 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
 
 // ------------------------------------------------------------------ tokens that take part
 
-__device__ __forceinline__ bool takes_part(const VocabArgs& a, int64_t t, bool grad) {
-  const int64_t id = load_id(a.target, a.id8, t);
-  if (id < 0 || id >= a.V) return false;
-  return !grad || a.g[t] != 0.f || (a.ge && a.ge[t] != 0.f);
-}
-
 constexpr int kRowThreads = 1024;
 constexpr int kRowAhead = 8;  // tokens of a thread in flight
 
-// The list of the tokens that take part, in order, their number, the scale of an fp16 dz, their hidden
-// rows copied together (where some token is left out) with zeros up to the next k-step of the
-// d_weight product, and the zeros of the others' results.  Every CTA looks at all tokens (a few
-// bytes each) to know how many take part, and how many before its own share of them: one launch
-// and no exchange.
+// Forward: the list of the tokens with a target, in order, their number, their hidden rows copied
+// together (where some token is left out), and the zeros of the others' results.  Every CTA looks
+// at all tokens (a few bytes each) to know how many take part, and how many before its own share of
+// them: one launch and no exchange.
 // (Id: a template, so that the loads of one thread need no branch between them.)
-template <bool kGrad, class Id>
+template <class Id>
 __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, Status st) {
   constexpr int kW = kRowThreads / 32;
   __shared__ int s_before[kW], s_all[kW], s_cnt[kW];
-  __shared__ float s_big[kW];
   __shared__ int s_list[kRowThreads];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   let_next_start();
   const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
   const Id* target = static_cast<const Id*>(a.target);
-  const int64_t te = kGrad && a.ge ? a.T : 0;  // (entropy gradients that there are)
   int before = 0, all = 0;
-  float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
   for (int64_t t0 = threadIdx.x; t0 < a.T; t0 += kRowAhead * kRowThreads) {
     Id id[kRowAhead];
-    float g[kRowAhead], e[kRowAhead];
+#pragma unroll
+    for (int k = 0; k < kRowAhead; ++k) id[k] = t0 + k * kRowThreads < a.T ? target[t0 + k * kRowThreads] : (Id)-1;
 #pragma unroll
     for (int k = 0; k < kRowAhead; ++k) {
       const int64_t t = t0 + k * kRowThreads;
-      id[k] = t < a.T ? target[t] : (Id)-1;
-      g[k] = kGrad && t < a.T ? a.g[t] : 1.f;
-      e[k] = kGrad && t < te ? a.ge[t] : 0.f;
-    }
-#pragma unroll
-    for (int k = 0; k < kRowAhead; ++k) {
-      const int64_t t = t0 + k * kRowThreads;
-      const bool in = id[k] >= 0 && id[k] < a.V && (!kGrad || g[k] != 0.f || e[k] != 0.f);
-      if (kGrad && in) bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
+      const bool in = id[k] >= 0 && id[k] < a.V;
       if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)t);
       all += in;
       before += in && t < ta;
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    all += __shfl_xor_sync(0xffffffffu, all, o);
-    before += __shfl_xor_sync(0xffffffffu, before, o);
-    bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
-  }
+  all = __reduce_add_sync(0xffffffffu, all);
+  before = __reduce_add_sync(0xffffffffu, before);
   if (lane == 0) {
     s_all[warp] = all;
     s_before[warp] = before;
-    s_big[warp] = bound;
   }
   __syncthreads();
-  all = before = 0;
-  for (int w = 0; w < kW; ++w) {
-    all += s_all[w];
-    before += s_before[w];
-    bound = fmaxf(bound, s_big[w]);
-  }
+  all = __reduce_add_sync(0xffffffffu, s_all[lane]);
+  int base = __reduce_add_sync(0xffffffffu, s_before[lane]);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    float s = 1.f;
-    if (kGrad && a.f16 && bound > 0.f && isfinite(bound)) {
-      int ex;
-      frexpf(bound, &ex);  // bound <= 2^ex: |dz| up to 2^14, within fp16's 65504
-      s = ldexpf(1.f, min(max(14 - ex, -100), 100));
-    }
     a.head->rows = all;
-    a.head->dz_scale = s;
+    a.head->dz_scale = 1.f;
   }
   const bool gather = all < a.T;
   const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
-  int base = before;
   for (int64_t t0 = ta; t0 < tb; t0 += kRowThreads) {
     const int64_t t = t0 + threadIdx.x;
-    const bool in = t < tb && takes_part(a, t, kGrad);
+    const Id id = t < tb ? target[t] : (Id)-1;
+    const bool in = id >= 0 && id < a.V;
     const uint32_t m = __ballot_sync(0xffffffffu, in);
     if (lane == 0) s_cnt[warp] = __popc(m);
     __syncthreads();
-    int lower = 0, n = 0;
-    for (int w = 0; w < kW; ++w) {
-      if (w < warp) lower += s_cnt[w];
-      n += s_cnt[w];
-    }
+    const int n = __reduce_add_sync(0xffffffffu, s_cnt[lane]);
+    const int lower = __reduce_add_sync(0xffffffffu, lane < warp ? s_cnt[lane] : 0);
     if (in) {
       const int r = lower + __popc(m & ((1u << lane) - 1u));
       s_list[r] = (int)t;
       a.idx[base + r] = (int)t;
-    } else if (!kGrad && t < tb) {
+    } else if (t < tb) {
       a.logp[t] = 0.f;
       if (a.lse_out) a.lse_out[t] = 0.f;
       if (a.ent_out) a.ent_out[t] = 0.f;
-    }
-    if (kGrad && a.dh) {  // rows without a gradient
-      for (uint32_t z = __ballot_sync(0xffffffffu, t < tb && !in); z; z &= z - 1u) {
-        uint16_t* dst = static_cast<uint16_t*>(a.dh) + (t0 + warp * 32 + __ffs(z) - 1) * a.dh_stride;
-        if (((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0) {
-          for (int c = lane; c < a.D / 8; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
-          for (int c = a.D / 8 * 8 + lane; c < a.D; c += 32) dst[c] = 0;
-        } else {
-          for (int c = lane; c < a.D; c += 32) dst[c] = 0;
-        }
-      }
     }
     __syncthreads();
     if (gather) {
@@ -663,7 +739,125 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
     base += n;
     __syncthreads();
   }
-  if (gather && blockIdx.x == gridDim.x - 1) {
+}
+
+constexpr int kOrderKeys = 8 * kRowThreads;  // targets that a CTA compares its own with at one time
+
+// Gradient: the tokens with a target and a gradient that is not 0, in the order of their targets and, for one
+// target, their own; their number, the scale of an fp16 dz, their hidden rows in that order with
+// zeros up to the next k-step of the d_weight product, and the zeros of the others' d_hidden.
+// A token's place is the number of those before it in that order: every CTA counts, for its share of the
+// tokens, through all of them (T^2 / 152 comparisons in shared memory: 27 tokens with 4096 in 0.3 us of a
+// warp each), with no exchange between CTAs and no second launch.
+template <class Id>
+__global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, Status st) {
+  constexpr int kW = kRowThreads / 32;
+  __shared__ int s_key[kOrderKeys];
+  __shared__ int s_own[kRowThreads], s_place[kRowThreads], s_all[kW];
+  __shared__ float s_big[kW];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  let_next_start();
+  const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
+  const Id* target = static_cast<const Id*>(a.target);
+  const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
+  const bool vec = ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0;
+  auto key_of = [&](Id id, float g, float e) { return id >= 0 && id < a.V && (g != 0.f || e != 0.f) ? (int)id : kNoKey; };
+  int all = 0;
+  float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
+  for (int64_t o = ta; o < tb || o == ta; o += kRowThreads) {  // (a CTA without tokens counts them all, too)
+    const int own = (int)max((int64_t)0, min((int64_t)kRowThreads, tb - o));
+    const bool mine = threadIdx.x < own;
+    const Id my_id = mine ? target[o + threadIdx.x] : (Id)-1;
+    const float my_g = mine ? a.g[o + threadIdx.x] : 0.f, my_e = mine && a.ge ? a.ge[o + threadIdx.x] : 0.f;
+    for (int64_t c = 0; c < a.T; c += kOrderKeys) {
+      const int n = (int)min((int64_t)kOrderKeys, a.T - c);
+      Id id[8];
+      float g[8], e[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int u = k * kRowThreads + threadIdx.x;
+        id[k] = u < n ? target[c + u] : (Id)-1;
+        g[k] = u < n ? a.g[c + u] : 0.f;
+        e[k] = 0.f;
+      }
+      if (a.ge) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (k * kRowThreads + threadIdx.x < n) e[k] = a.ge[c + k * kRowThreads + threadIdx.x];
+      }
+      __syncthreads();  // the last chunk's readers are done
+      if (c == 0 && mine) {
+        s_own[threadIdx.x] = key_of(my_id, my_g, my_e);
+        s_place[threadIdx.x] = 0;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int u = k * kRowThreads + threadIdx.x;
+        const int key = key_of(id[k], g[k], e[k]);
+        if (u < n) s_key[u] = key;
+        if (o == ta) {
+          if (key != kNoKey) {
+            ++all;
+            bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
+          }
+          if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)(c + u));
+        }
+      }
+      __syncthreads();
+      for (int w = warp; w < own; w += kW) {
+        const int key = s_own[w];
+        if (key == kNoKey) continue;
+        const int self = (int)min((int64_t)kOrderKeys, max((int64_t)0, o + w - c));  // tokens of the chunk before this one
+        int before = 0;
+#pragma unroll 4
+        for (int u = lane; u < n; u += 32) before += s_key[u] < key + (u < self ? 1 : 0);
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) s_place[w] += before;
+      }
+    }
+    __syncwarp();  // (a warp's own places: written by its lane 0)
+    for (int w = warp; w < own; w += kW) {
+      const int64_t t = o + w;
+      const int key = s_own[w];
+      if (key != kNoKey) {
+        const int r = s_place[w];
+        if (lane == 0) {
+          a.idx[r] = (int)t;
+          a.by_target[r] = key;
+        }
+        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + t * a.hidden_stride);
+        uint4* dst = reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride);
+#pragma unroll 8
+        for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+      } else if (a.dh) {
+        uint16_t* dst = static_cast<uint16_t*>(a.dh) + t * a.dh_stride;
+        const int whole = vec ? a.D / 8 : 0;
+        for (int c = lane; c < whole; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+        for (int c = whole * 8 + lane; c < a.D; c += 32) dst[c] = 0;
+      }
+    }
+  }
+  all = __reduce_add_sync(0xffffffffu, all);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
+  if (lane == 0) {
+    s_all[warp] = all;
+    s_big[warp] = bound;
+  }
+  __syncthreads();
+  all = __reduce_add_sync(0xffffffffu, s_all[lane]);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    for (int w = 0; w < kW; ++w) bound = fmaxf(bound, s_big[w]);
+    float s = 1.f;
+    if (a.f16 && bound > 0.f && isfinite(bound)) {
+      int ex;
+      frexpf(bound, &ex);  // bound <= 2^ex: |dz| up to 2^14, within fp16's 65504
+      s = ldexpf(1.f, min(max(14 - ex, -100), 100));
+    }
+    a.head->rows = all;
+    a.head->dz_scale = s;
+  }
+  if (blockIdx.x == gridDim.x - 1) {
     const int pad = (all + kTile16 - 1) / kTile16 * kTile16;
     for (int r = all + warp; r < pad; r += kW)
       for (int c = lane; c < chunks; c += 32) reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride)[c] = make_uint4(0u, 0u, 0u, 0u);
@@ -814,12 +1008,17 @@ cudaError_t setup_vocab() {
   return e;
 }
 
-cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool grad) {
+cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st) {
   const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
-  if (grad && a.id8) vocab_rows_kernel<true, int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
-  else if (grad) vocab_rows_kernel<true, int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
-  else if (a.id8) vocab_rows_kernel<false, int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
-  else vocab_rows_kernel<false, int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  if (a.id8) vocab_rows_kernel<int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else vocab_rows_kernel<int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st) {
+  const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
+  if (a.id8) vocab_order_kernel<int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  else vocab_order_kernel<int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();
 }
 
@@ -846,6 +1045,7 @@ int vocab_splits(int64_t T, int64_t vn, int64_t D) {
   const int64_t dt = (D + kPairN - 1) / kPairN, mt = (T + kPairM - 1) / kPairM, kb = (vn + kTile16 - 1) / kTile16;
   const int64_t work = mt * dt * kb + (vn + kPairN - 1) / kPairN * dt * ((T + kTile16 - 1) / kTile16);
   const int64_t share = max(work / kVocabPairs, (int64_t)8);  // k-steps of one pair
+  if (kb <= 24) return 1;  // (less time than the launch that adds the parts)
   return (int)max((int64_t)1, min(kb / share, (int64_t)kVocabMaxSplits));
 }
 

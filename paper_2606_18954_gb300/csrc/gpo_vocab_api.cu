@@ -17,7 +17,7 @@ constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 1024;  // tokens, vocabulary 
 constexpr int64_t kMaxMatrix = (int64_t)1 << 40;          // elements of a matrix
 
 struct VocabLayout {
-  size_t status, marks, head, idx, hc, pm, ps, pu, tz, dz, acc, total;
+  size_t status, marks, head, idx, hc, by_target, rest, pm, ps, pu, tz, dz, acc, total;
   bool few;           // forward in one launch
   bool listed;        // only the tokens that take part are multiplied
   int64_t tp, hc_stride, piece, acc_stride;
@@ -55,6 +55,8 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
     L.tz = take(sizeof(float) * (size_t)L.tp);
   }
   if (T > 0 && grad) {
+    L.by_target = take(sizeof(int) * (size_t)T);
+    L.rest = take(sizeof(float) * (size_t)L.tp);
     // pieces of about equal size, a whole number of column tiles each
     const int64_t cols = std::max<int64_t>(1, kVocabPieceBytes / (2 * L.tp) / kPairN) * kPairN;
     const int64_t n = (v.vocab + cols - 1) / cols;
@@ -242,7 +244,7 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
     return stage.done();
   }
   Stages stage(ctx, stream, at<void>(workspace, L.status));
-  if (L.listed) stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st, false); });
+  if (L.listed) stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st); });
   stage("vocab_lse", [&] { return launch_vocab_lse(stage.lc, m, a, stage.st, ent); });
   stage("vocab_join", [&] { return launch_vocab_join(stage.lc, a, stage.st, ent); });
   return stage.done();
@@ -284,6 +286,10 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.g = in->grad_logp;
   a.ent = in->entropy;
   a.ge = in->grad_entropy;
+  a.weight = v->weight;
+  a.weight_stride = v->weight_stride;
+  a.by_target = at<int>(workspace, L.by_target);
+  a.rest = at<float>(workspace, L.rest);
   a.dz = at<uint16_t>(workspace, L.dz);
   a.dz_stride = L.piece;
   a.acc = L.acc ? at<float>(workspace, L.acc) : nullptr;
@@ -296,7 +302,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.dw_stride = out->d_weight_stride;
   a.accumulate = out->accumulate != 0;
   Stages stage(ctx, stream, at<void>(workspace, L.status));
-  stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st, true); });
+  stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });
   for (int64_t v0 = 0; v0 < v->vocab; v0 += L.piece) {
     a.v0 = v0;
     a.vn = std::min(L.piece, v->vocab - v0);
