@@ -83,9 +83,9 @@ struct Cols {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) s[i] += E::get(e[i]);
   }
-  // row = scale s (+ what it holds)
+  // row = scale s (+ what it holds); stream: not to be kept in L2
   static __device__ __forceinline__ void store(T* row, int64_t block, int lane, int64_t d, const float (&s)[kPer],
-                                               float scale, bool add) {
+                                               float scale, bool add, bool stream) {
     Raw r;
     T* e = reinterpret_cast<T*>(&r.v);
     const bool whole = kVec && at(block, lane, kPer) <= d;
@@ -96,7 +96,8 @@ struct Cols {
       if (add && !whole && c < d) e[i] = row[c];
       e[i] = E::put(add ? fmaf(scale, s[i], E::get(e[i])) : scale * s[i]);
     }
-    if (whole) *reinterpret_cast<uint4*>(row + at(block, lane, 0)) = r.v;
+    if (whole && stream) __stcs(reinterpret_cast<uint4*>(row + at(block, lane, 0)), r.v);
+    else if (whole) *reinterpret_cast<uint4*>(row + at(block, lane, 0)) = r.v;
     else
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
@@ -106,7 +107,7 @@ struct Cols {
 
 // ------------------------------------------------------------------ lookup
 
-constexpr int kLookBlocks = 4;  // column blocks (512 bytes each) of one step of a warp
+constexpr int kLookBlocks = 8;  // column blocks (512 bytes each) of one step of a warp
 
 template <int kType, bool kVec>
 __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
 #pragma unroll
       for (int i = 0; i < C::kPer; ++i) s[i] = 0.f;
       C::add(r[b], s);
-      C::store(dst, b0 + b, lane, a.D, s, a.scale, false);
+      C::store(dst, b0 + b, lane, a.D, s, a.scale, false, false);
     }
   }
 }
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
       const int64_t v = (unit - pieces) * 32 + lane;
       uint32_t m = __ballot_sync(0xffffffffu, v < a.V && a.start[min(v, a.V - 1)] == a.start[min(v, a.V - 1) + 1]);
       for (; m; m &= m - 1u)
-        C::store(out + ((unit - pieces) * 32 + __ffs(m) - 1) * a.dst_stride, b, lane, a.D, s, 1.f, false);
+        C::store(out + ((unit - pieces) * 32 + __ffs(m) - 1) * a.dst_stride, b, lane, a.D, s, 1.f, false, true);
       continue;
     }
     const int64_t p0 = unit * piece, p1 = min(p0 + piece, (int64_t)n);
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
         for (int i = 0; i < C::kPer; ++i)
           if (C::at(b, lane, i) < a.D) part[C::at(b, lane, i)] = s[i];
       } else {
-        C::store(out + (int64_t)run * a.dst_stride, b, lane, a.D, s, a.scale, a.accumulate != 0);
+        C::store(out + (int64_t)run * a.dst_stride, b, lane, a.D, s, a.scale, a.accumulate != 0, true);
       }
 #pragma unroll
       for (int i = 0; i < C::kPer; ++i) s[i] = 0.f;
@@ -387,7 +388,7 @@ cudaError_t sums(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
   const int piece = embed_piece(a.T);
   const int64_t blocks = (a.D * esz + 511) / 512, pieces = (a.T + piece - 1) / piece;
   const int64_t units = (pieces + (a.accumulate ? 0 : (a.V + 31) / 32)) * blocks;
-  const unsigned grid = (unsigned)max((int64_t)1, min((units + 7) / 8, (int64_t)lc.num_sms * 4));
+  const unsigned grid = (unsigned)max((int64_t)1, min((units + 7) / 8, (int64_t)lc.num_sms * 16));
   const bool vec = vec_rows(a.src, a.src_stride, esz) && vec_rows(a.dst, a.dst_stride, esz);
   const cudaError_t e = launch_after(vec ? embed_sum_kernel<kType, true> : embed_sum_kernel<kType, false>, grid, kSumThreads,
                                      0, lc.stream, a, piece, st);

@@ -28,11 +28,16 @@ namespace gpo {
 
 namespace {
 
-enum Mode { kLse, kLseEnt, kDz, kDzEnt, kProducts };
+// Ent: with the entropy; Wide: dz of logits that are several accumulations (see kSegDz)
+enum Mode { kLse, kLseEnt, kDz, kDzEnt, kDzWide, kDzWideEnt, kProducts };
+__host__ __device__ constexpr bool is_lse(int mode) { return mode == kLse || mode == kLseEnt; }
+__host__ __device__ constexpr bool is_wide(int mode) { return mode == kDzWide || mode == kDzWideEnt; }
+__host__ __device__ constexpr bool has_ent(int mode) { return mode == kLseEnt || mode == kDzEnt || mode == kDzWideEnt; }
+__host__ __device__ constexpr bool keeps_logits(int mode) { return is_lse(mode) || is_wide(mode); }  // 128 of them per epilogue thread
 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
 constexpr int kVStages = 6;                        // of the logits
-constexpr int kPStages = 5;                        // of the products, beside their epilogue's sums
+constexpr int kPStages = 4;                        // of the products, beside their epilogue's sums
 constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 4..11 epilogue
 constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
@@ -40,9 +45,9 @@ constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
 // The split of each mode is one without spills: the loads' and the MMAs' lane would find theirs in an L1
 // that the epilogue's stores sweep, and fall behind the tensor cores.
 constexpr int kRegsLaunch = 168;
-__host__ __device__ constexpr int regs_few(int mode) { return mode == kDz || mode == kDzEnt ? 120 : 88; }
-__host__ __device__ constexpr int regs_many(int mode) { return mode == kDz || mode == kDzEnt ? 192 : 208; }
-static_assert(128 * regs_few(kDz) + 256 * regs_many(kDz) <= kVThreads * kRegsLaunch &&
+__host__ __device__ constexpr int regs_few(int mode) { return is_wide(mode) ? 120 : 88; }
+__host__ __device__ constexpr int regs_many(int mode) { return is_wide(mode) ? 192 : 208; }
+static_assert(128 * regs_few(kDzWide) + 256 * regs_many(kDzWide) <= kVThreads * kRegsLaunch &&
               128 * regs_few(kLse) + 256 * regs_many(kLse) <= kVThreads * kRegsLaunch, "register split");
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
 constexpr int kVStage = 4 * kVBox;                 // A and B halves of one k-step, per CTA
@@ -55,7 +60,7 @@ constexpr int kVCols = 512;                        // two accumulators of 256 co
 constexpr int kSegLse = 8, kSegDz = 32;
 template <int kMode>
 __device__ __forceinline__ constexpr int segment_of() {
-  return kMode == kProducts ? 1 << 30 : kMode == kDz || kMode == kDzEnt ? kSegDz : kSegLse;
+  return is_lse(kMode) ? kSegLse : is_wide(kMode) ? kSegDz : 1 << 30;
 }
 constexpr int kNoKey = 0x7fffffff;                 // above every target: a token without a gradient
 constexpr int kRaster = 32;                        // row tiles that share one pass over the columns
@@ -69,8 +74,8 @@ struct __align__(8) VocabCtl {
   uint32_t tmem_base;
 };
 
-// Per epilogue warp of the products: sums of 32 rows x 32 columns (see add_rests).
-constexpr int kRestRow = 33;
+// Per epilogue warp of the products: sums of 32 rows x 64 columns (see sum_rests).
+constexpr int kRestRow = 65;
 constexpr size_t kRestBytes = sizeof(float) * 32 * kRestRow * kVEpiWarps;
 constexpr size_t kVSmem = ((sizeof(VocabCtl) + 15) & ~size_t(15)) + 1023 +
                           ((size_t)kVStages * kVStage > (size_t)kPStages * kVStage + kRestBytes
@@ -105,13 +110,14 @@ struct Plan {
   int light0, nlight, extra;  // pairs from light0 on take `extra` d_weight tiles more, for the d_hidden tile they lack
 };
 
+constexpr int kEpiSteps = 12;  // k-steps that a tile's epilogue in the products takes the time of
 template <int kMode>
 __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   Plan q;
   q.p = (int)blockIdx.x >> 1;
   q.np = (int)gridDim.x >> 1;
   q.mt = (rows + kPairM - 1) / kPairM;
-  const int64_t cols = kMode == kLse || kMode == kLseEnt ? a.V : a.vn;
+  const int64_t cols = is_lse(kMode) ? a.V : a.vn;
   q.nt = (int)((cols + kPairN - 1) / kPairN);
   q.kb = (a.D + kTile16 - 1) / kTile16;
   q.dt = (a.D + kPairN - 1) / kPairN;
@@ -125,7 +131,7 @@ __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   q.own_dh = q.n_dh / q.np + (q.p < q.n_dh % q.np ? 1 : 0);
   q.light0 = q.n_dh % q.np;
   q.nlight = q.np - q.light0;
-  q.extra = q.light0 > 0 && q.kb_dw > 0 ? min(q.kb_dh / q.splits / q.kb_dw, q.n_dw / q.nlight) : 0;
+  q.extra = q.light0 > 0 ? min(max(q.kb_dh / q.splits, kEpiSteps) / max(q.kb_dw, kEpiSteps), q.n_dw / q.nlight) : 0;
   return q;
 }
 
@@ -181,31 +187,31 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8]) {
                : "memory");
 }
 
-// 16 bits of 32 consecutive columns of a row to memory, those below `cols`.
+// 16 bits of 32 consecutive columns of a row to memory, those below `cols` (vec: 16-byte accesses).
 __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int cols, bool vec, int f16, bool add) {
-  if (vec && cols >= 32) {
 #pragma unroll
-    for (int c = 0; c < 32; c += 8) {
-      uint4* p = reinterpret_cast<uint4*>(dst + c);
-      float y[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = x[c + i];
-      if (add) {
-        const uint4 o = *p;
-        const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[2 * i] += widen16((uint16_t)(w[i] & 0xFFFFu), f16);
-          y[2 * i + 1] += widen16((uint16_t)(w[i] >> 16), f16);
-        }
-      }
-      *p = make_uint4(pack16(y[0], y[1], f16), pack16(y[2], y[3], f16), pack16(y[4], y[5], f16), pack16(y[6], y[7], f16));
+  for (int c = 0; c < 32; c += 8) {
+    uint32_t o[4] = {0u, 0u, 0u, 0u};
+    const bool whole = vec && c + 8 <= cols;
+    if (add && whole) {
+      const uint4 u = *reinterpret_cast<const uint4*>(dst + c);
+      o[0] = u.x, o[1] = u.y, o[2] = u.z, o[3] = u.w;
+    } else if (add) {
+      for (int i = 0; i < 8 && c + i < cols; ++i) o[i >> 1] |= (uint32_t)dst[c + i] << (16 * (i & 1));
     }
-    return;
-  }
 #pragma unroll
-  for (int c = 0; c < 32; ++c)
-    if (c < cols) dst[c] = round16(add ? x[c] + widen16(dst[c], f16) : x[c], f16);
+    for (int i = 0; i < 4; ++i) {
+      const float lo = add ? widen16((uint16_t)(o[i] & 0xFFFFu), f16) : 0.f, hi = add ? widen16((uint16_t)(o[i] >> 16), f16) : 0.f;
+      o[i] = pack16(x[c + 2 * i] + lo, x[c + 2 * i + 1] + hi, f16);
+    }
+    if (whole) {
+      *reinterpret_cast<uint4*>(dst + c) = make_uint4(o[0], o[1], o[2], o[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < cols) dst[c + i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
+    }
+  }
 }
 
 // The first of n ascending numbers that is not below v, by one warp.
@@ -213,13 +219,17 @@ __device__ __forceinline__ int first_not_below(const int* x, int n, int v, int l
   int lo = 0, hi = n;
   while (hi - lo > 32) {
     const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && x[at] < v));
+    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && __ldcg(x + at) < v));
     lo += below * step;
     hi = min(hi, lo + step);
   }
-  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && x[lo + lane] < v));
+  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && __ldcg(x + lo + lane) < v));
 }
 
+// Brings `cols` 16-bit columns of a row into L1, for add_row.
+__device__ __forceinline__ void prefetch_row(const uint16_t* x, int cols) {
+  for (int c = 0; c < cols; c += 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(x + c));
+}
 // y[j] += w x[j] for 32 columns of a row of hidden or weight, those below `cols` rounded up to 8 (the
 // row has them; what lies past its width is not used).
 __device__ __forceinline__ void add_row(const uint16_t* x, float w, int cols, int f16, float (&y)[32]) {
@@ -241,424 +251,505 @@ __device__ __forceinline__ void add_row(const uint16_t* x, float w, int cols, in
 // the error that the gradients' own rounding leaves (the other entries' adds 1 %), so what that rounding takes away
 // (a.rest) is kept in fp32 and added in the products' epilogues: for d_hidden a row of the vocabulary
 // matrix per token (add_row), for d_weight the hidden rows of the tokens whose targets a warp's 32 rows are,
-// [ra, rb) in the order of their targets.  Where one row has more than kFewRests of them, by this:
-// a lane takes a column, the tokens one after another, eight in flight, each row's sum in a register until its
-// last token; then through shared memory to the rows' lanes.
+// [ra, rb) in the order of their targets.  Where one row has more than kFewRests of them, by this, for 64 columns:
+// a lane takes two, the tokens one after another, sixteen in flight, each row's sums in registers until its
+// last token; then through shared memory to the rows' lanes.  (Two frequent tokens are most of the tokens of a small
+// vocabulary: 4000 of 1608 x 208, the products in 94 us with one column of 32 and eight in flight.)
 constexpr int kFewRests = 3;
-__device__ __forceinline__ void add_rests(const VocabArgs& a, float* sums, int ra, int rb, int v, int c0, int lane,
-                                          float (&y)[32]) {
+constexpr int kRestsAhead = 16;
+__device__ __forceinline__ void sum_rests(const VocabArgs& a, float* sums, int ra, int rb, int v, int c0, int lane) {
+  for (int j = lane; j < 32 * kRestRow; j += 32) sums[j] = 0.f;
+  __syncwarp();
+  const int col = c0 + 2 * lane;
+  const uint16_t* h = a.hc + (col < a.hc_stride ? col : 0);  // (rows of whole 16 bytes: a pair never straddles their end)
+  float s0 = 0.f, s1 = 0.f;
+  int row = __ldcg(a.by_target + ra);
+  for (int r = ra; r < rb; r += kRestsAhead) {
+    uint32_t x[kRestsAhead];
+    float w[kRestsAhead];
+    int at[kRestsAhead];
 #pragma unroll
-  for (int j = 0; j < 32; ++j) sums[j * kRestRow + lane] = 0.f;
-  const bool in = c0 + lane < a.D;
-  const uint16_t* h = a.hc + (in ? c0 + lane : 0);
-  float s = 0.f;
-  int row = a.by_target[ra];
-  for (int r = ra; r < rb; r += 8) {
-    uint16_t x[8];
-    float w[8];
-    int at[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kRestsAhead; ++k) {
       const int rk = min(r + k, rb - 1);
-      x[k] = h[(int64_t)rk * a.hc_stride];
-      w[k] = r + k < rb ? a.rest[rk] : 0.f;
-      at[k] = a.by_target[rk];
+      x[k] = *reinterpret_cast<const uint32_t*>(h + (int64_t)rk * a.hc_stride);
+      w[k] = r + k < rb ? __ldcg(a.rest + rk) : 0.f;
+      at[k] = __ldcg(a.by_target + rk);
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kRestsAhead; ++k) {
       if (at[k] != row) {
-        sums[(row - v) * kRestRow + lane] = s;
-        s = 0.f;
+        sums[(row - v) * kRestRow + 2 * lane] = s0;
+        sums[(row - v) * kRestRow + 2 * lane + 1] = s1;
+        s0 = s1 = 0.f;
         row = at[k];
       }
-      s = fmaf(w[k], widen16(x[k], a.f16), s);
+      s0 = fmaf(w[k], widen16((uint16_t)(x[k] & 0xFFFFu), a.f16), s0);
+      s1 = fmaf(w[k], widen16((uint16_t)(x[k] >> 16), a.f16), s1);
     }
   }
-  sums[(row - v) * kRestRow + lane] = s;
-  __syncwarp();
-#pragma unroll
-  for (int j = 0; j < 32; ++j) y[j] += sums[lane * kRestRow + j];
+  sums[(row - v) * kRestRow + 2 * lane] = s0;
+  sums[(row - v) * kRestRow + 2 * lane + 1] = s1;
   __syncwarp();
 }
 
-template <int kMode>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
-    vocab_pair_kernel(const __grid_constant__ VocabMaps maps, VocabArgs a, Status st) {
-  extern __shared__ __align__(1024) unsigned char smem_raw[];
-  VocabCtl* ctl = reinterpret_cast<VocabCtl*>(smem_raw);
-  const uint32_t sbase = smem_u32(smem_raw);
-  constexpr uint32_t kCtlBytes = (sizeof(VocabCtl) + 15) & ~15u;
-  const uint32_t tiles = (sbase + kCtlBytes + 1023u) & ~1023u;  // the same offset in both CTAs
-  constexpr bool kLogits = kMode == kLse || kMode == kLseEnt;
-  constexpr int kStages = kMode == kProducts ? kPStages : kVStages;
+// What the roles of a CTA share.
+struct Cta {
+  VocabCtl* ctl;
+  unsigned char* smem;  // the dynamic shared memory
+  uint32_t tiles;       // the ring, the same offset in both CTAs
+  uint32_t tmem, rank;
+  int rows;             // tokens that are multiplied
+};
+// Where a role is in the ring and among the accumulations; it goes on from one pass over tiles to the next.
+struct Pipe {
+  int stage = 0;
+  uint32_t phase = 0;
+  uint32_t issued = 0;  // loads: stages filled
+  int sum = 0;          // accumulations: one per tile, or per segment of a logits tile
+};
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t rank = cluster_rank();
+// Loads of all tiles of this pair, by one thread of either CTA: its halves of the operands.  False after a timeout.
+template <int kMode, int kS>
+__device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArgs& a, const Status& st, const Cta& c,
+                                           Pipe& p) {
+  constexpr bool kLogits = is_lse(kMode);
+  const Plan plan = make_plan<kMode>(a, c.rows);
+  const CUtensorMap* hmap = a.idx && (!kLogits || c.rows < a.T) ? &maps.hc : &maps.h;
+  Tile t;
+  for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
+    const CUtensorMap* ma = kMode == kProducts ? &maps.dz : hmap;
+    const CUtensorMap* mb = kMode == kProducts && t.job == 1 ? hmap : &maps.w;
+    const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
+    const int am = t.m0 + (int)c.rank * (kPairM / 2), bn = t.n0 + (int)c.rank * (kPairN / 2);
+    const int v0 = kLogits ? 0 : (int)a.v0;
+    for (int k = 0; k < t.kb; ++k) {
+      if (!mbar_wait(&c.ctl->empty[p.stage], p.phase ^ 1u, st, 20)) return false;
+      const uint32_t sa = c.tiles + (uint32_t)p.stage * kVStage, sb = sa + 2 * kVBox;
+      const uint32_t bar = leader_addr(&c.ctl->full[p.stage]);
+      if (c.rank == 0) mbar_arrive_expect_tx(&c.ctl->full[p.stage], 2 * kVStage);
+      ++p.issued;
+      const int kx = (t.ka + k) * kTile16;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (a_mn) tma_load_2d_pair(sa + h * kVBox, ma, bar, am + h * kTile16, kx);
+        else tma_load_2d_pair(sa + h * kVBox, ma, bar, kx, am + h * kTile16);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (!b_mn) tma_load_2d_pair(sb + h * kVBox, mb, bar, kx, v0 + bn + h * kTile16);
+        else tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, (t.job == 0 ? v0 : 0) + kx);
+      }
+      if (++p.stage == kS) {
+        p.stage = 0;
+        p.phase ^= 1u;
+      }
+    }
+  }
+  return true;
+}
+
+// Their MMAs, by one thread of the leader.
+template <int kMode, int kS>
+__device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
   constexpr int seg = segment_of<kMode>();
+  const Plan plan = make_plan<kMode>(a, c.rows);
+  Tile t;
+  for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
+    const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
+    const uint32_t idesc = idesc_16_f32(kPairM, kPairN, a.f16 != 0, a_mn, b_mn);
+    for (int64_t k0 = 0; k0 < t.kb || k0 == 0; k0 += seg, ++p.sum) {
+      const int buf = p.sum & 1;
+      if (!mbar_wait_cluster(&c.ctl->tempty[buf], ((uint32_t)(p.sum >> 1) & 1u) ^ 1u, st, 22)) return false;
+      tc_fence_after();
+      const uint32_t dt = c.tmem + (uint32_t)(buf * kPairN);
+      const int k1 = (int)min((int64_t)t.kb, k0 + seg);
+      for (int k = (int)k0; k < k1; ++k) {
+        if (!mbar_wait(&c.ctl->full[p.stage], p.phase, st, 23)) return false;
+        tc_fence_after();
+        const uint32_t sa = c.tiles + (uint32_t)p.stage * kVStage, sb = sa + 2 * kVBox;
+        const uint64_t ad = a_mn ? smem_desc_mn128(sa, kVBox) : smem_desc_k128(sa);
+        const uint64_t bd = b_mn ? smem_desc_mn128(sb, kVBox) : smem_desc_k128(sb);
+        // 16 k: 32 bytes of a K-major row, 16 rows of 128 bytes otherwise (addresses >> 4)
+        const uint32_t as = a_mn ? 128u : 2u, bs = b_mn ? 128u : 2u;
+#pragma unroll
+        for (uint32_t kk = 0; kk < kTile16 / 16; ++kk)
+          mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, (k - (int)k0 | (int)kk) != 0);
+        mma_commit_pair(&c.ctl->empty[p.stage]);
+        if (++p.stage == kS) {
+          p.stage = 0;
+          p.phase ^= 1u;
+        }
+    }
+    mma_commit_pair(&c.ctl->tfull[buf]);
+    }
+  }
+  return true;
+}
 
-  let_next_start();
+// What a row's token brings to its dz.
+struct DzRow {
+  float l2, g, e, ent;  // lse in units of log 2, d loss / d logp and d entropy (times the scale of an fp16 dz), entropy
+};
+// dz of 32 columns from their logits z, rounded to 16 bits and stored: those below `cols`, zeros past them (p of a
+// padding row or column is no probability, and its row may hold anything).  tgt: the target's place; its dz into vt.
+template <bool kEnt>
+__device__ __forceinline__ void dz_columns(const VocabArgs& a, const DzRow& w, const float* z, int cols, int tgt, float& vt,
+                                           uint16_t* dst) {
+#pragma unroll
+  for (int c = 0; c < 32; c += 16) {
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      float y[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int j = c + i + h;
+        const float d = fmaf(z[j], a.sl2, -w.l2);  // log2 p
+        const float p = ex2(d);
+        float v = (j == tgt ? w.g : 0.f) - w.g * p;
+        if (kEnt) v = fmaf(-w.e * p, fmaf(d, 0.6931471805599453f, w.ent), v);
+        if (j == tgt) vt = v;
+        y[h] = j < cols ? v : 0.f;
+      }
+      o[i / 2] = pack16(y[0], y[1], a.f16);
+    }
+    st_global_32(dst + c, o);
+  }
+}
+
+// Their epilogues, by warps 4..11 of either CTA.  False (for the whole warp) after a timeout.
+// (dz of logits that are one accumulation goes 32 columns at a time: a fourth of the code, which a call of few
+// tiles runs cold.)
+template <int kMode, int kS>
+__device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
+  constexpr bool kLogits = is_lse(kMode);
+  constexpr int seg = segment_of<kMode>();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = c.rows;
+  const Plan plan = make_plan<kMode>(a, rows);
+  const int q = warp & 3, half = (warp - 4) >> 2;  // tensor memory lanes 32 q .., columns 128 half ..
+  const int r = (int)c.rank * (kPairM / 2) + q * 32 + lane;  // row in the tile
+  const uint32_t lanes = c.tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (kPairN / 2));
+  const uint32_t te = leader_addr(&c.ctl->tempty[0]);
+  // waits for the n-th accumulation; false (for the whole warp) when that gave up
+  auto ready = [&](int n) {
+    const bool got = __all_sync(0xffffffffu, mbar_wait(&c.ctl->tfull[n & 1], (uint32_t)(n >> 1) & 1u, st, 25));
+    tc_fence_after();
+    return got;
+  };
+  // this warp has read its part of the n-th accumulation
+  auto release = [&](int n) {
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive_cluster(te + 8u * (uint32_t)(n & 1));
+  };
+  Tile t;
+  for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
+    const int row = t.m0 + r;
+    const int n0 = t.n0 + half * (kPairN / 2);  // first column of this warp
+    if constexpr (kMode != kProducts) {
+      const bool live = row < rows;
+      // what the row's token brings
+      int64_t tok = 0;
+      int tgt = -1;
+      DzRow w = {0.f, 0.f, 0.f, 0.f};
+      if (live) {
+        tok = a.idx ? __ldcg(a.idx + row) : row;
+        const int64_t id = load_id(a.target, a.id8, tok);
+        if (id >= 0 && id < a.V) tgt = (int)(id - (kLogits ? 0 : a.v0)) - n0;  // its column, from n0 on
+        if (!kLogits) {
+          const float gs = __ldcg(&a.head->dz_scale);
+          w.l2 = a.lse[tok] * 1.4426950408889634f;
+          w.g = a.g[tok] * gs;
+          if (has_ent(kMode)) {
+            w.e = a.ge[tok] * gs;
+            w.ent = a.ent[tok];
+          }
+        }
+      }
+      if constexpr (kMode == kDz || kMode == kDzEnt) {
+        uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
+        float vt = 0.f;
+        if (!ready(p.sum)) return false;
+#pragma unroll 1
+        for (int ch = 0; ch < kPairN / 2; ch += 32) {
+          uint32_t x[32];
+          __syncwarp();
+          tmem_ld_32x32b_x32(lanes + (uint32_t)((p.sum & 1) * kPairN + ch), x);
+          tmem_wait_ld();
+          if (ch + 32 == kPairN / 2) release(p.sum);
+          float z[32];
+#pragma unroll
+          for (int j = 0; j < 32; ++j) z[j] = __uint_as_float(x[j]);
+          dz_columns<has_ent(kMode)>(a, w, z, (live ? (int)a.vn - n0 : 0) - ch, tgt - ch, vt, dst + ch);
+        }
+        ++p.sum;
+        if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
+      } else {
+      uint64_t zz[kPairN / 4];  // two logits each
+#pragma unroll
+      for (int c = 0; c < kPairN / 4; ++c) zz[c] = 0ull;
+      bool ok = true;
+      const bool any = __any_sync(0xffffffffu, live);
+      for (int k0 = 0; k0 < t.kb; k0 += seg, ++p.sum) {
+        ok = ready(p.sum);
+        if (!ok) break;
+        const uint32_t src = lanes + (uint32_t)((p.sum & 1) * kPairN);
+        if (any) {
+#pragma unroll
+        for (int c = 0; c < kPairN / 2; c += 32) {
+          uint32_t x[32];
+          tmem_ld_32x32b_x32(src + (uint32_t)c, x);
+          tmem_wait_ld();
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) zz[(c + j) / 2] = f2add(zz[(c + j) / 2], pack_f2(x[j], x[j + 1]));
+        }
+        }
+        release(p.sum);
+      }
+      if (!ok) return false;
+      if (kLogits && !any) continue;  // no row of this warp is a token's
+      float z[kPairN / 2];
+#pragma unroll
+      for (int c = 0; c < kPairN / 4; ++c) {
+        uint32_t lo, hi;
+        unpack_f2(zz[c], lo, hi);
+        z[2 * c] = __uint_as_float(lo);
+        z[2 * c + 1] = __uint_as_float(hi);
+      }
+      if constexpr (kLogits) {
+        const int cols = (int)a.V - n0;
+        if (cols < kPairN / 2) {
+#pragma unroll
+          for (int j = 0; j < kPairN / 2; ++j)
+            if (j >= cols) z[j] = kNone;
+        }
+        const bool here = tgt >= 0 && tgt < kPairN / 2;
+        if (__any_sync(0xffffffffu, here)) {  // the target's logit leaves the sums
+          float tz = 0.f;
+#pragma unroll
+          for (int j = 0; j < kPairN / 2; ++j)
+            if (j == tgt) {
+              tz = z[j];
+              z[j] = kNone;
+            }
+          if (here) a.tz[row] = tz * a.sl2;
+        }
+        float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+        for (int j = 4; j < kPairN / 2; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
+        const float m = fmaxf(kLow, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.sl2);
+        float s4[4] = {0.f, 0.f, 0.f, 0.f}, u4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < kPairN / 2; ++j) {
+          const float d = fmaf(z[j], a.sl2, -m);
+          const float p = ex2(d);
+          s4[j & 3] += p;
+          if (has_ent(kMode)) u4[j & 3] = fmaf(p, d, u4[j & 3]);
+        }
+        if (live) {
+          const int64_t at = (int64_t)row * a.part_row + (int64_t)(n0 / (kPairN / 2)) * a.part_col;
+          a.pm[at] = m;
+          a.ps[at] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+          if (has_ent(kMode)) a.pu[at] = (u4[0] + u4[1]) + (u4[2] + u4[3]);
+        }
+      } else {
+        uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
+        const int cols = live ? (int)a.vn - n0 : 0;
+        float vt = 0.f;
+#pragma unroll
+        for (int ch = 0; ch < kPairN / 2; ch += 32) dz_columns<has_ent(kMode)>(a, w, z + ch, cols - ch, tgt - ch, vt, dst + ch);
+        // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
+        if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
+      }
+      }
+    } else {
+      const bool live = row < (t.job == 1 ? (int)a.vn : rows);
+      float* rests = reinterpret_cast<float*>(c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage) + (warp - 4) * 32 * kRestRow;
+      int ra = 0, rb = 0, na = 0, nb = 0;  // d_weight: the tokens whose targets are rows of this warp, of this lane
+      float rest = 0.f;                    // d_hidden: the row's own
+      const uint16_t* wrow = nullptr;
+      if (t.job == 1) {
+        const int v = (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32;
+        ra = first_not_below(a.by_target, rows, v, lane);
+        for (rb = ra; rb < rows; rb += 32) {  // (few tokens' targets are near each other)
+          const int y = rb + lane < rows ? __ldcg(a.by_target + rb + lane) : kNoKey;
+          const int in = __popc(__ballot_sync(0xffffffffu, y < v + 32));
+          for (int k = 0; k < in; ++k) {
+            const int yk = __shfl_sync(0xffffffffu, y, k);
+            if (yk < v + lane) ++na;
+            if (yk <= v + lane) ++nb;
+          }
+          if (in < 32) {
+            rb += in;
+            break;
+          }
+        }
+        rb = min(rb, rows);
+        na += ra;
+        nb += ra;
+      } else if (live && t.split == 0) {
+        const int y = __ldcg(a.by_target + row);
+        if (y >= a.v0 && y < a.v0 + a.vn) {
+          rest = __ldcg(a.rest + row);
+          wrow = static_cast<const uint16_t*>(a.weight) + (int64_t)y * a.weight_stride;
+        }
+      }
+      const bool few = __all_sync(0xffffffffu, nb - na <= kFewRests);
+      // what is added to the sums is fetched while they are still being made
+      const int some = min(kPairN / 2, a.D - n0);
+      for (int i = na; few && i < nb; ++i) {
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(a.rest + i));
+        prefetch_row(a.hc + (int64_t)i * a.hc_stride + n0, some);
+      }
+      if (wrow) prefetch_row(wrow + n0, some);
+      if (!ready(p.sum)) return false;
+      const float f = t.kb > 0 ? a.scale / __ldcg(&a.head->dz_scale) : 0.f;
+#pragma unroll 1
+      for (int ch = 0; ch < kPairN / 2 / 32; ++ch) {
+        uint32_t x[32];
+        __syncwarp();
+        tmem_ld_32x32b_x32(lanes + (uint32_t)((p.sum & 1) * kPairN + ch * 32), x);
+        tmem_wait_ld();
+        if (ch == kPairN / 2 / 32 - 1) release(p.sum);
+        const int c0 = n0 + ch * 32;
+        const int cols = a.D - c0;
+        float y[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
+        if (!few) {
+          if ((ch & 1) == 0) sum_rests(a, rests, ra, rb, (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32, c0, lane);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) y[j] += rests[lane * kRestRow + (ch & 1) * 32 + j];
+        } else {
+#pragma unroll 1
+          for (int i = na; i < nb; ++i) add_row(a.hc + (int64_t)i * a.hc_stride + c0, a.rest[i], cols, a.f16, y);
+        }
+        if (rest != 0.f) add_row(wrow + c0, rest, cols, a.f16, y);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) y[j] *= f;
+        if (live && cols > 0 && t.job == 0) {
+          const bool out = a.last && a.splits == 1;  // the whole sum
+          if (!(a.first && out)) {  // several pieces or parts of k: the sums so far in fp32
+            // (rows of whole 128-byte lines: what lies past the width is written, and never used)
+            float* acc = a.acc + ((int64_t)t.split * a.acc_rows + row) * a.acc_stride + c0;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+              if (!a.first) {
+                const float4 o0 = __ldcg(reinterpret_cast<const float4*>(acc + i)), o1 = __ldcg(reinterpret_cast<const float4*>(acc + i + 4));
+                y[i] += o0.x, y[i + 1] += o0.y, y[i + 2] += o0.z, y[i + 3] += o0.w;
+                y[i + 4] += o1.x, y[i + 5] += o1.y, y[i + 6] += o1.z, y[i + 7] += o1.w;
+              }
+              if (!out) {
+                const uint32_t o[8] = {__float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]),
+                                       __float_as_uint(y[i + 3]), __float_as_uint(y[i + 4]), __float_as_uint(y[i + 5]),
+                                       __float_as_uint(y[i + 6]), __float_as_uint(y[i + 7])};
+                st_global_32(acc + i, o);
+              }
+            }
+          }
+          if (out) {
+            uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)__ldcg(a.idx + row) * a.dh_stride + c0;
+            store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
+          }
+        } else if (live && cols > 0) {
+          uint16_t* dst = static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0;
+          store16(dst, y, cols, ((a.dw_stride & 7) | (reinterpret_cast<uintptr_t>(a.dw) & 15)) == 0, a.f16,
+                  a.accumulate != 0);
+        }
+      }
+      ++p.sum;
+    }
+  }
+  return true;
+}
+
+// Barriers and tensor memory of a pair.
+template <int kS>
+__device__ __forceinline__ Cta begin_pair(unsigned char* smem) {
+  Cta c;
+  c.smem = smem;
+  c.ctl = reinterpret_cast<VocabCtl*>(smem);
+  constexpr uint32_t kCtlBytes = (sizeof(VocabCtl) + 15) & ~15u;
+  c.tiles = (smem_u32(smem) + kCtlBytes + 1023u) & ~1023u;
+  c.rank = cluster_rank();
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctl->full[s], 1);
-      mbar_init(&ctl->empty[s], 1);
+    for (int s = 0; s < kS; ++s) {
+      mbar_init(&c.ctl->full[s], 1);
+      mbar_init(&c.ctl->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
-      mbar_init(&ctl->tfull[b], 1);
-      mbar_init(&ctl->tempty[b], 2 * kVEpiWarps);
+      mbar_init(&c.ctl->tfull[b], 1);
+      mbar_init(&c.ctl->tempty[b], 2 * kVEpiWarps);
     }
-    mbar_init(&ctl->drain, 1);
+    mbar_init(&c.ctl->drain, 1);
     fence_mbar_init();
   }
-  if (warp == kMmaWarp) {
-    tmem_alloc_pair(&ctl->tmem_base, kVCols);
+  if (threadIdx.x >> 5 == kMmaWarp) {
+    tmem_alloc_pair(&c.ctl->tmem_base, kVCols);
     tmem_relinquish_pair();
   }
   tc_fence_before();
   __syncthreads();
   cluster_sync();
   tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
-  after_previous();
-  const int rows = a.idx ? a.head->rows : (int)a.T;
-  const Plan plan = make_plan<kMode>(a, rows);
-  const CUtensorMap* hmap = a.idx && (!kLogits || rows < a.T) ? &maps.hc : &maps.h;
+  c.tmem = c.ctl->tmem_base;
+  return c;
+}
 
-  if (warp < 4) {
-  if (kMode != kProducts) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(regs_few(kMode)));
-  if (warp == kLoadWarp) {
-    // ------------------------------------------------------------ loads (lane 0 of either CTA: its halves)
-    if (lane == 0) {
-      int stage = 0;
-      uint32_t phase = 0, issued = 0;
-      bool ok = true;
-      Tile t;
-      for (int s = 0; ok && next_tile<kMode>(plan, s, t); ++s) {
-        const CUtensorMap* ma = kMode == kProducts ? &maps.dz : hmap;
-        const CUtensorMap* mb = kMode == kProducts && t.job == 1 ? hmap : &maps.w;
-        const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
-        const int am = t.m0 + (int)rank * (kPairM / 2), bn = t.n0 + (int)rank * (kPairN / 2);
-        const int v0 = kLogits ? 0 : (int)a.v0;
-        for (int k = 0; k < t.kb; ++k) {
-          if (!mbar_wait(&ctl->empty[stage], phase ^ 1u, st, 20)) {
-            ok = false;
-            break;
-          }
-          const uint32_t sa = tiles + (uint32_t)stage * kVStage, sb = sa + 2 * kVBox;
-          const uint32_t bar = leader_addr(&ctl->full[stage]);
-          if (rank == 0) mbar_arrive_expect_tx(&ctl->full[stage], 2 * kVStage);
-          ++issued;
-          const int kx = (t.ka + k) * kTile16;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (a_mn) tma_load_2d_pair(sa + h * kVBox, ma, bar, am + h * kTile16, kx);
-            else tma_load_2d_pair(sa + h * kVBox, ma, bar, kx, am + h * kTile16);
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (!b_mn) tma_load_2d_pair(sb + h * kVBox, mb, bar, kx, v0 + bn + h * kTile16);
-            else tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, (t.job == 0 ? v0 : 0) + kx);
-          }
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1u;
-          }
-        }
-      }
-      // wind-down: the copies land before the CTAs may exit
-      if (rank == 0)
-        for (uint32_t s = 0; s < kStages; ++s)
-          if (s < issued) mbar_wait(&ctl->full[s], (issued - 1 - s) / kStages & 1u, st, 21, 200000000ull, false);
-    }
-    __syncwarp();
-  } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------ MMAs (lane 0 of the leader)
-    if (lane == 0 && rank == 0) {
-      int stage = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      if (a.debug_timeout) {
-        mbar_wait(&ctl->drain, 0, st, 27, kDebugTimeoutNs);  // returns false: reports GPO_ERR_TIMEOUT
-        ok = false;
-      }
-      Tile t;
-      int sum = 0;  // accumulations so far: one per tile, or per segment of a logits tile
-      for (int s = 0; ok && next_tile<kMode>(plan, s, t); ++s) {
-        const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
-        const uint32_t idesc = idesc_16_f32(kPairM, kPairN, a.f16 != 0, a_mn, b_mn);
-        for (int64_t k0 = 0; ok && (k0 < t.kb || k0 == 0); k0 += seg, ++sum) {
-        const int buf = sum & 1;
-        if (!mbar_wait_cluster(&ctl->tempty[buf], ((uint32_t)(sum >> 1) & 1u) ^ 1u, st, 22)) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        const uint32_t dt = tmem + (uint32_t)(buf * kPairN);
-        const int k1 = (int)min((int64_t)t.kb, k0 + seg);
-        for (int k = (int)k0; k < k1; ++k) {
-          if (!mbar_wait(&ctl->full[stage], phase, st, 23)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
-          const uint32_t sa = tiles + (uint32_t)stage * kVStage, sb = sa + 2 * kVBox;
-          const uint64_t ad = a_mn ? smem_desc_mn128(sa, kVBox) : smem_desc_k128(sa);
-          const uint64_t bd = b_mn ? smem_desc_mn128(sb, kVBox) : smem_desc_k128(sb);
-          // 16 k: 32 bytes of a K-major row, 16 rows of 128 bytes otherwise (addresses >> 4)
-          const uint32_t as = a_mn ? 128u : 2u, bs = b_mn ? 128u : 2u;
-#pragma unroll
-          for (uint32_t kk = 0; kk < kTile16 / 16; ++kk)
-            mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, (k - (int)k0 | (int)kk) != 0);
-          mma_commit_pair(&ctl->empty[stage]);
-          if (++stage == kStages) {
-            stage = 0;
-            phase ^= 1u;
-          }
-        }
-        if (ok) mma_commit_pair(&ctl->tfull[buf]);
-        }
-      }
-      // wind-down: all issued MMAs complete before tensor memory is released
-      mma_commit_pair(&ctl->drain);
-      mbar_wait(&ctl->drain, 0, st, 24, 200000000ull, false);
-    }
-    __syncwarp();
-  }
-  } else {
-    // ------------------------------------------------------------ epilogue
-    if (kMode != kProducts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
-    const int q = warp & 3, half = (warp - 4) >> 2;  // tensor memory lanes 32 q .., columns 128 half ..
-    const int r = (int)rank * (kPairM / 2) + q * 32 + lane;  // row in the tile
-    const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (kPairN / 2));
-    const uint32_t te = leader_addr(&ctl->tempty[0]);
-    // waits for the n-th accumulation; false (for the whole warp) when that gave up
-    auto ready = [&](int n) {
-      const bool got = __all_sync(0xffffffffu, mbar_wait(&ctl->tfull[n & 1], (uint32_t)(n >> 1) & 1u, st, 25));
-      tc_fence_after();
-      return got;
-    };
-    // this warp has read its part of the n-th accumulation
-    auto release = [&](int n) {
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(te + 8u * (uint32_t)(n & 1));
-    };
-    Tile t;
-    int sum = 0;
-    for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
-      const int row = t.m0 + r;
-      const int n0 = t.n0 + half * (kPairN / 2);  // first column of this warp
-      if constexpr (kMode != kProducts) {
-        const bool live = row < rows;
-        // what the row's token brings
-        int64_t tok = 0;
-        int tgt = -1;
-        float l2 = 0.f, g = 0.f, e = 0.f, ent = 0.f;
-        if (live) {
-          tok = a.idx ? a.idx[row] : row;
-          const int64_t id = load_id(a.target, a.id8, tok);
-          if (id >= 0 && id < a.V) tgt = (int)(id - (kLogits ? 0 : a.v0)) - n0;  // its column, from n0 on
-          if (!kLogits) {
-            const float gs = a.head->dz_scale;
-            l2 = a.lse[tok] * 1.4426950408889634f;
-            g = a.g[tok] * gs;
-            if (kMode == kDzEnt) {
-              e = a.ge[tok] * gs;
-              ent = a.ent[tok];
-            }
-          }
-        }
-        uint64_t zz[kPairN / 4];  // two logits each
-#pragma unroll
-        for (int c = 0; c < kPairN / 4; ++c) zz[c] = 0ull;
-        bool ok = true;
-        const bool any = __any_sync(0xffffffffu, live);
-        for (int k0 = 0; k0 < t.kb; k0 += seg, ++sum) {
-          ok = ready(sum);
-          if (!ok) break;
-          const uint32_t src = lanes + (uint32_t)((sum & 1) * kPairN);
-          if (any) {
-#pragma unroll
-          for (int c = 0; c < kPairN / 2; c += 32) {
-            uint32_t x[32];
-            tmem_ld_32x32b_x32(src + (uint32_t)c, x);
-            tmem_wait_ld();
-#pragma unroll
-            for (int j = 0; j < 32; j += 2) zz[(c + j) / 2] = f2add(zz[(c + j) / 2], pack_f2(x[j], x[j + 1]));
-          }
-          }
-          release(sum);
-        }
-        if (!ok) break;
-        if (kLogits && !any) continue;  // no row of this warp is a token's
-        float z[kPairN / 2];
-#pragma unroll
-        for (int c = 0; c < kPairN / 4; ++c) {
-          uint32_t lo, hi;
-          unpack_f2(zz[c], lo, hi);
-          z[2 * c] = __uint_as_float(lo);
-          z[2 * c + 1] = __uint_as_float(hi);
-        }
-        if constexpr (kLogits) {
-          const int cols = (int)a.V - n0;
-          if (cols < kPairN / 2) {
-#pragma unroll
-            for (int j = 0; j < kPairN / 2; ++j)
-              if (j >= cols) z[j] = kNone;
-          }
-          const bool here = tgt >= 0 && tgt < kPairN / 2;
-          if (__any_sync(0xffffffffu, here)) {  // the target's logit leaves the sums
-            float tz = 0.f;
-#pragma unroll
-            for (int j = 0; j < kPairN / 2; ++j)
-              if (j == tgt) {
-                tz = z[j];
-                z[j] = kNone;
-              }
-            if (here) a.tz[row] = tz * a.sl2;
-          }
-          float top[4] = {z[0], z[1], z[2], z[3]};
-#pragma unroll
-          for (int j = 4; j < kPairN / 2; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
-          const float m = fmaxf(kLow, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.sl2);
-          float s4[4] = {0.f, 0.f, 0.f, 0.f}, u4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = 0; j < kPairN / 2; ++j) {
-            const float d = fmaf(z[j], a.sl2, -m);
-            const float p = ex2(d);
-            s4[j & 3] += p;
-            if (kMode == kLseEnt) u4[j & 3] = fmaf(p, d, u4[j & 3]);
-          }
-          if (live) {
-            const int64_t at = (int64_t)row * a.part_row + (int64_t)(n0 / (kPairN / 2)) * a.part_col;
-            a.pm[at] = m;
-            a.ps[at] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-            if (kMode == kLseEnt) a.pu[at] = (u4[0] + u4[1]) + (u4[2] + u4[3]);
-          }
-        } else {
-          uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
-          const int cols = live ? (int)a.vn - n0 : 0;
-          float vt = 0.f;
-#pragma unroll
-          for (int c = 0; c < kPairN / 2; c += 16) {
-            uint32_t o[8];
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-              float y[2];
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const int j = c + i + h;
-                const float d = fmaf(z[j], a.sl2, -l2);  // log2 p
-                const float p = ex2(d);
-                float v = (j == tgt ? g : 0.f) - g * p;
-                if (kMode == kDzEnt) v = fmaf(-e * p, fmaf(d, 0.6931471805599453f, ent), v);
-                if (j == tgt) vt = v;
-                // (p of a padding row or column is no probability, and its row may hold anything)
-                y[h] = j < cols ? v : 0.f;
-              }
-              o[i / 2] = pack16(y[0], y[1], a.f16);
-            }
-            st_global_32(dst + c, o);
-          }
-          // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
-          if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
-        }
-      } else {
-        const bool live = row < (t.job == 1 ? (int)a.vn : rows);
-        float* rests = reinterpret_cast<float*>(smem_raw + (tiles - sbase) + kPStages * kVStage) + (warp - 4) * 32 * kRestRow;
-        int ra = 0, rb = 0, na = 0, nb = 0;  // d_weight: the tokens whose targets are rows of this warp, of this lane
-        float rest = 0.f;                    // d_hidden: the row's own
-        const uint16_t* wrow = nullptr;
-        if (t.job == 1) {
-          const int v = (int)a.v0 + t.m0 + (int)rank * (kPairM / 2) + q * 32;
-          ra = first_not_below(a.by_target, rows, v, lane);
-          for (rb = ra; rb < rows; rb += 32) {  // (few tokens' targets are near each other)
-            const int y = rb + lane < rows ? a.by_target[rb + lane] : kNoKey;
-            const int in = __popc(__ballot_sync(0xffffffffu, y < v + 32));
-            for (int k = 0; k < in; ++k) {
-              const int yk = __shfl_sync(0xffffffffu, y, k);
-              if (yk < v + lane) ++na;
-              if (yk <= v + lane) ++nb;
-            }
-            if (in < 32) {
-              rb += in;
-              break;
-            }
-          }
-          rb = min(rb, rows);
-          na += ra;
-          nb += ra;
-        } else if (live && t.split == 0) {
-          const int y = a.by_target[row];
-          if (y >= a.v0 && y < a.v0 + a.vn) {
-            rest = a.rest[row];
-            wrow = static_cast<const uint16_t*>(a.weight) + (int64_t)y * a.weight_stride;
-          }
-        }
-        const bool few = __all_sync(0xffffffffu, nb - na <= kFewRests);
-        if (!ready(sum)) break;
-        const float f = t.kb > 0 ? a.scale / a.head->dz_scale : 0.f;
-#pragma unroll 1
-        for (int ch = 0; ch < kPairN / 2 / 32; ++ch) {
-          uint32_t x[32];
-          __syncwarp();
-          tmem_ld_32x32b_x32(lanes + (uint32_t)((sum & 1) * kPairN + ch * 32), x);
-          tmem_wait_ld();
-          if (ch == kPairN / 2 / 32 - 1) release(sum);
-          const int c0 = n0 + ch * 32;
-          const int cols = a.D - c0;
-          float y[32];
-#pragma unroll
-          for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
-          if (!few) add_rests(a, rests, ra, rb, (int)a.v0 + t.m0 + (int)rank * (kPairM / 2) + q * 32, c0, lane, y);
-          else
-            for (int r = na; r < nb; ++r) add_row(a.hc + (int64_t)r * a.hc_stride + c0, a.rest[r], cols, a.f16, y);
-          if (rest != 0.f) add_row(wrow + c0, rest, cols, a.f16, y);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) y[j] *= f;
-          if (live && cols > 0 && t.job == 0) {
-            const bool out = a.last && a.splits == 1;  // the whole sum
-            if (!(a.first && out)) {  // several pieces or parts of k: the sums so far in fp32
-              float4* acc = reinterpret_cast<float4*>(a.acc + ((int64_t)t.split * a.acc_rows + row) * a.acc_stride + c0);
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                if (4 * i < cols) {
-                  if (!a.first) {
-                    const float4 o = acc[i];
-                    y[4 * i] += o.x;
-                    y[4 * i + 1] += o.y;
-                    y[4 * i + 2] += o.z;
-                    y[4 * i + 3] += o.w;
-                  }
-                  if (!out) acc[i] = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-                }
-              }
-            }
-            if (out) {
-              uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)a.idx[row] * a.dh_stride + c0;
-              store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
-            }
-          } else if (live && cols > 0) {
-            uint16_t* dst = static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0;
-            store16(dst, y, cols, ((a.dw_stride & 7) | (reinterpret_cast<uintptr_t>(a.dw) & 15)) == 0, a.f16,
-                    a.accumulate != 0);
-          }
-        }
-        ++sum;
-      }
-    }
-  }
-
+__device__ __forceinline__ void end_pair(const Status& st, const Cta& c) {
   // after a timeout: every copy that either CTA issued lands before the shared memory goes
   if (threadIdx.x == 0 && aborted(st)) {
     const uint64_t t0 = globaltimer_ns();
     while (globaltimer_ns() - t0 < 1000000ull) __nanosleep(1000);
   }
-  if (kMode == kProducts && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   tc_fence_before();
   __syncthreads();
   cluster_sync();
   tc_fence_after();
-  if (warp == kMmaWarp) tmem_dealloc_pair(tmem, kVCols);
+  if (threadIdx.x >> 5 == kMmaWarp) tmem_dealloc_pair(c.tmem, kVCols);
+}
+
+// Wind-down of the loading lane: the leader's barriers count both CTAs' copies, which land before the CTAs may exit.
+template <int kS>
+__device__ __forceinline__ void end_loads(const Status& st, const Cta& c, const Pipe& p) {
+  if (c.rank == 0)
+    for (uint32_t s = 0; s < kS; ++s)
+      if (s < p.issued) mbar_wait(&c.ctl->full[s], (p.issued - 1 - s) / kS & 1u, st, 21, 200000000ull, false);
+}
+// Of the MMA lane: all issued MMAs complete before tensor memory is released.
+__device__ __forceinline__ void end_mmas(const Status& st, const Cta& c) {
+  mma_commit_pair(&c.ctl->drain);
+  mbar_wait(&c.ctl->drain, 0, st, 24, 200000000ull, false);
+}
+
+template <int kMode>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
+    vocab_pair_kernel(const __grid_constant__ VocabMaps maps, VocabArgs a, Status st) {
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  constexpr int kS = kMode == kProducts ? kPStages : kVStages;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_start();
+  Cta c = begin_pair<kS>(smem_raw);
+  after_previous();
+  c.rows = a.idx ? a.head->rows : (int)a.T;
+  Pipe p;
+  if (warp < 4) {
+    if (keeps_logits(kMode)) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(regs_few(kMode)));
+    if (warp == kLoadWarp && lane == 0) {
+      load_tiles<kMode, kS>(maps, a, st, c, p);
+      end_loads<kS>(st, c, p);
+    } else if (warp == kMmaWarp && lane == 0 && c.rank == 0) {
+      if (a.debug_timeout) mbar_wait(&c.ctl->drain, 0, st, 27, kDebugTimeoutNs);  // reports GPO_ERR_TIMEOUT
+      else mma_tiles<kMode, kS>(a, st, c, p);
+      end_mmas(st, c);
+    }
+    __syncwarp();
+  } else {
+    if (keeps_logits(kMode)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
+    finish_tiles<kMode, kS>(a, st, c, p);
+  }
+  if (kMode == kProducts && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  end_pair(st, c);
 }
 
 // ------------------------------------------------------------------ tokens that take part
@@ -741,49 +832,60 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
   }
 }
 
-constexpr int kOrderKeys = 8 * kRowThreads;  // targets that a CTA compares its own with at one time
-
 // Gradient: the tokens with a target and a gradient that is not 0, in the order of their targets and, for one
 // target, their own; their number, the scale of an fp16 dz, their hidden rows in that order with
 // zeros up to the next k-step of the d_weight product, and the zeros of the others' d_hidden.
 // A token's place is the number of those before it in that order: every CTA counts, for its share of the
 // tokens, through all of them (T^2 / 152 comparisons in shared memory: 27 tokens with 4096 in 0.3 us of a
-// warp each), with no exchange between CTAs and no second launch.
-template <class Id>
-__global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, Status st) {
-  constexpr int kW = kRowThreads / 32;
-  __shared__ int s_key[kOrderKeys];
-  __shared__ int s_own[kRowThreads], s_place[kRowThreads], s_all[kW];
-  __shared__ float s_big[kW];
+// warp each), with no exchange between CTAs and no second launch.  smem: order_smem(kThreads) bytes.
+__host__ __device__ constexpr size_t order_smem(int threads) { return sizeof(int) * (size_t)(10 * threads + 2 * 32); }
+
+template <int kThreads>
+__device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& st, unsigned char* smem, int cta, int ctas) {
+  constexpr int kW = kThreads / 32, kKeys = 8 * kThreads;  // targets that own ones are compared with at one time
+  int* s_key = reinterpret_cast<int*>(smem);
+  int *s_own = s_key + kKeys, *s_place = s_own + kThreads, *s_all = s_place + kThreads;
+  float* s_big = reinterpret_cast<float*>(s_all + 32);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  let_next_start();
-  const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
-  const Id* target = static_cast<const Id*>(a.target);
+  const int64_t ta = a.T * cta / ctas, tb = a.T * (cta + 1) / ctas;
   const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
   const bool vec = ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0;
-  auto key_of = [&](Id id, float g, float e) { return id >= 0 && id < a.V && (g != 0.f || e != 0.f) ? (int)id : kNoKey; };
+  auto key_of = [&](int64_t id, float g, float e) { return id >= 0 && id < a.V && (g != 0.f || e != 0.f) ? (int)id : kNoKey; };
   int all = 0;
   float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
-  for (int64_t o = ta; o < tb || o == ta; o += kRowThreads) {  // (a CTA without tokens counts them all, too)
-    const int own = (int)max((int64_t)0, min((int64_t)kRowThreads, tb - o));
+  for (int64_t o = ta; o < tb || o == ta; o += kThreads) {  // (a CTA without tokens counts them all, too)
+    const int own = (int)max((int64_t)0, min((int64_t)kThreads, tb - o));
     const bool mine = threadIdx.x < own;
-    const Id my_id = mine ? target[o + threadIdx.x] : (Id)-1;
+    const int64_t my_id = mine ? load_id(a.target, a.id8, o + threadIdx.x) : -1;
     const float my_g = mine ? a.g[o + threadIdx.x] : 0.f, my_e = mine && a.ge ? a.ge[o + threadIdx.x] : 0.f;
-    for (int64_t c = 0; c < a.T; c += kOrderKeys) {
-      const int n = (int)min((int64_t)kOrderKeys, a.T - c);
-      Id id[8];
+    for (int64_t c = 0; c < a.T; c += kKeys) {
+      const int n = (int)min((int64_t)kKeys, a.T - c);
+      int64_t id[8];
       float g[8], e[8];
+      // (one branch around the loads of a thread, which are then in flight together)
+      if (a.id8) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int u = k * kThreads + threadIdx.x;
+          id[k] = u < n ? static_cast<const int64_t*>(a.target)[c + u] : -1;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int u = k * kThreads + threadIdx.x;
+          id[k] = u < n ? static_cast<const int32_t*>(a.target)[c + u] : -1;
+        }
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int u = k * kRowThreads + threadIdx.x;
-        id[k] = u < n ? target[c + u] : (Id)-1;
+        const int u = k * kThreads + threadIdx.x;
         g[k] = u < n ? a.g[c + u] : 0.f;
         e[k] = 0.f;
       }
       if (a.ge) {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          if (k * kRowThreads + threadIdx.x < n) e[k] = a.ge[c + k * kRowThreads + threadIdx.x];
+          if (k * kThreads + threadIdx.x < n) e[k] = a.ge[c + k * kThreads + threadIdx.x];
       }
       __syncthreads();  // the last chunk's readers are done
       if (c == 0 && mine) {
@@ -792,7 +894,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
       }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int u = k * kRowThreads + threadIdx.x;
+        const int u = k * kThreads + threadIdx.x;
         const int key = key_of(id[k], g[k], e[k]);
         if (u < n) s_key[u] = key;
         if (o == ta) {
@@ -800,14 +902,14 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
             ++all;
             bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
           }
-          if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, (int)(c + u));
+          if (id[k] >= a.V && cta == 0) report(st, GPO_ERR_SHAPE, 26, (int)(c + u));
         }
       }
       __syncthreads();
       for (int w = warp; w < own; w += kW) {
         const int key = s_own[w];
         if (key == kNoKey) continue;
-        const int self = (int)min((int64_t)kOrderKeys, max((int64_t)0, o + w - c));  // tokens of the chunk before this one
+        const int self = (int)min((int64_t)kKeys, max((int64_t)0, o + w - c));  // tokens of the chunk before this one
         int before = 0;
 #pragma unroll 4
         for (int u = lane; u < n; u += 32) before += s_key[u] < key + (u < self ? 1 : 0);
@@ -845,8 +947,8 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
     s_big[warp] = bound;
   }
   __syncthreads();
-  all = __reduce_add_sync(0xffffffffu, s_all[lane]);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
+  all = __reduce_add_sync(0xffffffffu, lane < kW ? s_all[lane] : 0);
+  if (cta == 0 && threadIdx.x == 0) {
     for (int w = 0; w < kW; ++w) bound = fmaxf(bound, s_big[w]);
     float s = 1.f;
     if (a.f16 && bound > 0.f && isfinite(bound)) {
@@ -857,29 +959,33 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
     a.head->rows = all;
     a.head->dz_scale = s;
   }
-  if (blockIdx.x == gridDim.x - 1) {
+  if (cta == ctas - 1) {
     const int pad = (all + kTile16 - 1) / kTile16 * kTile16;
     for (int r = all + warp; r < pad; r += kW)
       for (int c = lane; c < chunks; c += 32) reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride)[c] = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
-// d_hidden from the sums of its parts of k, added in order.
-__global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st) {
-  after_previous();
-  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
-  const int rows = a.head->rows, quads = (a.D + 3) / 4;
+__global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, Status st) {
+  __shared__ __align__(16) unsigned char smem[order_smem(kRowThreads)];
+  let_next_start();
+  order_tokens<kRowThreads>(a, st, smem, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// d_hidden from the sums of its parts of k, added in order, by threads i0, i0 + step, ..
+__device__ __forceinline__ void add_parts(const VocabArgs& a, int rows, int64_t i0, int64_t step) {
+  const int quads = (a.D + 3) / 4;
   const bool vec = ((a.dh_stride & 3) | (reinterpret_cast<uintptr_t>(a.dh) & 7)) == 0;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < (int64_t)rows * quads; i += (int64_t)gridDim.x * blockDim.x) {
+  for (int64_t i = i0; i < (int64_t)rows * quads; i += step) {
     const int row = (int)(i / quads), c = (int)(i - (int64_t)row * quads) * 4;
     const float* p = a.acc + (int64_t)row * a.acc_stride + c;
-    float4 s = *reinterpret_cast<const float4*>(p);
+    float4 s = __ldcg(reinterpret_cast<const float4*>(p));
 #pragma unroll 4
     for (int k = 1; k < a.splits; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(p + k * a.acc_rows * a.acc_stride);
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p + k * a.acc_rows * a.acc_stride));
       s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
     }
-    uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)a.idx[row] * a.dh_stride + c;
+    uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)__ldcg(a.idx + row) * a.dh_stride + c;
     const uint2 o = make_uint2(pack16(s.x, s.y, a.f16), pack16(s.z, s.w, a.f16));
     if (vec && c + 4 <= a.D) {
       *reinterpret_cast<uint2*>(dst) = o;
@@ -888,6 +994,12 @@ __global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st
       for (int j = 0; j < 4 && c + j < a.D; ++j) dst[j] = h[j];
     }
   }
+}
+
+__global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st) {
+  after_previous();
+  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  add_parts(a, a.head->rows, (int64_t)blockIdx.x * blockDim.x + threadIdx.x, (int64_t)gridDim.x * blockDim.x);
 }
 
 // ------------------------------------------------------------------ joining the parts of a row
@@ -971,7 +1083,7 @@ cudaError_t setup_mode() {
   const cudaError_t e = cudaFuncGetAttributes(&at, vocab_pair_kernel<kMode>);
   if (e != cudaSuccess) return e;
   // (a split that asks for more registers than the launch brings would wait for ever)
-  if (kMode != kProducts && at.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
+  if (keeps_logits(kMode) && at.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
   return cudaFuncSetAttribute(vocab_pair_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kVSmem);
 }
 
@@ -990,6 +1102,8 @@ cudaError_t setup_vocab() {
   if (e == cudaSuccess) e = setup_mode<kLseEnt>();
   if (e == cudaSuccess) e = setup_mode<kDz>();
   if (e == cudaSuccess) e = setup_mode<kDzEnt>();
+  if (e == cudaSuccess) e = setup_mode<kDzWide>();
+  if (e == cudaSuccess) e = setup_mode<kDzWideEnt>();
   if (e == cudaSuccess) e = setup_mode<kProducts>();
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -1017,8 +1131,7 @@ cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Sta
 
 cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st) {
   const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
-  if (a.id8) vocab_order_kernel<int64_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
-  else vocab_order_kernel<int32_t><<<grid, kRowThreads, 0, lc.stream>>>(a, st);
+  vocab_order_kernel<<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();
 }
 
@@ -1036,17 +1149,19 @@ cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Sta
 }
 
 cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {
-  return a.ge ? launch_pair<kDzEnt>(lc, m, a, st, tiles_of(a.T, a.vn)) : launch_pair<kDz>(lc, m, a, st, tiles_of(a.T, a.vn));
+  const int64_t tiles = tiles_of(a.T, a.vn);
+  if (a.D <= kTile16 * kSegDz) return a.ge ? launch_pair<kDzEnt>(lc, m, a, st, tiles) : launch_pair<kDz>(lc, m, a, st, tiles);
+  return a.ge ? launch_pair<kDzWideEnt>(lc, m, a, st, tiles) : launch_pair<kDzWide>(lc, m, a, st, tiles);
 }
 
 // With few row tiles the k of d_hidden, the vocabulary, is cut into parts for as many pairs as its share of
 // the work is worth (300 tokens, 8191 x 512: one pair's sum over 8191 rows took 35 of the call's 67 us).
 int vocab_splits(int64_t T, int64_t vn, int64_t D) {
   const int64_t dt = (D + kPairN - 1) / kPairN, mt = (T + kPairM - 1) / kPairM, kb = (vn + kTile16 - 1) / kTile16;
-  const int64_t work = mt * dt * kb + (vn + kPairN - 1) / kPairN * dt * ((T + kTile16 - 1) / kTile16);
-  const int64_t share = max(work / kVocabPairs, (int64_t)8);  // k-steps of one pair
+  const int64_t work = mt * dt * kb + (vn + kPairN - 1) / kPairN * dt * max((T + kTile16 - 1) / kTile16, (int64_t)kEpiSteps);
+  const int64_t share = max(work / kVocabPairs, (int64_t)kEpiSteps);  // k-steps of one pair
   if (kb <= 24) return 1;  // (less time than the launch that adds the parts)
-  return (int)max((int64_t)1, min(kb / share, (int64_t)kVocabMaxSplits));
+  return (int)max((int64_t)1, min((kb + share - 1) / share, (int64_t)kVocabMaxSplits));
 }
 
 cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {

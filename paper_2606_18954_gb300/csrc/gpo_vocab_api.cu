@@ -41,7 +41,8 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L.few = !grad && T <= kVocabFew;
   L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
   L.status = take(sizeof(uint32_t) * kStatusWords);
-  if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);  // (next to the status words: cleared with them)
+  // (next to the status words: cleared with them)
+  if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);
   L.head = take(sizeof(VocabHead));
   if (T > 0 && L.listed) {
     L.idx = take(sizeof(int) * (size_t)T);
