@@ -1027,6 +1027,7 @@ struct VocabArgs {
   void* dw;
   int64_t dw_stride;
   int accumulate;
+  int dw_bulk;           // d_weight's rows take bulk stores (maps.dw)
   int debug_timeout;
 };
 
@@ -1034,6 +1035,7 @@ struct VocabArgs {
 // (few tokens: 64 x vocab_few_columns of hidden, 64 x 32 of the matrix).
 struct VocabMaps {
   CUtensorMap h, hc, w, dz;
+  CUtensorMap dw;  // d_weight, boxes of 64 x 32
 };
 
 cudaError_t setup_vocab();

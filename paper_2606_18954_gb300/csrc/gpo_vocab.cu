@@ -62,6 +62,7 @@ template <int kMode>
 __device__ __forceinline__ constexpr int segment_of() {
   return is_lse(kMode) ? kSegLse : is_wide(kMode) ? kSegDz : 1 << 30;
 }
+constexpr int kEpiBar = 1;                          // named barrier of the epilogue warps
 constexpr int kNoKey = 0x7fffffff;                 // above every target: a token without a gradient
 constexpr int kRaster = 32;                        // row tiles that share one pass over the columns
 
@@ -74,12 +75,16 @@ struct __align__(8) VocabCtl {
   uint32_t tmem_base;
 };
 
-// Per epilogue warp of the products: sums of 32 rows x 64 columns (see sum_rests).
+// Shared memory of the products beside their ring: per epilogue warp the sums of 32 rows x 64 columns (see
+// sum_rests) or 32 rows of 128 bytes on their way out, then the targets of up to kListed tokens.
 constexpr int kRestRow = 65;
-constexpr size_t kRestBytes = sizeof(float) * 32 * kRestRow * kVEpiWarps;
-constexpr size_t kVSmem = ((sizeof(VocabCtl) + 15) & ~size_t(15)) + 1023 +
-                          ((size_t)kVStages * kVStage > (size_t)kPStages * kVStage + kRestBytes
-                               ? (size_t)kVStages * kVStage : (size_t)kPStages * kVStage + kRestBytes);
+constexpr int kWarpBytes = 9 * 1024;
+constexpr int kListed = 4096;
+static_assert(kWarpBytes >= 4 * 32 * kRestRow, "sums of one warp");
+constexpr size_t kVCtl = (sizeof(VocabCtl) + 15) & ~size_t(15);
+constexpr size_t kVSmem = kVCtl + 1023 + (size_t)kVStages * kVStage;
+constexpr size_t kPSmem = kVCtl + 1023 + (size_t)kPStages * kVStage + (size_t)kVEpiWarps * kWarpBytes + 4 * (size_t)kListed;
+__host__ __device__ constexpr size_t smem_of(int mode) { return mode == kProducts ? kPSmem : kVSmem; }
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int f16) {
   if (f16) {
@@ -110,7 +115,7 @@ struct Plan {
   int light0, nlight, extra;  // pairs from light0 on take `extra` d_weight tiles more, for the d_hidden tile they lack
 };
 
-constexpr int kEpiSteps = 12;  // k-steps that a tile's epilogue in the products takes the time of
+constexpr int kEpiSteps = 8;  // k-steps that a tile's epilogue in the products takes the time of
 template <int kMode>
 __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   Plan q;
@@ -219,11 +224,11 @@ __device__ __forceinline__ int first_not_below(const int* x, int n, int v, int l
   int lo = 0, hi = n;
   while (hi - lo > 32) {
     const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && __ldcg(x + at) < v));
+    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && x[at] < v));
     lo += below * step;
     hi = min(hi, lo + step);
   }
-  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && __ldcg(x + lo + lane) < v));
+  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && x[lo + lane] < v));
 }
 
 // Brings `cols` 16-bit columns of a row into L1, for add_row.
@@ -257,13 +262,13 @@ __device__ __forceinline__ void add_row(const uint16_t* x, float w, int cols, in
 // vocabulary: 4000 of 1608 x 208, the products in 94 us with one column of 32 and eight in flight.)
 constexpr int kFewRests = 3;
 constexpr int kRestsAhead = 16;
-__device__ __forceinline__ void sum_rests(const VocabArgs& a, float* sums, int ra, int rb, int v, int c0, int lane) {
+__device__ __forceinline__ void sum_rests(const VocabArgs& a, const int* by_target, float* sums, int ra, int rb, int v, int c0, int lane) {
   for (int j = lane; j < 32 * kRestRow; j += 32) sums[j] = 0.f;
   __syncwarp();
   const int col = c0 + 2 * lane;
   const uint16_t* h = a.hc + (col < a.hc_stride ? col : 0);  // (rows of whole 16 bytes: a pair never straddles their end)
   float s0 = 0.f, s1 = 0.f;
-  int row = __ldcg(a.by_target + ra);
+  int row = by_target[ra];
   for (int r = ra; r < rb; r += kRestsAhead) {
     uint32_t x[kRestsAhead];
     float w[kRestsAhead];
@@ -273,7 +278,7 @@ __device__ __forceinline__ void sum_rests(const VocabArgs& a, float* sums, int r
       const int rk = min(r + k, rb - 1);
       x[k] = *reinterpret_cast<const uint32_t*>(h + (int64_t)rk * a.hc_stride);
       w[k] = r + k < rb ? __ldcg(a.rest + rk) : 0.f;
-      at[k] = __ldcg(a.by_target + rk);
+      at[k] = by_target[rk];
     }
 #pragma unroll
     for (int k = 0; k < kRestsAhead; ++k) {
@@ -421,7 +426,7 @@ __device__ __forceinline__ void dz_columns(const VocabArgs& a, const DzRow& w, c
 // (dz of logits that are one accumulation goes 32 columns at a time: a fourth of the code, which a call of few
 // tiles runs cold.)
 template <int kMode, int kS>
-__device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
+__device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
   constexpr bool kLogits = is_lse(kMode);
   constexpr int seg = segment_of<kMode>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = c.rows;
@@ -442,6 +447,17 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
     __syncwarp();
     if (lane == 0) mbar_arrive_cluster(te + 8u * (uint32_t)(n & 1));
   };
+  // products: this warp's part of the shared memory, and the tokens' targets, where they fit
+  unsigned char* own = c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage + (warp - 4) * kWarpBytes;
+  const int* by_target = a.by_target;
+  if constexpr (kMode == kProducts) {
+    if (rows <= kListed) {
+      int* list = reinterpret_cast<int*>(c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage + kVEpiWarps * kWarpBytes);
+      for (int i = (int)threadIdx.x - 128; i < rows; i += 32 * kVEpiWarps) list[i] = a.by_target[i];
+      by_target = list;
+      asm volatile("bar.sync %0, %1;" ::"n"(kEpiBar), "n"(32 * kVEpiWarps) : "memory");
+    }
+  }
   Tile t;
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
     const int row = t.m0 + r;
@@ -564,15 +580,14 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
       }
     } else {
       const bool live = row < (t.job == 1 ? (int)a.vn : rows);
-      float* rests = reinterpret_cast<float*>(c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage) + (warp - 4) * 32 * kRestRow;
       int ra = 0, rb = 0, na = 0, nb = 0;  // d_weight: the tokens whose targets are rows of this warp, of this lane
       float rest = 0.f;                    // d_hidden: the row's own
       const uint16_t* wrow = nullptr;
       if (t.job == 1) {
         const int v = (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32;
-        ra = first_not_below(a.by_target, rows, v, lane);
+        ra = first_not_below(by_target, rows, v, lane);
         for (rb = ra; rb < rows; rb += 32) {  // (few tokens' targets are near each other)
-          const int y = rb + lane < rows ? __ldcg(a.by_target + rb + lane) : kNoKey;
+          const int y = rb + lane < rows ? by_target[rb + lane] : kNoKey;
           const int in = __popc(__ballot_sync(0xffffffffu, y < v + 32));
           for (int k = 0; k < in; ++k) {
             const int yk = __shfl_sync(0xffffffffu, y, k);
@@ -588,7 +603,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
         na += ra;
         nb += ra;
       } else if (live && t.split == 0) {
-        const int y = __ldcg(a.by_target + row);
+        const int y = by_target[row];
         if (y >= a.v0 && y < a.v0 + a.vn) {
           rest = __ldcg(a.rest + row);
           wrow = static_cast<const uint16_t*>(a.weight) + (int64_t)y * a.weight_stride;
@@ -602,6 +617,10 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
         prefetch_row(a.hc + (int64_t)i * a.hc_stride + n0, some);
       }
       if (wrow) prefetch_row(wrow + n0, some);
+      float* rests = reinterpret_cast<float*>(own);
+      const bool bulk = t.job == 1 && few && a.dw_bulk != 0;
+      if (lane == 0) bulk_read();  // (the last tile's rows have left)
+      __syncwarp();
       if (!ready(p.sum)) return false;
       const float f = t.kb > 0 ? a.scale / __ldcg(&a.head->dz_scale) : 0.f;
 #pragma unroll 1
@@ -617,7 +636,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
 #pragma unroll
         for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
         if (!few) {
-          if ((ch & 1) == 0) sum_rests(a, rests, ra, rb, (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32, c0, lane);
+          if ((ch & 1) == 0) sum_rests(a, by_target, rests, ra, rb, (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32, c0, lane);
 #pragma unroll
           for (int j = 0; j < 32; ++j) y[j] += rests[lane * kRestRow + (ch & 1) * 32 + j];
         } else {
@@ -651,6 +670,23 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
             uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)__ldcg(a.idx + row) * a.dh_stride + c0;
             store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
           }
+        } else if (bulk && cols > 0) {
+          // 64 columns of the warp's 32 rows, 128 bytes each with the 128-byte swizzle, go out as one bulk copy, which
+          // leaves out what lies past the matrix: with a store per lane and row a tile's took 4 us of the load and store unit
+          if ((ch & 1) == 0 && ch > 0) {
+            if (lane == 0) bulk_read();
+            __syncwarp();
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(own + lane * 128 + ((((ch & 1) * 4 + i) ^ (lane & 7)) << 4)) =
+                make_uint4(pack16(y[8 * i], y[8 * i + 1], a.f16), pack16(y[8 * i + 2], y[8 * i + 3], a.f16),
+                           pack16(y[8 * i + 4], y[8 * i + 5], a.f16), pack16(y[8 * i + 6], y[8 * i + 7], a.f16));
+          if ((ch & 1) == 1 || cols <= 32) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) bulk_store_2d(&maps.dw, own, n0 + (ch & ~1) * 32, (int)a.v0 + row);
+          }
         } else if (live && cols > 0) {
           uint16_t* dst = static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0;
           store16(dst, y, cols, ((a.dw_stride & 7) | (reinterpret_cast<uintptr_t>(a.dw) & 15)) == 0, a.f16,
@@ -659,6 +695,10 @@ __device__ __forceinline__ bool finish_tiles(const VocabArgs& a, const Status& s
       }
       ++p.sum;
     }
+  }
+  if constexpr (kMode == kProducts) {
+    if (lane == 0) bulk_done();
+    __syncwarp();
   }
   return true;
 }
@@ -746,7 +786,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     __syncwarp();
   } else {
     if (keeps_logits(kMode)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
-    finish_tiles<kMode, kS>(a, st, c, p);
+    finish_tiles<kMode, kS>(maps, a, st, c, p);
   }
   if (kMode == kProducts && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   end_pair(st, c);
@@ -1084,13 +1124,13 @@ cudaError_t setup_mode() {
   if (e != cudaSuccess) return e;
   // (a split that asks for more registers than the launch brings would wait for ever)
   if (keeps_logits(kMode) && at.numRegs < kRegsLaunch) return cudaErrorInvalidConfiguration;
-  return cudaFuncSetAttribute(vocab_pair_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kVSmem);
+  return cudaFuncSetAttribute(vocab_pair_kernel<kMode>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(kMode));
 }
 
 template <int kMode>
 cudaError_t launch_pair(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, int64_t tiles) {
   const int64_t pairs = min((int64_t)g_pairs, max(tiles, (int64_t)1));
-  return launch_after(vocab_pair_kernel<kMode>, (unsigned)(2 * pairs), kVThreads, kVSmem, lc.stream, m, a, st);
+  return launch_after(vocab_pair_kernel<kMode>, (unsigned)(2 * pairs), kVThreads, smem_of(kMode), lc.stream, m, a, st);
 }
 
 int64_t tiles_of(int64_t rows, int64_t cols) { return ((rows + kPairM - 1) / kPairM) * ((cols + kPairN - 1) / kPairN); }
@@ -1109,7 +1149,7 @@ cudaError_t setup_vocab() {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
   cfg.blockDim = dim3(kVThreads);
-  cfg.dynamicSmemBytes = kVSmem;
+  cfg.dynamicSmemBytes = kPSmem;
   cudaLaunchAttribute at;
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim.x = 2;

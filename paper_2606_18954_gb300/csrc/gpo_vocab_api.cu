@@ -37,7 +37,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   const int64_t T = v.num_tokens;
   L = VocabLayout();
   L.tp = up_to(T, kPairM);
-  L.hc_stride = up_to(v.d, 8);
+  L.hc_stride = up_to(v.d, 64);  // rows of whole 128-byte lines (see vocab_pack_kernel)
   L.few = !grad && T <= kVocabFew;
   L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
   L.status = take(sizeof(uint32_t) * kStatusWords);
@@ -302,6 +302,8 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.dw = out->d_weight;
   a.dw_stride = out->d_weight_stride;
   a.accumulate = out->accumulate != 0;
+  a.dw_bulk = a.dw && !a.accumulate && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
+              encode_map(&m.dw, encode_fn(), a.dw, v->d, v->vocab, a.dw_stride, a.f16, 32);
   Stages stage(ctx, stream, at<void>(workspace, L.status));
   stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });
   for (int64_t v0 = 0; v0 < v->vocab; v0 += L.piece) {
