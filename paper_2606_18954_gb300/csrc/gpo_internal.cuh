@@ -976,6 +976,9 @@ constexpr int kPairN = 256;      // columns of one tile
 // Products (tokens x vocabulary x width) from which on the forward pass first lists the tokens with a target:
 // all of them take 145 us or more then, the list 10
 constexpr int64_t kVocabListed = (int64_t)1 << 37;
+// Steps of 64 k after which the tensor cores' sum of a logit is taken over into registers: up to kVocabFew tokens,
+// forward, dz (see gpo_vocab.cu)
+constexpr int kVocabFewSeg = 2, kVocabSeg = 8, kVocabDzSeg = 32;
 constexpr int kVocabPairs = 76;      // CTA pairs that the split of d_hidden's k reckons with (GB300: 152 SMs)
 constexpr int kVocabMaxSplits = 32;
 int vocab_splits(int64_t T, int64_t vn, int64_t D);

@@ -28,7 +28,7 @@ namespace gpo {
 
 namespace {
 
-// Ent: with the entropy; Wide: dz of logits that are several accumulations (see kSegDz)
+// Ent: with the entropy; Wide: dz of logits that are several accumulations (see kVocabDzSeg)
 enum Mode { kLse, kLseEnt, kDz, kDzEnt, kDzWide, kDzWideEnt, kProducts };
 __host__ __device__ constexpr bool is_lse(int mode) { return mode == kLse || mode == kLseEnt; }
 __host__ __device__ constexpr bool is_wide(int mode) { return mode == kDzWide || mode == kDzWideEnt; }
@@ -52,15 +52,15 @@ static_assert(128 * regs_few(kDzWide) + 256 * regs_many(kDzWide) <= kVThreads * 
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
 constexpr int kVStage = 4 * kVBox;                 // A and B halves of one k-step, per CTA
 constexpr int kVCols = 512;                        // two accumulators of 256 columns
-// Logits: steps of 64 k after which the tensor cores' sum is taken over into registers.  Their fp32
-// additions drop the bits below the sum's last one, always towards zero, so that a sum of d products
-// shrinks by about d / 16 half ulps: 7e-6 of a logit at d = 4096, too much for the log-probability of
-// a nearly certain token.  Shorter sums, added in registers with rounding, keep that down, but reading
-// tensor memory holds up the MMAs.
-constexpr int kSegLse = 8, kSegDz = 32;
+// Logits: after kVocabSeg (dz: kVocabDzSeg) steps of 64 k the tensor cores' sum is taken over into registers.  Their
+// fp32 additions drop the bits below the sum's last one, always towards zero, so that a sum of d products
+// shrinks by about d / 130 ulps: 4e-6 of a logit at d = 4096, too much for the log-probability of
+// a nearly certain token.  Shorter sums, added in registers with rounding, keep that down (the mean of what is left
+// is given back by logit_scale on the host), but reading tensor memory holds up the MMAs: 8192 tokens, 131072 x 2048
+// take 2175 us in one sum, 2230 by 512 products, 2435 by 384, 2645 by 256.
 template <int kMode>
 __device__ __forceinline__ constexpr int segment_of() {
-  return is_lse(kMode) ? kSegLse : is_wide(kMode) ? kSegDz : 1 << 30;
+  return is_lse(kMode) ? kVocabSeg : is_wide(kMode) ? kVocabDzSeg : 1 << 30;
 }
 constexpr int kEpiBar = 1;                          // named barrier of the epilogue warps
 constexpr int kNoKey = 0x7fffffff;                 // above every target: a token without a gradient
@@ -1190,7 +1190,7 @@ cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Sta
 
 cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {
   const int64_t tiles = tiles_of(a.T, a.vn);
-  if (a.D <= kTile16 * kSegDz) return a.ge ? launch_pair<kDzEnt>(lc, m, a, st, tiles) : launch_pair<kDz>(lc, m, a, st, tiles);
+  if (a.D <= kTile16 * kVocabDzSeg) return a.ge ? launch_pair<kDzEnt>(lc, m, a, st, tiles) : launch_pair<kDz>(lc, m, a, st, tiles);
   return a.ge ? launch_pair<kDzWideEnt>(lc, m, a, st, tiles) : launch_pair<kDzWide>(lc, m, a, st, tiles);
 }
 

@@ -25,7 +25,6 @@ constexpr int kFewTile = 128;
 constexpr int kFewStages = 12;        // at most
 constexpr int kFewRing = 200 * 1024;  // bytes
 constexpr int kFewBufs = 4;           // accumulators of kN columns
-constexpr int kFewSeg = 2;            // k-steps of 64 per accumulation
 
 struct __align__(8) FewCtl {
   uint64_t full[kFewStages];
@@ -154,14 +153,14 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       const uint32_t idesc = (1u << 4) | (a.f16 ? 0u : (1u << 7) | (1u << 10)) | ((uint32_t)(kN >> 3) << 17) |
                              ((uint32_t)(kFewTile >> 4) << 24);
       for (int u = u0; ok && u < u1; u += kFewTile / kFewUnit) {
-        for (int k0 = 0; ok && k0 < kb; k0 += kFewSeg, ++sum) {
+        for (int k0 = 0; ok && k0 < kb; k0 += kVocabFewSeg, ++sum) {
           const int buf = sum % kFewBufs;
           if (!mbar_wait(&ctl->tempty[buf], ((uint32_t)(sum / kFewBufs) & 1u) ^ 1u, st, 43)) {
             ok = false;
             break;
           }
           tc_fence_after();
-          for (int k = k0; k < min(kb, k0 + kFewSeg); ++k) {
+          for (int k = k0; k < min(kb, k0 + kVocabFewSeg); ++k) {
             if (!mbar_wait(&ctl->full[stage], phase, st, 44)) {
               ok = false;
               break;
@@ -202,7 +201,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       float z[kCols];
 #pragma unroll
       for (int j = 0; j < kCols; ++j) z[j] = 0.f;
-      for (int k0 = 0; k0 < kb; k0 += kFewSeg, ++sum) {
+      for (int k0 = 0; k0 < kb; k0 += kVocabFewSeg, ++sum) {
         const int buf = sum % kFewBufs;
         ok = __all_sync(0xffffffffu, mbar_wait(&ctl->tfull[buf], (uint32_t)(sum / kFewBufs) & 1u, st, 46));
         if (!ok) break;
