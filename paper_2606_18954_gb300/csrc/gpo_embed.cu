@@ -228,8 +228,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(EmbedArgs a
       __syncwarp();
       if (in) {
         const int place = first[row] + at + __popc(same & ((1u << lane) - 1u));
-        a.perm[place] = (int)(t0 + 32 * k);
-        a.sid[place] = (int)id[k];
+        if (GPO_BOUNDS(st, place, a.T, kWhereEmbedPlace)) {
+          a.perm[place] = (int)(t0 + 32 * k);
+          a.sid[place] = (int)id[k];
+        }
         if (lane == __ffs(same) - 1) hist[warp * per + row] = at + __popc(same);
       }
       __syncwarp();
@@ -279,7 +281,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
 #pragma unroll
         for (int i = 0; i < C::kPer; ++i)
           if (C::at(b, lane, i) < a.D) part[C::at(b, lane, i)] = s[i];
-      } else {
+      } else if (GPO_BOUNDS(st, run, a.V, kWhereEmbedRow)) {
         C::store(out + (int64_t)run * a.dst_stride, b, lane, a.D, s, a.scale, a.accumulate != 0, true);
       }
 #pragma unroll

@@ -187,6 +187,10 @@ enum : int {
   kWhereEdges = 103,       // an item's spanning-forest edge
   kWhereNorms = 104,       // an fp32 norm of the similarity stage
   kWhereSmemRow = 105,     // a row of the fp32 group-resident kernel's shared-memory copy
+  kWhereVocabToken = 110,  // a token that a vocabulary kernel writes for
+  kWhereVocabRow = 111,    // a row of d_weight or of the gathered tokens
+  kWhereEmbedPlace = 112,  // a place in the list of sorted tokens
+  kWhereEmbedRow = 113,    // a row of the embedding's table
 };
 
 __device__ __forceinline__ uint64_t globaltimer_ns() {

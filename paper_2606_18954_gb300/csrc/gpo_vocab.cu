@@ -666,8 +666,9 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
               }
             }
           }
-          if (out) {
-            uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)__ldcg(a.idx + row) * a.dh_stride + c0;
+          const int tok = out ? __ldcg(a.idx + row) : 0;
+          if (out && GPO_BOUNDS(st, tok, a.T, kWhereVocabToken)) {
+            uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)tok * a.dh_stride + c0;
             store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
           }
         } else if (bulk && cols > 0) {
@@ -687,7 +688,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
             __syncwarp();
             if (lane == 0) bulk_store_2d(&maps.dw, own, n0 + (ch & ~1) * 32, (int)a.v0 + row);
           }
-        } else if (live && cols > 0) {
+        } else if (live && cols > 0 && GPO_BOUNDS(st, a.v0 + row, a.V, kWhereVocabRow)) {
           uint16_t* dst = static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0;
           store16(dst, y, cols, ((a.dw_stride & 7) | (reinterpret_cast<uintptr_t>(a.dw) & 15)) == 0, a.f16,
                   a.accumulate != 0);
@@ -852,7 +853,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
     if (in) {
       const int r = lower + __popc(m & ((1u << lane) - 1u));
       s_list[r] = (int)t;
-      a.idx[base + r] = (int)t;
+      if (GPO_BOUNDS(st, base + r, a.T, kWhereVocabRow)) a.idx[base + r] = (int)t;
     } else if (t < tb) {
       a.logp[t] = 0.f;
       if (a.lse_out) a.lse_out[t] = 0.f;
@@ -961,7 +962,7 @@ __device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& s
     for (int w = warp; w < own; w += kW) {
       const int64_t t = o + w;
       const int key = s_own[w];
-      if (key != kNoKey) {
+      if (key != kNoKey && GPO_BOUNDS(st, s_place[w], a.T, kWhereVocabRow)) {
         const int r = s_place[w];
         if (lane == 0) {
           a.idx[r] = (int)t;

@@ -68,6 +68,50 @@ def test_logp(gp, dtype, shape):
         close(plain[k], ref[k], ref["t_" + k], k)
 
 
+def test_logp_of_listed_tokens(gp):
+    """So many products that the tokens with a target are listed and their rows gathered first."""
+    import torch
+    from vocab_ref import close, head_exact, head_inputs
+    T, V, d = 9000, 30011, 520
+    assert T * V * d >= 1 << 37
+    for masked in (0.4, 0.0):
+        h, w, y = head_inputs(T, V, d, torch.bfloat16, masked=masked, seed=31)
+        out = gp.vocab_logp(h, w, y, entropy=True)
+        gp.check()
+        for a in range(0, T, 3000):
+            b = a + 3000
+            ref = head_exact(h[a:b], w, y[a:b], 1.0)
+            for k in ("logp", "lse", "entropy"):
+                close(out[k][a:b], ref[k], ref["t_" + k], k)
+                assert not out[k][a:b][y[a:b] < 0].any()
+            del ref
+    bad = y.clone()
+    bad[17] = V
+    import paper_2606_18954_gb300 as P
+    gp.vocab_logp(h, w, bad)
+    with pytest.raises(P.GraphPOError) as e:
+        gp.check()
+    assert e.value.code == SHAPE
+
+
+def test_logp_is_as_exact_as_32_bits(gp):
+    """2-norm errors of lse and logp against torch's own 32-bit products and sums of the same logits."""
+    import torch
+    from vocab_ref import head_exact, head_inputs
+    for dtype in (torch.bfloat16, torch.float16):
+        for T, V, d in ((40, 3000, 1024), (400, 6000, 2048)):
+            h, w, y = head_inputs(T, V, d, dtype, seed=T)
+            out = gp.vocab_logp(h, w, y)
+            gp.check()
+            ref = head_exact(h, w, y, 1.0)
+            z = h.float() @ w.float().t()
+            lse = torch.logsumexp(z, 1)
+            plain = {"lse": lse, "logp": z.gather(1, y.long()[:, None])[:, 0] - lse}
+            for k in plain:
+                err = lambda x: float((x.double() - ref[k]).norm() / ref[k].norm())  # noqa: E731
+                assert err(out[k]) <= max(1e-6, 1.5 * err(plain[k])), (k, dtype, T, err(out[k]), err(plain[k]))
+
+
 def test_a_certain_token_keeps_its_digits(gp):
     """log pi of a token with almost all the probability is -(the others' sum), a number far below
     the logits' own rounding to 1: relative to it the error is that of the logits' differences."""
@@ -163,6 +207,66 @@ def test_grad(gp, dtype, shape):
     only = gp.vocab_grad(h, w, y, f["lse"], gl, d_hidden=False, **kw)
     assert set(only) == {"d_weight"} and torch.equal(only["d_weight"], out["d_weight"])
     gp.check()
+
+
+# wide rows (logits of several accumulations), more tokens than are looked at in one go, all tokens on few targets
+GRAD_MORE = [  # tokens, vocabulary, width, pad, masked, entropy, targets
+    (70, 600, 2100, 0, 0.2, True, "any"),
+    (300, 1000, 4096, 1, 0.0, False, "any"),
+    (260, 300, 2056, 0, 0.3, True, "two"),
+    (500, 900, 200, 0, 0.1, False, "one"),
+    (4500, 700, 136, 0, 0.4, True, "two"),
+    (9000, 300, 40, 0, 0.3, True, "any"),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", GRAD_MORE)
+def test_grad_wide_rows_and_frequent_targets(gp, dtype, shape):
+    import torch
+    from vocab_ref import close, head_exact, head_inputs
+    T, V, d, pad, masked, entropy, which = shape
+    h, w, y = head_inputs(T, V, d, _types()[dtype], pad, masked, seed=T + 70, sure=8.0, id_dtype=torch.int64)
+    few = torch.tensor([V - 1, V - 1 if which == "one" else 5], device="cuda")
+    if which != "any":
+        y = torch.where(y < 0, y, few[torch.arange(T, device="cuda") % 2])
+    gl, ge = _grads(T, y, T + 1, entropy, 512.0 if dtype == "f16" else 1.0)
+    f = gp.vocab_logp(h, w, y, entropy=entropy)
+    kw = dict(entropy=f.get("entropy"), grad_entropy=ge)
+    out = gp.vocab_grad(h, w, y, f["lse"], gl, **kw)
+    again = gp.vocab_grad(h, w, y, f["lse"], gl, **kw)
+    gp.check()
+    ref = head_exact(h, w, y, 1.0, torch.nan_to_num(gl), None if ge is None else torch.nan_to_num(ge))
+    for k in ("d_hidden", "d_weight"):
+        close(out[k], ref[k], ref["t_" + k], k)
+        assert torch.equal(out[k], again[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_grad_is_as_exact_as_one_rounding(gp, dtype):
+    """The 2-norm error of the gradients against that of their exact values rounded once to the type: dz's own
+    rounding to 16 bits, whose largest part (at the targets) is kept in fp32, may add little to it.  Its other
+    entries are p g with sum of squares at most max p over the non-targets times (1 - p_target)^2, here below 0.2
+    of the target's square: with the targets' part kept, sqrt(1 + 0.2) bounds the ratio."""
+    import torch
+    from vocab_ref import head_exact, head_inputs
+    T, V, d = 500, 4000, 256
+    h, w, y = head_inputs(T, V, d, _types()[dtype], seed=21, sure=6.0)
+    gl = torch.randn(T, device="cuda") * (512.0 if dtype == "f16" else 1.0) / T
+    f = gp.vocab_logp(h, w, y)
+    out = gp.vocab_grad(h, w, y, f["lse"], gl)
+    gp.check()
+    ref = head_exact(h, w, y, 1.0, gl)
+    z = h.double() @ w.double().t()
+    p = torch.softmax(z, 1)
+    at = torch.arange(T, device="cuda")
+    py = p[at, y.long()].clone()
+    p[at, y.long()] = 0
+    share = (gl.double()[:, None] * p).square().sum() / (gl.double() * (1 - py)).square().sum()
+    assert float(share) < 0.2
+    for k in ("d_hidden", "d_weight"):
+        once = (ref[k].to(out[k].dtype).double() - ref[k]).norm()
+        assert float((out[k].double() - ref[k]).norm() / once) < math.sqrt(1.2), k
 
 
 def test_grad_against_differences(gp):
