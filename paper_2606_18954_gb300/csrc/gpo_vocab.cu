@@ -618,6 +618,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       }
       if (wrow) prefetch_row(wrow + n0, some);
       float* rests = reinterpret_cast<float*>(own);
+      const int tok = t.job == 0 && live ? __ldcg(a.idx + row) : 0;
       const bool bulk = t.job == 1 && few && a.dw_bulk != 0;
       if (lane == 0) bulk_read();  // (the last tile's rows have left)
       __syncwarp();
@@ -666,7 +667,6 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
               }
             }
           }
-          const int tok = out ? __ldcg(a.idx + row) : 0;
           if (out && GPO_BOUNDS(st, tok, a.T, kWhereVocabToken)) {
             uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)tok * a.dh_stride + c0;
             store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
