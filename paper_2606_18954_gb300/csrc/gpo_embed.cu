@@ -2,11 +2,7 @@
 //
 //   embed      embed_kernel: a warp per token and 2 KB (fp32: 2 KB) of its row, 16-byte accesses,
 //              four in flight per lane
-//   gradient   embed_sort_kernel: a stable counting sort of the tokens by id without any exchange
-//              between CTAs.  Each CTA owns up to 1024 rows of the table and reads all ids twice
-//              from L2 (4 bytes a token, against the thousands of bytes of a token's gradient row): first
-//              it counts those of its rows, per warp and row, and those of the rows before its own, which
-//              gives its place in the sorted list; then every warp places its tokens in their order.
+//   gradient   embed_sort_kernel: the tokens in the order of their ids (gpo_sort.cuh)
 //              embed_sum_kernel: the sorted tokens in pieces of equal length, a warp per piece and
 //              512 bytes of the rows: runs of one id are summed in order in fp32, a run inside the
 //              piece is a finished row, a run that the piece's ends cut leaves its sum in the
@@ -19,6 +15,7 @@
 #include <cuda_fp16.h>
 
 #include "gpo_internal.cuh"
+#include "gpo_sort.cuh"
 
 namespace gpo {
 
@@ -146,97 +143,29 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
 
 // ------------------------------------------------------------------ sort
 
-constexpr int kSortThreads = 1024;
-constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortAhead = 8;  // ids of a lane in flight
+// The ids of a CTA's tokens as the sort's keys.  (Id: a template, so that the loads of one thread need no
+// branch between them and are in flight together.)
+template <class Id>
+struct EmbedKeys {
+  using Key = Id;
+  const Id* ids;
+  __device__ __forceinline__ void load(int64_t t0, int64_t tb, Id (&id)[kSortAhead]) {
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) id[k] = t0 + 32 * k < tb ? ids[t0 + 32 * k] : (Id)-1;
+  }
+};
 
-size_t sort_smem(int rows) { return sizeof(int) * (size_t)(kSortWarps + 1) * rows; }
-
-// CTA b owns the rows [b * per, (b + 1) * per) of the table.  (Id: a template, so that the loads of
-// one thread need no branch between them and are in flight together.)
 template <class Id>
 __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(EmbedArgs a, int per, Status st) {
-  extern __shared__ int hist[];  // [kSortWarps][per] counts, then places; [per] first place of a row
-  __shared__ int wsum[kSortWarps];
-  __shared__ int s_base;
-  int* first = hist + kSortWarps * per;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const Id r0 = (Id)blockIdx.x * per, r1 = (Id)min((int64_t)r0 + per, a.V);
-  const int nr = (int)(r1 - r0);
+  extern __shared__ int hist[];
   let_next_start();
-  const Id* ids = static_cast<const Id*>(a.ids);
-  for (int i = threadIdx.x; i < kSortWarps * per; i += kSortThreads) hist[i] = 0;
-  if (threadIdx.x == 0) s_base = 0;
-  __syncthreads();
-  const int64_t seg = ((a.T + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;
-  const int64_t ta = min(a.T, warp * seg), tb = min(a.T, ta + seg);
-  int below = 0;
-  for (int64_t t0 = ta + lane; t0 < tb; t0 += 32 * kSortAhead) {
-    Id id[kSortAhead];
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) id[k] = t0 + 32 * k < tb ? ids[t0 + 32 * k] : (Id)-1;
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) {
-      if (id[k] >= r0 && id[k] < r1) atomicAdd(&hist[warp * per + (int)(id[k] - r0)], 1);
-      below += id[k] >= 0 && id[k] < r0;
-      if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 31, (int)(t0 + 32 * k));
-    }
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) below += __shfl_xor_sync(0xffffffffu, below, o);
-  if (lane == 0) atomicAdd(&s_base, below);
-  __syncthreads();
-  // thread i: row r0 + i (per <= kSortThreads)
-  const int i = threadIdx.x;
-  int total = 0;
-  if (i < nr) {
-    for (int w = 0; w < kSortWarps; ++w) {
-      const int c = hist[w * per + i];
-      hist[w * per + i] = total;
-      total += c;
-    }
-  }
-  int incl = total;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  if (lane == 31) wsum[warp] = incl;
-  __syncthreads();
-  int before = s_base;
-  for (int w = 0; w < warp; ++w) before += wsum[w];
-  if (i < nr) {
-    const int s = before + incl - total;
-    first[i] = s;
-    a.start[r0 + i] = s;
-    if ((int64_t)r0 + i == a.V - 1) a.start[a.V] = s + total;
-  }
-  __syncthreads();
-  for (int64_t t0 = ta + lane; t0 - lane < tb; t0 += 32 * kSortAhead) {
-    Id id[kSortAhead];
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) id[k] = t0 + 32 * k < tb ? ids[t0 + 32 * k] : (Id)-1;
-#pragma unroll
-    for (int k = 0; k < kSortAhead; ++k) {
-      const bool in = id[k] >= r0 && id[k] < r1;
-      if (!__any_sync(0xffffffffu, in)) continue;
-      const int row = in ? (int)(id[k] - r0) : -1;  // (few different values: match takes them one after another)
-      const uint32_t same = __match_any_sync(0xffffffffu, row);
-      int at = 0;
-      if (in) at = hist[warp * per + row];
-      __syncwarp();
-      if (in) {
-        const int place = first[row] + at + __popc(same & ((1u << lane) - 1u));
-        if (GPO_BOUNDS(st, place, a.T, kWhereEmbedPlace)) {
-          a.perm[place] = (int)(t0 + 32 * k);
-          a.sid[place] = (int)id[k];
-        }
-        if (lane == __ffs(same) - 1) hist[warp * per + row] = at + __popc(same);
-      }
-      __syncwarp();
-    }
-  }
+  EmbedKeys<Id> keys = {static_cast<const Id*>(a.ids)};
+  sort_tokens<31, kWhereEmbedPlace>(
+      keys, a.T, a.V, per, hist, st, [&](int64_t row, int first) { a.start[row] = first; },
+      [&](int place, int64_t t, Id id) {
+        a.perm[place] = (int)t;
+        a.sid[place] = (int)id;
+      });
 }
 
 // ------------------------------------------------------------------ sums of runs
@@ -405,7 +334,7 @@ cudaError_t sums(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
 int embed_piece(int64_t T) { return T <= 4096 ? 8 : T <= 16384 ? 32 : T <= 65536 ? 64 : 128; }
 
 cudaError_t setup_embed() {
-  const int bytes = (int)sort_smem(kEmbedMaxRows);
+  const int bytes = (int)sort_smem(kSortMaxRows);
   const cudaError_t e = cudaFuncSetAttribute(embed_sort_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(embed_sort_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -418,8 +347,7 @@ cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& 
 }
 
 cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st) {
-  const int64_t want = (a.V + lc.num_sms - 1) / lc.num_sms;
-  const int per = (int)min(max(want, (int64_t)32), (int64_t)kEmbedMaxRows);
+  const int per = sort_rows(a.V, lc.num_sms);
   const unsigned grid = (unsigned)((a.V + per - 1) / per);
   if (a.id8) embed_sort_kernel<int64_t><<<grid, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
   else embed_sort_kernel<int32_t><<<grid, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);

@@ -992,7 +992,7 @@ constexpr int kVocabFewCtas = 256;   // CTAs of that launch at most
 // parts of a forward row: the maxima and sums of the two column halves of every tile
 inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
 
-struct VocabHead {  // in the workspace, written by the index kernel
+struct VocabHead {  // in the workspace, written by the kernel that lists the tokens
   int rows;         // tokens that take part
   float dz_scale;   // power of two that brings dz into fp16's range (1 for bf16)
 };
@@ -1079,7 +1079,6 @@ struct EmbedArgs {
   int64_t part_stride;
 };
 int embed_piece(int64_t T);  // sorted tokens of one piece, for T tokens
-constexpr int kEmbedMaxRows = 1024;  // rows of the table that one CTA of the sort owns, at most
 
 cudaError_t setup_embed();
 cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);

@@ -22,6 +22,7 @@
 #include <cuda_fp16.h>
 
 #include "gpo_pair.cuh"
+#include "gpo_sort.cuh"
 #include "gpo_vocab_math.cuh"
 
 namespace gpo {
@@ -795,6 +796,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
 
 // ------------------------------------------------------------------ tokens that take part
 
+// Tokens up to which their order is found by comparing all with all, in one launch; beyond, by the sort and a
+// gathering launch (vocabulary 32000 x 512: 14.5 against 17.2 us for 2048 tokens, as long for 4096,
+// 36 against 19 for 8192; for 65536 890 against 66).
+constexpr int kVocabOrder = 4096;
 constexpr int kRowThreads = 1024;
 constexpr int kRowAhead = 8;  // tokens of a thread in flight
 
@@ -873,12 +878,42 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
   }
 }
 
+// A power of two that brings an fp16 dz, |dz| <= bound, into the type's range; 1 for bf16.  (|dz| is at most
+// |g| + |e| max p |log p + H|, whose last factor is below log V + 1 < 24.)
+__device__ __forceinline__ float scale_of_dz(const VocabArgs& a, float bound) {
+  if (!a.f16 || !(bound > 0.f) || !isfinite(bound)) return 1.f;
+  int ex;
+  frexpf(bound, &ex);  // bound <= 2^ex: |dz| up to 2^14, within fp16's 65504
+  return ldexpf(1.f, min(max(14 - ex, -100), 100));
+}
+// A token without a gradient gets a d_hidden of zeros, from one warp.
+__device__ __forceinline__ void no_d_hidden(const VocabArgs& a, int64_t t, bool vec, int lane) {
+  uint16_t* dst = static_cast<uint16_t*>(a.dh) + t * a.dh_stride;
+  const int whole = vec ? a.D / 8 : 0;
+  for (int c = lane; c < whole; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
+  for (int c = whole * 8 + lane; c < a.D; c += 32) dst[c] = 0;
+}
+// One hidden row to its place in hc, by one warp (rows hold a multiple of 16 bytes); t < 0: zeros, up to the next
+// k-step of the d_weight product.
+__device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t r, int64_t t, int lane) {
+  const int chunks = (a.D + 7) / 8;
+  uint4* dst = reinterpret_cast<uint4*>(a.hc + r * a.hc_stride);
+  if (t < 0) {
+    for (int c = lane; c < chunks; c += 32) dst[c] = make_uint4(0u, 0u, 0u, 0u);
+    return;
+  }
+  const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + t * a.hidden_stride);
+#pragma unroll 8
+  for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+}
+__device__ __forceinline__ bool dh_vec(const VocabArgs& a) { return ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0; }
+
 // Gradient: the tokens with a target and a gradient that is not 0, in the order of their targets and, for one
 // target, their own; their number, the scale of an fp16 dz, their hidden rows in that order with
 // zeros up to the next k-step of the d_weight product, and the zeros of the others' d_hidden.
 // A token's place is the number of those before it in that order: every CTA counts, for its share of the
-// tokens, through all of them (T^2 / 152 comparisons in shared memory: 27 tokens with 4096 in 0.3 us of a
-// warp each), with no exchange between CTAs and no second launch.  smem: order_smem(kThreads) bytes.
+// tokens, through all of them (T^2 / 152 comparisons in shared memory), with no exchange between CTAs and no
+// second launch.  smem: order_smem(kThreads) bytes.
 __host__ __device__ constexpr size_t order_smem(int threads) { return sizeof(int) * (size_t)(10 * threads + 2 * 32); }
 
 template <int kThreads>
@@ -889,11 +924,10 @@ __device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& s
   float* s_big = reinterpret_cast<float*>(s_all + 32);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t ta = a.T * cta / ctas, tb = a.T * (cta + 1) / ctas;
-  const int chunks = (a.D + 7) / 8;  // 16 bytes each (rows hold a multiple of them)
-  const bool vec = ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0;
+  const bool vec = dh_vec(a);
   auto key_of = [&](int64_t id, float g, float e) { return id >= 0 && id < a.V && (g != 0.f || e != 0.f) ? (int)id : kNoKey; };
   int all = 0;
-  float bound = 0.f;  // of |dz|: |g| + |e| max p |log p + H|, whose last factor is below log V + 1
+  float bound = 0.f;  // of |dz| (see scale_of_dz)
   for (int64_t o = ta; o < tb || o == ta; o += kThreads) {  // (a CTA without tokens counts them all, too)
     const int own = (int)max((int64_t)0, min((int64_t)kThreads, tb - o));
     const bool mine = threadIdx.x < own;
@@ -968,15 +1002,9 @@ __device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& s
           a.idx[r] = (int)t;
           a.by_target[r] = key;
         }
-        const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.hidden) + t * a.hidden_stride);
-        uint4* dst = reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride);
-#pragma unroll 8
-        for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
+        gather_row(a, r, t, lane);
       } else if (a.dh) {
-        uint16_t* dst = static_cast<uint16_t*>(a.dh) + t * a.dh_stride;
-        const int whole = vec ? a.D / 8 : 0;
-        for (int c = lane; c < whole; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
-        for (int c = whole * 8 + lane; c < a.D; c += 32) dst[c] = 0;
+        no_d_hidden(a, t, vec, lane);
       }
     }
   }
@@ -991,19 +1019,12 @@ __device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& s
   all = __reduce_add_sync(0xffffffffu, lane < kW ? s_all[lane] : 0);
   if (cta == 0 && threadIdx.x == 0) {
     for (int w = 0; w < kW; ++w) bound = fmaxf(bound, s_big[w]);
-    float s = 1.f;
-    if (a.f16 && bound > 0.f && isfinite(bound)) {
-      int ex;
-      frexpf(bound, &ex);  // bound <= 2^ex: |dz| up to 2^14, within fp16's 65504
-      s = ldexpf(1.f, min(max(14 - ex, -100), 100));
-    }
     a.head->rows = all;
-    a.head->dz_scale = s;
+    a.head->dz_scale = scale_of_dz(a, bound);
   }
   if (cta == ctas - 1) {
     const int pad = (all + kTile16 - 1) / kTile16 * kTile16;
-    for (int r = all + warp; r < pad; r += kW)
-      for (int c = lane; c < chunks; c += 32) reinterpret_cast<uint4*>(a.hc + (int64_t)r * a.hc_stride)[c] = make_uint4(0u, 0u, 0u, 0u);
+    for (int r = all + warp; r < pad; r += kW) gather_row(a, r, -1, lane);
   }
 }
 
@@ -1011,6 +1032,79 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
   __shared__ __align__(16) unsigned char smem[order_smem(kRowThreads)];
   let_next_start();
   order_tokens<kRowThreads>(a, st, smem, (int)blockIdx.x, (int)gridDim.x);
+}
+
+// The same for more than kVocabOrder tokens, whose comparisons would grow with T^2: the sort's work grows with T.
+template <class Id>
+struct VocabKeys {
+  using Key = Id;
+  const VocabArgs& a;
+  float bound = 0.f;  // of |dz| (see scale_of_dz)
+  __device__ explicit VocabKeys(const VocabArgs& args) : a(args) {}
+  __device__ __forceinline__ void load(int64_t t0, int64_t tb, Id (&id)[kSortAhead]) {
+    const Id* target = static_cast<const Id*>(a.target);
+    float g[kSortAhead], e[kSortAhead];
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      const bool in = t0 + 32 * k < tb;
+      id[k] = in ? target[t0 + 32 * k] : (Id)-1;
+      g[k] = in ? a.g[t0 + 32 * k] : 0.f;
+      e[k] = 0.f;
+    }
+    if (a.ge) {
+#pragma unroll
+      for (int k = 0; k < kSortAhead; ++k)
+        if (t0 + 32 * k < tb) e[k] = a.ge[t0 + 32 * k];
+    }
+#pragma unroll
+    for (int k = 0; k < kSortAhead; ++k) {
+      if (id[k] < 0 || id[k] >= a.V) continue;
+      if (g[k] != 0.f || e[k] != 0.f) bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
+      else id[k] = (Id)-1;
+    }
+  }
+};
+
+template <class Id>
+__global__ void __launch_bounds__(kSortThreads, 1) vocab_sort_kernel(VocabArgs a, int per, Status st) {
+  extern __shared__ int hist[];
+  __shared__ float s_big[kSortWarps];
+  let_next_start();
+  VocabKeys<Id> keys(a);
+  sort_tokens<26, kWhereVocabRow>(
+      keys, a.T, a.V, per, hist, st,
+      [&](int64_t row, int first) {
+        if (row == a.V) a.head->rows = first;
+      },
+      [&](int place, int64_t t, Id id) {
+        a.idx[place] = (int)t;
+        a.by_target[place] = (int)id;
+      });
+  float bound = keys.bound;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
+  if ((threadIdx.x & 31) == 0) s_big[threadIdx.x >> 5] = bound;
+  __syncthreads();
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    for (int w = 0; w < kSortWarps; ++w) bound = fmaxf(bound, s_big[w]);
+    a.head->dz_scale = scale_of_dz(a, bound);
+  }
+}
+
+__global__ void __launch_bounds__(256) vocab_gather_kernel(VocabArgs a) {
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), nwarps = (int64_t)gridDim.x * 8;
+  let_next_start();
+  after_previous();
+  const int64_t rows = a.head->rows, pad = (rows + kTile16 - 1) / kTile16 * kTile16;
+  for (int64_t r = warp; r < pad; r += nwarps) gather_row(a, r, r < rows ? a.idx[r] : -1, lane);
+  if (!a.dh) return;
+  const bool vec = dh_vec(a);
+  for (int64_t t = warp; t < a.T; t += nwarps) {
+    const int64_t id = load_id(a.target, a.id8, t);
+    if (id >= 0 && id < a.V && (a.g[t] != 0.f || (a.ge && a.ge[t] != 0.f))) continue;
+    no_d_hidden(a, t, vec, lane);
+  }
 }
 
 // d_hidden from the sums of its parts of k, added in order, by threads i0, i0 + step, ..
@@ -1146,6 +1240,9 @@ cudaError_t setup_vocab() {
   if (e == cudaSuccess) e = setup_mode<kDzWide>();
   if (e == cudaSuccess) e = setup_mode<kDzWideEnt>();
   if (e == cudaSuccess) e = setup_mode<kProducts>();
+  const int bytes = (int)sort_smem(kSortMaxRows);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(vocab_sort_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(vocab_sort_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2);
@@ -1171,6 +1268,15 @@ cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Sta
 }
 
 cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st) {
+  if (a.T > kVocabOrder) {
+    const int per = sort_rows(a.V, lc.num_sms);
+    const unsigned ctas = (unsigned)((a.V + per - 1) / per);
+    if (a.id8) vocab_sort_kernel<int64_t><<<ctas, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
+    else vocab_sort_kernel<int32_t><<<ctas, kSortThreads, sort_smem(per), lc.stream>>>(a, per, st);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    return launch_after(vocab_gather_kernel, (unsigned)min((a.T + 7) / 8, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a);
+  }
   const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
   vocab_order_kernel<<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();

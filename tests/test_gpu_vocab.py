@@ -242,6 +242,33 @@ def test_grad_wide_rows_and_frequent_targets(gp, dtype, shape):
         assert torch.equal(out[k], again[k]), k
 
 
+@pytest.mark.parametrize("T", [4095, 4096, 4097, 5000])
+def test_grad_of_many_tokens(gp, T):
+    """Around the number of tokens from which on they are sorted: 32-bit ids, tokens without a target or a
+    gradient, a vocabulary of fewer rows than there are SMs, and an id past the vocabulary."""
+    import torch
+    import paper_2606_18954_gb300 as P
+    from vocab_ref import close, head_exact, head_inputs
+    V, d = 150, 24
+    h, w, y = head_inputs(T, V, d, torch.float16, 0, 0.3, seed=T, sure=6.0)
+    gl, ge = _grads(T, y, T, True, 512.0)
+    f = gp.vocab_logp(h, w, y, entropy=True)
+    kw = dict(entropy=f["entropy"], grad_entropy=ge)
+    out = gp.vocab_grad(h, w, y, f["lse"], gl, **kw)
+    gp.check()
+    ref = head_exact(h, w, y, 1.0, torch.nan_to_num(gl), torch.nan_to_num(ge))
+    for k in ("d_hidden", "d_weight"):
+        close(out[k], ref[k], ref["t_" + k], k)
+    still = (y < 0) | ((torch.nan_to_num(gl) == 0) & (torch.nan_to_num(ge) == 0))
+    assert still.any() and not out["d_hidden"][still].any()
+    bad = y.clone()
+    bad[T - 1] = V
+    gp.vocab_grad(h, w, bad, f["lse"], gl, **kw)
+    with pytest.raises(P.GraphPOError) as e:
+        gp.check()
+    assert e.value.code == SHAPE
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_grad_is_as_exact_as_one_rounding(gp, dtype):
     """The 2-norm error of the gradients against that of their exact values rounded once to the type: dz's own
