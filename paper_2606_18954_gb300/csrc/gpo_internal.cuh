@@ -1021,6 +1021,7 @@ struct VocabArgs {
   const void* weight;
   int64_t weight_stride;
   int* by_target;        // the rows' targets, ascending (the gradient's rows are in that order)
+  int* tile_first;       // [tiles of 256 vocabulary rows + 1] rows before those whose targets are in the tile
   float* rest;           // [rows] what rounding took from the row's dz at its target
   uint16_t* dz;          // [rows up to a tile x dz_stride] of the piece [v0, v0 + vn) of the vocabulary
   int64_t dz_stride;

@@ -38,9 +38,9 @@ __host__ __device__ constexpr bool keeps_logits(int mode) { return is_lse(mode) 
 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
 constexpr int kVStages = 6;                        // of the logits
-constexpr int kPStages = 4;                        // of the products, beside their epilogue's sums
-constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 4..11 epilogue
-constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1;
+constexpr int kPStages = 5;                        // of the products, beside their epilogue's sums
+constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 rests, 4..11 epilogue
+constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
 // give back.  The shares add up to no more than the launch brings (setup_mode checks that).
 // The split of each mode is one without spills: the loads' and the MMAs' lane would find theirs in an L1
@@ -63,7 +63,6 @@ template <int kMode>
 __device__ __forceinline__ constexpr int segment_of() {
   return is_lse(kMode) ? kVocabSeg : is_wide(kMode) ? kVocabDzSeg : 1 << 30;
 }
-constexpr int kEpiBar = 1;                          // named barrier of the epilogue warps
 constexpr int kNoKey = 0x7fffffff;                 // above every target: a token without a gradient
 constexpr int kRaster = 32;                        // row tiles that share one pass over the columns
 
@@ -72,19 +71,19 @@ struct __align__(8) VocabCtl {
   uint64_t empty[kVStages];
   uint64_t tfull[2];
   uint64_t tempty[2];
+  uint64_t rfull[2];   // products: the operands of write_rests
+  uint64_t rempty[2];
   uint64_t drain;
   uint32_t tmem_base;
 };
 
-// Shared memory of the products beside their ring: per epilogue warp the sums of 32 rows x 64 columns (see
-// sum_rests) or 32 rows of 128 bytes on their way out, then the targets of up to kListed tokens.
-constexpr int kRestRow = 65;
-constexpr int kWarpBytes = 9 * 1024;
-constexpr int kListed = 4096;
-static_assert(kWarpBytes >= 4 * 32 * kRestRow, "sums of one warp");
+// Shared memory of the products beside their ring: two operands of write_rests, and per epilogue warp 32 rows of 128
+// bytes on their way out.
+constexpr int kRestBytes = 2 * kVBox;
+constexpr int kWarpBytes = 4 * 1024;
 constexpr size_t kVCtl = (sizeof(VocabCtl) + 15) & ~size_t(15);
 constexpr size_t kVSmem = kVCtl + 1023 + (size_t)kVStages * kVStage;
-constexpr size_t kPSmem = kVCtl + 1023 + (size_t)kPStages * kVStage + (size_t)kVEpiWarps * kWarpBytes + 4 * (size_t)kListed;
+constexpr size_t kPSmem = kVCtl + 1023 + (size_t)kPStages * kVStage + 2 * (size_t)kRestBytes + (size_t)kVEpiWarps * kWarpBytes;
 __host__ __device__ constexpr size_t smem_of(int mode) { return mode == kProducts ? kPSmem : kVSmem; }
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int f16) {
@@ -220,18 +219,6 @@ __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int
   }
 }
 
-// The first of n ascending numbers that is not below v, by one warp.
-__device__ __forceinline__ int first_not_below(const int* x, int n, int v, int lane) {
-  int lo = 0, hi = n;
-  while (hi - lo > 32) {
-    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-    const int below = __popc(__ballot_sync(0xffffffffu, at < hi && x[at] < v));
-    lo += below * step;
-    hi = min(hi, lo + step);
-  }
-  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < hi && x[lo + lane] < v));
-}
-
 // Brings `cols` 16-bit columns of a row into L1, for add_row.
 __device__ __forceinline__ void prefetch_row(const uint16_t* x, int cols) {
   for (int c = 0; c < cols; c += 64) asm volatile("prefetch.global.L1 [%0];" ::"l"(x + c));
@@ -253,51 +240,6 @@ __device__ __forceinline__ void add_row(const uint16_t* x, float w, int cols, in
   }
 }
 
-// Of a token's dz the target's entry is by far the largest part.  Its rounding to 16 bits would add 40 % to
-// the error that the gradients' own rounding leaves (the other entries' adds 1 %), so what that rounding takes away
-// (a.rest) is kept in fp32 and added in the products' epilogues: for d_hidden a row of the vocabulary
-// matrix per token (add_row), for d_weight the hidden rows of the tokens whose targets a warp's 32 rows are,
-// [ra, rb) in the order of their targets.  Where one row has more than kFewRests of them, by this, for 64 columns:
-// a lane takes two, the tokens one after another, sixteen in flight, each row's sums in registers until its
-// last token; then through shared memory to the rows' lanes.  (Two frequent tokens are most of the tokens of a small
-// vocabulary: 4000 of 1608 x 208, the products in 94 us with one column of 32 and eight in flight.)
-constexpr int kFewRests = 3;
-constexpr int kRestsAhead = 16;
-__device__ __forceinline__ void sum_rests(const VocabArgs& a, const int* by_target, float* sums, int ra, int rb, int v, int c0, int lane) {
-  for (int j = lane; j < 32 * kRestRow; j += 32) sums[j] = 0.f;
-  __syncwarp();
-  const int col = c0 + 2 * lane;
-  const uint16_t* h = a.hc + (col < a.hc_stride ? col : 0);  // (rows of whole 16 bytes: a pair never straddles their end)
-  float s0 = 0.f, s1 = 0.f;
-  int row = by_target[ra];
-  for (int r = ra; r < rb; r += kRestsAhead) {
-    uint32_t x[kRestsAhead];
-    float w[kRestsAhead];
-    int at[kRestsAhead];
-#pragma unroll
-    for (int k = 0; k < kRestsAhead; ++k) {
-      const int rk = min(r + k, rb - 1);
-      x[k] = *reinterpret_cast<const uint32_t*>(h + (int64_t)rk * a.hc_stride);
-      w[k] = r + k < rb ? __ldcg(a.rest + rk) : 0.f;
-      at[k] = by_target[rk];
-    }
-#pragma unroll
-    for (int k = 0; k < kRestsAhead; ++k) {
-      if (at[k] != row) {
-        sums[(row - v) * kRestRow + 2 * lane] = s0;
-        sums[(row - v) * kRestRow + 2 * lane + 1] = s1;
-        s0 = s1 = 0.f;
-        row = at[k];
-      }
-      s0 = fmaf(w[k], widen16((uint16_t)(x[k] & 0xFFFFu), a.f16), s0);
-      s1 = fmaf(w[k], widen16((uint16_t)(x[k] >> 16), a.f16), s1);
-    }
-  }
-  sums[(row - v) * kRestRow + 2 * lane] = s0;
-  sums[(row - v) * kRestRow + 2 * lane + 1] = s1;
-  __syncwarp();
-}
-
 // What the roles of a CTA share.
 struct Cta {
   VocabCtl* ctl;
@@ -312,7 +254,74 @@ struct Pipe {
   uint32_t phase = 0;
   uint32_t issued = 0;  // loads: stages filled
   int sum = 0;          // accumulations: one per tile, or per segment of a logits tile
+
+  template <int kS>
+  __device__ __forceinline__ void next() {
+    if (++stage == kS) {
+      stage = 0;
+      phase ^= 1u;
+    }
+  }
 };
+
+// The tokens whose targets are rows of a d_weight tile: [ra, rb) of the list.
+__device__ __forceinline__ void tokens_of(const VocabArgs& a, const Tile& t, int& ra, int& rb) {
+  const int* first = a.tile_first + ((int)a.v0 + t.m0) / kPairM;
+  ra = __ldcg(first);
+  rb = __ldcg(first + 1);
+}
+
+// Of a token's dz the target's entry is by far the largest part.  Its rounding to 16 bits would add 40 % to
+// the error that the gradients' own rounding leaves (the other entries' adds 1 %), so what that rounding takes away
+// (a.rest) is added to both products: to d_hidden in the epilogue, a row of the vocabulary matrix per
+// token (add_row); to d_weight as steps of its own after those of dz: the tokens whose targets are rows of the tile are
+// one run of the list, which is in the order of the targets, and 64 of them at a time are a step whose A is zeros but
+// for each token's rest in its target's row.  The rests are rounded to 16 bits there, 2^-17 (bf16) of the
+// entry of dz.  All tiles together take T / 64 such steps and one more each, however often a token occurs.
+// Here one warp of either CTA writes these A, two steps ahead of the MMAs, as a load of dz would leave them: 128 bytes
+// per k for 64 rows of the tile, swizzled.  A lane takes two k, and clears what it wrote two steps before.
+__device__ __forceinline__ bool write_rests(const VocabArgs& a, const Status& st, const Cta& c, int ring, int lane) {
+  const Plan plan = make_plan<kProducts>(a, c.rows);
+  unsigned char* buf = c.smem + (c.tiles - smem_u32(c.smem)) + ring;
+  for (int j = lane; j < 2 * kRestBytes / 16; j += 32) *reinterpret_cast<uint4*>(buf + 16 * j) = make_uint4(0u, 0u, 0u, 0u);
+  __syncwarp();
+  int was[2][2] = {{-1, -1}, {-1, -1}};
+  uint32_t n = 0;
+  Tile t;
+  for (int s = plan.own_dh; next_tile<kProducts>(plan, s, t); ++s) {
+    const int v = (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2);
+    int ra, rb;
+    tokens_of(a, t, ra, rb);
+    for (int r0 = ra; r0 < rb; r0 += kTile16, ++n) {
+      int at[2];
+      float rest[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + 32 * h + lane;
+        at[h] = r < rb ? __ldcg(a.by_target + r) - v : -1;
+        rest[h] = r < rb ? __ldcg(a.rest + r) : 0.f;
+      }
+      const uint32_t b = n & 1u;
+      if (!__all_sync(0xffffffffu, mbar_wait(&c.ctl->rempty[b], ((n >> 1) & 1u) ^ 1u, st, 28))) return false;
+      unsigned char* to = buf + b * kRestBytes;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int& old = b ? was[1][h] : was[0][h];
+        if (old >= 0) *reinterpret_cast<uint16_t*>(to + old) = 0;
+        old = -1;
+        const int k = 32 * h + lane, col = at[h] & 63;
+        if (at[h] >= 0 && at[h] < kPairM / 2) {
+          old = (at[h] >> 6) * kVBox + k * 128 + (((col >> 3) ^ (k & 7)) << 4) + 2 * (col & 7);
+          *reinterpret_cast<uint16_t*>(to + old) = round16(rest[h], a.f16);
+        }
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_release_cluster(leader_addr(&c.ctl->rfull[b]));
+    }
+  }
+  return true;
+}
 
 // Loads of all tiles of this pair, by one thread of either CTA: its halves of the operands.  False after a timeout.
 template <int kMode, int kS>
@@ -328,6 +337,8 @@ __device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArg
     const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
     const int am = t.m0 + (int)c.rank * (kPairM / 2), bn = t.n0 + (int)c.rank * (kPairN / 2);
     const int v0 = kLogits ? 0 : (int)a.v0;
+    int ra = 0, rb = 0;
+    if (kMode == kProducts && t.job == 1) tokens_of(a, t, ra, rb);
     for (int k = 0; k < t.kb; ++k) {
       if (!mbar_wait(&c.ctl->empty[p.stage], p.phase ^ 1u, st, 20)) return false;
       const uint32_t sa = c.tiles + (uint32_t)p.stage * kVStage, sb = sa + 2 * kVBox;
@@ -345,10 +356,17 @@ __device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArg
         if (!b_mn) tma_load_2d_pair(sb + h * kVBox, mb, bar, kx, v0 + bn + h * kTile16);
         else tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, (t.job == 0 ? v0 : 0) + kx);
       }
-      if (++p.stage == kS) {
-        p.stage = 0;
-        p.phase ^= 1u;
-      }
+      p.next<kS>();
+    }
+    for (int r = ra; r < rb; r += kTile16) {  // the hidden rows of write_rests
+      if (!mbar_wait(&c.ctl->empty[p.stage], p.phase ^ 1u, st, 20)) return false;
+      const uint32_t sb = c.tiles + (uint32_t)p.stage * kVStage + 2 * kVBox;
+      const uint32_t bar = leader_addr(&c.ctl->full[p.stage]);
+      if (c.rank == 0) mbar_arrive_expect_tx(&c.ctl->full[p.stage], kVStage);
+      ++p.issued;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, r);
+      p.next<kS>();
     }
   }
   return true;
@@ -359,34 +377,64 @@ template <int kMode, int kS>
 __device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
   constexpr int seg = segment_of<kMode>();
   const Plan plan = make_plan<kMode>(a, c.rows);
+  uint32_t rest = 0;  // steps of write_rests so far
   Tile t;
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
     const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
     const uint32_t idesc = idesc_16_f32(kPairM, kPairN, a.f16 != 0, a_mn, b_mn);
+    int ra = 0, rb = 0;
+    if (kMode == kProducts && t.job == 1) tokens_of(a, t, ra, rb);
+    // whole steps, and the instructions (16 k each) of the one that the operands end in
+    const int ends = kMode != kProducts ? a.D : t.job == 1 ? c.rows : (int)a.vn - t.ka * kTile16;
+    const int whole = min(t.kb, ends / kTile16), last = whole < t.kb ? (ends - whole * kTile16 + 15) / 16 : 0;
+    // (of the ring's first stage; addresses are in units of 16 bytes there)
+    const uint64_t a0 = a_mn ? smem_desc_mn128(c.tiles, kVBox) : smem_desc_k128(c.tiles);
+    const uint64_t b0 = (b_mn ? smem_desc_mn128(c.tiles, kVBox) : smem_desc_k128(c.tiles)) + (2 * kVBox >> 4);
+    // 16 k: 32 bytes of a K-major row, 16 rows of 128 bytes otherwise
+    const uint32_t as = a_mn ? 128u : 2u, bs = b_mn ? 128u : 2u;
     for (int64_t k0 = 0; k0 < t.kb || k0 == 0; k0 += seg, ++p.sum) {
       const int buf = p.sum & 1;
       if (!mbar_wait_cluster(&c.ctl->tempty[buf], ((uint32_t)(p.sum >> 1) & 1u) ^ 1u, st, 22)) return false;
       tc_fence_after();
       const uint32_t dt = c.tmem + (uint32_t)(buf * kPairN);
-      const int k1 = (int)min((int64_t)t.kb, k0 + seg);
-      for (int k = (int)k0; k < k1; ++k) {
+      const int k1 = (int)min((int64_t)t.kb, k0 + seg), kw = min(whole, k1);
+      uint32_t add = 0;
+      // (what this thread does between two steps' instructions shows in the time: whole steps by themselves)
+      for (int k = (int)k0; k < kw; ++k) {
         if (!mbar_wait(&c.ctl->full[p.stage], p.phase, st, 23)) return false;
         tc_fence_after();
-        const uint32_t sa = c.tiles + (uint32_t)p.stage * kVStage, sb = sa + 2 * kVBox;
-        const uint64_t ad = a_mn ? smem_desc_mn128(sa, kVBox) : smem_desc_k128(sa);
-        const uint64_t bd = b_mn ? smem_desc_mn128(sb, kVBox) : smem_desc_k128(sb);
-        // 16 k: 32 bytes of a K-major row, 16 rows of 128 bytes otherwise (addresses >> 4)
-        const uint32_t as = a_mn ? 128u : 2u, bs = b_mn ? 128u : 2u;
+        const uint32_t at = (uint32_t)p.stage * (kVStage >> 4);
 #pragma unroll
-        for (uint32_t kk = 0; kk < kTile16 / 16; ++kk)
-          mma_f16_pair(dt, ad + as * kk, bd + bs * kk, idesc, (k - (int)k0 | (int)kk) != 0);
+        for (uint32_t kk = 0; kk < kTile16 / 16; ++kk) mma_f16_pair(dt, a0 + at + as * kk, b0 + at + bs * kk, idesc, add | kk);
+        add = 1;
         mma_commit_pair(&c.ctl->empty[p.stage]);
-        if (++p.stage == kS) {
-          p.stage = 0;
-          p.phase ^= 1u;
+        p.next<kS>();
+      }
+      if (kw < k1) {
+        if (!mbar_wait(&c.ctl->full[p.stage], p.phase, st, 23)) return false;
+        tc_fence_after();
+        const uint32_t at = (uint32_t)p.stage * (kVStage >> 4);
+#pragma unroll 1
+        for (int kk = 0; kk < last; ++kk, add = 1) mma_f16_pair(dt, a0 + at + as * kk, b0 + at + bs * kk, idesc, add);
+        mma_commit_pair(&c.ctl->empty[p.stage]);
+        p.next<kS>();
+      }
+      if constexpr (kMode == kProducts) {
+#pragma unroll 1
+        for (int r = ra; r < rb; r += kTile16, ++rest) {  // the steps of write_rests
+          if (!mbar_wait(&c.ctl->full[p.stage], p.phase, st, 23)) return false;
+          if (!mbar_wait_cluster(&c.ctl->rfull[rest & 1u], (rest >> 1) & 1u, st, 29)) return false;
+          tc_fence_after();
+          const uint32_t aa = (kS * kVStage + (rest & 1u) * kRestBytes) >> 4, at = (uint32_t)p.stage * (kVStage >> 4);
+          const int n = min(kTile16 / 16, (rb - r + 15) / 16);
+#pragma unroll 1
+          for (int kk = 0; kk < n; ++kk) mma_f16_pair(dt, a0 + aa + as * kk, b0 + at + bs * kk, idesc, 1);
+          mma_commit_pair(&c.ctl->empty[p.stage]);
+          mma_commit_pair(&c.ctl->rempty[rest & 1u]);
+          p.next<kS>();
         }
-    }
-    mma_commit_pair(&c.ctl->tfull[buf]);
+      }
+      mma_commit_pair(&c.ctl->tfull[buf]);
     }
   }
   return true;
@@ -448,17 +496,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
     __syncwarp();
     if (lane == 0) mbar_arrive_cluster(te + 8u * (uint32_t)(n & 1));
   };
-  // products: this warp's part of the shared memory, and the tokens' targets, where they fit
-  unsigned char* own = c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage + (warp - 4) * kWarpBytes;
-  const int* by_target = a.by_target;
-  if constexpr (kMode == kProducts) {
-    if (rows <= kListed) {
-      int* list = reinterpret_cast<int*>(c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage + kVEpiWarps * kWarpBytes);
-      for (int i = (int)threadIdx.x - 128; i < rows; i += 32 * kVEpiWarps) list[i] = a.by_target[i];
-      by_target = list;
-      asm volatile("bar.sync %0, %1;" ::"n"(kEpiBar), "n"(32 * kVEpiWarps) : "memory");
-    }
-  }
+  unsigned char* own = c.smem + (c.tiles - smem_u32(c.smem)) + kS * kVStage + 2 * kRestBytes + (warp - 4) * kWarpBytes;  // (products)
   Tile t;
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
     const int row = t.m0 + r;
@@ -581,46 +619,19 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       }
     } else {
       const bool live = row < (t.job == 1 ? (int)a.vn : rows);
-      int ra = 0, rb = 0, na = 0, nb = 0;  // d_weight: the tokens whose targets are rows of this warp, of this lane
-      float rest = 0.f;                    // d_hidden: the row's own
+      float rest = 0.f;  // d_hidden: what rounding took at the row's target, and the target's row
       const uint16_t* wrow = nullptr;
-      if (t.job == 1) {
-        const int v = (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32;
-        ra = first_not_below(by_target, rows, v, lane);
-        for (rb = ra; rb < rows; rb += 32) {  // (few tokens' targets are near each other)
-          const int y = rb + lane < rows ? by_target[rb + lane] : kNoKey;
-          const int in = __popc(__ballot_sync(0xffffffffu, y < v + 32));
-          for (int k = 0; k < in; ++k) {
-            const int yk = __shfl_sync(0xffffffffu, y, k);
-            if (yk < v + lane) ++na;
-            if (yk <= v + lane) ++nb;
-          }
-          if (in < 32) {
-            rb += in;
-            break;
-          }
-        }
-        rb = min(rb, rows);
-        na += ra;
-        nb += ra;
-      } else if (live && t.split == 0) {
-        const int y = by_target[row];
+      if (t.job == 0 && live && t.split == 0) {
+        const int y = __ldcg(a.by_target + row);
         if (y >= a.v0 && y < a.v0 + a.vn) {
           rest = __ldcg(a.rest + row);
           wrow = static_cast<const uint16_t*>(a.weight) + (int64_t)y * a.weight_stride;
         }
       }
-      const bool few = __all_sync(0xffffffffu, nb - na <= kFewRests);
-      // what is added to the sums is fetched while they are still being made
-      const int some = min(kPairN / 2, a.D - n0);
-      for (int i = na; few && i < nb; ++i) {
-        asm volatile("prefetch.global.L1 [%0];" ::"l"(a.rest + i));
-        prefetch_row(a.hc + (int64_t)i * a.hc_stride + n0, some);
-      }
-      if (wrow) prefetch_row(wrow + n0, some);
-      float* rests = reinterpret_cast<float*>(own);
+      // (it is fetched while the sums are still being made)
+      if (wrow) prefetch_row(wrow + n0, min(kPairN / 2, a.D - n0));
       const int tok = t.job == 0 && live ? __ldcg(a.idx + row) : 0;
-      const bool bulk = t.job == 1 && few && a.dw_bulk != 0;
+      const bool bulk = t.job == 1 && a.dw_bulk != 0;
       if (lane == 0) bulk_read();  // (the last tile's rows have left)
       __syncwarp();
       if (!ready(p.sum)) return false;
@@ -637,14 +648,6 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
         float y[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
-        if (!few) {
-          if ((ch & 1) == 0) sum_rests(a, by_target, rests, ra, rb, (int)a.v0 + t.m0 + (int)c.rank * (kPairM / 2) + q * 32, c0, lane);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) y[j] += rests[lane * kRestRow + (ch & 1) * 32 + j];
-        } else {
-#pragma unroll 1
-          for (int i = na; i < nb; ++i) add_row(a.hc + (int64_t)i * a.hc_stride + c0, a.rest[i], cols, a.f16, y);
-        }
         if (rest != 0.f) add_row(wrow + c0, rest, cols, a.f16, y);
 #pragma unroll
         for (int j = 0; j < 32; ++j) y[j] *= f;
@@ -722,6 +725,8 @@ __device__ __forceinline__ Cta begin_pair(unsigned char* smem) {
     for (int b = 0; b < 2; ++b) {
       mbar_init(&c.ctl->tfull[b], 1);
       mbar_init(&c.ctl->tempty[b], 2 * kVEpiWarps);
+      mbar_init(&c.ctl->rfull[b], 2);
+      mbar_init(&c.ctl->rempty[b], 1);
     }
     mbar_init(&c.ctl->drain, 1);
     fence_mbar_init();
@@ -780,6 +785,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     if (warp == kLoadWarp && lane == 0) {
       load_tiles<kMode, kS>(maps, a, st, c, p);
       end_loads<kS>(st, c, p);
+    } else if (kMode == kProducts && warp == kRestWarp) {
+      if (a.dw) write_rests(a, st, c, kS * kVStage, lane);
     } else if (warp == kMmaWarp && lane == 0 && c.rank == 0) {
       if (a.debug_timeout) mbar_wait(&c.ctl->drain, 0, st, 27, kDebugTimeoutNs);  // reports GPO_ERR_TIMEOUT
       else mma_tiles<kMode, kS>(a, st, c, p);
@@ -893,8 +900,12 @@ __device__ __forceinline__ void no_d_hidden(const VocabArgs& a, int64_t t, bool 
   for (int c = lane; c < whole; c += 32) reinterpret_cast<uint4*>(dst)[c] = make_uint4(0u, 0u, 0u, 0u);
   for (int c = whole * 8 + lane; c < a.D; c += 32) dst[c] = 0;
 }
-// One hidden row to its place in hc, by one warp (rows hold a multiple of 16 bytes); t < 0: zeros, up to the next
-// k-step of the d_weight product.
+// One hidden row to its place in hc, by one warp (rows hold a multiple of 16 bytes); t < 0: zeros, in the rows
+// behind the last that the steps of the d_weight product meet: those of dz end at a multiple of 64, those of the
+// rests less than 64 behind the last row (what lies past the tensor map's end reads as zeros).
+__device__ __forceinline__ int64_t rows_behind(const VocabArgs& a, int64_t rows) {
+  return min((rows + kTile16 - 1) / kTile16 + 1, (a.T + kTile16 - 1) / kTile16) * kTile16;
+}
 __device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t r, int64_t t, int lane) {
   const int chunks = (a.D + 7) / 8;
   uint4* dst = reinterpret_cast<uint4*>(a.hc + r * a.hc_stride);
@@ -909,104 +920,57 @@ __device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t r, int64_
 __device__ __forceinline__ bool dh_vec(const VocabArgs& a) { return ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0; }
 
 // Gradient: the tokens with a target and a gradient that is not 0, in the order of their targets and, for one
-// target, their own; their number, the scale of an fp16 dz, their hidden rows in that order with
-// zeros up to the next k-step of the d_weight product, and the zeros of the others' d_hidden.
+// target, their own; their number, the scale of an fp16 dz, the number of tokens before each tile's targets, their hidden
+// rows in that order with zeros behind them (see gather_row), and the zeros of the others' d_hidden.
 // A token's place is the number of those before it in that order: every CTA counts, for its share of the
 // tokens, through all of them (T^2 / 152 comparisons in shared memory), with no exchange between CTAs and no
-// second launch.  smem: order_smem(kThreads) bytes.
-__host__ __device__ constexpr size_t order_smem(int threads) { return sizeof(int) * (size_t)(10 * threads + 2 * 32); }
-
-template <int kThreads>
-__device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& st, unsigned char* smem, int cta, int ctas) {
-  constexpr int kW = kThreads / 32, kKeys = 8 * kThreads;  // targets that own ones are compared with at one time
-  int* s_key = reinterpret_cast<int*>(smem);
-  int *s_own = s_key + kKeys, *s_place = s_own + kThreads, *s_all = s_place + kThreads;
-  float* s_big = reinterpret_cast<float*>(s_all + 32);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t ta = a.T * cta / ctas, tb = a.T * (cta + 1) / ctas;
-  const bool vec = dh_vec(a);
-  auto key_of = [&](int64_t id, float g, float e) { return id >= 0 && id < a.V && (g != 0.f || e != 0.f) ? (int)id : kNoKey; };
+// second launch.
+__global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, Status st) {
+  constexpr int kW = kRowThreads / 32, kPer = kVocabOrder / kRowThreads;
+  __shared__ int s_key[kVocabOrder];
+  __shared__ int s_all[kW];
+  __shared__ float s_big[kW];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, T = (int)a.T;
+  let_next_start();
+  int64_t id[kPer];
+  float g[kPer], e[kPer];
+  // (one branch around the loads of a thread, which are then in flight together)
+  if (a.id8) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int u = k * kRowThreads + threadIdx.x;
+      id[k] = u < T ? static_cast<const int64_t*>(a.target)[u] : -1;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      const int u = k * kRowThreads + threadIdx.x;
+      id[k] = u < T ? static_cast<const int32_t*>(a.target)[u] : -1;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) {
+    const int u = k * kRowThreads + threadIdx.x;
+    g[k] = u < T ? a.g[u] : 0.f;
+    e[k] = 0.f;
+  }
+  if (a.ge) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (k * kRowThreads + threadIdx.x < T) e[k] = a.ge[k * kRowThreads + threadIdx.x];
+  }
   int all = 0;
   float bound = 0.f;  // of |dz| (see scale_of_dz)
-  for (int64_t o = ta; o < tb || o == ta; o += kThreads) {  // (a CTA without tokens counts them all, too)
-    const int own = (int)max((int64_t)0, min((int64_t)kThreads, tb - o));
-    const bool mine = threadIdx.x < own;
-    const int64_t my_id = mine ? load_id(a.target, a.id8, o + threadIdx.x) : -1;
-    const float my_g = mine ? a.g[o + threadIdx.x] : 0.f, my_e = mine && a.ge ? a.ge[o + threadIdx.x] : 0.f;
-    for (int64_t c = 0; c < a.T; c += kKeys) {
-      const int n = (int)min((int64_t)kKeys, a.T - c);
-      int64_t id[8];
-      float g[8], e[8];
-      // (one branch around the loads of a thread, which are then in flight together)
-      if (a.id8) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int u = k * kThreads + threadIdx.x;
-          id[k] = u < n ? static_cast<const int64_t*>(a.target)[c + u] : -1;
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int u = k * kThreads + threadIdx.x;
-          id[k] = u < n ? static_cast<const int32_t*>(a.target)[c + u] : -1;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int u = k * kThreads + threadIdx.x;
-        g[k] = u < n ? a.g[c + u] : 0.f;
-        e[k] = 0.f;
-      }
-      if (a.ge) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (k * kThreads + threadIdx.x < n) e[k] = a.ge[c + k * kThreads + threadIdx.x];
-      }
-      __syncthreads();  // the last chunk's readers are done
-      if (c == 0 && mine) {
-        s_own[threadIdx.x] = key_of(my_id, my_g, my_e);
-        s_place[threadIdx.x] = 0;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int u = k * kThreads + threadIdx.x;
-        const int key = key_of(id[k], g[k], e[k]);
-        if (u < n) s_key[u] = key;
-        if (o == ta) {
-          if (key != kNoKey) {
-            ++all;
-            bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
-          }
-          if (id[k] >= a.V && cta == 0) report(st, GPO_ERR_SHAPE, 26, (int)(c + u));
-        }
-      }
-      __syncthreads();
-      for (int w = warp; w < own; w += kW) {
-        const int key = s_own[w];
-        if (key == kNoKey) continue;
-        const int self = (int)min((int64_t)kKeys, max((int64_t)0, o + w - c));  // tokens of the chunk before this one
-        int before = 0;
-#pragma unroll 4
-        for (int u = lane; u < n; u += 32) before += s_key[u] < key + (u < self ? 1 : 0);
-        before = __reduce_add_sync(0xffffffffu, before);
-        if (lane == 0) s_place[w] += before;
-      }
+  for (int k = 0; k < kPer; ++k) {
+    const int u = k * kRowThreads + threadIdx.x;
+    const bool in = id[k] >= 0 && id[k] < a.V && (g[k] != 0.f || e[k] != 0.f);
+    if (in) {
+      ++all;
+      bound = fmaxf(bound, fabsf(g[k]) + 24.f * fabsf(e[k]));
     }
-    __syncwarp();  // (a warp's own places: written by its lane 0)
-    for (int w = warp; w < own; w += kW) {
-      const int64_t t = o + w;
-      const int key = s_own[w];
-      if (key != kNoKey && GPO_BOUNDS(st, s_place[w], a.T, kWhereVocabRow)) {
-        const int r = s_place[w];
-        if (lane == 0) {
-          a.idx[r] = (int)t;
-          a.by_target[r] = key;
-        }
-        gather_row(a, r, t, lane);
-      } else if (a.dh) {
-        no_d_hidden(a, t, vec, lane);
-      }
-    }
+    if (id[k] >= a.V && blockIdx.x == 0) report(st, GPO_ERR_SHAPE, 26, u);
+    s_key[u] = in ? (int)id[k] : kNoKey;
   }
   all = __reduce_add_sync(0xffffffffu, all);
 #pragma unroll
@@ -1016,22 +980,42 @@ __device__ __forceinline__ void order_tokens(const VocabArgs& a, const Status& s
     s_big[warp] = bound;
   }
   __syncthreads();
-  all = __reduce_add_sync(0xffffffffu, lane < kW ? s_all[lane] : 0);
-  if (cta == 0 && threadIdx.x == 0) {
+  all = __reduce_add_sync(0xffffffffu, s_all[lane]);
+  const bool vec = dh_vec(a);
+  const int ta = (int)(a.T * blockIdx.x / gridDim.x), tb = (int)(a.T * (blockIdx.x + 1) / gridDim.x);
+  for (int t = ta + warp; t < tb; t += kW) {
+    const int key = s_key[t];
+    if (key != kNoKey) {
+      int r = 0;
+#pragma unroll 4
+      for (int u = lane; u < T; u += 32) r += s_key[u] < key + (u < t ? 1 : 0);
+      r = __reduce_add_sync(0xffffffffu, r);
+      if (!GPO_BOUNDS(st, r, a.T, kWhereVocabRow)) continue;
+      if (lane == 0) {
+        a.idx[r] = t;
+        a.by_target[r] = key;
+      }
+      gather_row(a, r, t, lane);
+    } else if (a.dh) {
+      no_d_hidden(a, t, vec, lane);
+    }
+  }
+  const int64_t tiles = (a.V + kPairM - 1) / kPairM;
+  for (int64_t j = blockIdx.x + (int64_t)gridDim.x * (kW - 1 - warp); j <= tiles; j += (int64_t)gridDim.x * kW) {
+    const int key = (int)min(j * kPairM, a.V);
+    int n = 0;
+#pragma unroll 4
+    for (int u = lane; u < T; u += 32) n += s_key[u] < key;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) a.tile_first[j] = n;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     for (int w = 0; w < kW; ++w) bound = fmaxf(bound, s_big[w]);
     a.head->rows = all;
     a.head->dz_scale = scale_of_dz(a, bound);
   }
-  if (cta == ctas - 1) {
-    const int pad = (all + kTile16 - 1) / kTile16 * kTile16;
-    for (int r = all + warp; r < pad; r += kW) gather_row(a, r, -1, lane);
-  }
-}
-
-__global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, Status st) {
-  __shared__ __align__(16) unsigned char smem[order_smem(kRowThreads)];
-  let_next_start();
-  order_tokens<kRowThreads>(a, st, smem, (int)blockIdx.x, (int)gridDim.x);
+  if (blockIdx.x == gridDim.x - 1)
+    for (int64_t r = all + warp; r < rows_behind(a, all); r += kW) gather_row(a, r, -1, lane);
 }
 
 // The same for more than kVocabOrder tokens, whose comparisons would grow with T^2: the sort's work grows with T.
@@ -1074,6 +1058,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) vocab_sort_kernel(VocabArgs a
   sort_tokens<26, kWhereVocabRow>(
       keys, a.T, a.V, per, hist, st,
       [&](int64_t row, int first) {
+        if (row % kPairM == 0 || row == a.V) a.tile_first[(row + kPairM - 1) / kPairM] = first;
         if (row == a.V) a.head->rows = first;
       },
       [&](int place, int64_t t, Id id) {
@@ -1096,7 +1081,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(VocabArgs a) {
   const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), nwarps = (int64_t)gridDim.x * 8;
   let_next_start();
   after_previous();
-  const int64_t rows = a.head->rows, pad = (rows + kTile16 - 1) / kTile16 * kTile16;
+  const int64_t rows = a.head->rows, pad = rows_behind(a, rows);
   for (int64_t r = warp; r < pad; r += nwarps) gather_row(a, r, r < rows ? a.idx[r] : -1, lane);
   if (!a.dh) return;
   const bool vec = dh_vec(a);

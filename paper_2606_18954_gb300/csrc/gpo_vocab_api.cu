@@ -17,7 +17,7 @@ constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 1024;  // tokens, vocabulary 
 constexpr int64_t kMaxMatrix = (int64_t)1 << 40;          // elements of a matrix
 
 struct VocabLayout {
-  size_t status, marks, head, idx, hc, by_target, rest, pm, ps, pu, tz, dz, acc, total;
+  size_t status, marks, head, idx, hc, by_target, tile_first, rest, pm, ps, pu, tz, dz, acc, total;
   bool few;           // forward in one launch
   bool listed;        // only the tokens that take part are multiplied
   int64_t tp, hc_stride, piece, acc_stride;
@@ -37,7 +37,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   const int64_t T = v.num_tokens;
   L = VocabLayout();
   L.tp = up_to(T, kPairM);
-  L.hc_stride = up_to(v.d, 64);  // rows of whole 128-byte lines (see vocab_pack_kernel)
+  L.hc_stride = up_to(v.d, 64);  // rows of whole 128-byte lines
   L.few = !grad && T <= kVocabFew;
   L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
   L.status = take(sizeof(uint32_t) * kStatusWords);
@@ -57,6 +57,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   }
   if (T > 0 && grad) {
     L.by_target = take(sizeof(int) * (size_t)T);
+    L.tile_first = take(sizeof(int) * (size_t)((v.vocab + kPairM - 1) / kPairM + 1));
     L.rest = take(sizeof(float) * (size_t)L.tp);
     // pieces of about equal size, a whole number of column tiles each
     const int64_t cols = std::max<int64_t>(1, kVocabPieceBytes / (2 * L.tp) / kPairN) * kPairN;
@@ -301,6 +302,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.weight = v->weight;
   a.weight_stride = v->weight_stride;
   a.by_target = at<int>(workspace, L.by_target);
+  a.tile_first = at<int>(workspace, L.tile_first);
   a.rest = at<float>(workspace, L.rest);
   a.dz = at<uint16_t>(workspace, L.dz);
   a.dz_stride = L.piece;
