@@ -192,12 +192,15 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8]) {
                : "memory");
 }
 
-// 16 bits of 32 consecutive columns of a row to memory, those below `cols` (vec: 16-byte accesses).
-__device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int cols, bool vec, int f16, bool add) {
+// Rows of whole, aligned 16 bytes.
+__device__ __forceinline__ bool vec_rows(const void* p, int64_t stride) { return ((stride & 7) | (reinterpret_cast<uintptr_t>(p) & 15)) == 0; }
+
+// 16 bits of 32 consecutive columns of a row to memory (add: added to what it holds), 16-byte aligned, those below `cols`.
+__device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int cols, int f16, bool add) {
 #pragma unroll
   for (int c = 0; c < 32; c += 8) {
     uint32_t o[4] = {0u, 0u, 0u, 0u};
-    const bool whole = vec && c + 8 <= cols;
+    const bool whole = c + 8 <= cols;
     if (add && whole) {
       const uint4 u = *reinterpret_cast<const uint4*>(dst + c);
       o[0] = u.x, o[1] = u.y, o[2] = u.z, o[3] = u.w;
@@ -217,6 +220,27 @@ __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int
         if (c + i < cols) dst[c + i] = (uint16_t)(o[i >> 1] >> (16 * (i & 1)));
     }
   }
+}
+
+// The same of a warp's 32 rows, a lane each (its row in memory: row, or none below 0), for rows of any alignment:
+// through `own`, 4 KB of shared memory, so that the warp takes row by row.  (2048 tokens of 30000 x 1001: the products
+// in 205 us; 480 with a lane for each row and its stores of 2 bytes.)
+__device__ __forceinline__ void store_rows(float* own, const float (&x)[32], uint16_t* dst, int64_t stride, int64_t row, int cols,
+                                           int f16, bool add, int lane) {
+#pragma unroll
+  for (int c = 0; c < 32; ++c) own[lane * 32 + (c ^ lane)] = x[c];
+  __syncwarp();
+  const bool in = lane < cols;
+#pragma unroll 8
+  for (int r = 0; r < 32; ++r) {
+    const int64_t to = __shfl_sync(0xffffffffu, row, r);
+    if (to >= 0 && in) {
+      uint16_t* at = dst + to * stride + lane;
+      const float y = own[r * 32 + (lane ^ r)];
+      *at = round16(add ? y + widen16(*at, f16) : y, f16);
+    }
+  }
+  __syncwarp();
 }
 
 // Brings `cols` 16-bit columns of a row into L1, for add_row.
@@ -632,6 +656,8 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       if (wrow) prefetch_row(wrow + n0, min(kPairN / 2, a.D - n0));
       const int tok = t.job == 0 && live ? __ldcg(a.idx + row) : 0;
       const bool bulk = t.job == 1 && a.dw_bulk != 0;
+      const bool vec = t.job == 1 ? vec_rows(a.dw, a.dw_stride) : vec_rows(a.dh, a.dh_stride);
+      const bool by_rows = !vec && (t.job == 1 || (a.last && a.splits == 1));
       if (lane == 0) bulk_read();  // (the last tile's rows have left)
       __syncwarp();
       if (!ready(p.sum)) return false;
@@ -671,10 +697,8 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
               }
             }
           }
-          if (out && GPO_BOUNDS(st, tok, a.T, kWhereVocabToken)) {
-            uint16_t* dst = static_cast<uint16_t*>(a.dh) + (int64_t)tok * a.dh_stride + c0;
-            store16(dst, y, cols, ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0, a.f16, false);
-          }
+          if (out && vec && GPO_BOUNDS(st, tok, a.T, kWhereVocabToken))
+            store16(static_cast<uint16_t*>(a.dh) + (int64_t)tok * a.dh_stride + c0, y, cols, a.f16, false);
         } else if (bulk && cols > 0) {
           // 64 columns of the warp's 32 rows, 128 bytes each with the 128-byte swizzle, go out as one bulk copy, which
           // leaves out what lies past the matrix: with a store per lane and row a tile's took 4 us of the load and store unit
@@ -692,10 +716,14 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
             __syncwarp();
             if (lane == 0) bulk_store_2d(&maps.dw, own, n0 + (ch & ~1) * 32, (int)a.v0 + row);
           }
-        } else if (live && cols > 0 && GPO_BOUNDS(st, a.v0 + row, a.V, kWhereVocabRow)) {
-          uint16_t* dst = static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0;
-          store16(dst, y, cols, ((a.dw_stride & 7) | (reinterpret_cast<uintptr_t>(a.dw) & 15)) == 0, a.f16,
-                  a.accumulate != 0);
+        } else if (vec && live && cols > 0 && GPO_BOUNDS(st, a.v0 + row, a.V, kWhereVocabRow)) {
+          store16(static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0, y, cols, a.f16, a.accumulate != 0);
+        }
+        if (by_rows && cols > 0) {
+          const int64_t at = t.job == 1 ? a.v0 + row : tok;
+          const bool put = live && GPO_BOUNDS(st, at, t.job == 1 ? a.V : a.T, t.job == 1 ? kWhereVocabRow : kWhereVocabToken);
+          store_rows(reinterpret_cast<float*>(own), y, static_cast<uint16_t*>(t.job == 1 ? a.dw : a.dh) + c0,
+                     t.job == 1 ? a.dw_stride : a.dh_stride, put ? at : -1, cols, a.f16, t.job == 1 && a.accumulate != 0, lane);
         }
       }
       ++p.sum;
@@ -917,8 +945,6 @@ __device__ __forceinline__ void gather_row(const VocabArgs& a, int64_t r, int64_
 #pragma unroll 8
   for (int c = lane; c < chunks; c += 32) dst[c] = src[c];
 }
-__device__ __forceinline__ bool dh_vec(const VocabArgs& a) { return ((a.dh_stride & 7) | (reinterpret_cast<uintptr_t>(a.dh) & 15)) == 0; }
-
 // Gradient: the tokens with a target and a gradient that is not 0, in the order of their targets and, for one
 // target, their own; their number, the scale of an fp16 dz, the number of tokens before each tile's targets, their hidden
 // rows in that order with zeros behind them (see gather_row), and the zeros of the others' d_hidden.
@@ -981,7 +1007,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
   }
   __syncthreads();
   all = __reduce_add_sync(0xffffffffu, s_all[lane]);
-  const bool vec = dh_vec(a);
+  const bool vec = vec_rows(a.dh, a.dh_stride);
   const int ta = (int)(a.T * blockIdx.x / gridDim.x), tb = (int)(a.T * (blockIdx.x + 1) / gridDim.x);
   for (int t = ta + warp; t < tb; t += kW) {
     const int key = s_key[t];
@@ -1084,7 +1110,7 @@ __global__ void __launch_bounds__(256) vocab_gather_kernel(VocabArgs a) {
   const int64_t rows = a.head->rows, pad = rows_behind(a, rows);
   for (int64_t r = warp; r < pad; r += nwarps) gather_row(a, r, r < rows ? a.idx[r] : -1, lane);
   if (!a.dh) return;
-  const bool vec = dh_vec(a);
+  const bool vec = vec_rows(a.dh, a.dh_stride);
   for (int64_t t = warp; t < a.T; t += nwarps) {
     const int64_t id = load_id(a.target, a.id8, t);
     if (id >= 0 && id < a.V && (a.g[t] != 0.f || (a.ge && a.ge[t] != 0.f))) continue;

@@ -111,6 +111,8 @@ gpo_status check_call(gpo_ctx* c, const void* workspace, size_t have, size_t nee
   return GPO_OK;
 }
 
+// (Fetching 256 bytes for a box's 128 takes rows that straddle lines 20 % longer: dz of 4000 tokens, 30000 x
+// 1000, 144 us against 125.)
 bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16,
                 int box_rows = 64) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
@@ -118,7 +120,7 @@ bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t col
   const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   return enc(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // The launches of one call: an NVTX range around each and, with timing on, a CUDA event after it.
