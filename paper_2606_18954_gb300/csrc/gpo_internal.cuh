@@ -1035,15 +1035,19 @@ struct VocabArgs {
   void* dw;
   int64_t dw_stride;
   int accumulate;
+  int w_blocks;          // the matrix's rows are whole blocks of 64 columns (maps.wb)
   int dw_bulk;           // d_weight's rows take bulk stores (maps.dw)
   int debug_timeout;
 };
 
-// Tensor maps of one call: hidden rows as given and gathered, the vocabulary matrix, dz; boxes of 64 x 64
-// (few tokens: 64 x vocab_few_columns of hidden, 64 x 32 of the matrix).
+// Tensor maps of one call.  K innermost, boxes of 64 x 128: hidden rows as given (few tokens: 64 x
+// vocab_few_columns) and gathered, the vocabulary matrix (few tokens: 64 x 32), dz.  The products' other operands, whose rows
+// are k, in blocks of 64 columns, boxes of 64 k of two blocks: the gathered rows, dz, the matrix (w_blocks 0: boxes of
+// 64 x 64).  d_weight in boxes of 64 x 32.
 struct VocabMaps {
   CUtensorMap h, hc, w, dz;
-  CUtensorMap dw;  // d_weight, boxes of 64 x 32
+  CUtensorMap hb, dzb, wb;
+  CUtensorMap dw;
 };
 
 cudaError_t setup_vocab();

@@ -78,6 +78,15 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
       : "memory");
 }
 
+// The same of a matrix seen as blocks of 64 columns (3-D: column in the block, row, block): whole blocks.
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar_addr, int row, int block) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, "
+      "%4, %5}], [%2];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(bar_addr), "r"(0), "r"(row), "r"(block)
+      : "memory");
+}
+
 // 2-D tiled store of a box from this CTA's shared memory, as a bulk group of its own; what lies past the tensor is
 // left out.
 __device__ __forceinline__ void bulk_store_2d(const CUtensorMap* map, const void* src, int x, int y) {

@@ -38,8 +38,10 @@ namespace gpo {
 
 namespace {
 
-// Ent: with the entropy; Wide: dz of logits that are several accumulations (see kVocabDzSeg)
-enum Mode { kLse, kLseEnt, kDz, kDzEnt, kDzWide, kDzWideEnt, kProducts };
+// Ent: with the entropy; Wide: dz of logits that are several accumulations (see kVocabDzSeg); Rows: products whose results
+// have rows of any alignment (see store_rows)
+enum Mode { kLse, kLseEnt, kDz, kDzEnt, kDzWide, kDzWideEnt, kProducts, kProductsRows };
+__host__ __device__ constexpr bool is_products(int mode) { return mode == kProducts || mode == kProductsRows; }
 __host__ __device__ constexpr bool is_lse(int mode) { return mode == kLse || mode == kLseEnt; }
 __host__ __device__ constexpr bool is_wide(int mode) { return mode == kDzWide || mode == kDzWideEnt; }
 __host__ __device__ constexpr bool has_ent(int mode) { return mode == kLseEnt || mode == kDzEnt || mode == kDzWideEnt; }
@@ -93,7 +95,7 @@ constexpr int kWarpBytes = 4 * 1024;
 constexpr size_t kVCtl = (sizeof(VocabCtl) + 15) & ~size_t(15);
 constexpr size_t kVSmem = kVCtl + 1023 + (size_t)kVStages * kVStage;
 constexpr size_t kPSmem = kVCtl + 1023 + (size_t)kPStages * kVStage + 2 * (size_t)kRestBytes + (size_t)kVEpiWarps * kWarpBytes;
-__host__ __device__ constexpr size_t smem_of(int mode) { return mode == kProducts ? kPSmem : kVSmem; }
+__host__ __device__ constexpr size_t smem_of(int mode) { return is_products(mode) ? kPSmem : kVSmem; }
 
 __device__ __forceinline__ uint32_t pack16(float a, float b, int f16) {
   if (f16) {
@@ -152,7 +154,7 @@ __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
 // The pair's s-th tile; false after the last.
 template <int kMode>
 __device__ __forceinline__ bool next_tile(const Plan& q, int s, Tile& t) {
-  if (kMode != kProducts) {
+  if (!is_products(kMode)) {
     const int64_t i = q.p + (int64_t)s * q.np;
     if (i >= (int64_t)q.mt * q.nt) return false;
     // kRaster row tiles take the columns together: what the pairs work on at one time is few columns of
@@ -202,7 +204,7 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&x)[8]) {
 }
 
 // Rows of whole, aligned 16 bytes.
-__device__ __forceinline__ bool vec_rows(const void* p, int64_t stride) { return ((stride & 7) | (reinterpret_cast<uintptr_t>(p) & 15)) == 0; }
+__host__ __device__ __forceinline__ bool vec_rows(const void* p, int64_t stride) { return ((stride & 7) | (reinterpret_cast<uintptr_t>(p) & 15)) == 0; }
 
 // 16 bits of 32 consecutive columns of a row to memory (add: added to what it holds), 16-byte aligned, those below `cols`.
 __device__ __forceinline__ void store16(uint16_t* dst, const float (&x)[32], int cols, int f16, bool add) {
@@ -365,13 +367,11 @@ __device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArg
   const CUtensorMap* hmap = a.idx && (!kLogits || c.rows < a.T) ? &maps.hc : &maps.h;
   Tile t;
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
-    const CUtensorMap* ma = kMode == kProducts ? &maps.dz : hmap;
-    const CUtensorMap* mb = kMode == kProducts && t.job == 1 ? hmap : &maps.w;
-    const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
     const int am = t.m0 + (int)c.rank * (kPairM / 2), bn = t.n0 + (int)c.rank * (kPairN / 2);
     const int v0 = kLogits ? 0 : (int)a.v0;
     int ra = 0, rb = 0;
-    if (kMode == kProducts && t.job == 1) tokens_of(a, t, ra, rb);
+    if (is_products(kMode) && t.job == 1) tokens_of(a, t, ra, rb);
+    // (few and large boxes: what this one thread issues for a step counts in the step's time)
     for (int k = 0; k < t.kb; ++k) {
       if (!mbar_wait(&c.ctl->empty[p.stage], p.phase ^ 1u, st, 20)) return false;
       const uint32_t sa = c.tiles + (uint32_t)p.stage * kVStage, sb = sa + 2 * kVBox;
@@ -379,26 +379,29 @@ __device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArg
       if (c.rank == 0) mbar_arrive_expect_tx(&c.ctl->full[p.stage], 2 * kVStage);
       ++p.issued;
       const int kx = (t.ka + k) * kTile16;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (a_mn) tma_load_2d_pair(sa + h * kVBox, ma, bar, am + h * kTile16, kx);
-        else tma_load_2d_pair(sa + h * kVBox, ma, bar, kx, am + h * kTile16);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (!b_mn) tma_load_2d_pair(sb + h * kVBox, mb, bar, kx, v0 + bn + h * kTile16);
-        else tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, (t.job == 0 ? v0 : 0) + kx);
+      if (!is_products(kMode)) {
+        tma_load_2d_pair(sa, hmap, bar, kx, am);
+        tma_load_2d_pair(sb, &maps.w, bar, kx, v0 + bn);
+      } else if (t.job == 0) {
+        tma_load_2d_pair(sa, &maps.dz, bar, kx, am);
+        if (a.w_blocks) {
+          tma_load_3d_pair(sb, &maps.wb, bar, v0 + kx, bn / kTile16);
+        } else {
+          tma_load_2d_pair(sb, &maps.wb, bar, bn, v0 + kx);
+          tma_load_2d_pair(sb + kVBox, &maps.wb, bar, bn + kTile16, v0 + kx);
+        }
+      } else {
+        tma_load_3d_pair(sa, &maps.dzb, bar, kx, am / kTile16);
+        tma_load_3d_pair(sb, &maps.hb, bar, kx, bn / kTile16);
       }
       p.next<kS>();
     }
     for (int r = ra; r < rb; r += kTile16) {  // the hidden rows of write_rests
       if (!mbar_wait(&c.ctl->empty[p.stage], p.phase ^ 1u, st, 20)) return false;
-      const uint32_t sb = c.tiles + (uint32_t)p.stage * kVStage + 2 * kVBox;
       const uint32_t bar = leader_addr(&c.ctl->full[p.stage]);
       if (c.rank == 0) mbar_arrive_expect_tx(&c.ctl->full[p.stage], kVStage);
       ++p.issued;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) tma_load_2d_pair(sb + h * kVBox, mb, bar, bn + h * kTile16, r);
+      tma_load_3d_pair(c.tiles + (uint32_t)p.stage * kVStage + 2 * kVBox, &maps.hb, bar, r, bn / kTile16);
       p.next<kS>();
     }
   }
@@ -413,12 +416,12 @@ __device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, 
   uint32_t rest = 0;  // steps of write_rests so far
   Tile t;
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
-    const bool a_mn = kMode == kProducts && t.job == 1, b_mn = kMode == kProducts;
+    const bool a_mn = is_products(kMode) && t.job == 1, b_mn = is_products(kMode);
     const uint32_t idesc = idesc_16_f32(kPairM, kPairN, a.f16 != 0, a_mn, b_mn);
     int ra = 0, rb = 0;
-    if (kMode == kProducts && t.job == 1) tokens_of(a, t, ra, rb);
+    if (is_products(kMode) && t.job == 1) tokens_of(a, t, ra, rb);
     // whole steps, and the instructions (16 k each) of the one that the operands end in
-    const int ends = kMode != kProducts ? a.D : t.job == 1 ? c.rows : (int)a.vn - t.ka * kTile16;
+    const int ends = !is_products(kMode) ? a.D : t.job == 1 ? c.rows : (int)a.vn - t.ka * kTile16;
     const int whole = min(t.kb, ends / kTile16), last = whole < t.kb ? (ends - whole * kTile16 + 15) / 16 : 0;
     // (of the ring's first stage; addresses are in units of 16 bytes there)
     const uint64_t a0 = a_mn ? smem_desc_mn128(c.tiles, kVBox) : smem_desc_k128(c.tiles);
@@ -452,7 +455,7 @@ __device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, 
         mma_commit_pair(&c.ctl->empty[p.stage]);
         p.next<kS>();
       }
-      if constexpr (kMode == kProducts) {
+      if constexpr (is_products(kMode)) {
 #pragma unroll 1
         for (int r = ra; r < rb; r += kTile16, ++rest) {  // the steps of write_rests
           if (!mbar_wait(&c.ctl->full[p.stage], p.phase, st, 23)) return false;
@@ -534,7 +537,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
   for (int s = 0; next_tile<kMode>(plan, s, t); ++s) {
     const int row = t.m0 + r;
     const int n0 = t.n0 + half * (kPairN / 2);  // first column of this warp
-    if constexpr (kMode != kProducts) {
+    if constexpr (!is_products(kMode)) {
       const bool live = row < rows;
       // what the row's token brings
       int64_t tok = 0;
@@ -666,7 +669,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       const int tok = t.job == 0 && live ? __ldcg(a.idx + row) : 0;
       const bool bulk = t.job == 1 && a.dw_bulk != 0;
       const bool vec = t.job == 1 ? vec_rows(a.dw, a.dw_stride) : vec_rows(a.dh, a.dh_stride);
-      const bool by_rows = !vec && (t.job == 1 || (a.last && a.splits == 1));
+      const bool by_rows = kMode == kProductsRows && !vec && (t.job == 1 || (a.last && a.splits == 1));
       if (lane == 0) bulk_read();  // (the last tile's rows have left)
       __syncwarp();
       if (!ready(p.sum)) return false;
@@ -728,7 +731,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
         } else if (vec && live && cols > 0 && GPO_BOUNDS(st, a.v0 + row, a.V, kWhereVocabRow)) {
           store16(static_cast<uint16_t*>(a.dw) + (a.v0 + row) * a.dw_stride + c0, y, cols, a.f16, a.accumulate != 0);
         }
-        if (by_rows && cols > 0) {
+        if (kMode == kProductsRows && by_rows && cols > 0) {
           const int64_t at = t.job == 1 ? a.v0 + row : tok;
           const bool put = live && GPO_BOUNDS(st, at, t.job == 1 ? a.V : a.T, t.job == 1 ? kWhereVocabRow : kWhereVocabToken);
           store_rows(reinterpret_cast<float*>(own), y, static_cast<uint16_t*>(t.job == 1 ? a.dw : a.dh) + c0,
@@ -738,7 +741,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       ++p.sum;
     }
   }
-  if constexpr (kMode == kProducts) {
+  if constexpr (is_products(kMode)) {
     if (lane == 0) bulk_done();
     __syncwarp();
   }
@@ -810,7 +813,7 @@ template <int kMode>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     vocab_pair_kernel(const __grid_constant__ VocabMaps maps, VocabArgs a, Status st) {
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  constexpr int kS = kMode == kProducts ? kPStages : kVStages;
+  constexpr int kS = is_products(kMode) ? kPStages : kVStages;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   let_next_start();
   Cta c = begin_pair<kS>(smem_raw);
@@ -822,7 +825,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     if (warp == kLoadWarp && lane == 0) {
       load_tiles<kMode, kS>(maps, a, st, c, p);
       end_loads<kS>(st, c, p);
-    } else if (kMode == kProducts && warp == kRestWarp) {
+    } else if (is_products(kMode) && warp == kRestWarp) {
       if (a.dw) write_rests(a, st, c, kS * kVStage, lane);
     } else if (warp == kMmaWarp && lane == 0 && c.rank == 0) {
       if (a.debug_timeout) mbar_wait(&c.ctl->drain, 0, st, 27, kDebugTimeoutNs);  // reports GPO_ERR_TIMEOUT
@@ -834,7 +837,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     if (keeps_logits(kMode)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
     finish_tiles<kMode, kS>(maps, a, st, c, p);
   }
-  if (kMode == kProducts && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
+  if (is_products(kMode) && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   end_pair(st, c);
 }
 
@@ -1260,6 +1263,7 @@ cudaError_t setup_vocab() {
   if (e == cudaSuccess) e = setup_mode<kDzWide>();
   if (e == cudaSuccess) e = setup_mode<kDzWideEnt>();
   if (e == cudaSuccess) e = setup_mode<kProducts>();
+  if (e == cudaSuccess) e = setup_mode<kProductsRows>();
   const int bytes = (int)sort_smem(kSortMaxRows);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(vocab_sort_kernel<int32_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(vocab_sort_kernel<int64_t>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -1332,7 +1336,9 @@ int vocab_splits(int64_t T, int64_t vn, int64_t D) {
 }
 
 cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {
-  const cudaError_t e = launch_pair<kProducts>(lc, m, a, st, (a.dh ? tiles_of(a.T, a.D) * a.splits : 0) + (a.dw ? tiles_of(a.vn, a.D) : 0));
+  const int64_t tiles = (a.dh ? tiles_of(a.T, a.D) * a.splits : 0) + (a.dw ? tiles_of(a.vn, a.D) : 0);
+  const bool vec = (!a.dh || vec_rows(a.dh, a.dh_stride)) && (!a.dw || vec_rows(a.dw, a.dw_stride));
+  const cudaError_t e = vec ? launch_pair<kProducts>(lc, m, a, st, tiles) : launch_pair<kProductsRows>(lc, m, a, st, tiles);
   if (e != cudaSuccess || !a.last || a.splits == 1) return e;
   const int64_t quads = a.T * ((a.D + 3) / 4);
   return launch_after(vocab_parts_kernel, (unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a, st);

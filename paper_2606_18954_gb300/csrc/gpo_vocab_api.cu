@@ -114,11 +114,21 @@ gpo_status check_call(gpo_ctx* c, const void* workspace, size_t have, size_t nee
 // (Fetching 256 bytes for a box's 128 takes rows that straddle lines 20 % longer: dz of 4000 tokens, 30000 x
 // 1000, 144 us against 125.)
 bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16,
-                int box_rows = 64) {
+                int box_rows) {
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   const cuuint64_t strides[1] = {(cuuint64_t)(stride * 2)};
   const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, estr[2] = {1, 1};
   return enc(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+             strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A matrix in blocks of 64 columns: cols a multiple of them, boxes of 64 rows of two blocks.
+bool encode_blocks(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16) {
+  const cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)(cols / 64)};
+  const cuuint64_t strides[2] = {(cuuint64_t)(stride * 2), 128};
+  const cuuint32_t box[3] = {64, 64, 2}, estr[3] = {1, 1, 1};
+  return enc(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims,
              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -199,11 +209,19 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
   a.debug_timeout = (ctx->params.flags & GPO_FLAG_DEBUG_TIMEOUT) != 0;
   EncodeTiledFn enc = encode_fn();
   if (!enc) return set_msg(ctx, "cuTensorMapEncodeTiled unavailable"), GPO_ERR_CUDA;
-  bool ok = encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16,
-                       L.few ? vocab_few_columns(a.T) : 64) &&
-            encode_map(&m.w, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, L.few ? 32 : 64);
-  if (L.listed) ok = ok && encode_map(&m.hc, enc, a.hc, v.d, up_to(v.num_tokens, 64), L.hc_stride, a.f16);
-  if (L.dz) ok = ok && encode_map(&m.dz, enc, at<void>(ws, L.dz), L.piece, L.tp, L.piece, a.f16);
+  const int64_t T64 = up_to(v.num_tokens, 64);
+  bool ok = encode_map(&m.w, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, L.few ? 32 : 128);
+  if (!L.dz) ok = ok && encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16, L.few ? vocab_few_columns(a.T) : 128);
+  if (L.listed) ok = ok && encode_map(&m.hc, enc, a.hc, v.d, T64, L.hc_stride, a.f16, 128);
+  if (L.dz) {
+    void* dz = at<void>(ws, L.dz);
+    a.w_blocks = v.d % 64 == 0;
+    ok = ok && encode_map(&m.dz, enc, dz, L.piece, L.tp, L.piece, a.f16, 128) &&
+         encode_blocks(&m.dzb, enc, dz, L.piece, L.tp, L.piece, a.f16) &&
+         encode_blocks(&m.hb, enc, a.hc, L.hc_stride, T64, L.hc_stride, a.f16) &&
+         (a.w_blocks ? encode_blocks(&m.wb, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16)
+                     : encode_map(&m.wb, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, 64));
+  }
   if (!ok) return set_msg(ctx, "cuTensorMapEncodeTiled failed"), GPO_ERR_UNSUPPORTED;
   return GPO_OK;
 }
