@@ -1043,7 +1043,7 @@ struct VocabArgs {
 // Tensor maps of one call.  K innermost, boxes of 64 x 128: hidden rows as given (few tokens: 64 x
 // vocab_few_columns) and gathered, the vocabulary matrix (few tokens: 64 x 32), dz.  The products' other operands, whose rows
 // are k, in blocks of 64 columns, boxes of 64 k of two blocks: the gathered rows, dz, the matrix (w_blocks 0: boxes of
-// 64 x 64).  d_weight in boxes of 64 x 32.
+// 64 x 64; few tokens: K innermost, 64 x 128).  d_weight in boxes of 64 x 32.
 struct VocabMaps {
   CUtensorMap h, hc, w, dz;
   CUtensorMap hb, dzb, wb;

@@ -17,11 +17,12 @@
 //            that is not 0, in the order of their targets, and their rows.  Bound by latency: 12 to 22 us up to 16384
 //            tokens, 66 for 65536
 //   dz       vocab_pair_kernel<kDz>: the logits again, dz in the epilogue, written in 16 bits.  Bound by the tensor
-//            cores: 1434 x 65536 x 2048 235 us, 1640 TFLOP/s
+//            cores: 1434 x 65536 x 2048 230 us, 1670 TFLOP/s
 //   products vocab_pair_kernel<kProducts>: d_hidden += dz W and d_weight = dz^T hidden in one launch;
-//            with few tokens the k of d_hidden in parts (vocab_splits) that vocab_parts_kernel adds.  Bound by what the
-//            loads bring an SM: a step of 64 k takes 0.35 us, where its MMAs take 0.27; 1434 x 65536 x 2048 500 us, 1540
-//            TFLOP/s.  (Six stages in place of five, and a ring whose boxes were fetched into L2 ahead, did not help.)
+//            with few tokens the k of d_hidden in parts (vocab_splits) that vocab_parts_kernel adds.  Bound by the
+//            tensor cores and what feeds them: a step of 64 k takes 0.32 us, where its MMAs take 0.27; 1434 x 65536 x
+//            2048 465 us, 1650 TFLOP/s.  (Six stages in place of five, boxes fetched into L2 ahead, a second loading
+//            thread: none of them faster.)
 // The tiles are as large as tensor memory allows with two accumulators of fp32, one for the MMAs and one for the epilogue:
 // each operand byte is used 128 times from shared memory, which both CTAs of a pair fill half and half.
 // Keeping the sum over the other tokens of the vocabulary apart from the target's term keeps the
