@@ -987,7 +987,11 @@ constexpr int kVocabPairs = 76;      // CTA pairs that the split of d_hidden's k
 constexpr int kVocabMaxSplits = 32;
 int vocab_splits(int64_t T, int64_t vn, int64_t D);
 constexpr int64_t kVocabPieceBytes = (int64_t)512 << 20;  // dz of one piece of the vocabulary at most
-constexpr int kVocabFew = 64;        // tokens up to which the forward pass is one launch (gpo_vocab_few.cu)
+// Tokens up to which the forward pass is the one launch of gpo_vocab_few.cu.  Its lanes keep every token's sums, so
+// its epilogue takes as long as the tiles' from some 16 tokens on (us, one launch against tiles: 131072 x 4096 1
+// token 181, 232, 8 182, 224, 16 184, 178; 131072 x 1024 59, 81, 59, 75, 61, 75; 8000 x 512 16, 21, 18, 20, 21, 21; with
+// 64 tokens 201, 179; 78, 59; 38, 21).
+constexpr int kVocabFew = 16;
 constexpr int kVocabFewCtas = 256;   // CTAs of that launch at most
 // parts of a forward row: the maxima and sums of the two column halves of every tile
 inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
@@ -1041,7 +1045,7 @@ struct VocabArgs {
 };
 
 // Tensor maps of one call.  K innermost, boxes of 64 x 128: hidden rows as given (few tokens: 64 x
-// vocab_few_columns) and gathered, the vocabulary matrix (few tokens: 64 x 32), dz.  The products' other operands, whose rows
+// kVocabFew) and gathered, the vocabulary matrix (few tokens: 64 x 32), dz.  The products' other operands, whose rows
 // are k, in blocks of 64 columns, boxes of 64 k of two blocks: the gathered rows, dz, the matrix (w_blocks 0: boxes of
 // 64 x 64; few tokens: K innermost, 64 x 128).  d_weight in boxes of 64 x 32.
 struct VocabMaps {
@@ -1057,7 +1061,6 @@ cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Sta
 cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
 // Up to kVocabFew tokens; marks: [kVocabFewCtas] in the workspace, mark: a value that no other call leaves there.
 cudaError_t setup_vocab_few();
-int vocab_few_columns(int64_t T);
 cudaError_t launch_vocab_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent,
                              uint64_t* marks, uint64_t mark);
 cudaError_t launch_vocab_lse(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent);

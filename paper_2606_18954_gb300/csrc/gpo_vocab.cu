@@ -1,7 +1,7 @@
 // Per-token log-probabilities from hidden states and the vocabulary matrix, and their gradients,
 // on the tcgen05 tensor cores (the formulas are in include/graphpo.h).
 //
-// Forward, two launches, and one more before them for large products (kVocabListed; up to 64 tokens:
+// Forward, two launches, and one more before them for large products (kVocabListed; up to 16 tokens:
 // gpo_vocab_few.cu):
 //   rows     vocab_rows_kernel lists the tokens with a target and copies their hidden rows together
 //            (not where every token has one): the others then cost no product.  Bound by the reads: every CTA looks at

@@ -211,7 +211,7 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
   if (!enc) return set_msg(ctx, "cuTensorMapEncodeTiled unavailable"), GPO_ERR_CUDA;
   const int64_t T64 = up_to(v.num_tokens, 64);
   bool ok = encode_map(&m.w, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, L.few ? 32 : 128);
-  if (!L.dz) ok = ok && encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16, L.few ? vocab_few_columns(a.T) : 128);
+  if (!L.dz) ok = ok && encode_map(&m.h, enc, v.hidden, v.d, v.num_tokens, v.hidden_stride, a.f16, L.few ? kVocabFew : 128);
   if (L.few) ok = ok && encode_map(&m.wb, enc, v.weight, v.d, v.vocab, v.weight_stride, a.f16, 128);
   if (L.listed) ok = ok && encode_map(&m.hc, enc, a.hc, v.d, T64, L.hc_stride, a.f16, 128);
   if (L.dz) {

@@ -1,8 +1,8 @@
-// Log-probabilities of up to 64 tokens (decoding, a step of a few rollouts) in one launch.
+// Log-probabilities of up to 16 tokens (decoding) in one launch.
 //
 // With few tokens every weight is read once and the products are cheap, so the roles are turned
-// round: 128 vocabulary rows at a time are the tensor cores' A operand, the tokens (16, 32 or
-// 64 columns of them) the B operand, which costs an MMA of few columns and little tensor memory to read.  A CTA
+// round: 128 vocabulary rows at a time are the tensor cores' A operand, the tokens (16 columns) the B operand,
+// which costs an MMA of few columns and little tensor memory to read.  A CTA
 // per SM streams an equal share of the vocabulary, in units of 32 rows, through a ring of TMA boxes; a
 // lane owns a vocabulary row and keeps the running maximum and sum of every token over its
 // rows in registers, with no exchange until the end.  Then the CTA joins its 128 lanes, and the CTA that
@@ -10,7 +10,7 @@
 // call's own tag: a mark left by another call is none.  Every CTA publishes its part, fences, and
 // then looks: whichever comes last sees all marks.  Two that both see them write the same results.)
 // The accumulators are taken over into registers every 128 products (see gpo_vocab.cu).
-// Bound by HBM: one token, 131072 x 4096, 1.074 GB read in 179 us, 6.0 TB/s; below some 30 MB by the chain of launch,
+// Bound by HBM: one token, 131072 x 4096, 1.074 GB read in 178 us, 6.0 TB/s; below some 30 MB by the chain of launch,
 // first loads and join: 7 tokens, 1009 x 256, 10 us.
 #define GPO_REPORT __noinline__
 #include "gpo_vocab_math.cuh"
@@ -60,7 +60,7 @@ __device__ __forceinline__ bool few_any(bool flag) {
   return out != 0;
 }
 
-template <int kN, bool kEnt>
+template <bool kEnt>
 __global__ void __launch_bounds__(kFewThreads, 1)
     vocab_few_kernel(const __grid_constant__ CUtensorMap wmap, const __grid_constant__ CUtensorMap tmap,
                      const __grid_constant__ CUtensorMap hmap, VocabArgs a, Status st, uint64_t* marks, uint64_t mark) {
@@ -70,10 +70,11 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   constexpr uint32_t kCtl = (sizeof(FewCtl) + 15) & ~15u;
   const uint32_t ring_off = ((sbase + kCtl + 1023u) & ~1023u) - sbase;
   unsigned char* ring = smem_raw + ring_off;
-  constexpr int kA = kFewTile * 128, kB = kN * 128, kStage = kA + kB;
+  constexpr int kN = kVocabFew, kA = kFewTile * 128, kB = kN * 128, kStage = kA + kB;
   constexpr int kStages = kFewRing / kStage < kFewStages ? kFewRing / kStage : kFewStages;
   constexpr int kCols = kN / 2;  // tokens of one epilogue thread
-  constexpr uint32_t kTmem = kFewBufs * kN <= 64 ? 64 : kFewBufs * kN <= 128 ? 128 : 256;
+  constexpr uint32_t kTmem = kFewBufs * kN;
+  static_assert(kTmem == 64 && kFewEpi % kN == 0, "tensor memory columns, threads of a token");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int cta = (int)blockIdx.x, nctas = (int)gridDim.x;
@@ -241,9 +242,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       }
     }
     // the CTA's part of every token: the 128 lanes' through shared memory (the ring is free: every
-    // accumulation is done), four threads a token
+    // accumulation is done), kPer threads a token
     if (!few_any(!ok)) {
-      constexpr int kRow = kFewTile + 1;
+      constexpr int kRow = kFewTile + 1, kPer = kFewEpi / kN;
       float* red = reinterpret_cast<float*>(ring);
 #pragma unroll
       for (int j = 0; j < kCols; ++j) {
@@ -253,24 +254,22 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         if (kEnt) red[2 * kN * kRow + at] = w[j];
       }
       few_any(false);
-      const int tok = te >> 2, part = te & 3;
+      const int tok = te / kPer, part = te % kPer;
       Part p = {kLow, 0.f, 0.f};
-      if (tok < kN) {
-        const int at = tok * kRow + part;
-        for (int i = 0; i < kFewTile; i += 4) p.m = fmaxf(p.m, red[at + i]);
-        for (int i = 0; i < kFewTile; i += 4) {
-          const float d = red[at + i] - p.m, e = ex2(d), si = red[kN * kRow + at + i];
-          p.s = fmaf(e, si, p.s);
-          if (kEnt) p.u = fmaf(e, fmaf(d, si, red[2 * kN * kRow + at + i]), p.u);
-        }
+      const float* mine = red + tok * kRow + part;
+      for (int i = 0; i < kFewTile; i += kPer) p.m = fmaxf(p.m, mine[i]);
+      for (int i = 0; i < kFewTile; i += kPer) {
+        const float d = mine[i] - p.m, e = ex2(d), si = mine[kN * kRow + i];
+        p.s = fmaf(e, si, p.s);
+        if (kEnt) p.u = fmaf(e, fmaf(d, si, mine[2 * kN * kRow + i]), p.u);
       }
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
+      for (int o = 1; o < kPer; o <<= 1) {
         const Part y = {__shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o),
                         __shfl_xor_sync(0xffffffffu, p.u, o)};
         p = join<kEnt>(p, y);
       }
-      if (part == 0 && tok < kN) {
+      if (part == 0) {
         const int at = cta * kVocabFew + tok;
         a.pm[at] = p.m;
         a.ps[at] = p.s;
@@ -322,41 +321,21 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   if (warp == 2) tmem_dealloc(tmem, kTmem);
 }
 
-template <int kN, bool kEnt>
-cudaError_t launch_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, uint64_t* marks,
-                       uint64_t mark) {
-  const int64_t units = (a.V + kFewUnit - 1) / kFewUnit;
-  const int64_t grid = min(units, (int64_t)min(lc.num_sms, kVocabFewCtas));
-  vocab_few_kernel<kN, kEnt><<<(unsigned)grid, kFewThreads, kFewSmem, lc.stream>>>(m.w, m.wb, m.h, a, st, marks, mark);
-  return cudaGetLastError();
-}
-
-template <int kN, bool kEnt>
-cudaError_t setup_few() {
-  return cudaFuncSetAttribute(vocab_few_kernel<kN, kEnt>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
-}
-
 }  // namespace
 
 cudaError_t setup_vocab_few() {
-  cudaError_t e = setup_few<16, false>();
-  if (e == cudaSuccess) e = setup_few<16, true>();
-  if (e == cudaSuccess) e = setup_few<32, false>();
-  if (e == cudaSuccess) e = setup_few<32, true>();
-  if (e == cudaSuccess) e = setup_few<64, false>();
-  if (e == cudaSuccess) e = setup_few<64, true>();
-  return e;
+  cudaError_t e = cudaFuncSetAttribute(vocab_few_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(vocab_few_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kFewSmem);
 }
-
-int vocab_few_columns(int64_t T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
 
 cudaError_t launch_vocab_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent,
                              uint64_t* marks, uint64_t mark) {
-  switch (vocab_few_columns(a.T)) {
-    case 16: return ent ? launch_few<16, true>(lc, m, a, st, marks, mark) : launch_few<16, false>(lc, m, a, st, marks, mark);
-    case 32: return ent ? launch_few<32, true>(lc, m, a, st, marks, mark) : launch_few<32, false>(lc, m, a, st, marks, mark);
-    default: return ent ? launch_few<64, true>(lc, m, a, st, marks, mark) : launch_few<64, false>(lc, m, a, st, marks, mark);
-  }
+  const int64_t units = (a.V + kFewUnit - 1) / kFewUnit;
+  const unsigned grid = (unsigned)min(units, (int64_t)min(lc.num_sms, kVocabFewCtas));
+  if (ent) vocab_few_kernel<true><<<grid, kFewThreads, kFewSmem, lc.stream>>>(m.w, m.wb, m.h, a, st, marks, mark);
+  else vocab_few_kernel<false><<<grid, kFewThreads, kFewSmem, lc.stream>>>(m.w, m.wb, m.h, a, st, marks, mark);
+  return cudaGetLastError();
 }
 
 }  // namespace gpo

@@ -36,7 +36,7 @@ def embedding(B, **kw):
 
 def test_vocab_workspace(B):
     size = lambda grad=False, **kw: B.vocab_workspace_size(vocab(B, **kw), grad)  # noqa: E731
-    assert 0 < size(num_tokens=0) < size(num_tokens=1) == size(num_tokens=64)  # up to 64 tokens: one launch's own parts
+    assert 0 < size(num_tokens=0) < size(num_tokens=1) == size(num_tokens=16)  # up to 16 tokens: one launch's own parts
     assert size(num_tokens=65) <= size(num_tokens=256) < size(num_tokens=257) < size(num_tokens=5000)
     # never a whole [T x V] matrix: the gradient's largest part is a piece of 512 MiB at most
     big = dict(num_tokens=1 << 17, vocab=1 << 18, d=1024, hidden_stride=1024, weight_stride=1024)
