@@ -314,11 +314,9 @@ def _vector(t, what: str, dev: int, n: int, dtype=None) -> int:
 _current_stream = None  # device index -> handle of its current stream
 
 
-def _stream_handle(stream, dev: int):
-    """The CUDA stream handle of `stream`, or of the current stream on device `dev`."""
+def _stream_handle(dev: int):
+    """The CUDA stream handle of the current stream on device `dev`."""
     global _current_stream
-    if stream is not None:
-        return stream.cuda_stream
     if _current_stream is None:
         import torch
         _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (  # (see _raw_stream)
@@ -475,6 +473,7 @@ class GraphPO:
         self._h = h
         self._ws = None
         self._sizes = {}  # workspace bytes by sizes (vocabulary ends)
+        self._rooms = {}  # their workspaces by stream
 
     def close(self):
         if getattr(self, "_h", None) and self._h.value:
@@ -627,9 +626,10 @@ class GraphPO:
 
     # ---- the model's vocabulary ends (gpo_vocab_logp / gpo_vocab_grad, gpo_embed / gpo_embed_grad)
 
-    def _room(self, key, size, dev, workspace):
-        """Address and bytes of the workspace: the caller's, or the context's, which holds at least
-        size() bytes (asked once for the sizes that `key` stands for)."""
+    def _room(self, key, size, dev, workspace, handle):
+        """Address and bytes of the workspace: the caller's, or the context's for this stream, which holds at
+        least size() bytes (asked once for the sizes that `key` stands for).  (Calls on several
+        streams may run at the same time.)"""
         if workspace is not None:
             return workspace.data_ptr(), workspace.numel()
         need = self._sizes.get(key)
@@ -637,10 +637,10 @@ class GraphPO:
             if len(self._sizes) > 1024:
                 self._sizes.clear()
             need = self._sizes[key] = size()
-        ws = self._ws
-        if ws is None or ws.numel() < need or ws.device != dev:
+        ws = self._rooms.get(handle)
+        if ws is None or ws.numel() < need:
             import torch
-            ws = self._ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+            ws = self._rooms[handle] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         return ws.data_ptr(), ws.numel()
 
     @staticmethod
@@ -662,6 +662,9 @@ class GraphPO:
         "entropy" (if entropy)}, or fills `out`.  The logits are never stored.  Enqueued on the
         current stream; `check()` raises on a target outside the vocabulary."""
         import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.vocab_logp(hidden, weight, target, scale, lse, entropy, out, workspace)
         dev, T, V, d, hs, ws, code, idb, tp = self._head(hidden, weight, target)
         f32 = torch.float32
         if out is None:
@@ -675,11 +678,12 @@ class GraphPO:
             ptrs = (po[0], po[1] if lse else 0, po[-1] if entropy else 0)
         else:
             ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("logp", "lse", "entropy")]
+        on = _stream_handle(dev)
         wp, wn = self._room((0, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0)),
-                            hidden.device, workspace)
+                            hidden.device, workspace, on)
         code = _fast["gpo_vocab_logp"](
             self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale),
-            _PACK_3(*ptrs), wp, wn, _stream_handle(stream, dev))
+            _PACK_3(*ptrs), wp, wn, on)
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -691,6 +695,10 @@ class GraphPO:
         vocab_logp's outputs, whose lse (and entropy) are given; or fills `out`, with `accumulate`
         adding to out["d_weight"].  Enqueued on the current stream."""
         import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.vocab_grad(hidden, weight, target, lse, grad_logp, scale, entropy, grad_entropy, accumulate,
+                                       d_hidden, d_weight, out, workspace)
         dev, T, V, d, hs, ws, code, idb, tp = self._head(hidden, weight, target)
         f32, dt = torch.float32, hidden.dtype
         if grad_entropy is not None and entropy is None:
@@ -711,12 +719,13 @@ class GraphPO:
         sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
         if T == 0 and dw is None:
             return out
+        on = _stream_handle(dev)
         wp, wn = self._room((1, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), True),
-                            hidden.device, workspace)
+                            hidden.device, workspace, on)
         code = _fast["gpo_vocab_grad"](
             self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins,
             _PACK_GRADS(0 if dh is None else dh.data_ptr(), 0 if dw is None else dw.data_ptr(), sh, sw, bool(accumulate)),
-            wp, wn, _stream_handle(stream, dev))
+            wp, wn, on)
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -725,6 +734,9 @@ class GraphPO:
         """Rows of `table` ([V, d] bfloat16, float16 or float32) by token id (int32 or int64 [T]; below
         0: a row of zeros), times `scale`: [T, d] of the table's type.  Enqueued on the current stream."""
         import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.embed(table, ids, scale, out, workspace)
         if len(table.shape) != 2 or len(ids.shape) != 1:
             raise ValueError("table must be [V, d] and ids [T]")
         dev, (V, d), T, dt = table.get_device(), table.shape, ids.shape[0], table.dtype
@@ -734,10 +746,11 @@ class GraphPO:
             out, rs = torch.empty(T, d, dtype=dt, device=table.device), d
         else:
             rs = _matrix(out, "out", dev, T, d, dt)
+        on = _stream_handle(dev)
         wp, wn = self._room((2,), lambda: embed_workspace_size(CEmbedding(T, 1, 1, 1, 1, None, code, idb, 1.0)), table.device,
-                            workspace)
+                            workspace, on)
         code = _fast["gpo_embed"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), table.data_ptr(),
-                                  out.data_ptr(), wp, wn, _stream_handle(stream, dev))
+                                  out.data_ptr(), wp, wn, on)
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -748,6 +761,9 @@ class GraphPO:
         to `out` (a table tied to the vocabulary matrix: vocab_grad's d_weight).  Enqueued on the
         current stream."""
         import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.embed_grad(grad, ids, vocab, scale, out, accumulate, workspace)
         if len(grad.shape) != 2:
             raise ValueError("grad must be [T, d]")
         dev, (T, d), V, dt = grad.get_device(), grad.shape, int(vocab), grad.dtype
@@ -759,10 +775,11 @@ class GraphPO:
             out, ts = torch.empty(V, d, dtype=dt, device=grad.device), d
         else:
             ts = _matrix(out, "out", dev, V, d, dt)
+        on = _stream_handle(dev)
         wp, wn = self._room((3, T, V, d), lambda: embed_workspace_size(CEmbedding(T, V, d, d, d, None, code, idb, 1.0), True),
-                            grad.device, workspace)
+                            grad.device, workspace, on)
         code = _fast["gpo_embed_grad"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), grad.data_ptr(),
-                                       out.data_ptr(), bool(accumulate), wp, wn, _stream_handle(stream, dev))
+                                       out.data_ptr(), bool(accumulate), wp, wn, on)
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out

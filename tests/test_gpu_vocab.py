@@ -446,6 +446,35 @@ def test_target_outside_the_vocabulary(gp):
         assert torch.equal(again["logp"], good["logp"])
 
 
+def test_two_streams_at_once(gp):
+    """Calls of one context on two streams, not ordered with one another: each stream has its own workspace, and
+    what a call with `stream` allocates is that stream's."""
+    import torch
+    from vocab_ref import head_inputs
+    cases = [head_inputs(T, V, d, torch.bfloat16, seed=T) for T, V, d in ((700, 9000, 256), (300, 30000, 128))]
+    ids = torch.randint(0, 500, (4000,), device="cuda", dtype=torch.int32)
+    rows = torch.randn(4000, 64, device="cuda")
+
+    def run(c, stream):
+        h, w, y = c
+        f = gp.vocab_logp(h, w, y, stream=stream)
+        d = gp.vocab_grad(h, w, y, f["lse"], f["logp"], stream=stream)
+        x = gp.embed(w, y, stream=stream)
+        e = gp.embed_grad(rows, ids, 500, stream=stream)
+        return [f["logp"], d["d_hidden"], d["d_weight"], x, e]
+
+    want = [run(c, None) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(20):
+        got.append([run(c, s) for c, s in zip(cases, streams)])
+    torch.cuda.synchronize()
+    for g in got:
+        for a, b in zip(g, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
 def test_another_stream_and_a_graph(gp):
     import torch
     from vocab_ref import head_inputs
