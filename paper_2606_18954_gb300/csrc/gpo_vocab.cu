@@ -127,7 +127,7 @@ struct Plan {
   int light0, nlight, extra;  // pairs from light0 on take `extra` d_weight tiles more, for the d_hidden tile they lack
 };
 
-constexpr int kEpiSteps = 8;  // k-steps that a tile's epilogue in the products takes the time of
+constexpr int kEpiSteps = 6;  // k-steps that a tile's epilogue in the products takes the time of
 template <int kMode>
 __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   Plan q;
@@ -139,7 +139,9 @@ __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   q.kb = (a.D + kTile16 - 1) / kTile16;
   q.dt = (a.D + kPairN - 1) / kPairN;
   // the longer d_hidden tiles first, round robin; the pairs that get one less take as much work in
-  // d_weight tiles, the rest of which go round robin too
+  // d_weight tiles, the rest of which go round robin too.  (A d_weight tile takes an eighth more than its steps,
+  // for those of write_rests and its ends: 700 tokens of 65536 x 1024 137 us instead of 144; a fourth is too much for
+  // 4000 of 30000 x 1000, 226 instead of 213.  kEpiSteps 8 instead of 6: 60 of 30000 x 1024 44.5 us instead of 39.)
   q.splits = a.splits;
   q.n_dh = a.dh ? q.mt * q.dt * q.splits : 0;
   q.n_dw = a.dw ? q.nt * q.dt : 0;
@@ -148,7 +150,7 @@ __device__ __forceinline__ Plan make_plan(const VocabArgs& a, int rows) {
   q.own_dh = q.n_dh / q.np + (q.p < q.n_dh % q.np ? 1 : 0);
   q.light0 = q.n_dh % q.np;
   q.nlight = q.np - q.light0;
-  q.extra = q.light0 > 0 ? min(max(q.kb_dh / q.splits, kEpiSteps) / max(q.kb_dw, kEpiSteps), q.n_dw / q.nlight) : 0;
+  q.extra = q.light0 > 0 ? min(max(q.kb_dh / q.splits, kEpiSteps) / max(q.kb_dw + q.kb_dw / 8, kEpiSteps), q.n_dw / q.nlight) : 0;
   return q;
 }
 
