@@ -461,7 +461,8 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
                           size_t workspace_bytes, void* stream);
 
 /* Enqueues the gradients on `stream`.  At least one of d_hidden and d_weight must be given (for
- * T = 0: d_weight alone has anything to write). */
+ * T = 0: d_weight alone has anything to write).  Host-checked alike; the rows of the gradients need no
+ * alignment beyond their elements'. */
 gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const gpo_vocab_grads* out,
                           void* workspace, size_t workspace_bytes, void* stream);
 

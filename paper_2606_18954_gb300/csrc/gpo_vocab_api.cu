@@ -248,6 +248,8 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
   gpo_status s = check_vocab(ctx, v);
   if (s != GPO_OK) return s;
   if (!out || (v->num_tokens > 0 && !out->logp)) return set_msg(ctx, "logp output is NULL"), GPO_ERR_INVALID_ARG;
+  if (!aligned(out->logp, 4) || !aligned(out->lse, 4) || !aligned(out->entropy, 4))
+    return set_msg(ctx, "outputs must be 4-byte aligned"), GPO_ERR_UNSUPPORTED;
   VocabLayout L;
   vocab_layout(*v, false, L);
   s = check_call(ctx, workspace, workspace_bytes, L.total);
@@ -297,6 +299,12 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
     return set_msg(ctx, "lse, grad_logp or (with grad_entropy) entropy NULL"), GPO_ERR_INVALID_ARG;
   if ((out->d_hidden && out->d_hidden_stride < v->d) || (out->d_weight && out->d_weight_stride < v->d))
     return set_msg(ctx, "row stride of a gradient < d"), GPO_ERR_INVALID_ARG;
+  if (!aligned(in->lse, 4) || !aligned(in->grad_logp, 4) || !aligned(in->entropy, 4) || !aligned(in->grad_entropy, 4) ||
+      !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
+    return set_msg(ctx, "inputs must be 4-byte, gradients 2-byte aligned"), GPO_ERR_UNSUPPORTED;
+  if ((out->d_hidden && (double)T * (double)out->d_hidden_stride >= (double)kMaxMatrix) ||
+      (out->d_weight && (double)v->vocab * (double)out->d_weight_stride >= (double)kMaxMatrix))
+    return set_msg(ctx, "gradient too large"), GPO_ERR_UNSUPPORTED;
   VocabLayout L;
   vocab_layout(*v, true, L);
   s = check_call(ctx, workspace, workspace_bytes, L.total);

@@ -559,6 +559,44 @@ def test_refusals(gp):
     torch.cuda.synchronize()
 
 
+def test_refusals_of_misaligned_and_huge_arrays(gp):
+    """At the C entry: pointers that are no multiple of their elements, gradient strides past any memory."""
+    import torch
+    import paper_2606_18954_gb300 as P
+    from paper_2606_18954_gb300 import binding as B
+    L = P.load()
+    T, V, d = 100, 300, 64
+    h = torch.zeros(T, d, device="cuda", dtype=torch.bfloat16)
+    w = torch.zeros(V, d, device="cuda", dtype=torch.bfloat16)
+    y = torch.zeros(T, device="cuda", dtype=torch.int32)
+    f = torch.zeros(T + 1, device="cuda")
+    v = B.CVocab(T, V, d, d, d, h.data_ptr(), w.data_ptr(), y.data_ptr(), 0, 4, 1.0)
+    room = torch.empty(max(B.vocab_workspace_size(v), B.vocab_workspace_size(v, True)), dtype=torch.uint8, device="cuda")
+
+    def forward(**k):
+        o = {"logp": f.data_ptr(), **k}
+        vo = B.VocabOutputs(*(o.get(n) for n in ("logp", "lse", "entropy")))
+        return L.gpo_vocab_logp(gp._h, ctypes.byref(v), ctypes.byref(vo), room.data_ptr(), room.numel(), None)
+
+    def gradient(ins=(), **k):
+        i = {"lse": f.data_ptr(), "grad_logp": f.data_ptr(), **dict(ins)}
+        gi = B.VocabGradInputs(*(i.get(n) for n in ("lse", "grad_logp", "entropy", "grad_entropy")))
+        g = {"d_hidden": h.data_ptr(), "d_weight": w.data_ptr(), "d_hidden_stride": d, "d_weight_stride": d, **k}
+        vg = B.VocabGrads(g["d_hidden"], g["d_weight"], g["d_hidden_stride"], g["d_weight_stride"], 0)
+        return L.gpo_vocab_grad(gp._h, ctypes.byref(v), ctypes.byref(gi), ctypes.byref(vg), room.data_ptr(), room.numel(), None)
+
+    for name in ("logp", "lse", "entropy"):
+        assert forward(**{name: f.data_ptr() + 2}) == UNSUPPORTED, name
+    for name in ("lse", "grad_logp", "entropy", "grad_entropy"):
+        both = {"entropy": f.data_ptr(), "grad_entropy": f.data_ptr(), name: f.data_ptr() + 2}
+        assert gradient(both) == UNSUPPORTED, name
+    for name in ("d_hidden", "d_weight"):
+        assert gradient(**{name: h.data_ptr() + 1}) == UNSUPPORTED, name
+        assert gradient(**{name + "_stride": 1 << 40}) == UNSUPPORTED, name
+        assert gradient(**{name + "_stride": d - 1}) == INVALID, name
+    torch.cuda.synchronize()
+
+
 def test_forced_timeout_then_a_normal_call(gp):
     """The bounded waits' failure path (GPO_FLAG_DEBUG_TIMEOUT): the status, then a correct call."""
     import torch
