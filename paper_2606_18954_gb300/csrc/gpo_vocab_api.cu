@@ -344,7 +344,8 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.dw = out->d_weight;
   a.dw_stride = out->d_weight_stride;
   a.accumulate = out->accumulate != 0;
-  a.dw_bulk = a.dw && !a.accumulate && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
+  // (a bulk store leaves out what lies past the matrix, but not to the element: of an odd width it wrote one more)
+  a.dw_bulk = a.dw && !a.accumulate && v->d % 8 == 0 && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
               encode_map(&m.dw, encode_fn(), a.dw, v->d, v->vocab, a.dw_stride, a.f16, 32);
   Stages stage(ctx, stream, at<void>(workspace, L.status));
   stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });

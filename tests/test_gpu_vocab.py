@@ -404,6 +404,26 @@ def test_outputs_of_any_stride_stay_inside(gp):
     assert torch.all(bh == 3.0) and torch.all(bw == 3.0)
 
 
+@pytest.mark.parametrize("d", [1, 5, 29, 37, 62, 63, 77, 100, 260, 333])
+def test_what_lies_beside_the_gradients_rows_stays(gp, d):
+    """Rows on 16-byte boundaries whose width is no multiple of 16 bytes: nothing past the width is written."""
+    import torch
+    from vocab_ref import close, head_exact, head_inputs
+    T, V, stride = 130, 300, (d + 7) // 8 * 8 + (8 if d % 8 == 0 else 0)
+    h, w, y = head_inputs(T, V, d, torch.bfloat16, seed=d, sure=6.0)
+    gl, _ = _grads(T, y, 5, False)
+    f = gp.vocab_logp(h, w, y)
+    bh = torch.full((T, stride), 7.0, device="cuda", dtype=torch.bfloat16)
+    bw = torch.full((V, stride), 7.0, device="cuda", dtype=torch.bfloat16)
+    out = {"d_hidden": bh[:, :d], "d_weight": bw[:, :d]}
+    gp.vocab_grad(h, w, y, f["lse"], gl, out=out)
+    gp.check()
+    ref = head_exact(h, w, y, 1.0, torch.nan_to_num(gl))
+    for k in out:
+        close(out[k], ref[k], ref["t_" + k], k)
+    assert torch.all(bh[:, d:] == 7.0) and torch.all(bw[:, d:] == 7.0)
+
+
 def test_no_tokens(gp):
     import torch
     w = torch.randn(300, 64, device="cuda").bfloat16()
