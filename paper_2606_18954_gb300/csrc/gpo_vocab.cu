@@ -1167,20 +1167,23 @@ __global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st
 
 constexpr int kJoinThreads = 256;
 
-// Parts of a row side by side: a CTA per row (few tokens).
+// Parts of a row side by side: a CTA per row (few tokens).  Where the tokens are listed, a row is one of the list: its
+// parts and its target's logit are at the row's number, its target and its results at the token's.
 template <bool kEnt>
 __global__ void __launch_bounds__(kJoinThreads) vocab_join_row_kernel(VocabArgs a, int parts, Status st) {
   __shared__ Part red[kJoinThreads / 32];
   const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   after_previous();
-  const int64_t id = load_id(a.target, a.id8, row);
   if (row == 0 && threadIdx.x == 0) sign_status(st);
+  if (a.idx && row >= a.head->rows) return;  // (vocab_rows_kernel has written the others' zeros)
+  const int64_t tok = a.idx ? a.idx[row] : row;
+  const int64_t id = load_id(a.target, a.id8, tok);
   if (id < 0 || id >= a.V) {
     if (threadIdx.x == 0) {
       if (id >= a.V) report(st, GPO_ERR_SHAPE, 26, row);
-      a.logp[row] = 0.f;
-      if (a.lse_out) a.lse_out[row] = 0.f;
-      if (kEnt) a.ent_out[row] = 0.f;
+      a.logp[tok] = 0.f;
+      if (a.lse_out) a.lse_out[tok] = 0.f;
+      if (kEnt) a.ent_out[tok] = 0.f;
     }
     return;
   }
@@ -1198,7 +1201,7 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_join_row_kernel(VocabArgs 
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kJoinThreads / 32; ++w) p = join<kEnt>(p, red[w]);
-    finish<kEnt>(a, row, a.tz[row], p);
+    finish<kEnt>(a, tok, a.tz[row], p);
   }
 }
 
