@@ -66,7 +66,7 @@ def train(steps=3, vocab=5000, d=256, groups=4, lr=0.5, entropy_weight=1e-3, tem
         loss = gp.token_loss(batch, plan, head["logp"], old, edge_adv=adv["edge_adv"])
         bonus = torch.full((T,), -entropy_weight / T, device="cuda")                        # of -weight * mean entropy
         grads = gp.vocab_grad(hidden, policy.table, target, head["lse"], loss["grad_logp"], scale=1.0 / temperature,
-                              entropy=head["entropy"], grad_entropy=bonus)
+                              entropy=head["entropy"], grad_entropy=bonus, logp=head["logp"])
         d_layer = policy.backward(gp, ids, x, t, grads["d_hidden"], grads["d_weight"])
         policy.table -= lr * grads["d_weight"]
         policy.layer -= lr * d_layer

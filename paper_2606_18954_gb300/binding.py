@@ -90,7 +90,7 @@ class VocabOutputs(ctypes.Structure):
 
 
 class VocabGradInputs(ctypes.Structure):
-    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "grad_logp", "entropy", "grad_entropy")]
+    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "grad_logp", "entropy", "grad_entropy", "logp")]
 
 
 class VocabGrads(ctypes.Structure):
@@ -124,7 +124,7 @@ _lock = threading.Lock()
 # building a ctypes structure costs 2 us a call, packing one 0.5.
 _PACK_VOCAB = struct.Struct("@5q3Q2id").pack
 _PACK_3 = struct.Struct("@3Q").pack
-_PACK_4 = struct.Struct("@4Q").pack
+_PACK_5 = struct.Struct("@5Q").pack
 _PACK_GRADS = struct.Struct("@2Q2qi4x").pack
 _PACK_EMBED = struct.Struct("@5qQ2id").pack
 
@@ -689,16 +689,18 @@ class GraphPO:
         return out
 
     def vocab_grad(self, hidden, weight, target, lse, grad_logp, scale=1.0, entropy=None, grad_entropy=None,
-                   accumulate=False, d_hidden=True, d_weight=True, out=None, workspace=None, stream=None) -> dict:
+                   accumulate=False, d_hidden=True, d_weight=True, out=None, workspace=None, stream=None,
+                   logp=None) -> dict:
         """Gradients {"d_hidden": [T, d], "d_weight": [V, d]} (each if asked for) of a loss with the
         gradients grad_logp (e.g. token_loss's) and optionally grad_entropy [T] float32 with respect to
         vocab_logp's outputs, whose lse (and entropy) are given; or fills `out`, with `accumulate`
-        adding to out["d_weight"].  Enqueued on the current stream."""
+        adding to out["d_weight"].  With vocab_logp's logp too, the gradient of a nearly certain token
+        keeps its digits (from 1 - p = 1e-4 down it has few without).  Enqueued on the current stream."""
         import torch
         if stream is not None:  # (what the call allocates belongs to the stream that uses it)
             with torch.cuda.stream(stream):
                 return self.vocab_grad(hidden, weight, target, lse, grad_logp, scale, entropy, grad_entropy, accumulate,
-                                       d_hidden, d_weight, out, workspace)
+                                       d_hidden, d_weight, out, workspace, None, logp)
         dev, T, V, d, hs, ws, code, idb, tp = self._head(hidden, weight, target)
         f32, dt = torch.float32, hidden.dtype
         if grad_entropy is not None and entropy is None:
@@ -711,9 +713,10 @@ class GraphPO:
                 out["d_hidden"] = torch.empty(T, d, dtype=dt, device=hidden.device)
             if d_weight:
                 out["d_weight"] = torch.empty(V, d, dtype=dt, device=hidden.device)
-        ins = _PACK_4(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
+        ins = _PACK_5(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
                       0 if grad_entropy is None else _vector(entropy, "entropy", dev, T, f32),
-                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32))
+                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32),
+                      0 if logp is None else _vector(logp, "logp", dev, T, f32))
         dh, dw = out.get("d_hidden"), out.get("d_weight")
         sh = 0 if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
         sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)

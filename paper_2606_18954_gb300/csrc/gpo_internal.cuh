@@ -1021,7 +1021,7 @@ struct VocabArgs {
   int64_t part_row, part_col;
   float *logp, *lse_out, *ent_out;
   // gradient
-  const float *lse, *g, *ent, *ge;
+  const float *lse, *g, *ent, *ge, *lp;  // (lp: logp, may be null)
   const void* weight;
   int64_t weight_stride;
   int* by_target;        // the rows' targets, ascending (the gradient's rows are in that order)

@@ -482,7 +482,15 @@ __device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, 
 // What a row's token brings to its dz.
 struct DzRow {
   float l2, g, e, ent;  // lse in units of log 2, d loss / d logp and d entropy (times the scale of an fp16 dz), entropy
+  float at;             // dz at the target from the row's logp; NaN without one: then as every other column's
 };
+// (1 - p of a nearly certain token as a difference would be the error of its logit and of lse, 1e-7 of them, not 1 - p.
+// logp, the forward pass's log1p of the sum over the other columns, still has its digits.)
+template <bool kEnt>
+__device__ __forceinline__ float dz_at_target(const DzRow& w, float lp) {
+  const float v = -w.g * expm1f(lp);
+  return kEnt ? fmaf(-w.e * expf(lp), lp + w.ent, v) : v;
+}
 // dz of 32 columns from their logits z, rounded to 16 bits and stored: those below `cols`, zeros past them (p of a
 // padding row or column is no probability, and its row may hold anything).  tgt: the target's place; its dz into vt.
 template <bool kEnt>
@@ -501,7 +509,10 @@ __device__ __forceinline__ void dz_columns(const VocabArgs& a, const DzRow& w, c
         const float p = ex2(d);
         float v = (j == tgt ? w.g : 0.f) - w.g * p;
         if (kEnt) v = fmaf(-w.e * p, fmaf(d, 0.6931471805599453f, w.ent), v);
-        if (j == tgt) vt = v;
+        if (j == tgt) {
+          if (w.at == w.at) v = w.at;
+          vt = v;
+        }
         y[h] = j < cols ? v : 0.f;
       }
       o[i / 2] = pack16(y[0], y[1], a.f16);
@@ -545,7 +556,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       // what the row's token brings
       int64_t tok = 0;
       int tgt = -1;
-      DzRow w = {0.f, 0.f, 0.f, 0.f};
+      DzRow w = {0.f, 0.f, 0.f, 0.f, __int_as_float(0x7fffffff)};
       if (live) {
         tok = a.idx ? __ldcg(a.idx + row) : row;
         const int64_t id = load_id(a.target, a.id8, tok);
@@ -558,6 +569,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
             w.e = a.ge[tok] * gs;
             w.ent = a.ent[tok];
           }
+          if (a.lp && tgt >= 0 && tgt < kPairN / 2) w.at = dz_at_target<has_ent(kMode)>(w, a.lp[tok]);
         }
       }
       if constexpr (kMode == kDz || kMode == kDzEnt) {

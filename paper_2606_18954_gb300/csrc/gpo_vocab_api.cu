@@ -300,7 +300,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   if ((out->d_hidden && out->d_hidden_stride < v->d) || (out->d_weight && out->d_weight_stride < v->d))
     return set_msg(ctx, "row stride of a gradient < d"), GPO_ERR_INVALID_ARG;
   if (!aligned(in->lse, 4) || !aligned(in->grad_logp, 4) || !aligned(in->entropy, 4) || !aligned(in->grad_entropy, 4) ||
-      !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
+      !aligned(in->logp, 4) || !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
     return set_msg(ctx, "inputs must be 4-byte, gradients 2-byte aligned"), GPO_ERR_UNSUPPORTED;
   if ((out->d_hidden && (double)T * (double)out->d_hidden_stride >= (double)kMaxMatrix) ||
       (out->d_weight && (double)v->vocab * (double)out->d_weight_stride >= (double)kMaxMatrix))
@@ -327,6 +327,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.g = in->grad_logp;
   a.ent = in->entropy;
   a.ge = in->grad_entropy;
+  a.lp = in->logp;
   a.sl2 = logit_scale(*v, 64 * kVocabDzSeg);
   a.weight = v->weight;
   a.weight_stride = v->weight_stride;
