@@ -471,6 +471,8 @@ class GraphPO:
         if code != GPO_OK:
             raise GraphPOError(code, "gpo_create")
         self._h = h
+        import torch
+        self._device = torch.cuda.current_device()  # (gpo_create's: the current one)
         self._ws = None
         self._sizes = {}  # workspace bytes by sizes (vocabulary ends)
         self._rooms = {}  # their workspaces by stream
@@ -626,12 +628,19 @@ class GraphPO:
 
     # ---- the model's vocabulary ends (gpo_vocab_logp / gpo_vocab_grad, gpo_embed / gpo_embed_grad)
 
+    def _here(self, dev: int) -> None:
+        """The kernels run on the context's device: arrays of another one are refused."""
+        if dev != self._device:
+            raise ValueError(f"the arrays are on device {dev}, the context on cuda:{self._device}")
+
     def _room(self, key, size, dev, workspace, handle):
         """Address and bytes of the workspace: the caller's, or the context's for this stream, which holds at
         least size() bytes (asked once for the sizes that `key` stands for).  (Calls on several
         streams may run at the same time.)"""
         if workspace is not None:
-            return workspace.data_ptr(), workspace.numel()
+            if workspace.get_device() != self._device or not workspace.is_contiguous():
+                raise ValueError(f"workspace must be contiguous, on cuda:{self._device}")
+            return workspace.data_ptr(), workspace.numel() * workspace.element_size()
         need = self._sizes.get(key)
         if need is None:
             if len(self._sizes) > 1024:
@@ -643,8 +652,7 @@ class GraphPO:
             ws = self._rooms[handle] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         return ws.data_ptr(), ws.numel()
 
-    @staticmethod
-    def _head(hidden, weight, target):
+    def _head(self, hidden, weight, target):
         """The checks that both directions share: device, sizes, strides, codes, the target's address."""
         if len(hidden.shape) != 2 or len(weight.shape) != 2:
             raise ValueError("hidden must be [T, d] and weight [V, d]")
@@ -652,6 +660,7 @@ class GraphPO:
         code = _dtype_code(hidden, "hidden")
         hs = _matrix(hidden, "hidden", dev, T, d, hidden.dtype)
         ws = _matrix(weight, "weight", dev, V, d, hidden.dtype)
+        self._here(dev)
         return dev, T, V, d, hs, ws, code, _id_bytes(target, "target"), _vector(target, "target", dev, T)
 
     def vocab_logp(self, hidden, weight, target, scale=1.0, lse=True, entropy=False, out=None, workspace=None,
@@ -745,6 +754,7 @@ class GraphPO:
         dev, (V, d), T, dt = table.get_device(), table.shape, ids.shape[0], table.dtype
         code, idb = _dtype_code(table, "table"), _id_bytes(ids, "ids")
         ts, ip = _matrix(table, "table", dev, V, d, dt), _vector(ids, "ids", dev, T)
+        self._here(dev)
         if out is None:
             out, rs = torch.empty(T, d, dtype=dt, device=table.device), d
         else:
@@ -772,6 +782,7 @@ class GraphPO:
         dev, (T, d), V, dt = grad.get_device(), grad.shape, int(vocab), grad.dtype
         code, idb = _dtype_code(grad, "grad"), _id_bytes(ids, "ids")
         rs, ip = _matrix(grad, "grad", dev, T, d, dt), _vector(ids, "ids", dev, T)
+        self._here(dev)
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs the gradient to add to in `out`")
