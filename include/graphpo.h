@@ -244,8 +244,11 @@ gpo_status gpo_compute_host(gpo_ctx* ctx, const gpo_batch* host, const gpo_batch
                             void* stream);
 
 /* Waits for `stream` and returns the first error the kernels of the last
- * gpo_compute (or of the gpo_compute_groups calls since the last clearing one), or of
- * the last other call that enqueues work, on this context reported (GPO_OK if none). */
+ * gpo_compute (or of the gpo_compute_groups calls since the last clearing one) or loss call
+ * on this context reported (GPO_OK if none).  Of the vocabulary ends' calls (gpo_vocab_*, gpo_embed*) it
+ * returns the first error of all since it last returned one, whatever has been enqueued
+ * after the failing call, which disturbs no other; an error of theirs is returned once.  (Of a captured call:
+ * the last replay's, as each replay clears its own.) */
 gpo_status gpo_sync_status(gpo_ctx* ctx, void* stream);
 
 /* Static description of a status code. */
@@ -411,7 +414,7 @@ gpo_status gpo_token_loss(gpo_ctx* ctx, const gpo_batch* batch, void* plan, cons
  * A target below 0 means no token (a prompt, tool output, padding): its outputs are 0, it has no
  * gradient, and its hidden row (NaN, say) reaches no other result.  Nor does the row of a token
  * whose incoming gradients are all 0: it counts as a token without a gradient.  A target >= vocab is
- * reported by gpo_sync_status (GPO_ERR_SHAPE); the outputs are then undefined.
+ * reported by gpo_sync_status (GPO_ERR_SHAPE); the call's outputs are then undefined.
  */
 typedef enum { GPO_DT_BF16 = 0, GPO_DT_F32 = 1, GPO_DT_F16 = 2 } gpo_dtype;
 

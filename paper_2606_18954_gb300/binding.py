@@ -815,6 +815,9 @@ class GraphPO:
         return {names[i].decode(): float(ms[i]) for i in range(n.value)}
 
     def check(self, stream=None) -> None:
+        """Waits for `stream` (the current one) and raises the first device-side error not raised yet of the
+        calls enqueued there: of the vocabulary ends every call since the last check, of the others the
+        last one."""
         import torch
         if stream is None:
             stream = torch.cuda.current_stream()

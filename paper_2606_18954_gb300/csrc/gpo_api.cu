@@ -235,7 +235,7 @@ gpo_status gpo_create(gpo_ctx** out, const gpo_params* params) {
   gpo_ctx* c = new (std::nothrow) gpo_ctx();
   if (!c) return GPO_ERR_CUDA;
   c->params = *params;
-  c->last_status = nullptr;
+  set_last_status(c, nullptr);
   c->msg[0] = 0;
   cudaDeviceProp prop;
   if (cudaGetDevice(&c->device) != cudaSuccess || cudaGetDeviceProperties(&prop, c->device) != cudaSuccess) {
@@ -261,8 +261,9 @@ gpo_status gpo_create(gpo_ctx** out, const gpo_params* params) {
       setup_fused_f32() != cudaSuccess ||
       setup_tree_prep() != cudaSuccess || setup_loss() != cudaSuccess || setup_vocab() != cudaSuccess ||
       setup_vocab_few() != cudaSuccess || setup_embed() != cudaSuccess ||
-      cudaMallocHost(&c->host_status, sizeof(uint32_t) * kStatusWords) != cudaSuccess) {
+      make_call_words(c) != cudaSuccess || cudaMallocHost(&c->host_status, sizeof(uint32_t) * kStatusWords) != cudaSuccess) {
     cudaGetLastError();
+    free_call_words(c);
     delete c;
     return GPO_ERR_CUDA;
   }
@@ -279,6 +280,7 @@ void gpo_destroy(gpo_ctx* ctx) {
     for (cudaEvent_t ev : ctx->pipe_ev) cudaEventDestroy(ev);
   }
   if (ctx->host_status) cudaFreeHost(ctx->host_status);
+  free_call_words(ctx);
   for (int i = 0; i <= kMaxStages; ++i)
     if (ctx->ev[i]) cudaEventDestroy(ctx->ev[i]);
   delete ctx;
@@ -489,7 +491,7 @@ gpo_status compute_impl(gpo_ctx* ctx, const gpo_batch* batch, const gpo_outputs*
     }
   }
   ctx->nstages = ns;
-  ctx->last_status = ws.status;
+  set_last_status(ctx, ws.status);
   if (e != cudaSuccess) return set_msg(ctx, "launch failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
   return GPO_OK;
 }
@@ -784,7 +786,7 @@ gpo_status gpo_loss_plan(gpo_ctx* ctx, const gpo_batch* batch, void* plan, size_
   cudaError_t e = cudaMemsetAsync(lp.status, 0, kLossPlanHead, lc.stream);
   if (e == cudaSuccess) e = launch_loss_plan(lc, *batch, loss_sizes(*batch), lp);
   ctx->nstages = 0;
-  ctx->last_status = lp.status;
+  set_last_status(ctx, lp.status);
   if (e != cudaSuccess) return set_msg(ctx, "launch failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
   return GPO_OK;
 }
@@ -850,7 +852,7 @@ gpo_status gpo_token_loss(gpo_ctx* ctx, const gpo_batch* batch, void* plan, cons
     e = cudaEventRecord(ctx->ev[++ns], lc.stream);
   }
   ctx->nstages = ns;
-  ctx->last_status = lp.status;
+  set_last_status(ctx, lp.status);
   if (e != cudaSuccess) return set_msg(ctx, "launch failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
   return GPO_OK;
 }
@@ -882,9 +884,11 @@ gpo_status gpo_sync_status(gpo_ctx* ctx, void* stream) {
   if (!ctx) return GPO_ERR_INVALID_ARG;
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return set_msg(ctx, "stream error: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
-  if (!ctx->last_status) return GPO_OK;
+  const gpo_status own = read_call_words(ctx, static_cast<cudaStream_t>(stream));
+  if (own != GPO_OK || !ctx->last_status) return own;
   e = cudaMemcpy(ctx->host_status, ctx->last_status, sizeof(uint32_t) * kStatusWords, cudaMemcpyDeviceToHost);
   if (e != cudaSuccess) return set_msg(ctx, "status read failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
+  ctx->last_read = true;
   auto word = [&](int i) { return (uint64_t)ctx->host_status[i + 1] << 32 | ctx->host_status[i]; };
   const uint32_t code = is_error(word(kStError), word(kStTag)) ? (uint32_t)(word(kStError) & 0xFFFFu) : 0u;
   if (code != 0)

@@ -115,7 +115,6 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
   const int lane = threadIdx.x & 31;
   const int64_t warp = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   const int64_t nwarps = (int64_t)gridDim.x * (blockDim.x >> 5);
-  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   const int64_t blocks = (a.D + 32 * C::kPer - 1) / (32 * C::kPer);
   const int64_t steps = (blocks + kLookBlocks - 1) / kLookBlocks;
   for (int64_t it = warp; it < a.T * steps; it += nwarps) {
@@ -189,7 +188,6 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(EmbedArgs a, int
   const int64_t pieces = ((int64_t)n + piece - 1) / piece;
   const int64_t empties = a.accumulate ? 0 : (a.V + 31) / 32;  // groups of 32 rows that may have no token
   T* out = static_cast<T*>(a.dst);
-  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   for (int64_t it = warp; it < (pieces + empties) * blocks; it += nwarps) {
     const int64_t unit = it / blocks, b = it - unit * blocks;
     float s[C::kPer];

@@ -852,7 +852,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
     if (keeps_logits(kMode)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(regs_many(kMode)));
     finish_tiles<kMode, kS>(maps, a, st, c, p);
   }
-  if (is_products(kMode) && a.last && a.splits == 1 && blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   end_pair(st, c);
 }
 
@@ -1169,9 +1168,8 @@ __device__ __forceinline__ void add_parts(const VocabArgs& a, int rows, int64_t 
   }
 }
 
-__global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a, Status st) {
+__global__ void __launch_bounds__(256) vocab_parts_kernel(VocabArgs a) {
   after_previous();
-  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   add_parts(a, a.head->rows, (int64_t)blockIdx.x * blockDim.x + threadIdx.x, (int64_t)gridDim.x * blockDim.x);
 }
 
@@ -1186,7 +1184,6 @@ __global__ void __launch_bounds__(kJoinThreads) vocab_join_row_kernel(VocabArgs 
   __shared__ Part red[kJoinThreads / 32];
   const int row = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   after_previous();
-  if (row == 0 && threadIdx.x == 0) sign_status(st);
   if (a.idx && row >= a.head->rows) return;  // (vocab_rows_kernel has written the others' zeros)
   const int64_t tok = a.idx ? a.idx[row] : row;
   const int64_t id = load_id(a.target, a.id8, tok);
@@ -1224,7 +1221,6 @@ __global__ void __launch_bounds__(1024) vocab_join_kernel(VocabArgs a, int parts
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   after_previous();
   const int row = blockIdx.x * 32 + lane, rows = a.idx ? a.head->rows : (int)a.T;
-  if (blockIdx.x == 0 && threadIdx.x == 0) sign_status(st);
   if (blockIdx.x * 32 >= rows) return;
   Part p = {kLow, 0.f, 0.f};
   if (row < rows) {
@@ -1359,7 +1355,7 @@ cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const
   const cudaError_t e = vec ? launch_pair<kProducts>(lc, m, a, st, tiles) : launch_pair<kProductsRows>(lc, m, a, st, tiles);
   if (e != cudaSuccess || !a.last || a.splits == 1) return e;
   const int64_t quads = a.T * ((a.D + 3) / 4);
-  return launch_after(vocab_parts_kernel, (unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a, st);
+  return launch_after(vocab_parts_kernel, (unsigned)min((quads + 255) / 256, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, a);
 }
 
 }  // namespace gpo

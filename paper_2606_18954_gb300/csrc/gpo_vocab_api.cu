@@ -1,5 +1,6 @@
 // Host side of the vocabulary ends (gpo_vocab_*, gpo_embed*): argument checks, workspace layout,
 // tensor maps and the launch sequences of gpo_vocab.cu and gpo_embed.cu.
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -17,7 +18,7 @@ constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 1024;  // tokens, vocabulary 
 constexpr int64_t kMaxMatrix = (int64_t)1 << 40;          // elements of a matrix
 
 struct VocabLayout {
-  size_t status, marks, head, idx, hc, by_target, tile_first, rest, pm, ps, pu, tz, dz, acc, total;
+  size_t marks, head, idx, hc, by_target, tile_first, rest, pm, ps, pu, tz, dz, acc, total;
   bool few;           // forward in one launch
   bool listed;        // only the tokens that take part are multiplied
   int64_t tp, hc_stride, piece, acc_stride;
@@ -40,8 +41,6 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L.hc_stride = up_to(v.d, 64);  // rows of whole 128-byte lines
   L.few = !grad && T <= kVocabFew;
   L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
-  L.status = take(sizeof(uint32_t) * kStatusWords);
-  // (next to the status words: cleared with them)
   if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);
   L.head = take(sizeof(VocabHead));
   if (T > 0 && L.listed) {
@@ -133,6 +132,14 @@ bool encode_blocks(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t 
              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Words of captured calls: the library's, as a graph may be replayed after its context is gone.  (A process that captures
+// more calls than there are gives words out again: two graphs then clear each other's.)
+__device__ __align__(256) uint32_t g_captured_words[kCapturedWords * kStatusWords];
+int captured_place() {
+  static std::atomic<uint32_t> next{0};
+  return (int)(next.fetch_add(1, std::memory_order_relaxed) % kCapturedWords);
+}
+
 // The launches of one call: an NVTX range around each and, with timing on, a CUDA event after it.
 struct Stages {
   gpo_ctx* ctx;
@@ -140,22 +147,30 @@ struct Stages {
   int n;
   cudaError_t e;
   Status st;
+  bool captured;
 
-  // Signs the status words with a tag of the call's own; in a graph, whose replays would share it,
-  // the words, and what else has to differ between calls (`bytes` in all), are cleared instead.
-  Stages(gpo_ctx* c, void* stream, void* status, size_t bytes = sizeof(uint32_t) * kStatusWords) : ctx(c), n(0), e(cudaSuccess) {
+  // The call's errors: in words and with a tag of its own; in a graph, whose replays share both, in words that no other
+  // call has and that are cleared first.
+  Stages(gpo_ctx* c, void* stream) : ctx(c), n(0), e(cudaSuccess) {
     lc.stream = static_cast<cudaStream_t>(stream);
     lc.num_sms = c->num_sms;
-    st.p = static_cast<uint32_t*>(status);
     if (ctx->timing) e = cudaEventRecord(ctx->ev[0], lc.stream);
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    if (cudaStreamIsCapturing(lc.stream, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone) {
+    captured = cudaStreamIsCapturing(lc.stream, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone;
+    if (captured) {
       cudaGetLastError();
+      const int i = captured_place();
+      ctx->captured.set(i);
+      st.p = ctx->captured_words + i * kStatusWords;
       st.tag = 0;
-      if (e == cudaSuccess) e = cudaMemsetAsync(st.p, 0, bytes, lc.stream);
+      clear(st.p, sizeof(uint32_t) * kStatusWords);
     } else {
-      st.tag = fresh_tag();
+      st.tag = ++ctx->calls;
+      st.p = ctx->call_words + ctx->calls % kCallWords * kStatusWords;
     }
+  }
+  void clear(void* p, size_t bytes) {
+    if (e == cudaSuccess) e = cudaMemsetAsync(p, 0, bytes, lc.stream);
   }
   template <class F>
   void operator()(const char* name, F launch) {
@@ -170,7 +185,7 @@ struct Stages {
   }
   gpo_status done() {
     ctx->nstages = n;
-    ctx->last_status = st.p;
+    if (ctx->last_read) ctx->last_status = nullptr;
     if (e != cudaSuccess) return set_msg(ctx, "launch failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
     return GPO_OK;
   }
@@ -229,6 +244,68 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
 
 }  // namespace
 
+namespace gpo {
+
+cudaError_t make_call_words(gpo_ctx* c) {
+  constexpr size_t bytes = sizeof(uint32_t) * kStatusWords * kCallWords;
+  c->calls = 0;
+  c->call_words = c->host_words = nullptr;
+  memset(c->returned, 0, sizeof c->returned);
+  cudaError_t e = cudaMalloc(&c->call_words, bytes);
+  if (e == cudaSuccess) e = cudaMallocHost(&c->host_words, bytes);
+  if (e == cudaSuccess) e = cudaMemset(c->call_words, 0, bytes);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+  void* p = nullptr;
+  if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, g_captured_words);
+  c->captured_words = static_cast<uint32_t*>(p);
+  return e;
+}
+
+void free_call_words(gpo_ctx* c) {
+  if (c->call_words) cudaFree(c->call_words);
+  if (c->host_words) cudaFreeHost(c->host_words);
+}
+
+gpo_status read_call_words(gpo_ctx* c, cudaStream_t stream) {
+  auto failed = [&](cudaError_t e) { return set_msg(c, "status read failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA; };
+  auto error = [&](const uint32_t* w) { return (uint64_t)w[kStError + 1] << 32 | w[kStError]; };
+  auto result = [&](const uint32_t* w) {
+    const gpo_status code = (gpo_status)(error(w) & 0xFFFFu);
+    set_msg(c, "%s (kernel %u, index %u)", gpo_status_string(code), w[kStWhere], w[kStDetail]);
+    return code;
+  };
+  if (c->calls > 0) {
+    cudaError_t e = cudaMemcpy(c->host_words, c->call_words, sizeof(uint32_t) * kStatusWords * kCallWords, cudaMemcpyDeviceToHost);
+    if (e != cudaSuccess) return failed(e);
+    uint64_t first = 0;
+    for (int i = 0; i < kCallWords; ++i) {
+      const uint64_t word = error(c->host_words + i * kStatusWords), call = word >> 16;
+      if ((word & 0xFFFFu) == 0 || call == c->returned[i]) continue;
+      c->returned[i] = call;
+      if (first == 0 || call < first) first = call;
+    }
+    if (first != 0) return result(c->host_words + first % kCallWords * kStatusWords);
+  }
+  for (int i0 = 0; c->captured.any() && i0 < kCapturedWords; i0 += kCallWords) {  // as many at a time as host_words holds
+    bool copied = false;
+    for (int i = i0; i < i0 + kCallWords; ++i) {
+      if (!c->captured[i]) continue;
+      cudaError_t e = copied ? cudaSuccess : cudaMemcpy(c->host_words, c->captured_words + i0 * kStatusWords,
+                                                        sizeof(uint32_t) * kStatusWords * kCallWords, cudaMemcpyDeviceToHost);
+      if (e != cudaSuccess) return failed(e);
+      copied = true;
+      const uint32_t* w = c->host_words + (i - i0) * kStatusWords;
+      if (!is_error(error(w), 0)) continue;
+      // (returned; a replay clears the words too)
+      e = cudaMemsetAsync(c->captured_words + i * kStatusWords, 0, sizeof(uint64_t), stream);
+      return e == cudaSuccess ? result(w) : failed(e);
+    }
+  }
+  return GPO_OK;
+}
+
+}  // namespace gpo
+
 extern "C" {
 
 gpo_status gpo_vocab_workspace_size(const gpo_vocab* v, int gradient, size_t* bytes) {
@@ -254,7 +331,7 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
   vocab_layout(*v, false, L);
   s = check_call(ctx, workspace, workspace_bytes, L.total);
   if (s != GPO_OK) return s;
-  if (v->num_tokens == 0) return ctx->nstages = 0, ctx->last_status = nullptr, GPO_OK;
+  if (v->num_tokens == 0) return ctx->nstages = 0, GPO_OK;
   VocabArgs a;
   VocabMaps m;
   s = vocab_args(ctx, *v, L, workspace, a, m);
@@ -272,13 +349,14 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
   a.sl2 = logit_scale(*v, 64 * (L.few ? kVocabFewSeg : kVocabSeg));
   const bool ent = out->entropy != nullptr;
   if (L.few) {
-    Stages stage(ctx, stream, at<void>(workspace, L.status), L.marks - L.status + sizeof(uint64_t) * kVocabFewCtas);
-    stage("vocab_few", [&] {
-      return launch_vocab_few(stage.lc, m, a, stage.st, ent, at<uint64_t>(workspace, L.marks), stage.st.tag + 1);
-    });
+    Stages stage(ctx, stream);
+    uint64_t* marks = at<uint64_t>(workspace, L.marks);
+    if (stage.captured) stage.clear(marks, sizeof(uint64_t) * kVocabFewCtas);
+    const uint64_t mark = stage.captured ? 1 : fresh_tag();
+    stage("vocab_few", [&] { return launch_vocab_few(stage.lc, m, a, stage.st, ent, marks, mark); });
     return stage.done();
   }
-  Stages stage(ctx, stream, at<void>(workspace, L.status));
+  Stages stage(ctx, stream);
   if (L.listed) stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st); });
   stage("vocab_lse", [&] { return launch_vocab_lse(stage.lc, m, a, stage.st, ent); });
   stage("vocab_join", [&] { return launch_vocab_join(stage.lc, a, stage.st, ent); });
@@ -311,7 +389,6 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   if (s != GPO_OK) return s;
   if (T == 0) {
     ctx->nstages = 0;
-    ctx->last_status = nullptr;
     if (out->d_weight && !out->accumulate) {
       const cudaError_t e = cudaMemset2DAsync(out->d_weight, 2 * (size_t)out->d_weight_stride, 0, 2 * (size_t)v->d,
                                               (size_t)v->vocab, static_cast<cudaStream_t>(stream));
@@ -348,7 +425,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   // (a bulk store leaves out what lies past the matrix, but not to the element: of an odd width it wrote one more)
   a.dw_bulk = a.dw && !a.accumulate && v->d % 8 == 0 && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
               encode_map(&m.dw, encode_fn(), a.dw, v->d, v->vocab, a.dw_stride, a.f16, 32);
-  Stages stage(ctx, stream, at<void>(workspace, L.status));
+  Stages stage(ctx, stream);
   stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });
   for (int64_t v0 = 0; v0 < v->vocab; v0 += L.piece) {
     a.v0 = v0;
@@ -366,7 +443,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
 namespace {
 
 struct EmbedLayout {
-  size_t status, perm, sid, start, part, total;
+  size_t perm, sid, start, part, total;
   int64_t part_stride;
 };
 
@@ -378,7 +455,7 @@ void embed_layout(const gpo_embedding& e, bool grad, EmbedLayout& L) {
     return at;
   };
   L = EmbedLayout();
-  L.status = take(sizeof(uint32_t) * kStatusWords);
+  if (!grad) take(1);  // (the lookup needs none; a workspace has at least one byte)
   if (grad) {
     L.part_stride = up_to(e.d, 4);
     L.perm = take(sizeof(int) * (size_t)e.num_tokens);
@@ -451,12 +528,12 @@ gpo_status gpo_embed(gpo_ctx* ctx, const gpo_embedding* e, const void* table, vo
   EmbedArgs a;
   const gpo_status s = embed_args(ctx, e, table, out, false, workspace, workspace_bytes, L, a);
   if (s != GPO_OK) return s;
-  if (a.T == 0) return ctx->nstages = 0, ctx->last_status = nullptr, GPO_OK;
+  if (a.T == 0) return ctx->nstages = 0, GPO_OK;
   a.src = table;
   a.src_stride = e->table_stride;
   a.dst = out;
   a.dst_stride = e->row_stride;
-  Stages stage(ctx, stream, at<void>(workspace, L.status));
+  Stages stage(ctx, stream);
   stage("embed", [&] { return launch_embed(stage.lc, a, stage.st); });
   return stage.done();
 }
@@ -479,7 +556,7 @@ gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad
   a.start = at<int>(workspace, L.start);
   a.part = at<float>(workspace, L.part);
   a.part_stride = L.part_stride;
-  Stages stage(ctx, stream, at<void>(workspace, L.status));
+  Stages stage(ctx, stream);
   stage("embed_grad", [&] { return launch_embed_grad(stage.lc, a, stage.st); });
   return stage.done();
 }

@@ -7,7 +7,7 @@
 // lane owns a vocabulary row and keeps the running maximum and sum of every token over its
 // rows in registers, with no exchange until the end.  Then the CTA joins its 128 lanes, and the CTA that
 // finds every other's mark joins the CTAs' parts: no second launch, no counter to reset.  (The marks are the
-// call's own tag: a mark left by another call is none.  Every CTA publishes its part, fences, and
+// call's own: a mark left by another call is none.  Every CTA publishes its part, fences, and
 // then looks: whichever comes last sees all marks.  Two that both see them write the same results.)
 // The accumulators are taken over into registers every 128 products (see gpo_vocab.cu).
 // Bound by HBM: one token, 131072 x 4096, 1.074 GB read in 178 us, 6.0 TB/s; below some 30 MB by the chain of launch,
@@ -93,7 +93,6 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     }
     mbar_init(&ctl->drain, 1);
     fence_mbar_init();
-    if (cta == 0) sign_status(st);
   }
   if (warp == 2) {
     tmem_alloc(&ctl->tmem_base, kTmem);
