@@ -481,6 +481,7 @@ class GraphPO:
         if getattr(self, "_h", None) and self._h.value:
             self._lib.gpo_destroy(self._h)
             self._h = ctypes.c_void_p()
+            self._rooms = {}  # (calls still running: the allocator gives their memory to later work of their streams)
 
     def __del__(self):
         try:
@@ -634,23 +635,28 @@ class GraphPO:
             raise ValueError(f"the arrays are on device {dev}, the context on cuda:{self._device}")
 
     def _room(self, key, size, dev, workspace, handle):
-        """Address and bytes of the workspace: the caller's, or the context's for this stream, which holds at
+        """The workspace, its address and bytes: the caller's, or the context's for this stream, which holds at
         least size() bytes (asked once for the sizes that `key` stands for).  (Calls on several
-        streams may run at the same time.)"""
+        streams may run at the same time.)  A call that is being captured gets one of its own, from the
+        graph's memory, which lives as long as the graph: the context's may be replaced by a larger one, or in use on
+        another stream, when the graph is replayed."""
         if workspace is not None:
             if workspace.get_device() != self._device or not workspace.is_contiguous():
                 raise ValueError(f"workspace must be contiguous, on cuda:{self._device}")
-            return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+            return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
         need = self._sizes.get(key)
         if need is None:
             if len(self._sizes) > 1024:
                 self._sizes.clear()
             need = self._sizes[key] = size()
-        ws = self._rooms.get(handle)
-        if ws is None or ws.numel() < need:
-            import torch
-            ws = self._rooms[handle] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
-        return ws.data_ptr(), ws.numel()
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            ws = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        else:
+            ws = self._rooms.get(handle)
+            if ws is None or ws.numel() < need:
+                ws = self._rooms[handle] = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        return ws, ws.data_ptr(), ws.numel()
 
     def _head(self, hidden, weight, target):
         """The checks that both directions share: device, sizes, strides, codes, the target's address."""
@@ -669,7 +675,9 @@ class GraphPO:
         softmax(scale * hidden weight^T), hidden [T, d] and weight [V, d] both bfloat16 or both
         float16: {"logp": [T] float32, "lse": the log-sum-exp (if lse; vocab_grad takes it),
         "entropy" (if entropy)}, or fills `out`.  The logits are never stored.  Enqueued on the
-        current stream; `check()` raises on a target outside the vocabulary."""
+        current stream; `check()` raises on a target outside the vocabulary.  workspace: a contiguous
+        tensor on the context's device, at least vocab_workspace_size bytes; if None the context's own for
+        the stream, which close() releases, or in a captured call one from the graph's memory."""
         import torch
         if stream is not None:  # (what the call allocates belongs to the stream that uses it)
             with torch.cuda.stream(stream):
@@ -688,7 +696,7 @@ class GraphPO:
         else:
             ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("logp", "lse", "entropy")]
         on = _stream_handle(dev)
-        wp, wn = self._room((0, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0)),
+        room, wp, wn = self._room((0, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0)),
                             hidden.device, workspace, on)
         code = _fast["gpo_vocab_logp"](
             self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale),
@@ -704,7 +712,8 @@ class GraphPO:
         gradients grad_logp (e.g. token_loss's) and optionally grad_entropy [T] float32 with respect to
         vocab_logp's outputs, whose lse (and entropy) are given; or fills `out`, with `accumulate`
         adding to out["d_weight"].  With vocab_logp's logp too, the gradient of a nearly certain token
-        keeps its digits (from 1 - p = 1e-4 down it has few without).  Enqueued on the current stream."""
+        keeps its digits (from 1 - p = 1e-4 down it has few without).  Enqueued on the current stream;
+        workspace and check() as for vocab_logp."""
         import torch
         if stream is not None:  # (what the call allocates belongs to the stream that uses it)
             with torch.cuda.stream(stream):
@@ -732,7 +741,7 @@ class GraphPO:
         if T == 0 and dw is None:
             return out
         on = _stream_handle(dev)
-        wp, wn = self._room((1, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), True),
+        room, wp, wn = self._room((1, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), True),
                             hidden.device, workspace, on)
         code = _fast["gpo_vocab_grad"](
             self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins,
@@ -744,7 +753,8 @@ class GraphPO:
 
     def embed(self, table, ids, scale=1.0, out=None, workspace=None, stream=None):
         """Rows of `table` ([V, d] bfloat16, float16 or float32) by token id (int32 or int64 [T]; below
-        0: a row of zeros), times `scale`: [T, d] of the table's type.  Enqueued on the current stream."""
+        0: a row of zeros), times `scale`: [T, d] of the table's type.  Enqueued on the current stream;
+        workspace and check() as for vocab_logp."""
         import torch
         if stream is not None:  # (what the call allocates belongs to the stream that uses it)
             with torch.cuda.stream(stream):
@@ -760,7 +770,7 @@ class GraphPO:
         else:
             rs = _matrix(out, "out", dev, T, d, dt)
         on = _stream_handle(dev)
-        wp, wn = self._room((2,), lambda: embed_workspace_size(CEmbedding(T, 1, 1, 1, 1, None, code, idb, 1.0)), table.device,
+        room, wp, wn = self._room((2,), lambda: embed_workspace_size(CEmbedding(T, 1, 1, 1, 1, None, code, idb, 1.0)), table.device,
                             workspace, on)
         code = _fast["gpo_embed"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), table.data_ptr(),
                                   out.data_ptr(), wp, wn, on)
@@ -772,7 +782,7 @@ class GraphPO:
         """Gradient [vocab, d] of embed's table from the gradient of its output (grad [T, d]): rows of
         one token added in token order in fp32, rows without tokens 0; or, with `accumulate`, added
         to `out` (a table tied to the vocabulary matrix: vocab_grad's d_weight).  Enqueued on the
-        current stream."""
+        current stream; workspace and check() as for vocab_logp."""
         import torch
         if stream is not None:  # (what the call allocates belongs to the stream that uses it)
             with torch.cuda.stream(stream):
@@ -790,7 +800,7 @@ class GraphPO:
         else:
             ts = _matrix(out, "out", dev, V, d, dt)
         on = _stream_handle(dev)
-        wp, wn = self._room((3, T, V, d), lambda: embed_workspace_size(CEmbedding(T, V, d, d, d, None, code, idb, 1.0), True),
+        room, wp, wn = self._room((3, T, V, d), lambda: embed_workspace_size(CEmbedding(T, V, d, d, d, None, code, idb, 1.0), True),
                             grad.device, workspace, on)
         code = _fast["gpo_embed_grad"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), grad.data_ptr(),
                                        out.data_ptr(), bool(accumulate), wp, wn, on)
