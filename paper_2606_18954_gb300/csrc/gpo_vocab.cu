@@ -688,7 +688,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
       if (lane == 0) bulk_read();  // (the last tile's rows have left)
       __syncwarp();
       if (!ready(p.sum)) return false;
-      const float f = t.kb > 0 ? a.scale / __ldcg(&a.head->dz_scale) : 0.f;
+      const float f = a.scale / __ldcg(&a.head->dz_scale);
 #pragma unroll 1
       for (int ch = 0; ch < kPairN / 2 / 32; ++ch) {
         uint32_t x[32];
@@ -700,7 +700,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
         const int cols = a.D - c0;
         float y[32];
 #pragma unroll
-        for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens: no product ran)
+        for (int j = 0; j < 32; ++j) y[j] = t.kb > 0 ? __uint_as_float(x[j]) : 0.f;  // (no tokens, or a short last piece's empty part of k: no product ran)
         if (rest != 0.f) add_row(wrow + c0, rest, cols, a.f16, y);
 #pragma unroll
         for (int j = 0; j < 32; ++j) y[j] *= f;
