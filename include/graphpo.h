@@ -488,7 +488,7 @@ typedef struct {
   const void* ids;      /* [T] int32 or int64 */
   int32_t dtype;        /* gpo_dtype of table and rows */
   int32_t id_bytes;     /* bytes of one id: 4 or 8 */
-  double scale;         /* finite */
+  double scale;         /* finite in fp32, in which it multiplies */
 } gpo_embedding;
 
 gpo_status gpo_embed_workspace_size(const gpo_embedding* e, int gradient, size_t* bytes);

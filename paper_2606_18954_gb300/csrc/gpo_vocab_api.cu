@@ -487,7 +487,7 @@ gpo_status embed_args(gpo_ctx* ctx, const gpo_embedding* e, const void* table, c
                       size_t bytes, EmbedLayout& L, EmbedArgs& a) {
   gpo_status s = check_embed_sizes(ctx, e);
   if (s != GPO_OK) return s;
-  if (!std::isfinite(e->scale)) return set_msg(ctx, "scale is not finite"), GPO_ERR_INVALID_ARG;
+  if (!std::isfinite((float)e->scale)) return set_msg(ctx, "scale is not a finite fp32 number"), GPO_ERR_INVALID_ARG;
   if (!table || (e->num_tokens > 0 && (!rows || !e->ids))) return set_msg(ctx, "table, rows or ids NULL"), GPO_ERR_INVALID_ARG;
   const uintptr_t esz = e->dtype == GPO_DT_F32 ? 4 : 2;
   if (!aligned(table, esz) || !aligned(rows, esz) || !aligned(e->ids, (size_t)e->id_bytes))
