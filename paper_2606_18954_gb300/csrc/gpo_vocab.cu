@@ -569,7 +569,8 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
             w.e = a.ge[tok] * gs;
             w.ent = a.ent[tok];
           }
-          if (a.lp && tgt >= 0 && tgt < kPairN / 2) w.at = dz_at_target<has_ent(kMode)>(w, a.lp[tok]);
+          // (kDzWideEnt takes it once its logits are summed: here, four of its registers would be spilled)
+          if (kMode != kDzWideEnt && a.lp && tgt >= 0 && tgt < kPairN / 2) w.at = dz_at_target<has_ent(kMode)>(w, a.lp[tok]);
         }
       }
       if constexpr (kMode == kDz || kMode == kDzEnt) {
@@ -662,6 +663,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
           uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
           const int cols = live ? (int)a.vn - n0 : 0;
           float vt = 0.f;
+          if (kMode == kDzWideEnt && a.lp && live && tgt >= 0 && tgt < kPairN / 2) w.at = dz_at_target<true>(w, a.lp[tok]);
 #pragma unroll
           for (int ch = 0; ch < kPairN / 2; ch += 32) dz_columns<has_ent(kMode)>(a, w, z + ch, cols - ch, tgt - ch, vt, dst + ch);
           // what the rounding takes from dz at the target, by far the row's largest part: the products' epilogues add it
