@@ -247,8 +247,8 @@ gpo_status gpo_compute_host(gpo_ctx* ctx, const gpo_batch* host, const gpo_batch
  * gpo_compute (or of the gpo_compute_groups calls since the last clearing one) or loss call
  * on this context reported (GPO_OK if none).  Of the vocabulary ends' calls (gpo_vocab_*, gpo_embed*) it
  * returns the first error of all since it last returned one, whatever has been enqueued
- * after the failing call, which disturbs no other; an error of theirs is returned once.  (Of a captured call:
- * the last replay's, as each replay clears its own.) */
+ * after the failing call, which disturbs no other; an error of theirs is returned once.  Replays of captured calls
+ * are calls like others there. */
 gpo_status gpo_sync_status(gpo_ctx* ctx, void* stream);
 
 /* Static description of a status code. */

@@ -140,6 +140,7 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs a, Status st) {
       C::store(dst, b0 + b, lane, a.D, s, a.scale, false, false);
     }
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
 }
 
 // ------------------------------------------------------------------ sort
@@ -167,6 +168,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) embed_sort_kernel(EmbedArgs a
         a.perm[place] = (int)t;
         a.sid[place] = (int)id;
       });
+  if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
 }
 
 // ------------------------------------------------------------------ sums of runs

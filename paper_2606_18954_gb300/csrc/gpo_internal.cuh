@@ -135,6 +135,14 @@ __device__ __forceinline__ void sign_status(const Status& st) {
   if (st.tag != 0 && st.tag != kStoredTag) *reinterpret_cast<volatile uint64_t*>(st.p + kStTag) = st.tag;
 }
 
+// A captured call of the vocabulary ends has words that no other call has, and takes the tag in them: by one thread of
+// its first kernel every replay gets the next one, so that the errors of the replays before, which stay for the
+// host to see, are not its own.  (An idle thread's, or at the kernel's end where it has no waits: the load took 0.8 us of
+// 16 tokens of 8000 x 512 by the thread that starts the others.)
+__device__ __forceinline__ void next_tag(const Status& st) {
+  if (st.tag == kStoredTag) ++*reinterpret_cast<volatile uint64_t*>(st.p + kStTag);
+}
+
 __device__ __forceinline__ bool aborted(const Status& st) {
   return is_error(*reinterpret_cast<volatile const uint64_t*>(st.p + kStError), status_tag(st));
 }

@@ -52,7 +52,7 @@ constexpr int kTile16 = 64;                        // elements of one 128-byte s
 constexpr int kVStages = 6;                        // of the logits
 constexpr int kPStages = 5;                        // of the products (with 4, 4000 x 30000 x 1000 take 6 % longer)
 constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 rests, 4..11 epilogue
-constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2;
+constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2, kIdleWarp = 3;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
 // give back.  The shares add up to no more than the launch brings (setup_mode checks that).
 // The split of each mode is one without spills: the loads' and the MMAs' lane would find theirs in an L1
@@ -835,6 +835,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kVThreads, 1)
   let_next_start();
   Cta c = begin_pair<kS>(smem_raw);
   after_previous();
+  // (as the call's first kernel; in the idle warp's own branch below, kLse and kLseEnt spill 100 bytes)
+  if (is_lse(kMode) && !a.idx && blockIdx.x == 0 && threadIdx.x == 32 * kIdleWarp) next_tag(st);
+  __syncwarp();
   c.rows = a.idx ? a.head->rows : (int)a.T;
   Pipe p;
   if (warp < 4) {
@@ -939,6 +942,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_rows_kernel(VocabArgs a, St
     base += n;
     __syncthreads();
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
 }
 
 // A power of two that brings an fp16 dz, |dz| <= bound, into the type's range; 1 for bf16.  (|dz| is at most
@@ -1070,6 +1074,7 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
   }
   if (blockIdx.x == gridDim.x - 1)
     for (int64_t r = all + warp; r < rows_behind(a, all); r += kW) gather_row(a, r, -1, lane);
+  if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
 }
 
 // The same for more than kVocabOrder tokens, whose comparisons would grow with T^2: the sort's work grows with T.
@@ -1127,6 +1132,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) vocab_sort_kernel(VocabArgs a
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     for (int w = 0; w < kSortWarps; ++w) bound = fmaxf(bound, s_big[w]);
     a.head->dz_scale = scale_of_dz(a, bound);
+    next_tag(st);
   }
 }
 

@@ -189,6 +189,9 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_wait(&ctl->drain, 0, st, 45, 200000000ull, false);
     }
     __syncwarp();
+  } else if (warp == 3) {
+    if (lane == 0 && cta == 0) next_tag(st);
+    __syncwarp();
   } else if (warp >= 4) {
     // ------------------------------------------------------------ epilogue
     const int q = warp & 3, half = (warp - 4) >> 2, te = threadIdx.x - 128;

@@ -166,3 +166,48 @@ def test_captured_calls(P, T):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out["logp"], want)
+
+
+@pytest.mark.parametrize("T", [9, 40, 4500])
+def test_replays_keep_their_errors_until_check(P, T):
+    """A replay's error is raised though others with valid inputs follow it, which it does not disturb; every kernel that
+    comes first in a call is captured once."""
+    import torch
+    gp = P.GraphPO()
+    c = Calls(gp, T)
+    want = {n: c.run(n).clone() for n in NAMES}
+    gp.check()
+    for name in NAMES:
+        bad, c.bad = c.bad, c.y.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = c.run(name, bad=True)  # (reads c.bad, which the replays change)
+        for _ in range(3):
+            c.bad.copy_(bad)
+            graph.replay()
+            c.bad.copy_(c.y)
+            for _ in range(2):
+                got.zero_()
+                graph.replay()
+                assert torch.equal(got, want[name]), name
+            raised(P, gp, SHAPE)
+        graph.replay()
+        gp.check()
+        c.bad = bad
+
+
+def test_a_replay_after_one_that_gave_up(P):
+    import torch
+    forced = P.GraphPO(flags=P.binding.FLAG_DEBUG_TIMEOUT)
+    for T in (9, 40):
+        c = Calls(P.GraphPO(), T)
+        graph = torch.cuda.CUDAGraph()
+        c.gp = forced
+        with torch.cuda.graph(graph):
+            c.run("logp")
+        for _ in range(2):
+            graph.replay()
+            graph.replay()  # (with the first one's status still there)
+            raised(P, forced, TIMEOUT)
+        c.run("embed")
+        forced.check()
