@@ -1,8 +1,9 @@
 // Token embedding and the gradient of its table (formulas in include/graphpo.h).
 //
 //   embed      embed_kernel: a warp per token and 4 KB of its row, 16-byte accesses, eight in flight per
-//              lane.  Bound by HBM: 32768 tokens of 4096 values (16 bits) out of 131072 rows 73 us, 126 MB read and
-//              210 written to HBM, 4.6 TB/s
+//              lane.  32768 tokens of 4096 values (16 bits) out of 131072 rows 73 us, 126 MB read and
+//              210 written to HBM, 4.6 TB/s: DRAM is busy 58 % of the time, so it is not what bounds it (the reads of
+//              scattered rows and their writes in one warp, most likely: the sums below reach 6.2)
 //   gradient   embed_sort_kernel: the tokens in the order of their ids (gpo_sort.cuh): 17 us for 32768
 //              embed_sum_kernel: the sorted tokens in pieces of equal length, a warp per piece and
 //              512 bytes of the rows: runs of one id are summed in order in fp32, a run inside the

@@ -51,7 +51,7 @@ __host__ __device__ constexpr bool keeps_logits(int mode) { return is_lse(mode) 
 constexpr int kTile16 = 64;                        // elements of one 128-byte swizzle row
 constexpr int kVStages = 6;                        // of the logits
 constexpr int kPStages = 5;                        // of the products (with 4, 4000 x 30000 x 1000 take 6 % longer)
-constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 rests, 4..11 epilogue
+constexpr int kVThreads = 384;                     // warps: 0 loads, 1 MMAs, 2 rests, 3 idle, 4..11 epilogue
 constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2, kIdleWarp = 3;
 // The epilogue of the logits keeps 128 of them per thread: its warps take registers that the other four
 // give back.  The shares add up to no more than the launch brings (setup_mode checks that).
@@ -309,9 +309,12 @@ __device__ __forceinline__ void tokens_of(const VocabArgs& a, const Tile& t, int
   rb = __ldcg(first + 1);
 }
 
-// Of a token's dz the target's entry is by far the largest part.  Its rounding to 16 bits would add 40 % to
-// the error that the gradients' own rounding leaves (the other entries' adds 1 %), so what that rounding takes away
-// (a.rest) is added to both products: to d_hidden in the epilogue, a row of the vocabulary matrix per
+// Of a token's dz the target's entry is the largest part, unless the policy is sure of another token.  Its rounding to 16
+// bits would add 40 % to the error that the gradients' own rounding leaves, so what that rounding takes away
+// (a.rest) is added to both products.  The other entries' rounding stays: it adds 1 % to the whole error (1.0016 and 1.0004
+// of one rounding, 2048 tokens of 65536 x 2048), but 41 % in rows of d_weight that are no token's target, and up to 26 %
+// to both gradients where every token is sure of another.  A second product of those rests would double the products' time.
+// The rest goes to d_hidden in the epilogue, a row of the vocabulary matrix per
 // token (add_row); to d_weight as steps of its own after those of dz: the tokens whose targets are rows of the tile are
 // one run of the list, which is in the order of the targets, and 64 of them at a time are a step whose A is zeros but
 // for each token's rest in its target's row.  The rests are rounded to 16 bits there, 2^-17 (bf16) of the
