@@ -9,7 +9,7 @@ def test_a_captured_call_leaves_the_contexts_workspaces_alone(monkeypatch):
     gp = object.__new__(binding.GraphPO)
     gp._device, gp._sizes, gp._rooms = 0, {}, {}
     capturing = False
-    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing)
+    monkeypatch.setattr(binding, "_capturing", lambda: capturing)
     room = lambda n: gp._room(n, lambda: n, "cpu", None, 7)[0]  # noqa: E731
     own = room(1000)
     assert room(500) is own and gp._rooms == {7: own}

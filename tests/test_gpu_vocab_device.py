@@ -18,11 +18,14 @@ def test_a_workspace_of_the_host_is_refused():
 
 
 def test_another_device_is_refused():
+    import torch
     gp = _cpu_context()
-    gp._here(0)
-    for dev in (-1, 1):
+    gp._device = 3  # (tensors of the host are on device -1)
+    h, w, y = torch.zeros(4, 64).bfloat16(), torch.zeros(9, 64).bfloat16(), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: gp.vocab_logp(h, w, y), lambda: gp.vocab_grad(h, w, y, y.float(), y.float()), lambda: gp.embed(w, y),
+                 lambda: gp.embed_grad(h, y, 9), lambda: gp._elsewhere(-1)):
         with pytest.raises(ValueError):
-            gp._here(dev)
+            call()
 
 
 def _calls(gp):
