@@ -447,10 +447,6 @@ typedef struct {
   const float* grad_logp;    /* [T] d loss / d logp (gpo_loss_outputs.grad_logp) */
   const float* entropy;      /* [T] of the forward pass; read only with grad_entropy */
   const float* grad_entropy; /* [T] optional: d loss / d entropy */
-  const float* logp;         /* [T] optional, of the forward pass: with it dz at the target is
-                                -grad_logp expm1(logp) - grad_entropy exp(logp) (logp + entropy), which keeps
-                                its digits for a nearly certain token.  Without it 1 - p is a difference of
-                                fp32 numbers, off by about 1e-7 |z|: of a token with 1 - p = 1e-5 a tenth */
 } gpo_vocab_grad_inputs;
 
 typedef struct {
@@ -476,6 +472,13 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
  * alignment beyond their elements'. */
 gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const gpo_vocab_grads* out,
                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same with the forward pass's logp ([T], 4-byte aligned; NULL: gpo_vocab_grad): dz at the target is
+ * -grad_logp expm1(logp) - grad_entropy exp(logp) (logp + entropy), which keeps its digits for a nearly
+ * certain token.  Without it 1 - p is a difference of fp32 numbers, off by about 1e-7 |z|: of a token with
+ * 1 - p = 1e-5 a tenth. */
+gpo_status gpo_vocab_grad_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const float* logp,
+                               const gpo_vocab_grads* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Token embedding: out_t = scale table[id_t], rounded once to the table's type; a row of zeros for
  * an id below 0 (no token); an id >= vocab is reported as for targets.

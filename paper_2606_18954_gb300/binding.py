@@ -90,7 +90,7 @@ class VocabOutputs(ctypes.Structure):
 
 
 class VocabGradInputs(ctypes.Structure):
-    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "grad_logp", "entropy", "grad_entropy", "logp")]
+    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "grad_logp", "entropy", "grad_entropy")]
 
 
 class VocabGrads(ctypes.Structure):
@@ -111,7 +111,7 @@ LOSS_NSTATS = 4
 EXPORTS = ["gpo_create", "gpo_workspace_size", "gpo_compute", "gpo_sync_status", "gpo_status_string",
            "gpo_last_error", "gpo_version", "gpo_destroy", "gpo_enable_timing", "gpo_stage_times", "gpo_compute_noalloc",
            "gpo_compute_groups", "gpo_compute_host", "gpo_loss_plan_size", "gpo_loss_plan", "gpo_token_loss",
-           "gpo_layer_budget", "gpo_vocab_workspace_size", "gpo_vocab_logp", "gpo_vocab_grad",
+           "gpo_layer_budget", "gpo_vocab_workspace_size", "gpo_vocab_logp", "gpo_vocab_grad", "gpo_vocab_grad_logp",
            "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad"]
 
 FUSED_MAX_STATES = 384  # largest group the group-resident path (and gpo_compute_groups) serves
@@ -124,7 +124,7 @@ _lock = threading.Lock()
 # building a ctypes structure costs 2 us a call, packing one 0.5.
 _PACK_VOCAB = struct.Struct("@5q3Q2id").pack
 _PACK_3 = struct.Struct("@3Q").pack
-_PACK_5 = struct.Struct("@5Q").pack
+_PACK_4 = struct.Struct("@4Q").pack
 _PACK_GRADS = struct.Struct("@2Q2qi4x").pack
 _PACK_EMBED = struct.Struct("@5qQ2id").pack
 
@@ -201,6 +201,9 @@ def load(build_if_missing: bool = False):
         L.gpo_vocab_grad.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(VocabGradInputs),
                                      ctypes.POINTER(VocabGrads), vp, sz, vp]
         L.gpo_vocab_grad.restype = ctypes.c_int
+        L.gpo_vocab_grad_logp.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(VocabGradInputs), vp,
+                                          ctypes.POINTER(VocabGrads), vp, sz, vp]
+        L.gpo_vocab_grad_logp.restype = ctypes.c_int
         L.gpo_embed_workspace_size.argtypes = [ctypes.POINTER(CEmbedding), ctypes.c_int, ctypes.POINTER(sz)]
         L.gpo_embed_workspace_size.restype = ctypes.c_int
         L.gpo_embed.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, vp, sz, vp]
@@ -208,7 +211,7 @@ def load(build_if_missing: bool = False):
         L.gpo_embed_grad.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, ctypes.c_int, vp, sz, vp]
         L.gpo_embed_grad.restype = ctypes.c_int
         raw = ctypes.c_char_p
-        for name, args in (("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad", [vp, raw, raw, raw, vp, sz, vp]),
+        for name, args in (("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad_logp", [vp, raw, raw, vp, raw, vp, sz, vp]),
                            ("gpo_embed", [vp, raw, vp, vp, vp, sz, vp]), ("gpo_embed_grad", [vp, raw, vp, vp, ctypes.c_int, vp, sz, vp])):
             f = L[name]  # (a function object of its own)
             f.argtypes, f.restype = args, ctypes.c_int
@@ -740,10 +743,10 @@ class GraphPO:
                 out["d_hidden"] = torch.empty(T, d, dtype=dt, device=hidden.device)
             if d_weight:
                 out["d_weight"] = torch.empty(V, d, dtype=dt, device=hidden.device)
-        ins = _PACK_5(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
+        ins = _PACK_4(_vector(lse, "lse", dev, T, f32), _vector(grad_logp, "grad_logp", dev, T, f32),
                       0 if grad_entropy is None else _vector(entropy, "entropy", dev, T, f32),
-                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32),
-                      0 if logp is None else _vector(logp, "logp", dev, T, f32))
+                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, T, f32))
+        lp = 0 if logp is None else _vector(logp, "logp", dev, T, f32)
         dh, dw = out.get("d_hidden"), out.get("d_weight")
         sh = 0 if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
         sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
@@ -752,8 +755,8 @@ class GraphPO:
         on = _stream_handle(dev)
         room, wp, wn = self._room((1, T, V, d), lambda: vocab_workspace_size(CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), True),
                             hidden.device, workspace, on)
-        code = _fast["gpo_vocab_grad"](
-            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins,
+        code = _fast["gpo_vocab_grad_logp"](
+            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins, lp,
             _PACK_GRADS(0 if dh is None else dh.data_ptr(), 0 if dw is None else dw.data_ptr(), sh, sw, bool(accumulate)),
             wp, wn, on)
         if code != GPO_OK:

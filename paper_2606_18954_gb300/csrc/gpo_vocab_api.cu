@@ -364,6 +364,11 @@ gpo_status gpo_vocab_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_outp
 
 gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const gpo_vocab_grads* out,
                           void* workspace, size_t workspace_bytes, void* stream) {
+  return gpo_vocab_grad_logp(ctx, v, in, nullptr, out, workspace, workspace_bytes, stream);
+}
+
+gpo_status gpo_vocab_grad_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad_inputs* in, const float* logp,
+                               const gpo_vocab_grads* out, void* workspace, size_t workspace_bytes, void* stream) {
   if (!ctx) return GPO_ERR_INVALID_ARG;
   ctx->msg[0] = 0;
   gpo_status s = check_vocab(ctx, v);
@@ -377,7 +382,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   if ((out->d_hidden && out->d_hidden_stride < v->d) || (out->d_weight && out->d_weight_stride < v->d))
     return set_msg(ctx, "row stride of a gradient < d"), GPO_ERR_INVALID_ARG;
   if (!aligned(in->lse, 4) || !aligned(in->grad_logp, 4) || !aligned(in->entropy, 4) || !aligned(in->grad_entropy, 4) ||
-      !aligned(in->logp, 4) || !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
+      !aligned(logp, 4) || !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
     return set_msg(ctx, "inputs must be 4-byte, gradients 2-byte aligned"), GPO_ERR_UNSUPPORTED;
   if ((out->d_hidden && (double)T * (double)out->d_hidden_stride >= (double)kMaxMatrix) ||
       (out->d_weight && (double)v->vocab * (double)out->d_weight_stride >= (double)kMaxMatrix))
@@ -403,7 +408,7 @@ gpo_status gpo_vocab_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab_grad
   a.g = in->grad_logp;
   a.ent = in->entropy;
   a.ge = in->grad_entropy;
-  a.lp = in->logp;
+  a.lp = logp;
   a.sl2 = logit_scale(*v, 64 * kVocabDzSeg);
   a.weight = v->weight;
   a.weight_stride = v->weight_stride;

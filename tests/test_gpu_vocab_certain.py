@@ -93,3 +93,36 @@ def test_without_logp_as_before_and_refusals(gp):
         gp.vocab_grad(h, w, y, f["lse"], g, logp=f["logp"][1:])
     with pytest.raises(ValueError):
         gp.vocab_grad(h, w, y, f["lse"], g, logp=f["logp"].cpu())
+
+
+def test_at_the_c_entries(gp):
+    """gpo_vocab_grad is gpo_vocab_grad_logp without logp; a logp off its 4 bytes is refused."""
+    import ctypes
+
+    import torch
+    import paper_2606_18954_gb300 as P
+    from paper_2606_18954_gb300 import binding as B
+    from vocab_ref import head_inputs
+    L = P.load()
+    T, V, d = 100, 300, 64
+    h, w, y = head_inputs(T, V, d, torch.bfloat16, seed=6)
+    g = torch.randn(T + 1, device="cuda")[:T]
+    f = gp.vocab_logp(h, w, y)
+    want = {lp is None: gp.vocab_grad(h, w, y, f["lse"], g, logp=lp) for lp in (None, f["logp"])}
+    gp.check()
+    v = B.CVocab(T, V, d, d, d, h.data_ptr(), w.data_ptr(), y.data_ptr(), 0, 4, 1.0)
+    gi = B.VocabGradInputs(f["lse"].data_ptr(), g.data_ptr(), None, None)
+    dh, dw = torch.empty_like(h), torch.empty_like(w)
+    vg = B.VocabGrads(dh.data_ptr(), dw.data_ptr(), d, d, 0)
+    room = torch.empty(B.vocab_workspace_size(v, True), dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    tail = (ctypes.byref(vg), room.data_ptr(), room.numel(), stream)
+    for lp in (None, 0, f["logp"].data_ptr()):
+        if lp is None:
+            assert L.gpo_vocab_grad(gp._h, ctypes.byref(v), ctypes.byref(gi), *tail) == 0
+        else:
+            assert L.gpo_vocab_grad_logp(gp._h, ctypes.byref(v), ctypes.byref(gi), lp, *tail) == 0
+        gp.check()
+        assert torch.equal(dh, want[not lp]["d_hidden"]) and torch.equal(dw, want[not lp]["d_weight"])
+    assert L.gpo_vocab_grad_logp(gp._h, ctypes.byref(v), ctypes.byref(gi), f["logp"].data_ptr() + 2, *tail) == 5
+    assert L.gpo_vocab_grad_logp(None, ctypes.byref(v), ctypes.byref(gi), None, *tail) == 1
