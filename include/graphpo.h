@@ -504,6 +504,88 @@ gpo_status gpo_embed(gpo_ctx* ctx, const gpo_embedding* e, const void* table, vo
 gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad, void* d_table, int accumulate,
                           void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Logits as a sampler takes them (GraphPO samples its rollouts from the policy; the paper has no counterpart of these
+ * calls): penalties for the tokens that a row has had, biases, a mask, a scale; the statistics of the distribution that is
+ * sampled from, of which gpo_loss_inputs.old_logp and logp are the log-probabilities; and the gradient back to the raw
+ * logits.  For row r with raw logits x, n_v occurrences of token v among the generated part of its history:
+ *
+ *   u_v = x_v / repetition (x_v > 0) or x_v repetition (otherwise) for the tokens of the whole history, x_v for others
+ *   y_v = scale (u_v - frequency n_v - presence 1[n_v > 0] + bias_v), -inf where the row's mask has a 0
+ *   lse = log sum_v exp y_v      logp = y_target - lse      entropy = lse - sum_v p_v y_v      p_v = exp(y_v - lse)
+ *   d x_v = scale du_v/dx_v (grad_logp (1[v = target] - p_v) - grad_entropy p_v (y_v - lse + entropy)), 0 where the mask has a 0
+ *
+ * Everything is fp32 (entries and gradients are rounded once, to their type).  The target is kept out of the sum over the other
+ * tokens, so that a nearly certain token's logp has its digits, and its gradient too.  Results are the same on every run.
+ *
+ * History: row r's is the tokens [spans[3r], spans[3r+2]) of `history`, of which those from spans[3r+1] on are generated
+ * ones; rows may share tokens (the positions of a rollout, the continuations of a prefix).  An id below 0 is no token.
+ * Biases: row r's are the entries [bias_spans[2r], bias_spans[2r+1]) of bias_ids and bias, the ids of a row
+ * strictly ascending.  Mask: bit v % 32 of word v / 32 of row mask_row[r] (below 0: every token is allowed).  Masked logits
+ * may hold anything, NaN too.  An adjusted logit of -7e27 or less counts as left out (a mask of the lowest value of
+ * bf16 or fp32; -inf); a row that nothing is left of has lse -inf, logp -inf, entropy 0 and no gradient.  A NaN or +inf that is left in a
+ * row makes its statistics and its gradient NaN.
+ *
+ * A target below 0 means no token: logp, lse and entropy are 0, there is no gradient, and the row is not read (its
+ * adjusted logits, if asked for, are written all the same, and then its lse and entropy are theirs).
+ * Found on the GPU and returned by gpo_sync_status: ids past the vocabulary, spans outside the list that they are of or
+ * in disorder, more than 2^30 - 1 tokens in one history, biases not strictly ascending, a mask row that is not there
+ * (GPO_ERR_SHAPE), a scale outside [1e-4, 1e4], a repetition that is not a positive number, a penalty that is not finite
+ * (GPO_ERR_INVALID_ARG); the call's outputs are then undefined. */
+typedef struct {
+  int64_t num_rows;      /* R >= 0 */
+  int64_t vocab;         /* V >= 1 */
+  int64_t logits_stride; /* elements between rows, >= vocab */
+  const void* logits;    /* [R x logits_stride] raw logits, aligned to their elements */
+  int32_t dtype;         /* gpo_dtype */
+  int32_t history_bytes; /* bytes of one id of the history: 4 or 8 */
+  int32_t bias_bytes;    /* the same of bias_ids */
+  int32_t target_bytes;  /* the same of target */
+  const float* scale;      /* [R] 1 / temperature; NULL: scale_all for every row */
+  const float* repetition; /* [R] > 0, 1: no penalty; NULL: repetition_all */
+  const float* presence;   /* [R] 0: none; NULL: presence_all */
+  const float* frequency;  /* [R] 0: none; NULL: frequency_all */
+  double scale_all, repetition_all, presence_all, frequency_all;
+  const void* history;     /* [history_len] token ids; read only with spans */
+  int64_t history_len;
+  const int64_t* spans;    /* [R x 3] begin, first generated, end; NULL: no histories */
+  const float* bias;       /* [bias_len] optional */
+  const void* bias_ids;    /* [bias_len] */
+  int64_t bias_len;
+  const int64_t* bias_spans; /* [R x 2] begin, end; NULL: every row has the whole list */
+  const uint32_t* mask;    /* [mask_rows x mask_stride] bits, 1: allowed; optional */
+  int64_t mask_rows;
+  int64_t mask_stride;     /* words between rows, >= ceil(V / 32) */
+  const int32_t* mask_row; /* [R]; NULL: row r's mask is row r, or the one that there is */
+  const void* target;      /* [R] token ids; required for logp and the gradient */
+} gpo_logits;
+
+typedef struct {
+  void* logits;          /* [R x logits_stride] optional: the adjusted logits; may be the raw ones (same stride and type) */
+  int64_t logits_stride; /* >= vocab */
+  int32_t dtype;         /* of the adjusted logits: the raw ones' or GPO_DT_F32 */
+  float* logp;           /* [R] optional, needs target */
+  float* lse;            /* [R] optional */
+  float* entropy;        /* [R] optional */
+} gpo_logits_outputs;
+
+typedef struct {
+  const float* lse;          /* [R] of gpo_logits_adjust */
+  const float* logp;         /* [R] of gpo_logits_adjust */
+  const float* grad_logp;    /* [R] d loss / d logp (gpo_loss_outputs.grad_logp) */
+  const float* entropy;      /* [R] of gpo_logits_adjust; read only with grad_entropy */
+  const float* grad_entropy; /* [R] optional: d loss / d entropy */
+} gpo_logits_grad_inputs;
+
+/* Enqueues the adjusted logits and their statistics on `stream` (at least one output).  One kernel, no
+ * workspace.  Host-checked: sizes, NULL pointers, the values for all rows, alignment to elements (GPO_ERR_UNSUPPORTED). */
+gpo_status gpo_logits_adjust(gpo_ctx* ctx, const gpo_logits* l, const gpo_logits_outputs* out, void* stream);
+
+/* Enqueues the gradient of the raw logits, in their type: d_logits [R x d_stride], overwritten, which may be the raw
+ * logits themselves (same stride). */
+gpo_status gpo_logits_grad(gpo_ctx* ctx, const gpo_logits* l, const gpo_logits_grad_inputs* in, void* d_logits,
+                           int64_t d_stride, void* stream);
+
 /* Library version string. */
 const char* gpo_version(void);
 

@@ -104,6 +104,27 @@ class CEmbedding(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("scale", ctypes.c_double)]
 
 
+class CLogits(ctypes.Structure):
+    _fields_ = [("num_rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("logits_stride", ctypes.c_int64), ("logits", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("history_bytes", ctypes.c_int32), ("bias_bytes", ctypes.c_int32),
+                ("target_bytes", ctypes.c_int32), ("scale", ctypes.c_void_p), ("repetition", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("frequency", ctypes.c_void_p), ("scale_all", ctypes.c_double),
+                ("repetition_all", ctypes.c_double), ("presence_all", ctypes.c_double), ("frequency_all", ctypes.c_double),
+                ("history", ctypes.c_void_p), ("history_len", ctypes.c_int64), ("spans", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("bias_ids", ctypes.c_void_p), ("bias_len", ctypes.c_int64), ("bias_spans", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_rows", ctypes.c_int64), ("mask_stride", ctypes.c_int64), ("mask_row", ctypes.c_void_p),
+                ("target", ctypes.c_void_p)]
+
+
+class LogitsOutputs(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("dtype", ctypes.c_int32), ("logp", ctypes.c_void_p),
+                ("lse", ctypes.c_void_p), ("entropy", ctypes.c_void_p)]
+
+
+class LogitsGradInputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("lse", "logp", "grad_logp", "entropy", "grad_entropy")]
+
+
 LOSS_FORMS = {"dual": 0, "split": 1}
 LOSS_NORMS = {"edge": 0, "token": 1}
 LOSS_NSTATS = 4
@@ -112,7 +133,7 @@ EXPORTS = ["gpo_create", "gpo_workspace_size", "gpo_compute", "gpo_sync_status",
            "gpo_last_error", "gpo_version", "gpo_destroy", "gpo_enable_timing", "gpo_stage_times", "gpo_compute_noalloc",
            "gpo_compute_groups", "gpo_compute_host", "gpo_loss_plan_size", "gpo_loss_plan", "gpo_token_loss",
            "gpo_layer_budget", "gpo_vocab_workspace_size", "gpo_vocab_logp", "gpo_vocab_grad", "gpo_vocab_grad_logp",
-           "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad"]
+           "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad", "gpo_logits_adjust", "gpo_logits_grad"]
 
 FUSED_MAX_STATES = 384  # largest group the group-resident path (and gpo_compute_groups) serves
 
@@ -120,13 +141,16 @@ _lib = None
 _fast = {}  # the calls of every step once more, with their structs as packed bytes (see _pack)
 _lock = threading.Lock()
 
-# Packed images of gpo_vocab, gpo_vocab_outputs, gpo_vocab_grad_inputs, gpo_vocab_grads and gpo_embedding:
-# building a ctypes structure costs 2 us a call, packing one 0.5.
+# Packed images of gpo_vocab, gpo_vocab_outputs, gpo_vocab_grad_inputs, gpo_vocab_grads, gpo_embedding, gpo_logits,
+# gpo_logits_outputs and gpo_logits_grad_inputs: building a ctypes structure costs 2 us a call, packing one 0.5.
 _PACK_VOCAB = struct.Struct("@5q3Q2id").pack
 _PACK_3 = struct.Struct("@3Q").pack
 _PACK_4 = struct.Struct("@4Q").pack
 _PACK_GRADS = struct.Struct("@2Q2qi4x").pack
 _PACK_EMBED = struct.Struct("@5qQ2id").pack
+_PACK_LOGITS = struct.Struct("@3qQ4i4Q4dQq3QqQQ2q2Q").pack
+_PACK_LOGITS_OUT = struct.Struct("@Qqi3Q").pack
+_PACK_5 = struct.Struct("@5Q").pack
 
 
 def lib_path() -> str:
@@ -210,8 +234,13 @@ def load(build_if_missing: bool = False):
         L.gpo_embed.restype = ctypes.c_int
         L.gpo_embed_grad.argtypes = [vp, ctypes.POINTER(CEmbedding), vp, vp, ctypes.c_int, vp, sz, vp]
         L.gpo_embed_grad.restype = ctypes.c_int
+        L.gpo_logits_adjust.argtypes = [vp, ctypes.POINTER(CLogits), ctypes.POINTER(LogitsOutputs), vp]
+        L.gpo_logits_adjust.restype = ctypes.c_int
+        L.gpo_logits_grad.argtypes = [vp, ctypes.POINTER(CLogits), ctypes.POINTER(LogitsGradInputs), vp, ctypes.c_int64, vp]
+        L.gpo_logits_grad.restype = ctypes.c_int
         raw = ctypes.c_char_p
-        for name, args in (("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad_logp", [vp, raw, raw, vp, raw, vp, sz, vp]),
+        for name, args in (("gpo_logits_adjust", [vp, raw, raw, vp]), ("gpo_logits_grad", [vp, raw, raw, vp, ctypes.c_int64, vp]),
+                           ("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad_logp", [vp, raw, raw, vp, raw, vp, sz, vp]),
                            ("gpo_embed", [vp, raw, vp, vp, vp, sz, vp]), ("gpo_embed_grad", [vp, raw, vp, vp, ctypes.c_int, vp, sz, vp])):
             f = L[name]  # (a function object of its own)
             f.argtypes, f.restype = args, ctypes.c_int
@@ -818,6 +847,129 @@ class GraphPO:
                             grad.device, workspace, on)
         code = _fast["gpo_embed_grad"](self._h, _PACK_EMBED(T, V, d, ts, rs, ip, code, idb, scale), grad.data_ptr(),
                                        out.data_ptr(), bool(accumulate), wp, wn, on)
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    # ---- logits as a sampler takes them (gpo_logits_adjust / gpo_logits_grad)
+
+    def _logits(self, logits, target, scale, mask, mask_row, history, spans, repetition, presence, frequency, bias, bias_ids,
+                bias_spans):
+        """The checks that both directions share; the device, the sizes, the dtype's code and the packed gpo_logits."""
+        import torch
+        if len(logits.shape) != 2:
+            raise ValueError("logits must be [R, V]")
+        dev, (R, V) = logits.get_device(), logits.shape
+        code = _dtype_code(logits, "logits")
+        stride = _matrix(logits, "logits", dev, R, V, logits.dtype)
+        if dev != self._device:
+            self._elsewhere(dev)
+        f32, i64, i32 = torch.float32, torch.int64, torch.int32
+        ptrs, values = [], []
+        for x, what in ((scale, "scale"), (repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
+            given = isinstance(x, torch.Tensor)
+            ptrs.append(_vector(x, what, dev, R, f32) if given else 0)
+            values.append(1.0 if given else x)
+        hb = bb = tb = hp = hn = sp = bp = ip = bn = bs = mp = mr = ms = mi = tp = 0
+        if (history is None) != (spans is None) or (bias is None) != (bias_ids is None):
+            raise ValueError("history needs spans, and bias needs bias_ids")
+        if spans is not None:
+            hb, hn = _id_bytes(history, "history"), history.numel()
+            hp = _vector(history, "history", dev, hn)
+            sp = self._spans(spans, "spans", dev, R, 3, i64)
+        if bias is not None:
+            bb, bn = _id_bytes(bias_ids, "bias_ids"), bias_ids.numel()
+            ip, bp = _vector(bias_ids, "bias_ids", dev, bn), _vector(bias, "bias", dev, bn, f32)
+            bs = 0 if bias_spans is None else self._spans(bias_spans, "bias_spans", dev, R, 2, i64)
+        if mask is not None:
+            if len(mask.shape) != 2 or mask.shape[1] < (V + 31) // 32:
+                raise ValueError(f"mask must be [masks, {(V + 31) // 32} or more] words of 32 tokens")
+            mr = mask.shape[0]
+            if mr == 0 or (mask_row is None and mr not in (1, R)):
+                raise ValueError("mask needs one row for all rows of logits, one each, or mask_row")
+            ms, mp = _matrix(mask, "mask", dev, mr, mask.shape[1], i32), mask.data_ptr()
+            mi = 0 if mask_row is None else _vector(mask_row, "mask_row", dev, R, i32)
+        if target is not None:
+            tb, tp = _id_bytes(target, "target"), _vector(target, "target", dev, R)
+        return dev, R, V, _PACK_LOGITS(R, V, stride, logits.data_ptr(), code, hb, bb, tb, *ptrs, *values, hp, hn, sp, bp, ip, bn, bs, mp,
+                                       mr, ms, mi, tp)
+
+    @staticmethod
+    def _spans(t, what: str, dev: int, rows: int, n: int, dtype) -> int:
+        if len(t.shape) != 2 or t.shape[0] != rows or t.shape[1] != n or not t.is_contiguous():
+            raise ValueError(f"{what} must be contiguous, [{rows}, {n}]")
+        if t.get_device() != dev or t.dtype is not dtype:
+            raise TypeError(f"{what} must be {dtype}, on the device of the logits")
+        return t.data_ptr()
+
+    def logits_adjust(self, logits, target=None, scale=1.0, mask=None, mask_row=None, history=None, spans=None, repetition=1.0,
+                      presence=0.0, frequency=0.0, bias=None, bias_ids=None, bias_spans=None, write=None, lse=True, entropy=False,
+                      out=None, stream=None) -> dict:
+        """Logits [R, V] (bfloat16, float16 or float32) as a sampler takes them, and the statistics of what it samples from:
+
+        * penalties for the tokens of each row's history: spans (int64 [R, 3]: begin, first generated token, end) into history
+          (int32 or int64); repetition divides positive logits and multiplies the others of every token there, frequency
+          (per occurrence) and presence are subtracted for generated ones;
+        * biases (float32) of the tokens bias_ids (ascending), for all rows, or of each row [bias_spans[r, 0], bias_spans[r, 1]);
+        * scale, 1 / temperature; scale and the three penalties are numbers or float32 [R];
+        * mask, int32 words of 32 tokens each, bit 1: allowed; one row, R rows, or those that mask_row (int32 [R], below 0:
+          none) names.
+
+        Returns {"lse": float32 [R] (if lse), "entropy" (if entropy), "logp" of `target` (int32 or int64 [R], below 0: no token, all
+        0; if given), "logits" (with write=torch.float32 or the logits' type)}, or fills `out`, whose "logits" may be the raw ones.
+        Enqueued on the current stream; `check()` raises on ids, spans, biases and values that are out of range."""
+        import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.logits_adjust(logits, target, scale, mask, mask_row, history, spans, repetition, presence, frequency, bias,
+                                          bias_ids, bias_spans, write, lse, entropy, out)
+        dev, R, V, packed = self._logits(logits, target, scale, mask, mask_row, history, spans, repetition, presence, frequency, bias,
+                                         bias_ids, bias_spans)
+        f32 = torch.float32
+        if out is None:
+            out = {k: torch.empty(R, dtype=f32, device=logits.device)
+                   for k, want in (("lse", lse), ("entropy", entropy), ("logp", target is not None)) if want}
+            if write is not None:
+                out["logits"] = torch.empty(R, V, dtype=write, device=logits.device)
+        ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, R, f32) for k in ("logp", "lse", "entropy")]
+        x, stride, code = out.get("logits"), 0, 0
+        if x is not None:
+            if x.dtype is not f32 and x.dtype is not logits.dtype:
+                raise TypeError(f"adjusted logits are float32 or {logits.dtype}, not {x.dtype}")
+            stride, code = _matrix(x, "logits", dev, R, V, x.dtype), _dtypes[x.dtype]
+        code = _fast["gpo_logits_adjust"](self._h, packed, _PACK_LOGITS_OUT(0 if x is None else x.data_ptr(), stride, code, *ptrs),
+                                          _stream_handle(dev))
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def logits_grad(self, logits, target, lse, logp, grad_logp, entropy=None, grad_entropy=None, scale=1.0, mask=None, mask_row=None,
+                    history=None, spans=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None, bias_ids=None, bias_spans=None,
+                    out=None, stream=None) -> dict:
+        """Gradient {"d_logits": [R, V]} of the raw logits, in their type, of a loss with the gradients grad_logp (e.g. token_loss's)
+        and optionally grad_entropy (float32 [R]) with respect to logits_adjust's outputs for the same arguments, whose lse and
+        logp (and entropy) are given; or fills `out`, whose "d_logits" may be the logits themselves.  Enqueued on the current
+        stream; check() as for logits_adjust."""
+        import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.logits_grad(logits, target, lse, logp, grad_logp, entropy, grad_entropy, scale, mask, mask_row, history, spans,
+                                        repetition, presence, frequency, bias, bias_ids, bias_spans, out)
+        if target is None:
+            raise ValueError("the gradient needs target")
+        if grad_entropy is not None and entropy is None:
+            raise ValueError("grad_entropy needs logits_adjust's entropy")
+        dev, R, V, packed = self._logits(logits, target, scale, mask, mask_row, history, spans, repetition, presence, frequency, bias,
+                                         bias_ids, bias_spans)
+        f32 = torch.float32
+        ins = _PACK_5(_vector(lse, "lse", dev, R, f32), _vector(logp, "logp", dev, R, f32), _vector(grad_logp, "grad_logp", dev, R, f32),
+                      0 if grad_entropy is None else _vector(entropy, "entropy", dev, R, f32),
+                      0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, R, f32))
+        if out is None:
+            out = {"d_logits": torch.empty(R, V, dtype=logits.dtype, device=logits.device)}
+        d = out["d_logits"]
+        stride = _matrix(d, "d_logits", dev, R, V, logits.dtype)
+        code = _fast["gpo_logits_grad"](self._h, packed, ins, d.data_ptr(), stride, _stream_handle(dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out

@@ -1100,4 +1100,38 @@ cudaError_t setup_embed();
 cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
 cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
 
+// ------------------------------------------------------------------ adjusted logits
+
+struct LogitsArgs {
+  int64_t R, V;
+  const void* z;
+  int64_t z_stride;
+  const float *scale, *rep, *pres, *freq;    // of every row; null: the one value
+  float scale1, rep1, pres1, freq1;
+  const void* hist;
+  int64_t hist_len;
+  const int64_t* spans;                      // [R x 3]; null: no histories
+  int hist8;                                 // the history is int64
+  const float* bias;                         // null: none
+  const void* bias_ids;
+  int64_t bias_len;
+  const int64_t* bias_spans;                 // [R x 2]; null: every row has the whole list
+  int bias8;
+  const uint32_t* mask;                      // null: every token is allowed
+  int64_t mask_rows, mask_stride;
+  const int32_t* mask_row;                   // null: row r's, or all rows' one
+  const void* target;
+  int target8;
+  void* out;                                 // adjusted logits, or the gradient
+  int64_t out_stride;
+  int out32;                                 // adjusted logits in fp32
+  float *logp, *lse, *ent;
+  // gradient
+  const float *lse_in, *logp_in, *g, *ent_in, *ge;
+};
+
+cudaError_t setup_logits();
+// The adjusted logits and their statistics; without `out` the statistics alone; with g the gradient.
+cudaError_t launch_logits(const LaunchCtx& lc, const LogitsArgs& a, int dtype, const Status& st);
+
 }  // namespace gpo

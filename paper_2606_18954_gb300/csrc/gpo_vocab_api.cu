@@ -6,16 +6,11 @@
 
 #include <algorithm>
 
-#include <nvtx3/nvToolsExt.h>
-
-#include "gpo_ctx.cuh"
+#include "gpo_stages.cuh"
 
 using namespace gpo;
 
 namespace {
-
-constexpr int64_t kMaxCount = ((int64_t)1 << 31) - 1024;  // tokens, vocabulary rows, width
-constexpr int64_t kMaxMatrix = (int64_t)1 << 40;          // elements of a matrix
 
 struct VocabLayout {
   size_t marks, head, idx, hc, by_target, tile_first, rest, pm, ps, pu, tz, dz, acc, total;
@@ -101,15 +96,6 @@ gpo_status check_vocab(gpo_ctx* c, const gpo_vocab* v) {
   return GPO_OK;
 }
 
-gpo_status check_call(gpo_ctx* c, const void* workspace, size_t have, size_t need) {
-  if (!workspace || !aligned(workspace, kWorkspaceAlign) || have < need)
-    return set_msg(c, "workspace needs %zu bytes, 256-byte aligned", need), GPO_ERR_WORKSPACE;
-  int dev = -1;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev != c->device)
-    return set_msg(c, "current device differs from the context's"), GPO_ERR_INVALID_ARG;
-  return GPO_OK;
-}
-
 // (Fetching 256 bytes for a box's 128 takes rows that straddle lines 20 % longer: dz of 4000 tokens, 30000 x
 // 1000, 144 us against 125.)
 bool encode_map(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t cols, int64_t rows, int64_t stride, int f16,
@@ -135,58 +121,6 @@ bool encode_blocks(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t 
 // Words of captured calls: the library's, as a graph may be replayed after its context is gone.  (A process that captures
 // more calls than there are gives words out again: a call may then return another's error, or stop at it.)
 __device__ __align__(256) uint32_t g_captured_words[kCapturedWords * kStatusWords];
-int captured_place() {
-  static std::atomic<uint32_t> next{0};
-  return (int)(next.fetch_add(1, std::memory_order_relaxed) % kCapturedWords);
-}
-
-// The launches of one call: an NVTX range around each and, with timing on, a CUDA event after it.
-struct Stages {
-  gpo_ctx* ctx;
-  LaunchCtx lc;
-  int n;
-  cudaError_t e;
-  Status st;
-  bool captured;
-
-  // The call's errors: in words and with a tag of its own; in a graph, whose replays share both, in words that no other
-  // call has, with a tag that every replay advances (next_tag; a memset node before it took 0.7 us of each).
-  Stages(gpo_ctx* c, void* stream) : ctx(c), n(0), e(cudaSuccess) {
-    lc.stream = static_cast<cudaStream_t>(stream);
-    lc.num_sms = c->num_sms;
-    if (ctx->timing) e = cudaEventRecord(ctx->ev[0], lc.stream);
-    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    captured = cudaStreamIsCapturing(lc.stream, &cap) != cudaSuccess || cap != cudaStreamCaptureStatusNone;
-    if (captured) {
-      cudaGetLastError();
-      const int i = captured_place();
-      ctx->captured.set(i);
-      st.p = ctx->captured_words + i * kStatusWords;
-      st.tag = kStoredTag;
-    } else {
-      st.tag = ++ctx->calls;
-      st.p = ctx->call_words + ctx->calls % kCallWords * kStatusWords;
-    }
-  }
-  template <class F>
-  void operator()(const char* name, F launch) {
-    if (e != cudaSuccess) return;
-    nvtxRangePushA(name);
-    e = launch();
-    nvtxRangePop();
-    if (ctx->timing && e == cudaSuccess && n < kMaxStages) {
-      ctx->stage_name[n] = name;
-      e = cudaEventRecord(ctx->ev[++n], lc.stream);
-    }
-  }
-  gpo_status done() {
-    ctx->nstages = n;
-    if (ctx->last_read) ctx->last_status = nullptr;
-    if (e != cudaSuccess) return set_msg(ctx, "launch failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
-    return GPO_OK;
-  }
-};
-
 template <class P>
 P* at(void* base, size_t off) { return reinterpret_cast<P*>(static_cast<unsigned char*>(base) + off); }
 
@@ -243,6 +177,11 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
 }  // namespace
 
 namespace gpo {
+
+int captured_place() {
+  static std::atomic<uint32_t> next{0};
+  return (int)(next.fetch_add(1, std::memory_order_relaxed) % kCapturedWords);
+}
 
 cudaError_t make_call_words(gpo_ctx* c) {
   constexpr size_t bytes = sizeof(uint32_t) * kStatusWords * kCallWords;
