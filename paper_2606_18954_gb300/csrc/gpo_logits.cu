@@ -20,90 +20,148 @@ namespace gpo {
 namespace {
 
 constexpr int kThreads = 384, kWarps = kThreads / 32;
-constexpr int kVecs = 4;                         // accesses of 16 bytes of a thread and slice
+constexpr int kVecs = 2;                         // accesses of 32 bytes of a thread that are in flight
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1;  // an entry's word: flags, occurrences
 enum Op { kAdjust, kScore, kGrad };              // write the adjusted logits, only their statistics, the gradient
 
-// A vector of 16 bytes of logits, of which lane bits say which entries count.
+// A vector of 32 bytes of logits.
+struct Vec {
+  uint32_t w[8];
+};
+// (streamed: nothing reads a row again but the few special entries)
+__device__ __forceinline__ Vec load_global(const void* p) {
+  Vec r;
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
+               : "l"(p)
+               : "memory");
+  return r;
+}
+__device__ __forceinline__ void store_global(void* p, const Vec& x) {
+  asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
+               "r"(x.w[3]), "r"(x.w[4]), "r"(x.w[5]), "r"(x.w[6]), "r"(x.w[7])
+               : "memory");
+}
+
 template <int kType>
 struct Raw;
 template <>
 struct Raw<GPO_DT_F32> {
   using T = float;
-  static constexpr int kPer = 4;
-  static __device__ __forceinline__ uint4 keep(const uint4& r, uint32_t take, uint32_t other) {
-    return make_uint4(take & 1u ? r.x : other, take & 2u ? r.y : other, take & 4u ? r.z : other, take & 8u ? r.w : other);
+  static constexpr int kPer = 8;
+  static constexpr bool kFloors = false;
+  // the entries of `take`, `other` in the place of the rest; those of `b` in the places `of_b`
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other) {
+    Vec x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.w[i] = take >> i & 1u ? r.w[i] : other;
+    return x;
   }
-  static __device__ __forceinline__ uint4 keep(const uint4& r, uint32_t take) { return keep(r, take, 0xFF800000u); }  // -inf
-  static __device__ __forceinline__ uint4 zero(const uint4& r, uint32_t take) { return keep(r, take, 0u); }
-  static __device__ __forceinline__ uint4 choose(const uint4& a, const uint4& b, uint32_t of_b) {
-    return make_uint4(of_b & 1u ? b.x : a.x, of_b & 2u ? b.y : a.y, of_b & 4u ? b.z : a.z, of_b & 8u ? b.w : a.w);
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return keep(r, take, 0xFF800000u); }  // -inf
+  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b) {
+    Vec x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x.w[i] = of_b >> i & 1u ? b.w[i] : a.w[i];
+    return x;
   }
-  static __device__ __forceinline__ float top(const uint4& r) {
-    return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+  static __device__ __forceinline__ Vec floor(const Vec& r) { return r; }
+  static __device__ __forceinline__ float top(const Vec& r) {
+    float t = __uint_as_float(r.w[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t = fmaxf(t, __uint_as_float(r.w[i]));
+    return t;
   }
-  static __device__ __forceinline__ void widen(const uint4& r, float (&y)[4]) {
-    y[0] = __uint_as_float(r.x), y[1] = __uint_as_float(r.y), y[2] = __uint_as_float(r.z), y[3] = __uint_as_float(r.w);
+  static __device__ __forceinline__ void widen(const Vec& r, float (&y)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(r.w[i]);
   }
-  static __device__ __forceinline__ uint4 narrow(const float (&y)[4]) {
-    return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+  static __device__ __forceinline__ Vec narrow(const float (&y)[8]) {
+    Vec r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.w[i] = __float_as_uint(y[i]);
+    return r;
   }
-  static __device__ __forceinline__ float get(uint32_t w, int) { return __uint_as_float(w); }
+  static __device__ __forceinline__ float get(const Vec& r, int i) { return __uint_as_float(r.w[i]); }
   static __device__ __forceinline__ float get1(T x) { return x; }
   static __device__ __forceinline__ T put(float x) { return x; }
 };
 // (two 16-bit entries per word)
 struct Raw16 {
-  static constexpr int kPer = 8;
-  // entry i counts: 16 ones in its half of word i / 2.  A nibble's bits go to the sign bits of four bytes (i + 7 (j + 1) is
-  // different for every bit i and factor bit j, so that nothing carries), which prmt spreads.
+  static constexpr int kPer = 16;
   template <uint32_t kSel>
   static __device__ __forceinline__ uint32_t spread(uint32_t x) {
     uint32_t r;
     asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(x), "n"(kSel));
     return r;
   }
-  static __device__ __forceinline__ uint4 mask(uint32_t take) {
-    const uint32_t a = (take & 15u) * 0x10204080u & 0x80808080u, b = (take >> 4) * 0x10204080u & 0x80808080u;
-    return make_uint4(spread<0x9988>(a), spread<0xBBAA>(a), spread<0x9988>(b), spread<0xBBAA>(b));
+  // Sixteen ones in the half of word i / 2 for every bit i.  A nibble's bits go to the sign bits of four bytes (i + 7 (j + 1) is
+  // different for every bit i and factor bit j, so that nothing carries), which prmt spreads.
+  static __device__ __forceinline__ Vec mask(uint32_t take) {
+    Vec m;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t a = (take >> 4 * i & 15u) * 0x10204080u & 0x80808080u;
+      m.w[2 * i] = spread<0x9988>(a);
+      m.w[2 * i + 1] = spread<0xBBAA>(a);
+    }
+    return m;
   }
-  static __device__ __forceinline__ uint4 keep(const uint4& r, uint32_t take, uint32_t other) {
-    const uint4 m = mask(take);
-    return make_uint4((r.x & m.x) | (other & ~m.x), (r.y & m.y) | (other & ~m.y), (r.z & m.z) | (other & ~m.z), (r.w & m.w) | (other & ~m.w));
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other) {
+    Vec m = mask(take);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m.w[i] = (r.w[i] & m.w[i]) | (other & ~m.w[i]);
+    return m;
   }
-  static __device__ __forceinline__ uint4 zero(const uint4& r, uint32_t take) { return keep(r, take, 0u); }
-  static __device__ __forceinline__ uint4 choose(const uint4& a, const uint4& b, uint32_t of_b) {
-    const uint4 m = mask(of_b);
-    return make_uint4((a.x & ~m.x) | (b.x & m.x), (a.y & ~m.y) | (b.y & m.y), (a.z & ~m.z) | (b.z & m.z), (a.w & ~m.w) | (b.w & m.w));
+  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b) {
+    Vec m = mask(of_b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m.w[i] = (a.w[i] & ~m.w[i]) | (b.w[i] & m.w[i]);
+    return m;
   }
 };
 template <>
 struct Raw<GPO_DT_BF16> : Raw16 {
   using T = __nv_bfloat16;
   using Raw16::keep;
-  static __device__ __forceinline__ uint4 keep(const uint4& r, uint32_t take) { return Raw16::keep(r, take, 0xFF80FF80u); }
+  static constexpr bool kFloors = true;
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return Raw16::keep(r, take, 0xFF80FF80u); }
   static __device__ __forceinline__ __nv_bfloat162 h2(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
-  static __device__ __forceinline__ float top(const uint4& r) {
-    const __nv_bfloat162 t = __hmax2(__hmax2(h2(r.x), h2(r.y)), __hmax2(h2(r.z), h2(r.w)));
+  // -1e33 for -inf and what is below it, which for every scale is left out of a row all the same; a NaN stays one
+  static __device__ __forceinline__ Vec floor(const Vec& r) {
+    Vec x;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __nv_bfloat162 t = __hmax2_nan(h2(r.w[i]), h2(0xF645F645u));
+      x.w[i] = *reinterpret_cast<const uint32_t*>(&t);
+    }
+    return x;
+  }
+  static __device__ __forceinline__ float top(const Vec& r) {
+    __nv_bfloat162 t = h2(r.w[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t = __hmax2(t, h2(r.w[i]));
     return fmaxf(__low2float(t), __high2float(t));
   }
-  static __device__ __forceinline__ void widen(const uint4& r, float (&y)[8]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  static __device__ __forceinline__ void widen(const Vec& r, float (&y)[16]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[2 * i] = __uint_as_float(w[i] << 16);
-      y[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    for (int i = 0; i < 8; ++i) {
+      y[2 * i] = __uint_as_float(r.w[i] << 16);
+      y[2 * i + 1] = __uint_as_float(r.w[i] & 0xFFFF0000u);
     }
   }
-  static __device__ __forceinline__ uint32_t pair(float a, float b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+  static __device__ __forceinline__ Vec narrow(const float (&y)[16]) {
+    Vec r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+      r.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return r;
   }
-  static __device__ __forceinline__ uint4 narrow(const float (&y)[8]) {
-    return make_uint4(pair(y[0], y[1]), pair(y[2], y[3]), pair(y[4], y[5]), pair(y[6], y[7]));
+  static __device__ __forceinline__ float get(const Vec& r, int i) {
+    return __uint_as_float(i & 1 ? r.w[i / 2] & 0xFFFF0000u : r.w[i / 2] << 16);
   }
-  static __device__ __forceinline__ float get(uint32_t w, int j) { return __uint_as_float(j & 1 ? w & 0xFFFF0000u : w << 16); }
   static __device__ __forceinline__ float get1(T x) { return __bfloat162float(x); }
   static __device__ __forceinline__ T put(float x) { return __float2bfloat16_rn(x); }
 };
@@ -111,29 +169,36 @@ template <>
 struct Raw<GPO_DT_F16> : Raw16 {
   using T = __half;
   using Raw16::keep;
-  static __device__ __forceinline__ uint4 keep(const uint4& r, uint32_t take) { return Raw16::keep(r, take, 0xFC00FC00u); }
+  static constexpr bool kFloors = false;  // (fp16 has no number that is below all that counts)
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return Raw16::keep(r, take, 0xFC00FC00u); }
   static __device__ __forceinline__ __half2 h2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
-  static __device__ __forceinline__ float top(const uint4& r) {
-    const __half2 t = __hmax2(__hmax2(h2(r.x), h2(r.y)), __hmax2(h2(r.z), h2(r.w)));
+  static __device__ __forceinline__ Vec floor(const Vec& r) { return r; }
+  static __device__ __forceinline__ float top(const Vec& r) {
+    __half2 t = h2(r.w[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) t = __hmax2(t, h2(r.w[i]));
     return fmaxf(__low2float(t), __high2float(t));
   }
-  static __device__ __forceinline__ void widen(const uint4& r, float (&y)[8]) {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+  static __device__ __forceinline__ void widen(const Vec& r, float (&y)[16]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(h2(w[i]));
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = __half22float2(h2(r.w[i]));
       y[2 * i] = f.x;
       y[2 * i + 1] = f.y;
     }
   }
-  static __device__ __forceinline__ uint32_t pair(float a, float b) {
-    const __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&h);
+  static __device__ __forceinline__ Vec narrow(const float (&y)[16]) {
+    Vec r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const __half2 h = __floats2half2_rn(y[2 * i], y[2 * i + 1]);
+      r.w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return r;
   }
-  static __device__ __forceinline__ uint4 narrow(const float (&y)[8]) {
-    return make_uint4(pair(y[0], y[1]), pair(y[2], y[3]), pair(y[4], y[5]), pair(y[6], y[7]));
+  static __device__ __forceinline__ float get(const Vec& r, int i) {
+    return __half2float(__ushort_as_half((unsigned short)(i & 1 ? r.w[i / 2] >> 16 : r.w[i / 2])));
   }
-  static __device__ __forceinline__ float get(uint32_t w, int j) { return __half2float(__ushort_as_half((unsigned short)(j & 1 ? w >> 16 : w))); }
   static __device__ __forceinline__ float get1(T x) { return __half2float(x); }
   static __device__ __forceinline__ T put(float x) { return __float2half_rn(x); }
 };
@@ -142,8 +207,8 @@ struct Raw<GPO_DT_F16> : Raw16 {
 struct Row {
   const void* z;
   void* out;
-  int shift;                  // elements between the 16-byte boundary before the row and the row
-  int vecs;                   // accesses of 16 bytes that hold the row
+  int shift;                  // elements between the 32-byte boundary before the row and the row
+  int vecs;                   // accesses of 32 bytes that hold the row
   int live;                   // has a target, or a gradient, or needs none
   int vec;                    // the output's accesses of a whole vector are aligned
   int special;                // some entry may be special
@@ -176,7 +241,7 @@ struct Smem {
   uint32_t before[kWords];            // special entries in the words before
   uint32_t list[kCap];                // the round's special entries, in their order,
   uint32_t count[kCap];               // and their flags and occurrences
-  float stage[kWarps][256];           // values of each warp on their way out
+  float stage[kWarps][512];           // values of each warp on their way out
 };
 
 // The bias of v among the row's (ascending).
@@ -246,11 +311,11 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   Row w;
   const T* z = static_cast<const T*>(a.z) + r * a.z_stride;
   w.z = z;
-  w.shift = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(T));
+  w.shift = (int)((reinterpret_cast<uintptr_t>(z) & 31) / sizeof(T));
   w.vecs = (int)((a.V + w.shift + E::kPer - 1) / E::kPer);
   const size_t osz = a.out32 ? 4 : sizeof(T);
   w.out = kOp == kScore ? nullptr : static_cast<char*>(a.out) + r * a.out_stride * osz;
-  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) - w.shift * osz) & 15) == 0;
+  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) - w.shift * osz) & 31) == 0;
   w.scale = f32(0, a.scale, a.scale1);
   w.rep = f32(1, a.rep, a.rep1);
   w.pres = f32(2, a.pres, a.pres1);
@@ -339,12 +404,16 @@ __device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st,
   }
 }
 
-// The number of special entries of the span, and of those before each word.
-__device__ __forceinline__ int rank_span(int n, Smem& sm) {
+// The number of special entries of the span, and of those before each word; these leave the allowed ones.
+__device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int j0 = min((n + 31) / 32, (int)threadIdx.x * kOwn), j1 = min((n + 31) / 32, j0 + kOwn);
   int own = 0;
-  for (int j = j0; j < j1; ++j) own += __popc(sm.special[j]);
+  for (int j = j0; j < j1; ++j) {
+    const uint32_t x = sm.special[j];
+    own += __popc(x);
+    sm.allow[j] = masked ? sm.allow[j] & ~x : ~x;
+  }
   int upto = own;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -403,24 +472,22 @@ __device__ __forceinline__ uint32_t in_row(int v, int V) {
 
 // A vector of the row, whose first entry is v; entries outside the row are 0.
 template <int kType>
-__device__ __forceinline__ uint4 load_vec(const void* row, int v, int V) {
+__device__ __forceinline__ Vec load_vec(const void* row, int v, int V) {
   using E = Raw<kType>;
   using T = typename E::T;
   const T* z = static_cast<const T*>(row);
-  uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (v >= 0 && v + E::kPer <= V) return __ldcs(reinterpret_cast<const uint4*>(z + v));
-  T* e = reinterpret_cast<T*>(&r);
+  if (v >= 0 && v + E::kPer <= V) return load_global(z + v);
+  float y[E::kPer];
 #pragma unroll
-  for (int i = 0; i < E::kPer; ++i)
-    if (v + i >= 0 && v + i < V) e[i] = z[v + i];
-  return r;
+  for (int i = 0; i < E::kPer; ++i) y[i] = v + i >= 0 && v + i < V ? E::get1(z[v + i]) : 0.f;
+  return E::narrow(y);
 }
 
 // kPer values of every lane to the row, by a whole warp: lane 0's first entry is v0, `in` says which of a lane's are to be written (none from `end` on).
 // In an aligned row a lane's are one or two accesses; in others the warp's go through shared memory, so that an access
 // takes 32 entries side by side.
 template <int kType>
-__device__ __forceinline__ void store_vec(bool wide, const Row& w, const float (&y)[Raw<kType>::kPer], const uint4& narrow, int v0, uint32_t in,
+__device__ __forceinline__ void store_vec(bool wide, const Row& w, const float (&y)[Raw<kType>::kPer], const Vec& narrow, int v0, uint32_t in,
                                           int end, float* stage, int lane) {
   using E = Raw<kType>;
   using T = typename E::T;
@@ -429,18 +496,22 @@ __device__ __forceinline__ void store_vec(bool wide, const Row& w, const float (
   const bool whole = in == (1u << kPer) - 1u;
   if (w.vec && whole) {
     if (wide) {
-      float4* p = reinterpret_cast<float4*>(static_cast<float*>(w.out) + v);
+      float* p = static_cast<float*>(w.out) + v;
 #pragma unroll
-      for (int i = 0; i < kPer / 4; ++i) __stcs(p + i, make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]));
+      for (int i = 0; i < kPer / 8; ++i) {
+        Vec x;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x.w[k] = __float_as_uint(y[8 * i + k]);
+        store_global(p + 8 * i, x);
+      }
     } else {
-      __stcs(reinterpret_cast<uint4*>(static_cast<T*>(w.out) + v), narrow);
+      store_global(static_cast<T*>(w.out) + v, narrow);
     }
   }
   if (w.vec && __all_sync(0xffffffffu, whole)) return;
   __syncwarp();
-  const uint32_t words[4] = {narrow.x, narrow.y, narrow.z, narrow.w};
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) stage[lane * kPer + i] = wide || sizeof(T) == 4 ? y[i] : E::get(words[i / (kPer / 4)], i);
+  for (int i = 0; i < kPer; ++i) stage[lane * kPer + i] = wide || sizeof(T) == 4 ? y[i] : E::get(narrow, i);
   __syncwarp();
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
@@ -513,22 +584,22 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
   if (warp == 0 && r < a.R) read_row<kType, kOp>(a, st, r, sh.row[0], lane, rank == 0);
   __syncthreads();
   // this CTA's share of a row's vectors (in whole words of the bitmaps)
-  auto begins = [&](const Row& w) { return min(w.vecs, rank * ((w.vecs + cluster * 8 - 1) / (cluster * 8) * 8)); };
-  auto finishes = [&](const Row& w) { return min(w.vecs, (rank + 1) * ((w.vecs + cluster * 8 - 1) / (cluster * 8) * 8)); };
-  // Vectors of the row that a warp takes without a look at its ends: [first, last) hold 8 (4) entries of the row each.
+  auto begins = [&](const Row& w) { return min(w.vecs, rank * ((w.vecs + cluster * 4 - 1) / (cluster * 4) * 4)); };
+  auto finishes = [&](const Row& w) { return min(w.vecs, (rank + 1) * ((w.vecs + cluster * 4 - 1) / (cluster * 4) * 4)); };
+  // Vectors of the row that a warp takes without a look at its ends: [whole0, whole1) are full of its entries.
   auto whole0 = [&](const Row& w) { return w.shift ? 1 : 0; };
   auto whole1 = [&](const Row& w) { return (V + w.shift) / kPer; };
   auto vec_at = [&](const Row& w, int idx) {
-    return reinterpret_cast<const uint4*>(static_cast<const char*>(w.z) - w.shift * sizeof(T)) + idx;
+    return reinterpret_cast<const Vec*>(static_cast<const char*>(w.z) - w.shift * sizeof(T)) + idx;
   };
-  uint4 raw[kVecs];
+  Vec raw[kVecs];
   // a batch's vectors, where the warp's are all whole and before `end`
   auto fetch = [&](const Row& w, int b, int end) {
     const int x0 = whole0(w), n = min(end, whole1(w)) - 32 - x0, at = b + warp * 32 - x0;
-    const uint4* src = vec_at(w, b + tid);
+    const Vec* src = vec_at(w, b + tid);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i)
-      if (n >= 0 && (uint32_t)(at + i * kThreads) <= (uint32_t)n) raw[i] = __ldcs(src + i * kThreads);
+      if (n >= 0 && (uint32_t)(at + i * kThreads) <= (uint32_t)n) raw[i] = load_global(src + i * kThreads);
   };
   bool ready = false;  // raw holds the row's first vectors
   Running p = {kLow, {0.f, 0.f}, {0.f, 0.f}};
@@ -549,12 +620,12 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
       if (n > 0 && marked) mark_span(a, st, w, lo, n, s1 == w.vecs, sm);
       __syncthreads();
       if (n <= 0) break;
-      const int total = w.special ? rank_span(n, sm) : 0;
+      const int total = w.special ? rank_span(n, w.mask != nullptr, sm) : 0;
       const int trel = w.target >= 0 && w.target >= lo && w.target < (int64_t)lo + n ? (int)w.target - lo : -1, tvec = trel < 0 ? -1 : trel / kPer;
       // a special entry, or the target: rel its place in the span
       auto single = [&](int rel, uint32_t slot) {
         const int v = lo + rel;
-        const bool may = !w.mask || (sm.allow[rel >> 5] >> (rel & 31) & 1u);
+        const bool may = !w.mask || (__ldg(w.mask + (v >> 5)) >> (v & 31) & 1u);
         const float z = may ? E::get1(static_cast<const T*>(w.z)[v]) : 0.f;
         float slope = 1.f;
         const float y = !may ? -INFINITY : slot ? adjusted(a, w, slot, z, v, slope) : z;
@@ -582,15 +653,24 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
         }
       };
       // a warp's 32 vectors, idx this lane's; edge: some may be outside the row or the span
-      auto dense = [&](const uint4& z, int idx, bool edge) {
+      auto dense = [&](const Vec& z, int idx, bool edge) {
         const int v = idx * kPer - w.shift, at = idx - s0;
-        uint32_t in = kAll, take = kAll, sp = 0u;
-        if (edge) in = idx >= s1 ? 0u : v < 0 || v + kPer > V ? in_row<kPer>(v, V) & kAll : kAll;
-        const int byte = edge ? min(at * kPer / 8, kSpan / 8 - 1) : at * kPer / 8, nib = kPer == 8 ? 0 : (at & 1) * 4;
-        if (w.mask) take = reinterpret_cast<const uint8_t*>(sm.allow)[byte] >> nib & kAll;
-        if (total) sp = reinterpret_cast<const uint8_t*>(sm.special)[byte] >> nib & kAll;
-        if (at == tvec) sp |= 1u << (uint32_t)trel % kPer;
-        take &= in & ~sp;
+        uint32_t take = kAll, sp = 0u, in = kAll;
+        if (edge) in = idx >= s1 ? 0u : in_row<kPer>(v, V) & kAll;
+        if (marked) {
+          const int k = edge ? min(at, kSpan / kPer - 1) : at;
+          auto bits = [&](const uint32_t* p) -> uint32_t {
+            return kPer == 16 ? reinterpret_cast<const uint16_t*>(p)[k] : reinterpret_cast<const uint8_t*>(p)[k];
+          };
+          take = bits(sm.allow);
+          if (kOp != kScore && total) sp = bits(sm.special);
+        }
+        if (edge) take &= in;
+        if (at == tvec) {
+          const uint32_t bit = 1u << (uint32_t)trel % kPer;
+          sp |= bit;
+          take &= ~bit;
+        }
         if (kOp == kGrad) {
           // d y_j = -gs p_j - es p_j (log p_j + H)
           float y[kPer];
@@ -602,20 +682,21 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
             const float x = ex2(d * kLog2e);
             y[j] = kEnt ? x * fmaf(-es, d + w_ent, -gs) : -gs * x;
           }
-          uint4 o = E::narrow(y);
-          if (take != kAll) o = E::zero(o, take);
+          Vec o = E::narrow(y);
+          if (take != kAll) o = E::keep(o, take, 0u);
           if (sp) o = E::choose(o, z, sp);  // (special ones keep theirs: `out` may be the logits, and they are read once more)
           if (sizeof(T) == 4) E::widen(o, y);
           store_vec<kType>(false, w, y, o, v - lane * kPer, in, min(V, s1 * kPer - w.shift), stage, lane);
         } else {
-          uint4 x = z;
+          Vec x = z;
           if (take != kAll) x = E::keep(x, take);
+          if (kEnt && kOp == kScore) x = E::floor(x);
           const float top = E::top(x) * sl2;
           float y[kPer];
           if (kOp == kAdjust) {
             E::widen(x, y);
             float o[kPer];
-            uint4 q = x;
+            Vec q = x;
 #pragma unroll
             for (int j = 0; j < kPer; ++j) o[j] = y[j] * scale;
             if (scale != 1.f && !wide) q = E::narrow(o);
@@ -630,7 +711,8 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
           for (int j = 0; j < kPer; ++j) {
             const float d = fmaf(y[j], sl2, -p.m), e = ex2(d);
             p.s[j & 1] += e;
-            if (kEnt) p.u[j & 1] = fmaf(e, fmaxf(d, -200.f), p.u[j & 1]);  // (0 times -inf is 0 here)
+            // (0 times -inf is 0 here)
+            if (kEnt) p.u[j & 1] = fmaf(e, kOp == kScore && E::kFloors ? d : fmaxf(d, -200.f), p.u[j & 1]);
           }
         }
       };
@@ -643,14 +725,14 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
         const Row& wn = other ? next : w;
         const int n0 = other ? begins(next) : b + kBatch < s1 ? b + kBatch : s1;
         const int nx = whole0(wn), ny = !(same || other) ? -1 : min(other ? finishes(next) : v1, whole1(wn)) - 32 - nx, nat = n0 + warp * 32 - nx;
-        const uint4* src = vec_at(wn, n0 + tid);
+        const Vec* src = vec_at(wn, n0 + tid);
         fresh = other;
         const int x0 = whole0(w), n32 = min(s1, whole1(w)) - 32 - x0, at = b + warp * 32 - x0;
         uint32_t rest = 0u;  // vectors at the ends
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-          const uint4 z = raw[i];
-          if (ny >= 0 && (uint32_t)(nat + i * kThreads) <= (uint32_t)ny) raw[i] = __ldcs(src + i * kThreads);
+          const Vec z = raw[i];
+          if (ny >= 0 && (uint32_t)(nat + i * kThreads) <= (uint32_t)ny) raw[i] = load_global(src + i * kThreads);
           if (n32 >= 0 && (uint32_t)(at + i * kThreads) <= (uint32_t)n32) dense(z, b + i * kThreads + tid, false);
           else rest |= 1u << i;
         }
@@ -687,7 +769,7 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
 #pragma unroll 1
       for (int b = begins(w) + tid; b - lane < e1; b += kThreads) {
         const int v = b * kPer - w.shift;
-        store_vec<kType>(false, w, d, make_uint4(0u, 0u, 0u, 0u), v - lane * kPer, b < e1 ? in_row<kPer>(v, V) : 0u, end, stage, lane);
+        store_vec<kType>(false, w, d, E::narrow(d), v - lane * kPer, b < e1 ? in_row<kPer>(v, V) : 0u, end, stage, lane);
       }
     }
     if (kOp != kGrad) {
