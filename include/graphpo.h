@@ -505,6 +505,65 @@ gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad
                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Distillation from a teacher's top tokens, on the same hidden states and matrix (the paper has no counterpart; a policy that
+ * samples its own rollouts learns from a larger model's distribution over the tokens of theirs).  For token t with
+ * the teacher's entries S (ids, and logits l or log-probabilities), z, lse and p as above, r the vocabulary outside S:
+ *
+ *   q_v = exp(scale_T l_v) / sum over S, q_r = 0                  (tail = 0: the teacher renormalised on its entries)
+ *   q_v = exp(l_v) / max(1, sum), q_r = 1 - sum of q_v            (tail = 1: all other tokens one more outcome; 0 without any)
+ *   rest_lse = log sum_{v in r} exp z_v      p_r = exp(rest_lse - lse)
+ *   loss_t = sum_{v in S} q_v log(q_v / p_v) + q_r log(q_r / p_r)      delta_v = p_v - q_v (v in S)      rest = p_r - q_r
+ *   dz_v = grad_loss_t delta_v (v in S),      grad_loss_t rest exp(z_v - rest_lse) (elsewhere)
+ *   d_hidden_t = scale sum_v dz[t][v] weight_v    d_weight_v = scale sum_t dz[t][v] hidden_t
+ *
+ * The entries are kept out of the sum over the other tokens, so that rest, delta and the gradient have their
+ * digits where p or q is nearly 1.  dz is rounded to the operands' type once, and the gradients after it: they have the
+ * error of up to 1.5 roundings.  Products, sums and their order as for gpo_vocab_logp and gpo_vocab_grad.
+ *
+ * An id below 0 is no entry (a teacher with fewer; its delta is 0); an entry whose logit is -inf is one of probability 0.  A token
+ * without entries, or with tail = 0 without one above -inf, has no teacher: its outputs are 0, it has no gradient, and its
+ * hidden row (NaN, say) reaches no other result.  Nor does that of a token whose grad_loss is 0.  Found on the GPU and returned by
+ * gpo_sync_status: an id >= vocab, the same id twice in a row (GPO_ERR_SHAPE; the gradient does not look for the second), a
+ * teacher's logit that is NaN or +inf (GPO_ERR_NONFINITE); the call's outputs are then undefined. */
+#define GPO_MAX_TEACHER 512 /* entries of a token's teacher */
+
+typedef struct {
+  int64_t k;             /* entries per token, 1 .. GPO_MAX_TEACHER */
+  int64_t ids_stride;    /* elements between rows, >= k */
+  int64_t logits_stride; /* the same of the logits */
+  const void* ids;       /* [T x ids_stride] int32 or int64, in any order */
+  const void* logits;    /* [T x logits_stride] logits, or with tail log-probabilities (not read by the gradient) */
+  int32_t id_bytes;      /* bytes of one id: 4 or 8 */
+  int32_t dtype;         /* gpo_dtype of logits */
+  int32_t tail;          /* the log-probabilities' remainder is one more outcome */
+  double scale;          /* of the logits, in [1e-4, 1e4]; 1 with tail */
+} gpo_teacher;
+
+typedef struct {
+  float* loss;           /* [T] */
+  float* delta;          /* [T x delta_stride] p - q of the entries, in the order that they have in ids */
+  float* rest;           /* [T] */
+  float* rest_lse;       /* [T] -inf where the entries are the whole vocabulary */
+  float* lse;            /* [T] optional */
+  int64_t delta_stride;  /* >= k */
+} gpo_distill_outputs;
+
+typedef struct {
+  const float* grad_loss; /* [T] d loss / d loss_t */
+  const float* delta;     /* of gpo_vocab_distill */
+  const float* rest;
+  const float* rest_lse;
+  int64_t delta_stride;   /* >= k */
+} gpo_distill_grad_inputs;
+
+/* Of gpo_vocab target and id_bytes are not read.  Workspace, checks and errors as for gpo_vocab_logp. */
+gpo_status gpo_vocab_distill_workspace_size(const gpo_vocab* v, const gpo_teacher* t, int gradient, size_t* bytes);
+gpo_status gpo_vocab_distill(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher* t, const gpo_distill_outputs* out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+gpo_status gpo_vocab_distill_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher* t, const gpo_distill_grad_inputs* in,
+                                  const gpo_vocab_grads* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Logits as a sampler takes them (GraphPO samples its rollouts from the policy; the paper has no counterpart of these
  * calls): penalties for the tokens that a row has had, biases, a mask, a scale; the statistics of the distribution that is
  * sampled from, of which gpo_loss_inputs.old_logp and logp are the log-probabilities; and the gradient back to the raw

@@ -104,6 +104,20 @@ class CEmbedding(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("id_bytes", ctypes.c_int32), ("scale", ctypes.c_double)]
 
 
+class CTeacher(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int64), ("ids_stride", ctypes.c_int64), ("logits_stride", ctypes.c_int64), ("ids", ctypes.c_void_p),
+                ("logits", ctypes.c_void_p), ("id_bytes", ctypes.c_int32), ("dtype", ctypes.c_int32), ("tail", ctypes.c_int32),
+                ("scale", ctypes.c_double)]
+
+
+class DistillOutputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("loss", "delta", "rest", "rest_lse", "lse")] + [("delta_stride", ctypes.c_int64)]
+
+
+class DistillGradInputs(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("grad_loss", "delta", "rest", "rest_lse")] + [("delta_stride", ctypes.c_int64)]
+
+
 class CLogits(ctypes.Structure):
     _fields_ = [("num_rows", ctypes.c_int64), ("vocab", ctypes.c_int64), ("logits_stride", ctypes.c_int64), ("logits", ctypes.c_void_p),
                 ("dtype", ctypes.c_int32), ("history_bytes", ctypes.c_int32), ("bias_bytes", ctypes.c_int32),
@@ -133,7 +147,9 @@ EXPORTS = ["gpo_create", "gpo_workspace_size", "gpo_compute", "gpo_sync_status",
            "gpo_last_error", "gpo_version", "gpo_destroy", "gpo_enable_timing", "gpo_stage_times", "gpo_compute_noalloc",
            "gpo_compute_groups", "gpo_compute_host", "gpo_loss_plan_size", "gpo_loss_plan", "gpo_token_loss",
            "gpo_layer_budget", "gpo_vocab_workspace_size", "gpo_vocab_logp", "gpo_vocab_grad", "gpo_vocab_grad_logp",
-           "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad", "gpo_logits_adjust", "gpo_logits_grad"]
+           "gpo_embed_workspace_size", "gpo_embed", "gpo_embed_grad", "gpo_logits_adjust", "gpo_logits_grad",
+           "gpo_vocab_distill_workspace_size", "gpo_vocab_distill", "gpo_vocab_distill_grad"]
+MAX_TEACHER = 512  # entries of a token's teacher
 
 FUSED_MAX_STATES = 384  # largest group the group-resident path (and gpo_compute_groups) serves
 
@@ -141,8 +157,8 @@ _lib = None
 _fast = {}  # the calls of every step once more, with their structs as packed bytes (see _pack)
 _lock = threading.Lock()
 
-# Packed images of gpo_vocab, gpo_vocab_outputs, gpo_vocab_grad_inputs, gpo_vocab_grads, gpo_embedding, gpo_logits,
-# gpo_logits_outputs and gpo_logits_grad_inputs: building a ctypes structure costs 2 us a call, packing one 0.5.
+# Packed images of gpo_vocab, gpo_vocab_outputs, gpo_vocab_grad_inputs, gpo_vocab_grads, gpo_embedding, gpo_teacher,
+# gpo_distill_outputs, gpo_distill_grad_inputs, gpo_logits, gpo_logits_outputs and gpo_logits_grad_inputs: building a ctypes structure costs 2 us a call, packing one 0.5.
 _PACK_VOCAB = struct.Struct("@5q3Q2id").pack
 _PACK_3 = struct.Struct("@3Q").pack
 _PACK_4 = struct.Struct("@4Q").pack
@@ -151,6 +167,9 @@ _PACK_EMBED = struct.Struct("@5qQ2id").pack
 _PACK_LOGITS = struct.Struct("@3qQ4i4Q4dQq3QqQQ2q2Q").pack
 _PACK_LOGITS_OUT = struct.Struct("@Qqi3Q").pack
 _PACK_5 = struct.Struct("@5Q").pack
+_PACK_TEACHER = struct.Struct("@3q2Q3id").pack
+_PACK_DISTILL_OUT = struct.Struct("@5Qq").pack
+_PACK_DISTILL_IN = struct.Struct("@4Qq").pack
 
 
 def lib_path() -> str:
@@ -238,8 +257,16 @@ def load(build_if_missing: bool = False):
         L.gpo_logits_adjust.restype = ctypes.c_int
         L.gpo_logits_grad.argtypes = [vp, ctypes.POINTER(CLogits), ctypes.POINTER(LogitsGradInputs), vp, ctypes.c_int64, vp]
         L.gpo_logits_grad.restype = ctypes.c_int
+        L.gpo_vocab_distill_workspace_size.argtypes = [ctypes.POINTER(CVocab), ctypes.POINTER(CTeacher), ctypes.c_int, ctypes.POINTER(sz)]
+        L.gpo_vocab_distill_workspace_size.restype = ctypes.c_int
+        L.gpo_vocab_distill.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(CTeacher), ctypes.POINTER(DistillOutputs), vp, sz, vp]
+        L.gpo_vocab_distill.restype = ctypes.c_int
+        L.gpo_vocab_distill_grad.argtypes = [vp, ctypes.POINTER(CVocab), ctypes.POINTER(CTeacher), ctypes.POINTER(DistillGradInputs),
+                                             ctypes.POINTER(VocabGrads), vp, sz, vp]
+        L.gpo_vocab_distill_grad.restype = ctypes.c_int
         raw = ctypes.c_char_p
-        for name, args in (("gpo_logits_adjust", [vp, raw, raw, vp]), ("gpo_logits_grad", [vp, raw, raw, vp, ctypes.c_int64, vp]),
+        for name, args in (("gpo_vocab_distill", [vp, raw, raw, raw, vp, sz, vp]), ("gpo_vocab_distill_grad", [vp, raw, raw, raw, raw, vp, sz, vp]),
+                           ("gpo_logits_adjust", [vp, raw, raw, vp]), ("gpo_logits_grad", [vp, raw, raw, vp, ctypes.c_int64, vp]),
                            ("gpo_vocab_logp", [vp, raw, raw, vp, sz, vp]), ("gpo_vocab_grad_logp", [vp, raw, raw, vp, raw, vp, sz, vp]),
                            ("gpo_embed", [vp, raw, vp, vp, vp, sz, vp]), ("gpo_embed_grad", [vp, raw, vp, vp, ctypes.c_int, vp, sz, vp])):
             f = L[name]  # (a function object of its own)
@@ -280,6 +307,16 @@ def vocab_workspace_size(v: CVocab, gradient: bool = False) -> int:
     code = load().gpo_vocab_workspace_size(ctypes.byref(v), int(gradient), ctypes.byref(n))
     if code != GPO_OK:
         raise GraphPOError(code, "gpo_vocab_workspace_size")
+    return n.value
+
+
+def distill_workspace_size(v: CVocab, t: CTeacher, gradient: bool = False) -> int:
+    """Device workspace bytes of gpo_vocab_distill, or with `gradient` of gpo_vocab_distill_grad, for these
+    sizes (no device needed)."""
+    n = ctypes.c_size_t()
+    code = load().gpo_vocab_distill_workspace_size(ctypes.byref(v), ctypes.byref(t), int(gradient), ctypes.byref(n))
+    if code != GPO_OK:
+        raise GraphPOError(code, "gpo_vocab_distill_workspace_size")
     return n.value
 
 
@@ -788,6 +825,93 @@ class GraphPO:
             self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), tp, code, idb, scale), ins, lp,
             _PACK_GRADS(0 if dh is None else dh.data_ptr(), 0 if dw is None else dw.data_ptr(), sh, sw, bool(accumulate)),
             wp, wn, on)
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def _taught(self, hidden, weight, ids):
+        """The checks that both directions of the distillation share: device, sizes, strides, codes."""
+        if len(hidden.shape) != 2 or len(weight.shape) != 2 or len(ids.shape) != 2:
+            raise ValueError("hidden must be [T, d], weight [V, d] and ids [T, k]")
+        dev, (T, d), V, K = hidden.get_device(), hidden.shape, weight.shape[0], ids.shape[1]
+        code = _dtype_code(hidden, "hidden")
+        hs = _matrix(hidden, "hidden", dev, T, d, hidden.dtype)
+        ws = _matrix(weight, "weight", dev, V, d, hidden.dtype)
+        idb = _id_bytes(ids, "ids")
+        ks = _matrix(ids, "ids", dev, T, K, ids.dtype)
+        if dev != self._device:
+            self._elsewhere(dev)
+        return dev, T, V, d, K, hs, ws, ks, code, idb
+
+    def vocab_distill(self, hidden, weight, ids, logits, scale=1.0, teacher_scale=1.0, tail=False, lse=False, out=None, workspace=None,
+                      stream=None) -> dict:
+        """Kullback-Leibler divergence from a teacher's top tokens to softmax(scale * hidden weight^T), hidden [T, d] and weight
+        [V, d] both bfloat16 or both float16, without ever storing the logits: ids [T, k] (int32 or int64, k up to 512, in any
+        order; below 0: no entry) and the teacher's logits [T, k] (bfloat16, float16 or float32), renormalised as
+        softmax(teacher_scale * logits); or with `tail` its log-probabilities, all other tokens one more outcome.  Returns
+        {"loss": [T] float32, "delta": [T, k] (p - q of the entries), "rest": [T] (of the other tokens together), "rest_lse": [T]
+        (their log-sum-exp), "lse" (of all, if lse)}, or fills `out`; vocab_distill_grad takes delta, rest and rest_lse.  A token
+        without entries: zeros.  Enqueued on the current stream; workspace and check() as for vocab_logp."""
+        import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.vocab_distill(hidden, weight, ids, logits, scale, teacher_scale, tail, lse, out, workspace)
+        dev, T, V, d, K, hs, ws, ks, code, idb = self._taught(hidden, weight, ids)
+        f32 = torch.float32
+        tc = _dtype_code(logits, "logits")
+        ls = _matrix(logits, "logits", dev, T, K, logits.dtype)
+        if out is None:
+            out = {k: torch.empty(T, dtype=f32, device=hidden.device) for k in ("loss", "rest", "rest_lse") + (("lse",) if lse else ())}
+            out["delta"] = torch.empty(T, K, dtype=f32, device=hidden.device)
+        delta = out["delta"]
+        ds = _matrix(delta, "delta", dev, T, K, f32)
+        po = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("loss", "rest", "rest_lse", "lse")]
+        on = _stream_handle(dev)
+        room, wp, wn = self._room((4, T, V, d, K), lambda: distill_workspace_size(
+            CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), CTeacher(K, K, K, None, None, 4, 0, 0, 1.0)), hidden.device, workspace, on)
+        code = _fast["gpo_vocab_distill"](
+            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), 0, code, 4, scale),
+            _PACK_TEACHER(K, ks, ls, ids.data_ptr(), logits.data_ptr(), idb, tc, bool(tail), teacher_scale),
+            _PACK_DISTILL_OUT(po[0], delta.data_ptr(), po[1], po[2], po[3], ds), wp, wn, on)
+        if code != GPO_OK:
+            raise GraphPOError(code, self.last_error())
+        return out
+
+    def vocab_distill_grad(self, hidden, weight, ids, delta, rest, rest_lse, grad_loss, scale=1.0, accumulate=False, d_hidden=True,
+                           d_weight=True, out=None, workspace=None, stream=None) -> dict:
+        """Gradients {"d_hidden": [T, d], "d_weight": [V, d]} (each if asked for) of a loss with the gradient grad_loss [T]
+        float32 with respect to vocab_distill's losses, whose delta, rest and rest_lse are given; or fills `out`, with
+        `accumulate` adding to out["d_weight"].  Enqueued on the current stream; workspace and check() as for vocab_logp."""
+        import torch
+        if stream is not None:  # (what the call allocates belongs to the stream that uses it)
+            with torch.cuda.stream(stream):
+                return self.vocab_distill_grad(hidden, weight, ids, delta, rest, rest_lse, grad_loss, scale, accumulate, d_hidden, d_weight,
+                                               out, workspace)
+        dev, T, V, d, K, hs, ws, ks, code, idb = self._taught(hidden, weight, ids)
+        f32, dt = torch.float32, hidden.dtype
+        ds = _matrix(delta, "delta", dev, T, K, f32)
+        ins = _PACK_DISTILL_IN(_vector(grad_loss, "grad_loss", dev, T, f32), delta.data_ptr(), _vector(rest, "rest", dev, T, f32),
+                               _vector(rest_lse, "rest_lse", dev, T, f32), ds)
+        if out is None:
+            if accumulate and d_weight:
+                raise ValueError("accumulate needs the d_weight to add to in `out`")
+            out = {}
+            if d_hidden:
+                out["d_hidden"] = torch.empty(T, d, dtype=dt, device=hidden.device)
+            if d_weight:
+                out["d_weight"] = torch.empty(V, d, dtype=dt, device=hidden.device)
+        dh, dw = out.get("d_hidden"), out.get("d_weight")
+        sh = 0 if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
+        sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
+        if T == 0 and dw is None:
+            return out
+        on = _stream_handle(dev)
+        room, wp, wn = self._room((5, T, V, d, K), lambda: distill_workspace_size(
+            CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), CTeacher(K, K, K, None, None, 4, 0, 0, 1.0), True), hidden.device, workspace, on)
+        code = _fast["gpo_vocab_distill_grad"](
+            self._h, _PACK_VOCAB(T, V, d, hs, ws, hidden.data_ptr(), weight.data_ptr(), 0, code, 4, scale),
+            _PACK_TEACHER(K, ks, K, ids.data_ptr(), 0, idb, 0, 0, 1.0), ins,
+            _PACK_GRADS(0 if dh is None else dh.data_ptr(), 0 if dw is None else dw.data_ptr(), sh, sw, bool(accumulate)), wp, wn, on)
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out

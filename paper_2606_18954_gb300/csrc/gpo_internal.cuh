@@ -1050,6 +1050,11 @@ struct VocabArgs {
   int w_blocks;          // the matrix's rows are whole blocks of 64 columns (maps.wb)
   int dw_bulk;           // d_weight's rows take bulk stores (maps.dw)
   int debug_timeout;
+  // distillation: each token's teacher entries by id, top_n of them in rows of top_stride, and their logits in units of log 2
+  const int* top_id;
+  const int* top_n;
+  float* top_z;
+  int64_t top_stride;
 };
 
 // Tensor maps of one call.  K innermost, boxes of 64 x 128: hidden rows as given (few tokens: 64 x
@@ -1067,11 +1072,16 @@ cudaError_t setup_vocab();
 cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
 // The same of the tokens with a gradient, in the order of their targets.
 cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
+// The same of the tokens with a target of 0, in their own order and without a place for what rounding takes at a target;
+// bound: [T] what |dz| of a token is at most.
+cudaError_t launch_vocab_order_taught(const LaunchCtx& lc, const VocabArgs& a, const float* bound, const Status& st);
 // Up to kVocabFew tokens; marks: [kVocabFewCtas] in the workspace, mark: a value that no other call leaves there.
 cudaError_t setup_vocab_few();
 cudaError_t launch_vocab_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent,
                              uint64_t* marks, uint64_t mark);
 cudaError_t launch_vocab_lse(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent);
+// The same of the tokens that have a teacher: its entries' logits apart from the sums over the others.
+cudaError_t launch_vocab_taught(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);
 cudaError_t launch_vocab_join(const LaunchCtx& lc, const VocabArgs& a, const Status& st, bool ent);
 cudaError_t launch_vocab_dz(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);
 cudaError_t launch_vocab_products(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st);
@@ -1099,6 +1109,44 @@ int embed_piece(int64_t T);  // sorted tokens of one piece, for T tokens
 cudaError_t setup_embed();
 cudaError_t launch_embed(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
 cudaError_t launch_embed_grad(const LaunchCtx& lc, const EmbedArgs& a, const Status& st);
+
+// ------------------------------------------------------------------ distillation
+
+constexpr int kTeachMax = 512;  // entries of a teacher
+
+struct TeachArgs {
+  int64_t T, V;
+  int k;
+  const void* ids;               // [T x ids_stride]
+  int64_t ids_stride;
+  int id8;
+  const void* logits;            // [T x logits_stride] the teacher's
+  int64_t logits_stride;
+  int dtype;
+  float scale;                   // of them
+  int tail;                      // they are log-probabilities, and the other tokens one more outcome
+  // the entries by id, in rows of `stride`: ids, places in the given order, probabilities and their logarithms; their
+  // number, and the probability of the others
+  int64_t stride;
+  int *id, *n;
+  int16_t* place;
+  float *q, *lq, *qr;
+  int* target;                   // 0: has a teacher, -1: has none
+  // results
+  float *loss, *lse, *rest, *rest_lse, *delta;
+  int64_t delta_stride;
+  // gradient
+  const float *g, *delta_in, *rest_in, *rest_lse_in;
+  float *dense, *dense_lse, *bound;  // [T] for vocab_pair_kernel: g, lse; |g|
+  int *none;                     // [T] -1
+};
+
+cudaError_t launch_teach_sort(const LaunchCtx& lc, const TeachArgs& t, const Status& st);
+// Joins the parts of vocab_pair_kernel's sums (a) with the entries' logits.
+cudaError_t launch_teach_join(const LaunchCtx& lc, const TeachArgs& t, const VocabArgs& a, const Status& st);
+cudaError_t launch_teach_grad(const LaunchCtx& lc, const TeachArgs& t, const Status& st);
+// dz of the entries that are in the piece of a.
+cudaError_t launch_teach_entries(const LaunchCtx& lc, const TeachArgs& t, const VocabArgs& a, const Status& st);
 
 // ------------------------------------------------------------------ adjusted logits
 

@@ -1,0 +1,258 @@
+// Distillation from a teacher's top tokens: what goes before and after the products of gpo_vocab.cu (formulas in
+// include/graphpo.h).
+//
+// Forward:  teach_sort_kernel   a warp per token puts the teacher's entries in the order of their ids (by counting the smaller
+//                               ones: k^2 / 32 comparisons a lane) with their probabilities
+//           vocab_pair_kernel   <kLseTop>: logits tiles that stay in tensor memory; a row's entries are taken out of its
+//                               maximum and sum, which are then those of the other tokens
+//           teach_join_kernel   the parts of a row joined, divergence and p - q from them and the entries' logits
+// Gradient: outside the entries dz is g (p - q of all others together) times the softmax over the others, for either form of the
+//           loss; inside it is g (p - q).  So vocab_pair_kernel's dz of a token without a target, with the others' log-sum-exp,
+//           is right for all but the entries, which teach_entries_kernel writes over it, rounded once; then the products.
+// Keeping the entries out of the sum over the others keeps the digits of both: where the student is nearly certain of one
+// of the teacher's tokens, 1 - p is a sum of small terms here, and so is the others' share p_r.
+#define GPO_REPORT __noinline__
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "gpo_vocab_math.cuh"
+
+namespace gpo {
+
+namespace {
+
+constexpr int kSortWarps = 4;
+constexpr int kNoId = 0x7fffffff;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float load_value(const void* p, int dtype, int64_t i) {
+  if (dtype == GPO_DT_F32) return static_cast<const float*>(p)[i];
+  if (dtype == GPO_DT_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+  return __half2float(static_cast<const __half*>(p)[i]);
+}
+
+template <class F>
+__device__ __forceinline__ float over_warp(float x, F f) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float warp_max(float x) { return over_warp(x, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float warp_sum(float x) { return over_warp(x, [](float a, float b) { return a + b; }); }
+// The lowest index (below 2^31) of any lane.
+__device__ __forceinline__ int warp_first(int x) { return (int)__reduce_min_sync(0xffffffffu, (unsigned)x); }
+
+__global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t, Status st) {
+  __shared__ int s_id[kSortWarps][kTeachMax];
+  __shared__ float s_v[kSortWarps][kTeachMax];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  let_next_start();
+  const int64_t tok = (int64_t)blockIdx.x * kSortWarps + warp;
+  if (tok >= t.T) return;
+  int *ids = s_id[warp], n = 0;
+  float *v = s_v[warp], m = -INFINITY;
+  bool bad = false;
+  for (int j = lane; j < t.k; j += 32) {
+    const int64_t id = load_id(t.ids, t.id8, tok * t.ids_stride + j);
+    const bool in = id >= 0 && id < t.V;
+    if (id >= t.V) report(st, GPO_ERR_SHAPE, 50, (int)tok);
+    ids[j] = in ? (int)id : kNoId;
+    const float x = in ? load_value(t.logits, t.dtype, tok * t.logits_stride + j) : -INFINITY;
+    bad |= !(x < INFINITY);
+    v[j] = x * t.scale;
+    m = fmaxf(m, v[j]);
+    n += in;
+  }
+  n = __reduce_add_sync(0xffffffffu, n);
+  m = warp_max(m);
+  if (__any_sync(0xffffffffu, bad)) {
+    if (lane == 0) report(st, GPO_ERR_NONFINITE, 51, (int)tok);
+    n = 0;
+  }
+  if (!t.tail && m == -INFINITY) n = 0;  // (no distribution)
+  __syncwarp();
+  float shift = 0.f, qr = 0.f;  // log q = v - shift
+  if (n > 0 && !t.tail) {
+    // the largest apart: log q of a nearly certain token has its digits
+    int first = kNoId;
+    for (int j = lane; j < t.k; j += 32)
+      if (v[j] == m) first = min(first, j);
+    first = warp_first(first);
+    float others = 0.f;
+    for (int j = lane; j < t.k; j += 32)
+      if (j != first) others += expf(v[j] - m);
+    shift = log1pf(warp_sum(others));
+  } else if (n > 0) {
+    // (in 64 bits: 1 - the sum may be small)
+    double sum = 0.0;
+    for (int j = lane; j < t.k; j += 32) sum += (double)expf(v[j]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    m = 0.f;
+    if (sum > 1.0) shift = logf((float)sum);  // (probabilities rounded to fewer bits)
+    else qr = (float)(1.0 - sum);
+  }
+  float* delta = t.delta + tok * t.delta_stride;
+  for (int j = lane; j < t.k; j += 32) {
+    if (n == 0 || ids[j] == kNoId) {
+      delta[j] = 0.f;
+      continue;
+    }
+    int rank = 0;
+    bool twice = false;
+    for (int i = 0; i < t.k; ++i) {
+      rank += ids[i] < ids[j] || (ids[i] == ids[j] && i < j);
+      twice |= ids[i] == ids[j] && i != j;
+    }
+    if (twice) report(st, GPO_ERR_SHAPE, 52, (int)tok);
+    const int64_t at = tok * t.stride + rank;
+    const float lq = v[j] - m - shift;
+    t.id[at] = ids[j];
+    t.place[at] = (int16_t)j;
+    t.lq[at] = lq;
+    t.q[at] = expf(lq);
+  }
+  if (lane == 0) {
+    t.n[tok] = n;
+    t.qr[tok] = qr;
+    t.target[tok] = n > 0 ? 0 : -1;
+    if (n == 0) {
+      t.loss[tok] = 0.f;
+      t.rest[tok] = 0.f;
+      t.rest_lse[tok] = 0.f;
+      if (t.lse) t.lse[tok] = 0.f;
+    }
+  }
+}
+
+// A CTA takes 32 rows: their parts by its warps in turn, then a row each.
+__global__ void __launch_bounds__(1024) teach_join_kernel(TeachArgs t, VocabArgs a, int parts) {
+  __shared__ Part red[32][33];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  after_previous();
+  const int rows = a.idx ? a.head->rows : (int)a.T, row0 = blockIdx.x * 32;
+  if (row0 >= rows) return;
+  Part p = {kLow, 0.f, 0.f};
+  if (row0 + lane < rows) {
+#pragma unroll 8
+    for (int i = warp; i < parts; i += 32) {
+      const int64_t at = (row0 + lane) * a.part_row + (int64_t)i * a.part_col;
+      p = join<false>(p, Part{a.pm[at], a.ps[at], 0.f});
+    }
+  }
+  red[warp][lane] = p;
+  __syncthreads();
+  if (row0 + warp >= rows) return;
+  const int64_t tok = a.idx ? a.idx[row0 + warp] : row0 + warp;
+  const int n = t.n[tok];
+  if (n == 0) return;
+  p = red[lane][warp];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    p = join<false>(p, Part{__shfl_xor_sync(0xffffffffu, p.m, o), __shfl_xor_sync(0xffffffffu, p.s, o), 0.f});
+  // logits in units of log 2; the largest entry apart
+  const float *z = a.top_z + tok * t.stride, *q = t.q + tok * t.stride, *lq = t.lq + tok * t.stride;
+  float most = -INFINITY;
+  for (int j = lane; j < n; j += 32) most = fmaxf(most, z[j]);
+  most = warp_max(most);
+  int first = kNoId;
+  for (int j = lane; j < n; j += 32)
+    if (z[j] == most) first = min(first, j);
+  first = warp_first(first);  // (none where they are NaN)
+  const bool some = p.s > 0.f;  // tokens other than the entries
+  const float top = some ? fmaxf(p.m, most) : most, er = some ? p.s * exp2f(p.m - top) : 0.f, ef = exp2f(most - top);
+  float others = 0.f, q_others = 0.f;
+  for (int j = lane; j < n; j += 32) {
+    if (j == first) continue;
+    others += exp2f(z[j] - top);
+    q_others += q[j];
+  }
+  others = warp_sum(others) + er;
+  const float qr = some ? t.qr[tok] : 0.f;  // (of no tokens: what the teacher's probabilities were rounded by)
+  q_others = warp_sum(q_others) + qr;
+  const float total = others + ef, lt = top == most ? log1pf(others) : logf(total), inv = 1.f / total;
+  float loss = 0.f;
+  float* delta = t.delta + tok * t.delta_stride;
+  for (int j = lane; j < n; j += 32) {
+    const float y = z[j] - top, qj = q[j];
+    if (qj > 0.f) loss = fmaf(qj, lq[j] - fmaf(y, kLn2, -lt), loss);
+    // (1 - q less 1 - p of the largest, whose digits p and q may not have)
+    delta[t.place[tok * t.stride + j]] = j == first ? q_others - others * inv : fmaf(exp2f(y), inv, -qj);
+  }
+  loss = warp_sum(loss);
+  if (lane == 0) {
+    const float log_others = some ? fmaf(p.m, kLn2, logf(p.s)) : -INFINITY;
+    if (qr > 0.f) loss = fmaf(qr, logf(qr) - (fmaf(p.m - top, kLn2, logf(p.s)) - lt), loss);
+    t.loss[tok] = loss;
+    t.rest[tok] = er * inv - qr;
+    t.rest_lse[tok] = log_others;
+    if (t.lse) t.lse[tok] = fmaf(top, kLn2, lt);
+  }
+}
+
+// What vocab_pair_kernel's dz takes of a token, and whether it has a gradient.
+__global__ void __launch_bounds__(256) teach_grad_kernel(TeachArgs t, Status st) {
+  const int lane = threadIdx.x & 31;
+  let_next_start();
+  const int64_t tok = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (tok >= t.T) return;
+  bool some = false;
+  for (int j = lane; j < t.k; j += 32) {
+    const int64_t id = load_id(t.ids, t.id8, tok * t.ids_stride + j);
+    if (id >= t.V) report(st, GPO_ERR_SHAPE, 53, (int)tok);
+    some |= id >= 0 && id < t.V;
+  }
+  some = __any_sync(0xffffffffu, some);
+  if (lane != 0) return;
+  const float g = t.g[tok], lse = t.rest_lse_in[tok];
+  const bool live = some && g != 0.f;
+  t.target[tok] = live ? 0 : -1;
+  t.none[tok] = -1;
+  t.dense[tok] = live ? -g * t.rest_in[tok] : 0.f;
+  t.dense_lse[tok] = lse == -INFINITY ? INFINITY : lse;  // (no other tokens: their p is 0)
+  t.bound[tok] = live ? fabsf(g) : 0.f;
+}
+
+__global__ void __launch_bounds__(256) teach_entries_kernel(TeachArgs t, VocabArgs a, Status st) {
+  const int lane = threadIdx.x & 31;
+  let_next_start();
+  after_previous();
+  const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), nwarps = (int64_t)gridDim.x * 8;
+  const int rows = a.head->rows;
+  const float gs = a.head->dz_scale;
+  for (int64_t r = warp; r < rows; r += nwarps) {
+    const int64_t tok = a.idx[r];
+    const float g = t.g[tok] * gs;
+    for (int j = lane; j < t.k; j += 32) {
+      const int64_t id = load_id(t.ids, t.id8, tok * t.ids_stride + j);
+      if (id < a.v0 || id >= a.v0 + a.vn || id >= t.V) continue;
+      const float x = g * t.delta_in[tok * t.delta_stride + j];
+      if (!GPO_BOUNDS(st, id - a.v0, a.dz_stride, kWhereVocabRow)) continue;
+      uint16_t* dst = a.dz + r * a.dz_stride + (id - a.v0);
+      if (a.f16) *reinterpret_cast<__half*>(dst) = __float2half_rn(x);
+      else *reinterpret_cast<__nv_bfloat16*>(dst) = __float2bfloat16_rn(x);
+    }
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_teach_sort(const LaunchCtx& lc, const TeachArgs& t, const Status& st) {
+  teach_sort_kernel<<<(unsigned)((t.T + kSortWarps - 1) / kSortWarps), 32 * kSortWarps, 0, lc.stream>>>(t, st);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_teach_join(const LaunchCtx& lc, const TeachArgs& t, const VocabArgs& a, const Status&) {
+  return launch_after(teach_join_kernel, (unsigned)((t.T + 31) / 32), 1024, 0, lc.stream, t, a, (int)vocab_parts(t.V));
+}
+
+cudaError_t launch_teach_grad(const LaunchCtx& lc, const TeachArgs& t, const Status& st) {
+  teach_grad_kernel<<<(unsigned)((t.T + 7) / 8), 256, 0, lc.stream>>>(t, st);
+  return cudaGetLastError();
+}
+
+cudaError_t launch_teach_entries(const LaunchCtx& lc, const TeachArgs& t, const VocabArgs& a, const Status& st) {
+  return launch_after(teach_entries_kernel, (unsigned)std::min<int64_t>((t.T + 7) / 8, (int64_t)lc.num_sms * 8), 256, 0, lc.stream, t, a, st);
+}
+
+}  // namespace gpo

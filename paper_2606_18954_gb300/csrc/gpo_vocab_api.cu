@@ -1,5 +1,5 @@
 // Host side of the vocabulary ends (gpo_vocab_*, gpo_embed*): argument checks, workspace layout,
-// tensor maps and the launch sequences of gpo_vocab.cu and gpo_embed.cu.
+// tensor maps and the launch sequences of gpo_vocab.cu, gpo_teach.cu and gpo_embed.cu.
 #include <atomic>
 #include <cmath>
 #include <cstring>
@@ -22,8 +22,8 @@ struct VocabLayout {
 
 int64_t up_to(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
-// The workspace of either direction; no pointers are read.
-void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
+// The workspace of either direction; no pointers are read.  (taught: of a distillation, which always goes in tiles.)
+void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L, bool taught = false) {
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -34,7 +34,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L = VocabLayout();
   L.tp = up_to(T, kPairM);
   L.hc_stride = up_to(v.d, 64);  // rows of whole 128-byte lines
-  L.few = !grad && T <= kVocabFew;
+  L.few = !grad && !taught && T <= kVocabFew;
   L.listed = grad || (!L.few && (double)T * (double)v.vocab * (double)v.d >= (double)kVocabListed);
   if (T > 0 && L.few) L.marks = take(sizeof(uint64_t) * kVocabFewCtas);
   L.head = take(sizeof(VocabHead));
@@ -65,7 +65,7 @@ void vocab_layout(const gpo_vocab& v, bool grad, VocabLayout& L) {
   L.total = o;
 }
 
-gpo_status check_sizes(gpo_ctx* c, const gpo_vocab* v) {
+gpo_status check_sizes(gpo_ctx* c, const gpo_vocab* v, bool targets = true) {
   if (!v) return set_msg(c, "vocab arguments NULL"), GPO_ERR_INVALID_ARG;
   if (v->num_tokens < 0 || v->vocab < 1 || v->d < 1) return set_msg(c, "negative size, or vocab or d < 1"), GPO_ERR_INVALID_ARG;
   if (v->num_tokens > kMaxCount || v->vocab > kMaxCount || v->d > kMaxCount)
@@ -79,19 +79,19 @@ gpo_status check_sizes(gpo_ctx* c, const gpo_vocab* v) {
   if (tiles >= 1e9) return set_msg(c, "too many logits"), GPO_ERR_UNSUPPORTED;
   if (v->dtype != GPO_DT_BF16 && v->dtype != GPO_DT_F16)
     return set_msg(c, "hidden and weight must be bf16 or fp16"), v->dtype == GPO_DT_F32 ? GPO_ERR_UNSUPPORTED : GPO_ERR_INVALID_ARG;
-  if (v->id_bytes != 4 && v->id_bytes != 8) return set_msg(c, "id_bytes must be 4 or 8"), GPO_ERR_INVALID_ARG;
+  if (targets && v->id_bytes != 4 && v->id_bytes != 8) return set_msg(c, "id_bytes must be 4 or 8"), GPO_ERR_INVALID_ARG;
   return GPO_OK;
 }
 
-gpo_status check_vocab(gpo_ctx* c, const gpo_vocab* v) {
-  gpo_status s = check_sizes(c, v);
+gpo_status check_vocab(gpo_ctx* c, const gpo_vocab* v, bool targets = true) {
+  gpo_status s = check_sizes(c, v, targets);
   if (s != GPO_OK) return s;
   if (!(v->scale >= 1e-4 && v->scale <= 1e4)) return set_msg(c, "scale outside [1e-4, 1e4]"), GPO_ERR_INVALID_ARG;
-  if (!v->weight || (v->num_tokens > 0 && (!v->hidden || !v->target)))
+  if (!v->weight || (v->num_tokens > 0 && (!v->hidden || (targets && !v->target))))
     return set_msg(c, "hidden, weight or target NULL"), GPO_ERR_INVALID_ARG;
   if (v->hidden_stride % 8 != 0 || v->weight_stride % 8 != 0)
     return set_msg(c, "row bytes of hidden and weight must be a multiple of 16"), GPO_ERR_UNSUPPORTED;
-  if (!aligned(v->weight, 16) || !aligned(v->hidden, 16) || !aligned(v->target, (size_t)v->id_bytes))
+  if (!aligned(v->weight, 16) || !aligned(v->hidden, 16) || (targets && !aligned(v->target, (size_t)v->id_bytes)))
     return set_msg(c, "hidden and weight must be 16-byte aligned, targets to their size"), GPO_ERR_UNSUPPORTED;
   return GPO_OK;
 }
@@ -121,6 +121,7 @@ bool encode_blocks(CUtensorMap* m, EncodeTiledFn enc, const void* base, int64_t 
 // Words of captured calls: the library's, as a graph may be replayed after its context is gone.  (A process that captures
 // more calls than there are gives words out again: a call may then return another's error, or stop at it.)
 __device__ __align__(256) uint32_t g_captured_words[kCapturedWords * kStatusWords];
+
 template <class P>
 P* at(void* base, size_t off) { return reinterpret_cast<P*>(static_cast<unsigned char*>(base) + off); }
 
@@ -172,6 +173,57 @@ gpo_status vocab_args(gpo_ctx* ctx, const gpo_vocab& v, const VocabLayout& L, vo
   }
   if (!ok) return set_msg(ctx, "cuTensorMapEncodeTiled failed"), GPO_ERR_UNSUPPORTED;
   return GPO_OK;
+}
+
+// The checks of either gradient's outputs.
+gpo_status check_grads(gpo_ctx* ctx, const gpo_vocab& v, const gpo_vocab_grads& out) {
+  if (!out.d_weight && !out.d_hidden) return set_msg(ctx, "neither d_hidden nor d_weight is given"), GPO_ERR_INVALID_ARG;
+  if ((out.d_hidden && out.d_hidden_stride < v.d) || (out.d_weight && out.d_weight_stride < v.d))
+    return set_msg(ctx, "row stride of a gradient < d"), GPO_ERR_INVALID_ARG;
+  if (!aligned(out.d_hidden, 2) || !aligned(out.d_weight, 2)) return set_msg(ctx, "gradients must be 2-byte aligned"), GPO_ERR_UNSUPPORTED;
+  if ((out.d_hidden && (double)v.num_tokens * (double)out.d_hidden_stride >= (double)kMaxMatrix) ||
+      (out.d_weight && (double)v.vocab * (double)out.d_weight_stride >= (double)kMaxMatrix))
+    return set_msg(ctx, "gradient too large"), GPO_ERR_UNSUPPORTED;
+  return GPO_OK;
+}
+
+// Gradients of no tokens.
+gpo_status no_tokens(gpo_ctx* ctx, const gpo_vocab& v, const gpo_vocab_grads& out, void* stream) {
+  ctx->nstages = 0;
+  if (out.d_weight && !out.accumulate) {
+    const cudaError_t e = cudaMemset2DAsync(out.d_weight, 2 * (size_t)out.d_weight_stride, 0, 2 * (size_t)v.d, (size_t)v.vocab,
+                                            static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) return set_msg(ctx, "memset failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
+  }
+  return GPO_OK;
+}
+
+// The arguments that either gradient has.
+void grad_args(const gpo_vocab& v, const gpo_vocab_grads& out, const VocabLayout& L, void* workspace, VocabArgs& a) {
+  a.sl2 = logit_scale(v, 64 * kVocabDzSeg);
+  a.weight = v.weight;
+  a.weight_stride = v.weight_stride;
+  a.by_target = at<int>(workspace, L.by_target);
+  a.tile_first = at<int>(workspace, L.tile_first);
+  a.rest = at<float>(workspace, L.rest);
+  a.dz = at<uint16_t>(workspace, L.dz);
+  a.dz_stride = L.piece;
+  a.acc = L.acc ? at<float>(workspace, L.acc) : nullptr;
+  a.acc_rows = L.tp;
+  a.acc_stride = L.acc_stride;
+  a.splits = out.d_hidden ? L.splits : 1;
+  a.dh = out.d_hidden;
+  a.dh_stride = out.d_hidden_stride;
+  a.dw = out.d_weight;
+  a.dw_stride = out.d_weight_stride;
+  a.accumulate = out.accumulate != 0;
+}
+
+// Whether d_weight's rows leave as bulk stores, and their tensor map.
+// (a bulk store leaves out what lies past the matrix, but not to the element: of an odd width it wrote one more)
+bool bulk_rows(const gpo_vocab& v, const VocabArgs& a, VocabMaps& m) {
+  return a.dw && !a.accumulate && v.d % 8 == 0 && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
+         encode_map(&m.dw, encode_fn(), a.dw, v.d, v.vocab, a.dw_stride, a.f16, 32);
 }
 
 }  // namespace
@@ -314,31 +366,18 @@ gpo_status gpo_vocab_grad_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab
   if (s != GPO_OK) return s;
   const int64_t T = v->num_tokens;
   if (!in || !out) return set_msg(ctx, "inputs or outputs NULL"), GPO_ERR_INVALID_ARG;
-  if (!out->d_weight && (!out->d_hidden || T == 0) && !(T == 0 && out->d_hidden))
-    return set_msg(ctx, "neither d_hidden nor d_weight is given"), GPO_ERR_INVALID_ARG;
   if (T > 0 && (!in->lse || !in->grad_logp || (in->grad_entropy && !in->entropy)))
     return set_msg(ctx, "lse, grad_logp or (with grad_entropy) entropy NULL"), GPO_ERR_INVALID_ARG;
-  if ((out->d_hidden && out->d_hidden_stride < v->d) || (out->d_weight && out->d_weight_stride < v->d))
-    return set_msg(ctx, "row stride of a gradient < d"), GPO_ERR_INVALID_ARG;
   if (!aligned(in->lse, 4) || !aligned(in->grad_logp, 4) || !aligned(in->entropy, 4) || !aligned(in->grad_entropy, 4) ||
-      !aligned(logp, 4) || !aligned(out->d_hidden, 2) || !aligned(out->d_weight, 2))
-    return set_msg(ctx, "inputs must be 4-byte, gradients 2-byte aligned"), GPO_ERR_UNSUPPORTED;
-  if ((out->d_hidden && (double)T * (double)out->d_hidden_stride >= (double)kMaxMatrix) ||
-      (out->d_weight && (double)v->vocab * (double)out->d_weight_stride >= (double)kMaxMatrix))
-    return set_msg(ctx, "gradient too large"), GPO_ERR_UNSUPPORTED;
+      !aligned(logp, 4))
+    return set_msg(ctx, "inputs must be 4-byte aligned"), GPO_ERR_UNSUPPORTED;
+  s = check_grads(ctx, *v, *out);
+  if (s != GPO_OK) return s;
   VocabLayout L;
   vocab_layout(*v, true, L);
   s = check_call(ctx, workspace, workspace_bytes, L.total);
   if (s != GPO_OK) return s;
-  if (T == 0) {
-    ctx->nstages = 0;
-    if (out->d_weight && !out->accumulate) {
-      const cudaError_t e = cudaMemset2DAsync(out->d_weight, 2 * (size_t)out->d_weight_stride, 0, 2 * (size_t)v->d,
-                                              (size_t)v->vocab, static_cast<cudaStream_t>(stream));
-      if (e != cudaSuccess) return set_msg(ctx, "memset failed: %s", cudaGetErrorString(e)), GPO_ERR_CUDA;
-    }
-    return GPO_OK;
-  }
+  if (T == 0) return no_tokens(ctx, *v, *out, stream);
   VocabArgs a;
   VocabMaps m;
   s = vocab_args(ctx, *v, L, workspace, a, m);
@@ -348,26 +387,8 @@ gpo_status gpo_vocab_grad_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab
   a.ent = in->entropy;
   a.ge = in->grad_entropy;
   a.lp = logp;
-  a.sl2 = logit_scale(*v, 64 * kVocabDzSeg);
-  a.weight = v->weight;
-  a.weight_stride = v->weight_stride;
-  a.by_target = at<int>(workspace, L.by_target);
-  a.tile_first = at<int>(workspace, L.tile_first);
-  a.rest = at<float>(workspace, L.rest);
-  a.dz = at<uint16_t>(workspace, L.dz);
-  a.dz_stride = L.piece;
-  a.acc = L.acc ? at<float>(workspace, L.acc) : nullptr;
-  a.acc_rows = L.tp;
-  a.acc_stride = L.acc_stride;
-  a.splits = out->d_hidden ? L.splits : 1;
-  a.dh = out->d_hidden;
-  a.dh_stride = out->d_hidden_stride;
-  a.dw = out->d_weight;
-  a.dw_stride = out->d_weight_stride;
-  a.accumulate = out->accumulate != 0;
-  // (a bulk store leaves out what lies past the matrix, but not to the element: of an odd width it wrote one more)
-  a.dw_bulk = a.dw && !a.accumulate && v->d % 8 == 0 && a.dw_stride % 8 == 0 && aligned(a.dw, 16) &&
-              encode_map(&m.dw, encode_fn(), a.dw, v->d, v->vocab, a.dw_stride, a.f16, 32);
+  grad_args(*v, *out, L, workspace, a);
+  a.dw_bulk = bulk_rows(*v, a, m);
   Stages stage(ctx, stream);
   stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });
   for (int64_t v0 = 0; v0 < v->vocab; v0 += L.piece) {
@@ -376,6 +397,226 @@ gpo_status gpo_vocab_grad_logp(gpo_ctx* ctx, const gpo_vocab* v, const gpo_vocab
     a.first = v0 == 0;
     a.last = v0 + L.piece >= v->vocab;
     stage("vocab_dz", [&] { return launch_vocab_dz(stage.lc, m, a, stage.st); });
+    stage("vocab_products", [&] { return launch_vocab_products(stage.lc, m, a, stage.st); });
+  }
+  return stage.done();
+}
+
+}  // extern "C"
+
+namespace {
+
+// The workspace of a distillation: that of the products, then the teacher's.
+struct TeachLayout {
+  VocabLayout v;
+  size_t id, place, q, lq, z, n, qr, target;         // forward
+  size_t none, dense, dense_lse, bound;              // gradient (and target)
+  size_t total;
+  int64_t stride;
+};
+
+void teach_layout(const gpo_vocab& v, int64_t k, bool grad, TeachLayout& L) {
+  L = TeachLayout();
+  vocab_layout(v, grad, L.v, true);
+  size_t o = L.v.total;
+  auto take = [&](size_t bytes) {
+    const size_t at = o;
+    o = workspace_up(o + bytes);
+    return at;
+  };
+  const size_t T = (size_t)v.num_tokens;
+  L.stride = up_to(k, 8);
+  const size_t all = T * (size_t)L.stride;
+  if (T > 0) L.target = take(4 * T);
+  if (T > 0 && !grad) {
+    L.id = take(4 * all);
+    L.place = take(2 * all);
+    L.q = take(4 * all);
+    L.lq = take(4 * all);
+    L.z = take(4 * all);
+    L.n = take(4 * T);
+    L.qr = take(4 * T);
+  }
+  if (T > 0 && grad) {
+    L.none = take(4 * T);
+    L.dense = take(4 * T);
+    L.dense_lse = take(4 * T);
+    L.bound = take(4 * T);
+  }
+  L.total = o;
+}
+
+gpo_status check_teacher_sizes(gpo_ctx* c, const gpo_vocab& v, const gpo_teacher* t, bool grad) {
+  if (!t) return set_msg(c, "teacher arguments NULL"), GPO_ERR_INVALID_ARG;
+  if (t->k < 1) return set_msg(c, "k < 1"), GPO_ERR_INVALID_ARG;
+  if (t->k > GPO_MAX_TEACHER) return set_msg(c, "more than %d entries of a teacher", GPO_MAX_TEACHER), GPO_ERR_UNSUPPORTED;
+  if (t->ids_stride < t->k || (!grad && t->logits_stride < t->k)) return set_msg(c, "row stride < k"), GPO_ERR_INVALID_ARG;
+  const double rows = (double)std::max<int64_t>(v.num_tokens, 1);
+  if (rows * (double)t->ids_stride >= (double)kMaxMatrix || (!grad && rows * (double)t->logits_stride >= (double)kMaxMatrix))
+    return set_msg(c, "teacher too large"), GPO_ERR_UNSUPPORTED;
+  if (t->id_bytes != 4 && t->id_bytes != 8) return set_msg(c, "id_bytes must be 4 or 8"), GPO_ERR_INVALID_ARG;
+  return GPO_OK;
+}
+
+gpo_status check_teacher(gpo_ctx* c, const gpo_vocab& v, const gpo_teacher* t, bool grad) {
+  const gpo_status s = check_teacher_sizes(c, v, t, grad);
+  if (s != GPO_OK) return s;
+  if (!grad) {
+    if (t->dtype != GPO_DT_BF16 && t->dtype != GPO_DT_F16 && t->dtype != GPO_DT_F32)
+      return set_msg(c, "unknown dtype %d of the teacher", t->dtype), GPO_ERR_INVALID_ARG;
+    if (!(t->scale >= 1e-4 && t->scale <= 1e4)) return set_msg(c, "teacher's scale outside [1e-4, 1e4]"), GPO_ERR_INVALID_ARG;
+    if (t->tail && t->scale != 1.0) return set_msg(c, "log-probabilities have no scale"), GPO_ERR_INVALID_ARG;
+  }
+  if (v.num_tokens > 0 && (!t->ids || (!grad && !t->logits))) return set_msg(c, "teacher's ids or logits NULL"), GPO_ERR_INVALID_ARG;
+  if (!aligned(t->ids, (size_t)t->id_bytes) || (!grad && !aligned(t->logits, t->dtype == GPO_DT_F32 ? 4 : 2)))
+    return set_msg(c, "teacher's arrays must be aligned to their elements"), GPO_ERR_UNSUPPORTED;
+  return GPO_OK;
+}
+
+void teach_args(const gpo_vocab& v, const gpo_teacher& t, const TeachLayout& L, void* ws, TeachArgs& a) {
+  memset(&a, 0, sizeof a);
+  a.T = v.num_tokens;
+  a.V = v.vocab;
+  a.k = (int)t.k;
+  a.ids = t.ids;
+  a.ids_stride = t.ids_stride;
+  a.id8 = t.id_bytes == 8;
+  a.logits = t.logits;
+  a.logits_stride = t.logits_stride;
+  a.dtype = t.dtype;
+  a.scale = (float)t.scale;
+  a.tail = t.tail != 0;
+  a.stride = L.stride;
+  a.target = at<int>(ws, L.target);
+}
+
+}  // namespace
+
+extern "C" {
+
+gpo_status gpo_vocab_distill_workspace_size(const gpo_vocab* v, const gpo_teacher* t, int gradient, size_t* bytes) {
+  if (!bytes) return GPO_ERR_INVALID_ARG;
+  gpo_status s = check_sizes(nullptr, v, false);
+  if (s == GPO_OK) s = check_teacher_sizes(nullptr, *v, t, gradient != 0);
+  if (s != GPO_OK) return s;
+  TeachLayout L;
+  teach_layout(*v, t->k, gradient != 0, L);
+  *bytes = L.total;
+  return GPO_OK;
+}
+
+gpo_status gpo_vocab_distill(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher* t, const gpo_distill_outputs* out, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  if (!ctx) return GPO_ERR_INVALID_ARG;
+  ctx->msg[0] = 0;
+  gpo_status s = check_vocab(ctx, v, false);
+  if (s == GPO_OK) s = check_teacher(ctx, *v, t, false);
+  if (s != GPO_OK) return s;
+  if (!out || (v->num_tokens > 0 && (!out->loss || !out->delta || !out->rest || !out->rest_lse)))
+    return set_msg(ctx, "loss, delta, rest or rest_lse NULL"), GPO_ERR_INVALID_ARG;
+  if (out->delta_stride < t->k) return set_msg(ctx, "row stride of delta < k"), GPO_ERR_INVALID_ARG;
+  if ((double)v->num_tokens * (double)out->delta_stride >= (double)kMaxMatrix) return set_msg(ctx, "delta too large"), GPO_ERR_UNSUPPORTED;
+  if (!aligned(out->loss, 4) || !aligned(out->delta, 4) || !aligned(out->rest, 4) || !aligned(out->rest_lse, 4) || !aligned(out->lse, 4))
+    return set_msg(ctx, "outputs must be 4-byte aligned"), GPO_ERR_UNSUPPORTED;
+  TeachLayout L;
+  teach_layout(*v, t->k, false, L);
+  s = check_call(ctx, workspace, workspace_bytes, L.total);
+  if (s != GPO_OK) return s;
+  if (v->num_tokens == 0) return ctx->nstages = 0, GPO_OK;
+  VocabArgs a;
+  VocabMaps m;
+  s = vocab_args(ctx, *v, L.v, workspace, a, m);
+  if (s != GPO_OK) return s;
+  TeachArgs ta;
+  teach_args(*v, *t, L, workspace, ta);
+  ta.id = at<int>(workspace, L.id);
+  ta.place = at<int16_t>(workspace, L.place);
+  ta.q = at<float>(workspace, L.q);
+  ta.lq = at<float>(workspace, L.lq);
+  ta.n = at<int>(workspace, L.n);
+  ta.qr = at<float>(workspace, L.qr);
+  ta.loss = out->loss;
+  ta.lse = out->lse;
+  ta.rest = out->rest;
+  ta.rest_lse = out->rest_lse;
+  ta.delta = out->delta;
+  ta.delta_stride = out->delta_stride;
+  a.target = ta.target;
+  a.id8 = 0;
+  a.pm = at<float>(workspace, L.v.pm);
+  a.ps = at<float>(workspace, L.v.ps);
+  a.pu = at<float>(workspace, L.v.pu);
+  a.tz = at<float>(workspace, L.v.tz);
+  a.part_row = 1;
+  a.part_col = L.v.tp;
+  a.logp = out->loss;  // (launch_vocab_rows: zeros of the tokens that take no part)
+  a.sl2 = logit_scale(*v, 64 * kVocabSeg);
+  a.top_id = ta.id;
+  a.top_n = ta.n;
+  a.top_z = at<float>(workspace, L.z);
+  a.top_stride = L.stride;
+  Stages stage(ctx, stream);
+  stage("teach_sort", [&] { return launch_teach_sort(stage.lc, ta, stage.st); });
+  if (L.v.listed) stage("vocab_rows", [&] { return launch_vocab_rows(stage.lc, a, stage.st); });
+  stage("vocab_taught", [&] { return launch_vocab_taught(stage.lc, m, a, stage.st); });
+  stage("teach_join", [&] { return launch_teach_join(stage.lc, ta, a, stage.st); });
+  return stage.done();
+}
+
+gpo_status gpo_vocab_distill_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher* t, const gpo_distill_grad_inputs* in,
+                                  const gpo_vocab_grads* out, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!ctx) return GPO_ERR_INVALID_ARG;
+  ctx->msg[0] = 0;
+  gpo_status s = check_vocab(ctx, v, false);
+  if (s == GPO_OK) s = check_teacher(ctx, *v, t, true);
+  if (s != GPO_OK) return s;
+  const int64_t T = v->num_tokens;
+  if (!in || !out) return set_msg(ctx, "inputs or outputs NULL"), GPO_ERR_INVALID_ARG;
+  if (T > 0 && (!in->grad_loss || !in->delta || !in->rest || !in->rest_lse))
+    return set_msg(ctx, "grad_loss, delta, rest or rest_lse NULL"), GPO_ERR_INVALID_ARG;
+  if (in->delta_stride < t->k) return set_msg(ctx, "row stride of delta < k"), GPO_ERR_INVALID_ARG;
+  if ((double)T * (double)in->delta_stride >= (double)kMaxMatrix) return set_msg(ctx, "delta too large"), GPO_ERR_UNSUPPORTED;
+  if (!aligned(in->grad_loss, 4) || !aligned(in->delta, 4) || !aligned(in->rest, 4) || !aligned(in->rest_lse, 4))
+    return set_msg(ctx, "inputs must be 4-byte aligned"), GPO_ERR_UNSUPPORTED;
+  s = check_grads(ctx, *v, *out);
+  if (s != GPO_OK) return s;
+  TeachLayout L;
+  teach_layout(*v, t->k, true, L);
+  s = check_call(ctx, workspace, workspace_bytes, L.total);
+  if (s != GPO_OK) return s;
+  if (T == 0) return no_tokens(ctx, *v, *out, stream);
+  VocabArgs a;
+  VocabMaps m;
+  s = vocab_args(ctx, *v, L.v, workspace, a, m);
+  if (s != GPO_OK) return s;
+  TeachArgs ta;
+  teach_args(*v, *t, L, workspace, ta);
+  ta.g = in->grad_loss;
+  ta.delta_in = in->delta;
+  ta.delta_stride = in->delta_stride;
+  ta.rest_in = in->rest;
+  ta.rest_lse_in = in->rest_lse;
+  ta.none = at<int>(workspace, L.none);
+  ta.dense = at<float>(workspace, L.dense);
+  ta.dense_lse = at<float>(workspace, L.dense_lse);
+  ta.bound = at<float>(workspace, L.bound);
+  grad_args(*v, *out, L.v, workspace, a);
+  a.id8 = 0;
+  a.lse = ta.dense_lse;
+  a.g = ta.dense;
+  a.dw_bulk = bulk_rows(*v, a, m);
+  Stages stage(ctx, stream);
+  stage("teach_grad", [&] { return launch_teach_grad(stage.lc, ta, stage.st); });
+  a.target = ta.target;
+  stage("vocab_order", [&] { return launch_vocab_order_taught(stage.lc, a, ta.bound, stage.st); });
+  a.target = ta.none;  // (the products' kernels know no targets)
+  for (int64_t v0 = 0; v0 < v->vocab; v0 += L.v.piece) {
+    a.v0 = v0;
+    a.vn = std::min(L.v.piece, v->vocab - v0);
+    a.first = v0 == 0;
+    a.last = v0 + L.v.piece >= v->vocab;
+    stage("vocab_dz", [&] { return launch_vocab_dz(stage.lc, m, a, stage.st); });
+    stage("teach_entries", [&] { return launch_teach_entries(stage.lc, ta, a, stage.st); });
     stage("vocab_products", [&] { return launch_vocab_products(stage.lc, m, a, stage.st); });
   }
   return stage.done();
