@@ -1072,9 +1072,6 @@ cudaError_t setup_vocab();
 cudaError_t launch_vocab_rows(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
 // The same of the tokens with a gradient, in the order of their targets.
 cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const Status& st);
-// The same of the tokens with a target of 0, in their own order and without a place for what rounding takes at a target;
-// bound: [T] what |dz| of a token is at most.
-cudaError_t launch_vocab_order_taught(const LaunchCtx& lc, const VocabArgs& a, const float* bound, const Status& st);
 // Up to kVocabFew tokens; marks: [kVocabFewCtas] in the workspace, mark: a value that no other call leaves there.
 cudaError_t setup_vocab_few();
 cudaError_t launch_vocab_few(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st, bool ent,
@@ -1131,13 +1128,13 @@ struct TeachArgs {
   int *id, *n;
   int16_t* place;
   float *q, *lq, *qr;
-  int* target;                   // 0: has a teacher, -1: has none
+  int* target;                   // forward 0, gradient the entry of the largest |delta|; -1: has no teacher
   // results
   float *loss, *lse, *rest, *rest_lse, *delta;
   int64_t delta_stride;
   // gradient
   const float *g, *delta_in, *rest_in, *rest_lse_in;
-  float *dense, *dense_lse, *bound;  // [T] for vocab_pair_kernel: g, lse; |g|
+  float *dense, *dense_lse;      // [T] for vocab_pair_kernel: g, lse
   int *none;                     // [T] -1
 };
 

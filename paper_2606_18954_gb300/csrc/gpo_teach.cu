@@ -9,6 +9,8 @@
 // Gradient: outside the entries dz is g (p - q of all others together) times the softmax over the others, for either form of the
 //           loss; inside it is g (p - q).  So vocab_pair_kernel's dz of a token without a target, with the others' log-sum-exp,
 //           is right for all but the entries, which teach_entries_kernel writes over it, rounded once; then the products.
+//           The largest entry takes the place that a target has there: the tokens are in the order of those, and what its
+//           rounding takes is added to both products.
 // Keeping the entries out of the sum over the others keeps the digits of both: where the student is nearly certain of one
 // of the teacher's tokens, 1 - p is a sum of small terms here, and so is the others' share p_r.
 #define GPO_REPORT __noinline__
@@ -196,21 +198,27 @@ __global__ void __launch_bounds__(256) teach_grad_kernel(TeachArgs t, Status st)
   let_next_start();
   const int64_t tok = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (tok >= t.T) return;
-  bool some = false;
+  int top = -1;  // the entry of the largest |delta|, of equal ones that of the lowest id
+  float most = -1.f;
   for (int j = lane; j < t.k; j += 32) {
     const int64_t id = load_id(t.ids, t.id8, tok * t.ids_stride + j);
     if (id >= t.V) report(st, GPO_ERR_SHAPE, 53, (int)tok);
-    some |= id >= 0 && id < t.V;
+    if (id < 0 || id >= t.V) continue;
+    const float x = fabsf(t.delta_in[tok * t.delta_stride + j]);
+    if (top < 0 || x > most || (x == most && id < top)) top = (int)id, most = x;
   }
-  some = __any_sync(0xffffffffu, some);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const int id = __shfl_xor_sync(0xffffffffu, top, o);
+    const float x = __shfl_xor_sync(0xffffffffu, most, o);
+    if (id >= 0 && (top < 0 || x > most || (x == most && id < top))) top = id, most = x;
+  }
   if (lane != 0) return;
-  const float g = t.g[tok], lse = t.rest_lse_in[tok];
-  const bool live = some && g != 0.f;
-  t.target[tok] = live ? 0 : -1;
+  const float lse = t.rest_lse_in[tok];
+  t.target[tok] = top;
   t.none[tok] = -1;
-  t.dense[tok] = live ? -g * t.rest_in[tok] : 0.f;
+  t.dense[tok] = -t.g[tok] * t.rest_in[tok];
   t.dense_lse[tok] = lse == -INFINITY ? INFINITY : lse;  // (no other tokens: their p is 0)
-  t.bound[tok] = live ? fabsf(g) : 0.f;
 }
 
 __global__ void __launch_bounds__(256) teach_entries_kernel(TeachArgs t, VocabArgs a, Status st) {
@@ -229,8 +237,17 @@ __global__ void __launch_bounds__(256) teach_entries_kernel(TeachArgs t, VocabAr
       const float x = g * t.delta_in[tok * t.delta_stride + j];
       if (!GPO_BOUNDS(st, id - a.v0, a.dz_stride, kWhereVocabRow)) continue;
       uint16_t* dst = a.dz + r * a.dz_stride + (id - a.v0);
-      if (a.f16) *reinterpret_cast<__half*>(dst) = __float2half_rn(x);
-      else *reinterpret_cast<__nv_bfloat16*>(dst) = __float2bfloat16_rn(x);
+      float rounded;
+      if (a.f16) {
+        const __half h = __float2half_rn(x);
+        *reinterpret_cast<__half*>(dst) = h;
+        rounded = __half2float(h);
+      } else {
+        const __nv_bfloat16 h = __float2bfloat16_rn(x);
+        *reinterpret_cast<__nv_bfloat16*>(dst) = h;
+        rounded = __bfloat162float(h);
+      }
+      if (id == a.by_target[r]) a.rest[r] = x - rounded;
     }
   }
 }

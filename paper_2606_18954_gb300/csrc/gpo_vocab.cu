@@ -1118,85 +1118,6 @@ __global__ void __launch_bounds__(kRowThreads) vocab_order_kernel(VocabArgs a, S
   if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
 }
 
-// For a teacher's gradient: the tokens with a target of 0, in their own order; no target of theirs is a row of the matrix, and no
-// part of dz is kept for it.  Every CTA looks at all tokens, as in vocab_rows_kernel.
-__global__ void __launch_bounds__(kRowThreads) vocab_taught_order_kernel(VocabArgs a, const float* bounds, Status st) {
-  constexpr int kW = kRowThreads / 32;
-  __shared__ int s_before[kW], s_all[kW], s_cnt[kW];
-  __shared__ float s_big[kW];
-  __shared__ int s_list[kRowThreads];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  let_next_start();
-  after_previous();
-  const int64_t ta = a.T * blockIdx.x / gridDim.x, tb = a.T * (blockIdx.x + 1) / gridDim.x;
-  const int* target = static_cast<const int*>(a.target);
-  int before = 0, all = 0;
-  float bound = 0.f;
-  for (int64_t t0 = threadIdx.x; t0 < a.T; t0 += kRowAhead * kRowThreads) {
-    int id[kRowAhead];
-    float big[kRowAhead];
-#pragma unroll
-    for (int k = 0; k < kRowAhead; ++k) {
-      const int64_t t = t0 + k * kRowThreads;
-      id[k] = t < a.T ? target[t] : -1;
-      big[k] = t < a.T ? bounds[t] : 0.f;
-    }
-#pragma unroll
-    for (int k = 0; k < kRowAhead; ++k) {
-      all += id[k] >= 0;
-      before += id[k] >= 0 && t0 + k * kRowThreads < ta;
-      bound = fmaxf(bound, big[k]);
-    }
-  }
-  all = __reduce_add_sync(0xffffffffu, all);
-  before = __reduce_add_sync(0xffffffffu, before);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) bound = fmaxf(bound, __shfl_xor_sync(0xffffffffu, bound, o));
-  if (lane == 0) {
-    s_all[warp] = all;
-    s_before[warp] = before;
-    s_big[warp] = bound;
-  }
-  __syncthreads();
-  all = __reduce_add_sync(0xffffffffu, s_all[lane]);
-  int base = __reduce_add_sync(0xffffffffu, s_before[lane]);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    for (int w = 0; w < kW; ++w) bound = fmaxf(bound, s_big[w]);
-    a.head->rows = all;
-    a.head->dz_scale = scale_of_dz(a, bound);
-  }
-  const bool vec = vec_rows(a.dh, a.dh_stride);
-  for (int64_t t0 = ta; t0 < tb; t0 += kRowThreads) {
-    const int64_t t = t0 + threadIdx.x;
-    const bool in = t < tb && target[t] >= 0;
-    const uint32_t m = __ballot_sync(0xffffffffu, in);
-    if (lane == 0) s_cnt[warp] = __popc(m);
-    __syncthreads();
-    const int n = __reduce_add_sync(0xffffffffu, s_cnt[lane]);
-    const int lower = __reduce_add_sync(0xffffffffu, lane < warp ? s_cnt[lane] : 0);
-    if (in) {
-      const int r = lower + __popc(m & ((1u << lane) - 1u));
-      s_list[r] = (int)t;
-      if (GPO_BOUNDS(st, base + r, a.T, kWhereVocabRow)) {
-        a.idx[base + r] = (int)t;
-        a.by_target[base + r] = -1;
-      }
-    }
-    __syncthreads();
-    for (int r = warp; r < n; r += kW) gather_row(a, base + r, s_list[r], lane);
-    if (a.dh)
-      for (uint32_t out = ~m & __ballot_sync(0xffffffffu, t < tb); out; out &= out - 1)
-        no_d_hidden(a, t0 + warp * 32 + __ffs(out) - 1, vec, lane);
-    base += n;
-    __syncthreads();
-  }
-  const int64_t tiles = (a.V + kPairM - 1) / kPairM;
-  for (int64_t j = blockIdx.x * (int64_t)kRowThreads + threadIdx.x; j <= tiles; j += (int64_t)gridDim.x * kRowThreads) a.tile_first[j] = 0;
-  if (blockIdx.x == gridDim.x - 1)
-    for (int64_t r = all + warp; r < rows_behind(a, all); r += kW) gather_row(a, r, -1, lane);
-  if (blockIdx.x == 0 && threadIdx.x == 0) next_tag(st);
-}
-
 // The same for more than kVocabOrder tokens, whose comparisons would grow with T^2: the sort's work grows with T.
 template <class Id>
 struct VocabKeys {
@@ -1447,11 +1368,6 @@ cudaError_t launch_vocab_order(const LaunchCtx& lc, const VocabArgs& a, const St
   const int grid = (int)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
   vocab_order_kernel<<<grid, kRowThreads, 0, lc.stream>>>(a, st);
   return cudaGetLastError();
-}
-
-cudaError_t launch_vocab_order_taught(const LaunchCtx& lc, const VocabArgs& a, const float* bound, const Status& st) {
-  const unsigned grid = (unsigned)max((int64_t)1, min(a.T / 4, (int64_t)lc.num_sms));
-  return launch_after(vocab_taught_order_kernel, grid, kRowThreads, 0, lc.stream, a, bound, st);
 }
 
 cudaError_t launch_vocab_taught(const LaunchCtx& lc, const VocabMaps& m, const VocabArgs& a, const Status& st) {

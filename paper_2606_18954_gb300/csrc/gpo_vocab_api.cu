@@ -410,7 +410,7 @@ namespace {
 struct TeachLayout {
   VocabLayout v;
   size_t id, place, q, lq, z, n, qr, target;         // forward
-  size_t none, dense, dense_lse, bound;              // gradient (and target)
+  size_t none, dense, dense_lse;                     // gradient (and target)
   size_t total;
   int64_t stride;
 };
@@ -441,7 +441,6 @@ void teach_layout(const gpo_vocab& v, int64_t k, bool grad, TeachLayout& L) {
     L.none = take(4 * T);
     L.dense = take(4 * T);
     L.dense_lse = take(4 * T);
-    L.bound = take(4 * T);
   }
   L.total = o;
 }
@@ -599,17 +598,17 @@ gpo_status gpo_vocab_distill_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_te
   ta.none = at<int>(workspace, L.none);
   ta.dense = at<float>(workspace, L.dense);
   ta.dense_lse = at<float>(workspace, L.dense_lse);
-  ta.bound = at<float>(workspace, L.bound);
   grad_args(*v, *out, L.v, workspace, a);
   a.id8 = 0;
-  a.lse = ta.dense_lse;
-  a.g = ta.dense;
   a.dw_bulk = bulk_rows(*v, a, m);
   Stages stage(ctx, stream);
   stage("teach_grad", [&] { return launch_teach_grad(stage.lc, ta, stage.st); });
   a.target = ta.target;
-  stage("vocab_order", [&] { return launch_vocab_order_taught(stage.lc, a, ta.bound, stage.st); });
-  a.target = ta.none;  // (the products' kernels know no targets)
+  a.g = in->grad_loss;
+  stage("vocab_order", [&] { return launch_vocab_order(stage.lc, a, stage.st); });
+  a.target = ta.none;  // (dz: of no target)
+  a.g = ta.dense;
+  a.lse = ta.dense_lse;
   for (int64_t v0 = 0; v0 < v->vocab; v0 += L.v.piece) {
     a.v0 = v0;
     a.vn = std::min(L.v.piece, v->vocab - v0);

@@ -86,7 +86,10 @@ def exact(hidden, weight, ids, teacher, scale=1.0, teacher_scale=1.0, tail=False
     first[torch.arange(T, device=z.device), torch.where(entry, z.gather(1, i), -math.inf).argmax(1)] = True
     sums = EX2 + (k / 32 + 64) * U
     t_delta = 2 * tz[:, None] * p * (1 - p) + q * (1 - q) * 2 * tq[:, None] + eq[:, None] * first + sums * torch.where(first, (1 - p) + (1 - q), p + q)
-    t_rest = 2 * tz * pr * (1 - pr) + 2 * eq + sums * (pr + qr)
+    # what 64 bits leave of p - q here: exponents that are differences of numbers as large as lse, the products' sums
+    own = 2.0 ** -52 * (8 * (lse.abs() + mass.abs().nan_to_num(0, 0, 0) + 1) + 4 * tz / U)
+    t_delta = t_delta + own[:, None] * (p + q)
+    t_rest = 2 * tz * pr * (1 - pr) + 2 * eq + sums * (pr + qr) + own * (pr + qr)
     out = dict(loss=zero(loss), delta=torch.where(entry & live[:, None], p - q, 0.0), rest=zero(pr - qr), rest_lse=zero(lr), lse=zero(lse),
                t_loss=t_loss, t_delta=t_delta, t_rest=t_rest, t_rest_lse=tr, t_lse=tl)
     if g is None:
