@@ -19,7 +19,8 @@ namespace gpo {
 
 namespace {
 
-constexpr int kThreads = 384, kWarps = kThreads / 32;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kCtas = 4;                         // on one SM
 constexpr int kVecs = 2;                         // accesses of 32 bytes of a thread that are in flight
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1;  // an entry's word: flags, occurrences
@@ -37,6 +38,16 @@ __device__ __forceinline__ Vec load_global(const void* p) {
                : "l"(p)
                : "memory");
   return r;
+}
+// The same where `take` says so, else r stays as it is.
+__device__ __forceinline__ void load_global_if(Vec& r, const void* p, bool take) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.s32 q, %9, 0;\n\t"
+      "@q ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
+      : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]), "+r"(r.w[4]), "+r"(r.w[5]), "+r"(r.w[6]), "+r"(r.w[7])
+      : "l"(p), "r"((int)take)
+      : "memory");
 }
 __device__ __forceinline__ void store_global(void* p, const Vec& x) {
   asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
@@ -203,7 +214,7 @@ struct Raw<GPO_DT_F16> : Raw16 {
   static __device__ __forceinline__ T put(float x) { return __float2half_rn(x); }
 };
 
-// A row, read by one warp before the row's first slice.
+// A row, read by one warp.
 struct Row {
   const void* z;
   void* out;
@@ -222,26 +233,31 @@ struct Row {
 };
 
 struct Shared {
-  Row row[2];
-  Part part[2][kWarps];       // of the row of the same place
-  float at[2];                // the target's adjusted logit
-  Part cluster[2][8];
-  float cluster_at[2];
+  Row row;
+  Part part[kWarps];
+  float at;                   // the target's adjusted logit
+  Part cluster[8];
+  float cluster_at;
   int before[kWarps];         // special entries of each warp's words
 };
 
 constexpr int kSpan = 131072;         // entries of which it is known at one time which are special
 constexpr int kWords = kSpan / 32;
-constexpr int kOwn = (kWords + kThreads - 1) / kThreads;  // words of a thread, side by side
-constexpr int kCap = 4096;            // special entries that are looked at in one round
+constexpr int kGroups = kWords / 4;   // groups of four words, whose special entries are counted together
+constexpr int kOwn = kGroups / kWarps;  // groups of a warp, side by side
+constexpr int kCap = 2048;            // special entries that are looked at in one round
 struct Smem {
   Shared sh;
-  uint32_t special[kWords];
-  uint32_t allow[kWords];
-  uint32_t before[kWords];            // special entries in the words before
-  uint32_t list[kCap];                // the round's special entries, in their order,
-  uint32_t count[kCap];               // and their flags and occurrences
-  float stage[kWarps][512];           // values of each warp on their way out
+  alignas(16) uint32_t special[kWords];
+  alignas(16) uint32_t allow[kWords];
+  uint32_t before[kGroups];           // special entries in the groups before
+  union {
+    struct {
+      uint32_t list[kCap];            // the round's special entries, in their order,
+      uint32_t count[kCap];           // and their flags and occurrences
+    };
+    float stage[kWarps][512];         // values of each warp on their way out
+  };
 };
 
 // The bias of v among the row's (ascending).
@@ -404,49 +420,62 @@ __device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st,
   }
 }
 
-// The number of special entries of the span, and of those before each word; these leave the allowed ones.
+// The number of special entries of the span, and of those before each group of words; these leave the allowed ones.
 __device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int j0 = min((n + 31) / 32, (int)threadIdx.x * kOwn), j1 = min((n + 31) / 32, j0 + kOwn);
-  int own = 0;
-  for (int j = j0; j < j1; ++j) {
-    const uint32_t x = sm.special[j];
-    own += __popc(x);
-    sm.allow[j] = masked ? sm.allow[j] & ~x : ~x;
-  }
-  int upto = own;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (n + 127) / 128;
+  int sum = 0;
+#pragma unroll 1
+  for (int g0 = warp * kOwn; g0 < min(groups, (warp + 1) * kOwn); g0 += 32) {
+    const int g = g0 + lane;
+    const uint4 x = reinterpret_cast<const uint4*>(sm.special)[g];
+    uint4& al = reinterpret_cast<uint4*>(sm.allow)[g];
+    al = masked ? make_uint4(al.x & ~x.x, al.y & ~x.y, al.z & ~x.z, al.w & ~x.w) : make_uint4(~x.x, ~x.y, ~x.z, ~x.w);
+    const int own = __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
+    int upto = own;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, upto, o);
-    if (lane >= o) upto += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    sm.before[g] = sum + upto - own;
+    sum += __shfl_sync(0xffffffffu, upto, 31);
   }
-  if (lane == 31) sm.sh.before[warp] = upto;
+  if (lane == 0) sm.sh.before[warp] = sum;
   __syncthreads();
-  int before = upto - own, all = 0;
+  int before = 0, all = 0;
 #pragma unroll
   for (int k = 0; k < kWarps; ++k) {
     const int y = sm.sh.before[k];
     if (k < warp) before += y;
     all += y;
   }
-  for (int j = j0; j < j1; ++j) {
-    sm.before[j] = before;
-    before += __popc(sm.special[j]);
-  }
+  for (int g = warp * kOwn + lane; g < min(groups, (warp + 1) * kOwn); g += 32) sm.before[g] += before;
   return all;
 }
 
 // The round's special entries, those of ranks [first, first + kCap), and their flags and counts.  Between barriers of the caller.
 __device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, int lo, int n, int first, int total, Smem& sm) {
-  const int j0 = min((n + 31) / 32, (int)threadIdx.x * kOwn), j1 = min((n + 31) / 32, j0 + kOwn);
-  for (int j = j0; j < j1; ++j) {
-    int k = (int)sm.before[j] - first;
-    for (uint32_t bits = sm.special[j]; bits; bits &= bits - 1, ++k)
-      if (k >= 0 && k < kCap) sm.list[k] = 32 * j + __ffs(bits) - 1;
+  for (int g = threadIdx.x; g < (n + 127) / 128; g += kThreads) {
+    const uint4 x = reinterpret_cast<const uint4*>(sm.special)[g];
+    int k = (int)sm.before[g] - first;
+    auto put = [&](uint32_t bits, int rel) {
+      for (; bits; bits &= bits - 1, ++k)
+        if (k >= 0 && k < kCap) sm.list[k] = rel + __ffs(bits) - 1;
+    };
+    put(x.x, 128 * g);
+    put(x.y, 128 * g + 32);
+    put(x.z, 128 * g + 64);
+    put(x.w, 128 * g + 96);
   }
-  for (int k = threadIdx.x; k < min(kCap, total - first); k += kThreads) sm.count[k] = 0;
+  for (int c = threadIdx.x; c < min(kCap, total - first); c += kThreads) sm.count[c] = 0;
   __syncthreads();
-  auto at = [&](uint32_t rel) { return (int)(sm.before[rel >> 5] + __popc(sm.special[rel >> 5] & ((1u << (rel & 31u)) - 1u))) - first; };
+  auto at = [&](uint32_t rel) {
+    const uint32_t word = rel >> 5 & 3u, low = (1u << (rel & 31u)) - 1u;
+    const uint4 x = reinterpret_cast<const uint4*>(sm.special)[rel >> 7];
+    const uint32_t own = word == 0 ? x.x : word == 1 ? x.y : word == 2 ? x.z : x.w;
+    return (int)sm.before[rel >> 7] - first + __popc(own & low) + (word > 0 ? __popc(x.x) : 0) + (word > 1 ? __popc(x.y) : 0) +
+           (word > 2 ? __popc(x.z) : 0);
+  };
   for_history(a, w, lo, min((int64_t)n, a.V - lo), [&](int64_t rel, int64_t i) {
     const int k = at((uint32_t)rel);
     if (k < 0 || k >= kCap) return;
@@ -564,7 +593,7 @@ __device__ __forceinline__ void raise(Running& p, float top) {
 }
 
 template <int kType, int kOp, bool kEnt>
-__global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int cluster, Status st) {
+__global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, int cluster, Status st) {
   using E = Raw<kType>;
   using T = typename E::T;
   constexpr int kPer = E::kPer, kSpanVecs = kSpan / kPer, kBatch = kThreads * kVecs;
@@ -575,51 +604,61 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = (int)a.V;
   float* stage = sm.stage[warp];
   const int rank = cluster > 1 ? (int)cluster_rank() : 0;
-  const int64_t step = gridDim.x / cluster;
+  const int64_t r = blockIdx.x / cluster;
   const bool wide = a.out32 && sizeof(T) == 2;
-  for (int j = tid; j < kWords; j += kThreads) sm.special[j] = 0;
-
-  int64_t r = blockIdx.x / cluster;
-  int place = 0;
-  if (warp == 0 && r < a.R) read_row<kType, kOp>(a, st, r, sh.row[0], lane, rank == 0);
+  if (warp == 0) read_row<kType, kOp>(a, st, r, sh.row, lane, rank == 0);
+  if (a.spans || a.bias)
+    for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
+  if (blockIdx.x == 0 && tid == 32) next_tag(st);
   __syncthreads();
-  // this CTA's share of a row's vectors (in whole words of the bitmaps)
-  auto begins = [&](const Row& w) { return min(w.vecs, rank * ((w.vecs + cluster * 4 - 1) / (cluster * 4) * 4)); };
-  auto finishes = [&](const Row& w) { return min(w.vecs, (rank + 1) * ((w.vecs + cluster * 4 - 1) / (cluster * 4) * 4)); };
-  // Vectors of the row that a warp takes without a look at its ends: [whole0, whole1) are full of its entries.
-  auto whole0 = [&](const Row& w) { return w.shift ? 1 : 0; };
-  auto whole1 = [&](const Row& w) { return (V + w.shift) / kPer; };
-  auto vec_at = [&](const Row& w, int idx) {
-    return reinterpret_cast<const Vec*>(static_cast<const char*>(w.z) - w.shift * sizeof(T)) + idx;
+  const Row& w = sh.row;
+  // this CTA's share of the row's vectors (in whole words of the bitmaps)
+  const int share = (w.vecs + cluster * 4 - 1) / (cluster * 4) * 4, v0 = min(w.vecs, rank * share), v1 = min(w.vecs, v0 + share);
+  if (!w.live) {
+    if (kOp == kGrad) {  // zeros
+      float d[kPer];
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) d[j] = 0.f;
+      const int end = min(V, v1 * kPer - w.shift);
+#pragma unroll 1
+      for (int b = v0 + tid; b - lane < v1; b += kThreads) {
+        const int v = b * kPer - w.shift;
+        store_vec<kType>(false, w, d, E::narrow(d), v - lane * kPer, b < v1 ? in_row<kPer>(v, V) : 0u, end, stage, lane);
+      }
+    } else if (rank == 0 && tid == 0) {
+      if (a.logp) a.logp[r] = 0.f;
+      if (a.lse) a.lse[r] = 0.f;
+      if (a.ent) a.ent[r] = 0.f;
+    }
+    return;
+  }
+  const bool marked = w.special || w.mask;
+  const float scale = w.scale, sl2 = w.sl2;
+  const float gs = kOp == kGrad ? w.g * scale : 0.f, es = kOp == kGrad ? w.e * scale : 0.f;
+  const float w_lse = kOp == kGrad ? w.lse : 0.f, w_ent = kOp == kGrad ? w.ent : 0.f;
+  const Vec* base = reinterpret_cast<const Vec*>(static_cast<const char*>(w.z) - w.shift * sizeof(T)) + tid;
+  // vectors that are full of the row's entries
+  const int whole0 = w.shift ? 1 : 0, whole1 = min(v1, (V + w.shift) / kPer);
+  // whether the warp's 32 vectors, the first at b + i kThreads + 32 warp, are all whole and before `end`
+  auto full = [&](int b, int i, int end) {
+    const int n = end - 32 - whole0, at = b + i * kThreads + warp * 32 - whole0;
+    return (uint32_t)at <= (uint32_t)n && n >= 0;
   };
   Vec raw[kVecs];
-  // a batch's vectors, where the warp's are all whole and before `end`
-  auto fetch = [&](const Row& w, int b, int end) {
-    const int x0 = whole0(w), n = min(end, whole1(w)) - 32 - x0, at = b + warp * 32 - x0;
-    const Vec* src = vec_at(w, b + tid);
 #pragma unroll
-    for (int i = 0; i < kVecs; ++i)
-      if (n >= 0 && (uint32_t)(at + i * kThreads) <= (uint32_t)n) raw[i] = load_global(src + i * kThreads);
-  };
-  bool ready = false;  // raw holds the row's first vectors
+  for (int i = 0; i < kVecs; ++i) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) raw[i].w[k] = 0u;
+    load_global_if(raw[i], base + v0 + i * kThreads, full(v0, i, whole1));
+  }
   Running p = {kLow, {0.f, 0.f}, {0.f, 0.f}};
-  while (r < a.R) {
-    const Row& w = sh.row[place];
-    const Row& next = sh.row[place ^ 1];
-    const int64_t rn = r + step;
-    const bool marked = w.special || w.mask;
-    const int v0 = w.live ? begins(w) : 0, v1 = w.live ? finishes(w) : 0;
-    const float scale = w.scale, sl2 = w.sl2;
-    const float gs = kOp == kGrad ? w.g * scale : 0.f, es = kOp == kGrad ? w.e * scale : 0.f;
-    const float w_lse = kOp == kGrad ? w.lse : 0.f, w_ent = kOp == kGrad ? w.ent : 0.f;
-    // (by the warp that joins the parts: it has done so with the row before, which was in the same place)
-    if (warp == 0 && rn < a.R) read_row<kType, kOp>(a, st, rn, sh.row[place ^ 1], lane, rank == 0);
-    bool fresh = false;  // raw holds the next row's first vectors
-    for (int s0 = v0; s0 == v0 || s0 < v1; s0 += kSpanVecs) {
+#pragma unroll 1
+  for (int s0 = v0; s0 < v1; s0 += kSpanVecs) {
       const int s1 = min(v1, s0 + kSpanVecs), lo = s0 * kPer - w.shift, n = (s1 - s0) * kPer;
-      if (n > 0 && marked) mark_span(a, st, w, lo, n, s1 == w.vecs, sm);
-      __syncthreads();
-      if (n <= 0) break;
+      if (marked) {
+        mark_span(a, st, w, lo, n, s1 == w.vecs, sm);
+        __syncthreads();
+      }
       const int total = w.special ? rank_span(n, w.mask != nullptr, sm) : 0;
       const int trel = w.target >= 0 && w.target >= lo && w.target < (int64_t)lo + n ? (int)w.target - lo : -1, tvec = trel < 0 ? -1 : trel / kPer;
       // a special entry, or the target: rel its place in the span
@@ -629,7 +668,7 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
         const float z = may ? E::get1(static_cast<const T*>(w.z)[v]) : 0.f;
         float slope = 1.f;
         const float y = !may ? -INFINITY : slot ? adjusted(a, w, slot, z, v, slope) : z;
-        if (kOp != kGrad && rel == trel) sh.at[place] = y;
+        if (kOp != kGrad && rel == trel) sh.at = y;
         if (kOp == kGrad) {
           float d = 0.f;
           if (may && rel == trel) {  // (p from its log-probability, which has the digits of 1 - p)
@@ -716,25 +755,15 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
           }
         }
       };
-      if (!ready) fetch(w, s0, s1);
-      ready = true;
 #pragma unroll 1
       for (int b = s0; b < s1; b += kBatch) {
-        // the batch after this one: of the span, the next span, the next row
-        const bool same = b + kBatch < s1 || s1 < v1, other = !same && rn < a.R && next.live;
-        const Row& wn = other ? next : w;
-        const int n0 = other ? begins(next) : b + kBatch < s1 ? b + kBatch : s1;
-        const int nx = whole0(wn), ny = !(same || other) ? -1 : min(other ? finishes(next) : v1, whole1(wn)) - 32 - nx, nat = n0 + warp * 32 - nx;
-        const Vec* src = vec_at(wn, n0 + tid);
-        fresh = other;
-        const int x0 = whole0(w), n32 = min(s1, whole1(w)) - 32 - x0, at = b + warp * 32 - x0;
-        uint32_t rest = 0u;  // vectors at the ends
+        const int next = b + kBatch < s1 ? b + kBatch : s1;  // (of the span, or the next span's first)
+        uint32_t rest = 0u;                                  // vectors at the ends
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-          const Vec z = raw[i];
-          if (ny >= 0 && (uint32_t)(nat + i * kThreads) <= (uint32_t)ny) raw[i] = load_global(src + i * kThreads);
-          if (n32 >= 0 && (uint32_t)(at + i * kThreads) <= (uint32_t)n32) dense(z, b + i * kThreads + tid, false);
+          if (full(b, i, min(s1, whole1))) dense(raw[i], b + i * kThreads + tid, false);
           else rest |= 1u << i;
+          load_global_if(raw[i], base + next + i * kThreads, full(next, i, whole1));
         }
 #pragma unroll 1
         for (; rest; rest &= rest - 1) {
@@ -754,81 +783,47 @@ __global__ void __launch_bounds__(kThreads, 2) logits_kernel(LogitsArgs a, int c
         __syncthreads();
         if (tid == 0) single(trel, 0u);
       }
-      if (total) {
+      if (s1 < v1 && marked) {
         __syncthreads();
-        for (int j = tid; j < (n + 31) / 32; j += kThreads) sm.special[j] = 0;
+        if (total)
+          for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
+        __syncthreads();
       }
-      if (s1 < v1 && marked) __syncthreads();
-    }
-    ready = fresh;
-    if (kOp == kGrad && !w.live) {  // zeros
-      float d[kPer];
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) d[j] = 0.f;
-      const int e1 = finishes(w), end = min(V, e1 * kPer - w.shift);
-#pragma unroll 1
-      for (int b = begins(w) + tid; b - lane < e1; b += kThreads) {
-        const int v = b * kPer - w.shift;
-        store_vec<kType>(false, w, d, E::narrow(d), v - lane * kPer, b < e1 ? in_row<kPer>(v, V) : 0u, end, stage, lane);
-      }
-    }
-    if (kOp != kGrad) {
-      Part x = {p.m, p.s[0] + p.s[1], p.u[0] + p.u[1]};
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const Part y = {__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
-                        __shfl_xor_sync(0xffffffffu, x.u, o)};
-        x = join<kEnt>(x, y);
-      }
-      if (lane == 0) sh.part[place][warp] = x;
-      p = Running{kLow, {0.f, 0.f}, {0.f, 0.f}};
-    }
-    __syncthreads();
-    if (kOp != kGrad) {
-      auto done = [&](const Part& x, float at) {
-        if (w.live) {
-          finish_row(a, r, w.target >= 0, w.target >= 0 ? at * w.sl2 : 0.f, x);
-        } else {
-          if (a.logp) a.logp[r] = 0.f;
-          if (a.lse) a.lse[r] = 0.f;
-          if (a.ent) a.ent[r] = 0.f;
-        }
-      };
-      if (warp == 0) {
-        Part x = lane < kWarps ? sh.part[place][lane] : Part{kLow, 0.f, 0.f};
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) {
-          const Part y = {__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
-                          __shfl_xor_sync(0xffffffffu, x.u, o)};
-          x = join<kEnt>(x, y);
-        }
-        if (lane == 0) {
-          if (cluster > 1) {
-            st_remote(remote(&sh.cluster[place][rank].m, 0), x.m);
-            st_remote(remote(&sh.cluster[place][rank].s, 0), x.s);
-            st_remote(remote(&sh.cluster[place][rank].u, 0), x.u);
-            // (who has the target's logit passes it on)
-            const int64_t tv = w.target < 0 ? -1 : (w.target + w.shift) / kPer;
-            if (tv >= v0 && tv < v1) st_remote(remote(&sh.cluster_at[place], 0), sh.at[place]);
-          } else {
-            done(x, sh.at[place]);
-          }
-        }
-        __syncwarp();
-      }
-      if (cluster > 1) {
-        cluster_sync();
-        if (rank == 0 && tid == 0) {
-          Part x = sh.cluster[place][0];
-          for (int c = 1; c < cluster; ++c) x = join<kEnt>(x, sh.cluster[place][c]);
-          done(x, sh.cluster_at[place]);
-        }
-      }
-    }
-    r = rn;
-    place ^= 1;
   }
-  if (blockIdx.x == 0 && tid == 0) next_tag(st);
+  if (kOp == kGrad) return;
+  Part x = {p.m, p.s[0] + p.s[1], p.u[0] + p.u[1]};
+  auto join_lanes = [&](int from) {
+    for (int o = from; o > 0; o >>= 1) {
+      const Part y = {__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
+                      __shfl_xor_sync(0xffffffffu, x.u, o)};
+      x = join<kEnt>(x, y);
+    }
+  };
+  join_lanes(16);
+  if (lane == 0) sh.part[warp] = x;
+  __syncthreads();
+  if (warp == 0) {
+    x = lane < kWarps ? sh.part[lane] : Part{kLow, 0.f, 0.f};
+    join_lanes(kWarps / 2);
+    if (lane == 0 && cluster > 1) {
+      st_remote(remote(&sh.cluster[rank].m, 0), x.m);
+      st_remote(remote(&sh.cluster[rank].s, 0), x.s);
+      st_remote(remote(&sh.cluster[rank].u, 0), x.u);
+      // (who has the target's logit passes it on)
+      const int64_t tv = w.target < 0 ? -1 : (w.target + w.shift) / kPer;
+      if (tv >= v0 && tv < v1) st_remote(remote(&sh.cluster_at, 0), sh.at);
+    }
+    __syncwarp();
+  }
+  if (cluster > 1) cluster_sync();
+  if (rank != 0 || tid != 0) return;
+  float at = sh.at;
+  if (cluster > 1) {
+    at = sh.cluster_at;
+    x = sh.cluster[0];
+    for (int c = 1; c < cluster; ++c) x = join<kEnt>(x, sh.cluster[c]);
+  }
+  finish_row(a, r, w.target >= 0, w.target >= 0 ? at * w.sl2 : 0.f, x);
 }
 
 template <int kType, int kOp, bool kEnt>
@@ -848,8 +843,8 @@ cudaError_t setup_type() {
 
 template <int kType, int kOp, bool kEnt>
 cudaError_t launch_one(const LaunchCtx& lc, const LogitsArgs& a, const Status& st) {
-  // two CTAs fit an SM; a row of few gets a cluster, each of whose CTAs has a batch of its vectors or more
-  const int64_t ctas = 2 * (int64_t)lc.num_sms, batches = (a.V / Raw<kType>::kPer + kThreads * kVecs - 1) / (kThreads * kVecs);
+  // a row of few gets a cluster, each of whose CTAs has a batch of its vectors or more
+  const int64_t ctas = kCtas * (int64_t)lc.num_sms, batches = (a.V / Raw<kType>::kPer + kThreads * kVecs - 1) / (kThreads * kVecs);
   int cluster = 1;
   while (cluster < 8 && 2 * cluster * a.R <= ctas && 2 * cluster <= batches) cluster *= 2;
   cudaLaunchAttribute at;
@@ -857,7 +852,7 @@ cudaError_t launch_one(const LaunchCtx& lc, const LogitsArgs& a, const Status& s
   at.val.clusterDim.x = (unsigned)cluster;
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(cluster * std::min<int64_t>(a.R, ctas / cluster)));
+  cfg.gridDim = dim3((unsigned)(cluster * a.R));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = sizeof(Smem);
   cfg.stream = lc.stream;
