@@ -199,6 +199,7 @@ enum : int {
   kWhereVocabRow = 111,    // a row of d_weight or of the gathered tokens
   kWhereEmbedPlace = 112,  // a place in the list of sorted tokens
   kWhereEmbedRow = 113,    // a row of the embedding's table
+  kWhereLogits = 114,      // a special entry of a row of logits
 };
 
 __device__ __forceinline__ uint64_t globaltimer_ns() {

@@ -20,40 +20,20 @@ namespace gpo {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kCtas = 4;                         // on one SM
-constexpr int kVecs = 2;                         // accesses of 32 bytes of a thread that are in flight
+constexpr int kCtas = 2;                         // on one SM
+constexpr int kChunk = 2048;                     // bytes of a row that a warp fetches at a time,
+constexpr int kChunkVecs = kChunk / 16;          // accesses of 16 bytes,
+constexpr int kDeep = 3;                         // and how many of them are in flight
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1;  // an entry's word: flags, occurrences
-enum Op { kAdjust, kScore, kGrad };              // write the adjusted logits, only their statistics, the gradient
+// the adjusted logits (in fp32, of 16-bit ones), only their statistics, the gradient
+enum Op { kAdjust, kAdjust32, kScore, kGrad };
+__host__ __device__ constexpr bool writes(int op) { return op == kAdjust || op == kAdjust32; }
 
-// A vector of 32 bytes of logits.
+// 32 bytes of logits: two accesses of 16 bytes, 512 bytes apart.
 struct Vec {
   uint32_t w[8];
 };
-// (streamed: nothing reads a row again but the few special entries)
-__device__ __forceinline__ Vec load_global(const void* p) {
-  Vec r;
-  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7])
-               : "l"(p)
-               : "memory");
-  return r;
-}
-// The same where `take` says so, else r stays as it is.
-__device__ __forceinline__ void load_global_if(Vec& r, const void* p, bool take) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "setp.ne.s32 q, %9, 0;\n\t"
-      "@q ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t}"
-      : "+r"(r.w[0]), "+r"(r.w[1]), "+r"(r.w[2]), "+r"(r.w[3]), "+r"(r.w[4]), "+r"(r.w[5]), "+r"(r.w[6]), "+r"(r.w[7])
-      : "l"(p), "r"((int)take)
-      : "memory");
-}
-__device__ __forceinline__ void store_global(void* p, const Vec& x) {
-  asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
-               "r"(x.w[3]), "r"(x.w[4]), "r"(x.w[5]), "r"(x.w[6]), "r"(x.w[7])
-               : "memory");
-}
 
 template <int kType>
 struct Raw;
@@ -218,10 +198,8 @@ struct Raw<GPO_DT_F16> : Raw16 {
 struct Row {
   const void* z;
   void* out;
-  int shift;                  // elements between the 32-byte boundary before the row and the row
-  int vecs;                   // accesses of 32 bytes that hold the row
   int live;                   // has a target, or a gradient, or needs none
-  int vec;                    // the output's accesses of a whole vector are aligned
+  int vec;                    // the output's accesses of 16 bytes are aligned where the row's are
   int special;                // some entry may be special
   float scale, sl2;           // and times log2(e)
   float rep, inv, pres, freq; // repetition and 1 / it
@@ -245,19 +223,19 @@ constexpr int kSpan = 131072;         // entries of which it is known at one tim
 constexpr int kWords = kSpan / 32;
 constexpr int kGroups = kWords / 4;   // groups of four words, whose special entries are counted together
 constexpr int kOwn = kGroups / kWarps;  // groups of a warp, side by side
-constexpr int kCap = 2048;            // special entries that are looked at in one round
+static_assert((kWarps & (kWarps - 1)) == 0 && kOwn % 32 == 0, "whole accesses of a warp, a join in halves");
+constexpr int kCap = 1536;            // special entries that are looked at in one round
+constexpr int kIds = 16;              // ids of the history that a thread holds
 struct Smem {
   Shared sh;
   alignas(16) uint32_t special[kWords];
   alignas(16) uint32_t allow[kWords];
   uint32_t before[kGroups];           // special entries in the groups before
-  union {
-    struct {
-      uint32_t list[kCap];            // the round's special entries, in their order,
-      uint32_t count[kCap];           // and their flags and occurrences
-    };
-    float stage[kWarps][512];         // values of each warp on their way out
-  };
+  uint32_t list[kCap];                // the round's special entries, in their order,
+  uint32_t count[kCap];               // and their flags and occurrences
+  uint32_t stage[kWarps][128];        // words of each warp on their way out
+  uint64_t full[kWarps][kDeep];
+  alignas(128) unsigned char ring[kWarps][kDeep][kChunk];
 };
 
 // The bias of v among the row's (ascending).
@@ -281,11 +259,21 @@ __device__ __forceinline__ float adjusted(const LogitsArgs& a, const Row& w, uin
   return y;
 }
 
+// A row: `head` entries before the first 16-byte boundary, `vecs` whole accesses, then less than one.
+template <class T>
+struct Edges {
+  int head, vecs;
+  __device__ __forceinline__ Edges(const T* z, int64_t V) {
+    constexpr int kPer = 16 / sizeof(T);
+    head = (int)min(V, (int64_t)((0 - (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T))) & (kPer - 1)));
+    vecs = (int)(V - head) / kPer;
+  }
+};
+
 // One warp reads a row's arguments, a lane each, and checks them.
 template <int kType, int kOp>
 __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, int64_t r, Row& out, int lane, bool first) {
-  using E = Raw<kType>;
-  using T = typename E::T;
+  using T = typename Raw<kType>::T;
   const char* p = nullptr;
   bool wide = false;
   auto from = [&](const void* base, int64_t i, bool is8) {
@@ -327,11 +315,9 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   Row w;
   const T* z = static_cast<const T*>(a.z) + r * a.z_stride;
   w.z = z;
-  w.shift = (int)((reinterpret_cast<uintptr_t>(z) & 31) / sizeof(T));
-  w.vecs = (int)((a.V + w.shift + E::kPer - 1) / E::kPer);
-  const size_t osz = a.out32 ? 4 : sizeof(T);
+  const size_t osz = kOp == kAdjust32 ? 4 : sizeof(T);
   w.out = kOp == kScore ? nullptr : static_cast<char*>(a.out) + r * a.out_stride * osz;
-  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) - w.shift * osz) & 31) == 0;
+  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) + Edges<T>(z, a.V).head * osz) & 15) == 0;
   w.scale = f32(0, a.scale, a.scale1);
   w.rep = f32(1, a.rep, a.rep1);
   w.pres = f32(2, a.pres, a.pres1);
@@ -363,7 +349,7 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
     bad(GPO_ERR_SHAPE, 5);
     w.target = -1;
   }
-  w.live = kOp == kAdjust || w.target >= 0;
+  w.live = writes(kOp) || w.target >= 0;
   w.g = f32(11, a.g, 0.f);
   w.e = f32(12, a.ge, 0.f);
   w.ent = f32(13, a.ge, 0.f);
@@ -374,61 +360,82 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   if (lane == 0) out = w;
 }
 
-// Calls f(id - lo, i) for the ids of the history in the n entries from lo on, i their place.
+// kIds ids of each thread from place `from` of the row's history on (-1 behind its end).
+__device__ __forceinline__ void load_ids(const LogitsArgs& a, const Row& w, int from, int (&id)[kIds]) {
+  const int len = (int)(w.h1 - w.h0) - from - (int)threadIdx.x;
+  // (one branch around the loads, which are then in flight together)
+  if (a.hist8) {
+    const int64_t* ids = static_cast<const int64_t*>(a.hist) + w.h0 + from + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) {
+      const int64_t x = k * kThreads < len ? ids[k * kThreads] : -1;
+      id[k] = x < 0 ? -1 : (int)min(x, a.V);
+    }
+  } else {
+    const int32_t* ids = static_cast<const int32_t*>(a.hist) + w.h0 + from + threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < kIds; ++k) id[k] = k * kThreads < len ? ids[k * kThreads] : -1;
+  }
+}
+// Calls f(id - lo, k) for those of [lo + r0, lo + r1).
 template <class F>
-__device__ __forceinline__ void for_history(const LogitsArgs& a, const Row& w, int lo, int64_t n, F f) {
-  for (int64_t i = w.h0 + threadIdx.x; i < w.h1; i += 4 * kThreads) {
-    int64_t id[4];
-    // (one branch around the loads of a thread, which are then in flight together)
-    if (a.hist8) {
+__device__ __forceinline__ void each_id(const int (&id)[kIds], int lo, int r0, int r1, F f) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) id[k] = i + k * kThreads < w.h1 ? static_cast<const int64_t*>(a.hist)[i + k * kThreads] : -1;
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) id[k] = i + k * kThreads < w.h1 ? static_cast<const int32_t*>(a.hist)[i + k * kThreads] : -1;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int64_t rel = id[k] - lo;
-      if (id[k] >= 0 && rel >= 0 && rel < n) f(rel, i + k * kThreads);
-    }
+  for (int k = 0; k < kIds; ++k) {
+    const int rel = id[k] - lo;  // (lo is -8 or more, and -1 is no entry of the row: it is below r0)
+    if ((uint32_t)(rel - r0) < (uint32_t)(r1 - r0)) f((uint32_t)rel, k);
   }
 }
 
-// Marks the special entries of a span of n from entry lo on (below 0: before the row) in their bitmap, which was zeros, and
-// writes that of the allowed ones where the row has a mask.
-// (last: of the row; ids past the vocabulary are found there)
-__device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st, const Row& w, int lo, int n, bool last, Smem& sm) {
+// A span of a row: bit j of the bitmaps is entry lo + j; [r0, r1) of them are the span's, r1 <= kSpan.
+struct Span {
+  int lo, r0, r1;
+};
+
+// Marks the special entries of a span in their bitmap, which was zeros, and writes that of the allowed ones where the row has a
+// mask.  id: the last ids of the history.
+__device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st, const Row& w, const Span& s, int trel, int (&id)[kIds], Smem& sm) {
   const int V = (int)a.V;
+  auto mark = [&](uint32_t rel) { atomicOr(sm.special + (rel >> 5), 1u << (rel & 31u)); };
+  if (w.special) {
+    const int len = (int)(w.h1 - w.h0);
+    bool bad = false;
+    for (int from = 0; from < len; from += kIds * kThreads) {
+      load_ids(a, w, from, id);
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) bad |= id[k] >= V;
+      each_id(id, s.lo, s.r0, s.r1, [&](uint32_t rel, int) { mark(rel); });
+    }
+    if (bad) report(st, GPO_ERR_SHAPE, 46, (int)w.h0);
+    for (int64_t i = w.b0 + threadIdx.x; i < w.b1; i += kThreads) {
+      const int64_t x = load_id(a.bias_ids, a.bias8, i), rel = x - s.lo;
+      if (x < 0 || x >= V || (i > w.b0 && load_id(a.bias_ids, a.bias8, i - 1) >= x)) report(st, GPO_ERR_SHAPE, 47, (int)i);
+      else if (rel >= s.r0 && rel < s.r1) mark((uint32_t)rel);
+    }
+    if (trel >= 0 && threadIdx.x == 0) mark((uint32_t)trel);
+  }
   if (w.mask) {
-    const int words = (V + 31) >> 5, sh = lo & 31, at0 = lo >> 5;
-    for (int j = threadIdx.x; j < (n + 31) / 32; j += kThreads) {
+    const int words = (V + 31) >> 5, sh = s.lo & 31, at0 = s.lo >> 5;
+    for (int j = threadIdx.x; j < (s.r1 + 31) / 32; j += kThreads) {
       const int at = at0 + j;
       const uint32_t x0 = at >= 0 && at < words ? __ldg(w.mask + at) : 0u, x1 = at + 1 < words ? __ldg(w.mask + at + 1) : 0u;
       sm.allow[j] = __funnelshift_r(x0, x1, (uint32_t)sh);
     }
   }
-  if (!w.special) return;
-  for_history(a, w, lo, last ? INT64_MAX : n, [&](int64_t rel, int64_t i) {
-    if (lo + rel >= V) report(st, GPO_ERR_SHAPE, 46, (int)i);
-    else atomicOr(sm.special + (rel >> 5), 1u << (rel & 31u));
-  });
-  for (int64_t i = w.b0 + threadIdx.x; i < w.b1; i += kThreads) {
-    const int64_t id = load_id(a.bias_ids, a.bias8, i), rel = id - lo;
-    if (id < 0 || id >= V || (i > w.b0 && load_id(a.bias_ids, a.bias8, i - 1) >= id)) report(st, GPO_ERR_SHAPE, 47, (int)i);
-    else if (rel >= 0 && rel < n) atomicOr(sm.special + (rel >> 5), 1u << (rel & 31u));
-  }
 }
 
-// The number of special entries of the span, and of those before each group of words; these leave the allowed ones.
+// The number of special entries of the span that are allowed, which alone stay special, and of those before each group of words;
+// they leave the allowed ones.
 __device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (n + 127) / 128;
   int sum = 0;
 #pragma unroll 1
   for (int g0 = warp * kOwn; g0 < min(groups, (warp + 1) * kOwn); g0 += 32) {
     const int g = g0 + lane;
-    const uint4 x = reinterpret_cast<const uint4*>(sm.special)[g];
+    uint4& sp = reinterpret_cast<uint4*>(sm.special)[g];
     uint4& al = reinterpret_cast<uint4*>(sm.allow)[g];
+    uint4 x = sp;
+    if (masked) sp = x = make_uint4(x.x & al.x, x.y & al.y, x.z & al.z, x.w & al.w);
     al = masked ? make_uint4(al.x & ~x.x, al.y & ~x.y, al.z & ~x.z, al.w & ~x.w) : make_uint4(~x.x, ~x.y, ~x.z, ~x.w);
     const int own = __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
     int upto = own;
@@ -454,8 +461,9 @@ __device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
 }
 
 // The round's special entries, those of ranks [first, first + kCap), and their flags and counts.  Between barriers of the caller.
-__device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, int lo, int n, int first, int total, Smem& sm) {
-  for (int g = threadIdx.x; g < (n + 127) / 128; g += kThreads) {
+// id: the last ids of the history.
+__device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, const Span& s, int first, int total, int (&id)[kIds], Smem& sm) {
+  for (int g = threadIdx.x; g < (s.r1 + 127) / 128; g += kThreads) {
     const uint4 x = reinterpret_cast<const uint4*>(sm.special)[g];
     int k = (int)sm.before[g] - first;
     auto put = [&](uint32_t bits, int rel) {
@@ -469,88 +477,91 @@ __device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, 
   }
   for (int c = threadIdx.x; c < min(kCap, total - first); c += kThreads) sm.count[c] = 0;
   __syncthreads();
+  // the place of a special entry in the list, of others far above its end
   auto at = [&](uint32_t rel) {
-    const uint32_t word = rel >> 5 & 3u, low = (1u << (rel & 31u)) - 1u;
+    const uint32_t word = rel >> 5 & 3u, bit = 1u << (rel & 31u);
     const uint4 x = reinterpret_cast<const uint4*>(sm.special)[rel >> 7];
     const uint32_t own = word == 0 ? x.x : word == 1 ? x.y : word == 2 ? x.z : x.w;
-    return (int)sm.before[rel >> 7] - first + __popc(own & low) + (word > 0 ? __popc(x.x) : 0) + (word > 1 ? __popc(x.y) : 0) +
-           (word > 2 ? __popc(x.z) : 0);
+    const int k = (int)sm.before[rel >> 7] - first + __popc(own & (bit - 1u)) + (word > 0 ? __popc(x.x) : 0) + (word > 1 ? __popc(x.y) : 0) +
+                  (word > 2 ? __popc(x.z) : 0);
+    return own & bit ? (uint32_t)k : 0xFFFFFFFFu;
   };
-  for_history(a, w, lo, min((int64_t)n, a.V - lo), [&](int64_t rel, int64_t i) {
-    const int k = at((uint32_t)rel);
-    if (k < 0 || k >= kCap) return;
-    if (i >= w.hg) atomicAdd(sm.count + k, 1u);
-    else atomicOr(sm.count + k, kSeen);
-  });
+  const int len = (int)(w.h1 - w.h0), generated = (int)(w.hg - w.h0) - (int)threadIdx.x;
+  constexpr int kPart = kIds * kThreads;
+  // (from the part that the thread holds back to the first)
+  for (int from = len > 0 ? (len - 1) / kPart * kPart : -1; from >= 0; from -= kPart) {
+    if (from + kPart < len || first > 0) load_ids(a, w, from, id);
+    each_id(id, s.lo, s.r0, s.r1, [&](uint32_t rel, int k) {
+      const uint32_t to = at(rel);
+      if (to >= (uint32_t)kCap) return;
+      if (from + k * kThreads >= generated) atomicAdd(sm.count + to, 1u);
+      else atomicOr(sm.count + to, kSeen);
+    });
+  }
   for (int64_t i = w.b0 + threadIdx.x; i < w.b1; i += kThreads) {
-    const int64_t id = load_id(a.bias_ids, a.bias8, i), rel = id - lo;
-    if (id < 0 || id >= a.V || rel < 0 || rel >= n || !(sm.special[rel >> 5] >> (rel & 31) & 1u)) continue;
-    const int k = at((uint32_t)rel);
-    if (k >= 0 && k < kCap) atomicOr(sm.count + k, kBiased);
+    const int64_t rel = load_id(a.bias_ids, a.bias8, i) - s.lo;
+    if (rel < s.r0 || rel >= s.r1) continue;
+    const uint32_t to = at((uint32_t)rel);
+    if (to < (uint32_t)kCap) atomicOr(sm.count + to, kBiased);
   }
 }
 
-// Which entries of the vector at v are in the row.
-template <int kPer>
-__device__ __forceinline__ uint32_t in_row(int v, int V) {
-  uint32_t in = (1u << kPer) - 1u;
-  if (v < 0) in &= v <= -kPer ? 0u : in << -v;
-  if (v + kPer > V) in &= v >= V ? 0u : in >> (v + kPer - V);
-  return in;
+__device__ __forceinline__ uint4 load_shared(const void* p) {
+  uint4 r;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem_u32(p)) : "memory");
+  return r;
+}
+__device__ __forceinline__ void store_global(void* p, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// Bytes (a multiple of 16, as are the addresses) to this CTA's shared memory, counted on a barrier.
+__device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(to)), "l"(from),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
 }
 
-// A vector of the row, whose first entry is v; entries outside the row are 0.
-template <int kType>
-__device__ __forceinline__ Vec load_vec(const void* row, int v, int V) {
-  using E = Raw<kType>;
-  using T = typename E::T;
-  const T* z = static_cast<const T*>(row);
-  if (v >= 0 && v + E::kPer <= V) return load_global(z + v);
-  float y[E::kPer];
+// Four words of every lane to a row of any alignment, by a whole warp: entries of 4 or 2 bytes, lane 0's first v0, the next lane's
+// `stride` after it, none from `end` on.  Through shared memory, so that an access takes 32 words side by side.  (A call of its own:
+// few rows need it, and its registers are the others' spills.)
+__device__ __noinline__ void store_ragged(void* out, bool four, uint4 x, int v0, int stride, int end, uint32_t* stage) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+  reinterpret_cast<uint4*>(stage)[lane] = x;
+  __syncwarp();
 #pragma unroll
-  for (int i = 0; i < E::kPer; ++i) y[i] = v + i >= 0 && v + i < V ? E::get1(z[v + i]) : 0.f;
-  return E::narrow(y);
-}
-
-// kPer values of every lane to the row, by a whole warp: lane 0's first entry is v0, `in` says which of a lane's are to be written (none from `end` on).
-// In an aligned row a lane's are one or two accesses; in others the warp's go through shared memory, so that an access
-// takes 32 entries side by side.
-template <int kType>
-__device__ __forceinline__ void store_vec(bool wide, const Row& w, const float (&y)[Raw<kType>::kPer], const Vec& narrow, int v0, uint32_t in,
-                                          int end, float* stage, int lane) {
-  using E = Raw<kType>;
-  using T = typename E::T;
-  constexpr int kPer = E::kPer;
-  const int v = v0 + lane * kPer;
-  const bool whole = in == (1u << kPer) - 1u;
-  if (w.vec && whole) {
-    if (wide) {
-      float* p = static_cast<float*>(w.out) + v;
-#pragma unroll
-      for (int i = 0; i < kPer / 8; ++i) {
-        Vec x;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x.w[k] = __float_as_uint(y[8 * i + k]);
-        store_global(p + 8 * i, x);
-      }
+  for (int i = 0; i < 4; ++i) {
+    const int at = i * 32 + lane, v = v0 + at / 4 * stride + (four ? at % 4 : 2 * (at % 4));
+    const uint32_t y = stage[at];
+    if (four) {
+      if (v < end) static_cast<uint32_t*>(out)[v] = y;
     } else {
-      store_global(static_cast<T*>(w.out) + v, narrow);
+      if (v < end) static_cast<uint16_t*>(out)[v] = (uint16_t)y;
+      if (v + 1 < end) static_cast<uint16_t*>(out)[v + 1] = (uint16_t)(y >> 16);
     }
   }
-  if (w.vec && __all_sync(0xffffffffu, whole)) return;
   __syncwarp();
+}
+
+// One access of every lane to the row, by a whole warp: lane 0's first entry is v0, none from `end` on, which lies between two lanes'.
+// y: the same in fp32, for rows of those.
+template <int kType, bool kWide>
+__device__ __forceinline__ void store_vec(const Row& w, const float* y, const uint32_t* x, int v0, int end, uint32_t* stage, int lane) {
+  using T = typename Raw<kType>::T;
+  constexpr int kEach = 16 / sizeof(T);
+  const int v = v0 + lane * kEach;
+  if (kWide) {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) stage[lane * kPer + i] = wide || sizeof(T) == 4 ? y[i] : E::get(narrow, i);
-  __syncwarp();
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int x = v0 + i * 32 + lane;
-    const float f = stage[i * 32 + lane];
-    if (x < 0 || x >= end) continue;
-    if (wide) static_cast<float*>(w.out)[x] = f;
-    else static_cast<T*>(w.out)[x] = E::put(f);
+    for (int i = 0; i < kEach; i += 4) {
+      const uint4 o = make_uint4(__float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]), __float_as_uint(y[i + 3]));
+      if (!w.vec) store_ragged(w.out, true, o, v0 + i, kEach, end, stage);
+      else if (v < end) store_global(static_cast<float*>(w.out) + v + i, o.x, o.y, o.z, o.w);
+    }
+  } else if (!w.vec) {
+    store_ragged(w.out, sizeof(T) == 4, make_uint4(x[0], x[1], x[2], x[3]), v0, kEach, end, stage);
+  } else if (v < end) {
+    store_global(static_cast<T*>(w.out) + v, x[0], x[1], x[2], x[3]);
   }
-  __syncwarp();
 }
 
 // The statistics of a row from its joined parts; zy: the target's logit in units of log 2, which is in no part.
@@ -576,19 +587,40 @@ __device__ __forceinline__ void st_remote(uint32_t addr, float x) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(x) : "memory");
 }
 
+// Two numbers in one register pair, which the packed instructions take.
+__device__ __forceinline__ float lo_f2(uint64_t a) { return __uint_as_float((uint32_t)a); }
+__device__ __forceinline__ float hi_f2(uint64_t a) { return __uint_as_float((uint32_t)(a >> 32)); }
+__device__ __forceinline__ uint64_t make_f2(float a, float b) { return pack_f2(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ uint64_t ex2_f2(uint64_t a) { return make_f2(ex2(lo_f2(a)), ex2(hi_f2(a))); }
+__device__ __forceinline__ uint64_t max_f2(uint64_t a, float b) { return make_f2(fmaxf(lo_f2(a), b), fmaxf(hi_f2(a), b)); }
+template <int kN>
+__device__ __forceinline__ void pairs_of(const float (&x)[kN], uint64_t (&y)[kN / 2]) {
+#pragma unroll
+  for (int j = 0; j < kN / 2; ++j) y[j] = make_f2(x[2 * j], x[2 * j + 1]);
+}
+template <int kN>
+__device__ __forceinline__ void of_pairs(const uint64_t (&y)[kN / 2], float (&x)[kN]) {
+#pragma unroll
+  for (int j = 0; j < kN / 2; ++j) x[2 * j] = lo_f2(y[j]), x[2 * j + 1] = hi_f2(y[j]);
+}
+
 // Sums of exponentials so far, in two chains, relative to m.
 struct Running {
-  float m, s[2], u[2];
+  float m;
+  uint64_t s, u;
 };
+template <bool kB>
+struct Bool {
+  static constexpr bool value = kB;
+};
+
 template <bool kEnt>
 __device__ __forceinline__ void raise(Running& p, float top) {
   if (!(top > p.m)) return;
-  const float c = p.m - top, e = ex2(c);
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    if (kEnt) p.u[k] = e * fmaf(c, p.s[k], p.u[k]);
-    p.s[k] *= e;
-  }
+  const float c = p.m - top;
+  const uint64_t e = f2splat(ex2(c));
+  if (kEnt) p.u = f2mul(e, f2fma(f2splat(c), p.s, p.u));
+  p.s = f2mul(e, p.s);
   p.m = top;
 }
 
@@ -596,35 +628,72 @@ template <int kType, int kOp, bool kEnt>
 __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, int cluster, Status st) {
   using E = Raw<kType>;
   using T = typename E::T;
-  constexpr int kPer = E::kPer, kSpanVecs = kSpan / kPer, kBatch = kThreads * kVecs;
+  constexpr int kPer = E::kPer, kEach = kPer / 2;            // entries of a Vec, of one access
+  constexpr int kSpanVecs = (kSpan - 16) / kEach / kChunkVecs * kChunkVecs;
   constexpr uint32_t kAll = (1u << kPer) - 1u;
-  extern __shared__ __align__(16) unsigned char smem[];
+  constexpr bool wide = kOp == kAdjust32;
+  extern __shared__ __align__(128) unsigned char smem[];
   Smem& sm = *reinterpret_cast<Smem*>(smem);
   Shared& sh = sm.sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = (int)a.V;
-  float* stage = sm.stage[warp];
+  uint32_t* stage = sm.stage[warp];
   const int rank = cluster > 1 ? (int)cluster_rank() : 0;
   const int64_t r = blockIdx.x / cluster;
-  const bool wide = a.out32 && sizeof(T) == 2;
+  const T* z0 = static_cast<const T*>(a.z) + r * a.z_stride;
+  const Edges<T> row(z0, V);
+  // this CTA's share of the row's accesses, in chunks; the warps take them in turn
+  const int chunks = (row.vecs + kChunkVecs - 1) / kChunkVecs, share = (chunks + cluster - 1) / cluster;
+  const int c0 = min(chunks, rank * share), c1 = min(chunks, c0 + share);
+  uint64_t* full = sm.full[warp];
+  int fetched = 0, taken = 0;  // chunks of this warp
+  auto fetch = [&]() {
+    const int c = c0 + fetched * kWarps + warp;
+    if (c >= c1) return;
+    if (lane == 0) {
+      const uint32_t bytes = 16u * (uint32_t)min(kChunkVecs, row.vecs - c * kChunkVecs);
+      mbar_arrive_expect_tx(full + fetched % kDeep, bytes);
+      bulk_load(sm.ring[warp][fetched % kDeep], z0 + row.head + (int64_t)c * kChunkVecs * kEach, bytes, full + fetched % kDeep);
+    }
+    ++fetched;
+  };
+  // The row's first bytes are on their way before anything else is known of it but that it is read
+  // (bounded waits for them are below, for every chunk that is fetched).
+  const int64_t wanted = a.target && !writes(kOp) ? load_id(a.target, a.target8, r) : 0;
+  if (lane == 0) {
+    for (int k = 0; k < kDeep; ++k) mbar_init(full + k, 1);
+    fence_mbar_init();
+  }
+  __syncwarp();
+  const bool early = wanted >= 0 && wanted < V;
+  if (early)
+    for (int k = 0; k < kDeep; ++k) fetch();
   if (warp == 0) read_row<kType, kOp>(a, st, r, sh.row, lane, rank == 0);
   if (a.spans || a.bias)
     for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
   if (blockIdx.x == 0 && tid == 32) next_tag(st);
   __syncthreads();
   const Row& w = sh.row;
-  // this CTA's share of the row's vectors (in whole words of the bitmaps)
-  const int share = (w.vecs + cluster * 4 - 1) / (cluster * 4) * 4, v0 = min(w.vecs, rank * share), v1 = min(w.vecs, v0 + share);
+  bool ok = true;  // (of the whole warp)
+  auto arrived = [&]() {
+    ok = ok && __all_sync(0xffffffffu, mbar_wait(full + taken % kDeep, (uint32_t)(taken / kDeep) & 1u, st, 48));
+    return ok;
+  };
+  // every copy that was asked for lands before the shared memory goes
+  auto drain = [&]() {
+    for (; taken < fetched; ++taken) mbar_wait(full + taken % kDeep, (uint32_t)(taken / kDeep) & 1u, st, 48, 200000000ull, false);
+  };
   if (!w.live) {
+    drain();
     if (kOp == kGrad) {  // zeros
-      float d[kPer];
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) d[j] = 0.f;
-      const int end = min(V, v1 * kPer - w.shift);
+      const float none[kPer] = {};
+      const uint32_t zero[4] = {0u, 0u, 0u, 0u};
+      const int body = row.head + min(row.vecs, c0 * kChunkVecs) * kEach, whole = row.head + min(row.vecs, c1 * kChunkVecs) * kEach;
+      const int first = rank == 0 ? 0 : body, end = rank == cluster - 1 ? V : whole;
+      T* out = static_cast<T*>(w.out);
+      for (int v = first + tid; v < body; v += kThreads) out[v] = E::put(0.f);
 #pragma unroll 1
-      for (int b = v0 + tid; b - lane < v1; b += kThreads) {
-        const int v = b * kPer - w.shift;
-        store_vec<kType>(false, w, d, E::narrow(d), v - lane * kPer, b < v1 ? in_row<kPer>(v, V) : 0u, end, stage, lane);
-      }
+      for (int v = body + warp * 32 * kEach; v < whole; v += kThreads * kEach) store_vec<kType, false>(w, none, zero, v, whole, stage, lane);
+      for (int v = whole + tid; v < end; v += kThreads) out[v] = E::put(0.f);
     } else if (rank == 0 && tid == 0) {
       if (a.logp) a.logp[r] = 0.f;
       if (a.lse) a.lse[r] = 0.f;
@@ -636,162 +705,221 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   const float scale = w.scale, sl2 = w.sl2;
   const float gs = kOp == kGrad ? w.g * scale : 0.f, es = kOp == kGrad ? w.e * scale : 0.f;
   const float w_lse = kOp == kGrad ? w.lse : 0.f, w_ent = kOp == kGrad ? w.ent : 0.f;
-  const Vec* base = reinterpret_cast<const Vec*>(static_cast<const char*>(w.z) - w.shift * sizeof(T)) + tid;
-  // vectors that are full of the row's entries
-  const int whole0 = w.shift ? 1 : 0, whole1 = min(v1, (V + w.shift) / kPer);
-  // whether the warp's 32 vectors, the first at b + i kThreads + 32 warp, are all whole and before `end`
-  auto full = [&](int b, int i, int end) {
-    const int n = end - 32 - whole0, at = b + i * kThreads + warp * 32 - whole0;
-    return (uint32_t)at <= (uint32_t)n && n >= 0;
-  };
-  Vec raw[kVecs];
-#pragma unroll
-  for (int i = 0; i < kVecs; ++i) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) raw[i].w[k] = 0u;
-    load_global_if(raw[i], base + v0 + i * kThreads, full(v0, i, whole1));
-  }
-  Running p = {kLow, {0.f, 0.f}, {0.f, 0.f}};
+  if (!early)
+    for (int k = 0; k < kDeep; ++k) fetch();
+  bool holds = false;  // the target
+  Running p = {kLow, 0ull, 0ull};
 #pragma unroll 1
-  for (int s0 = v0; s0 < v1; s0 += kSpanVecs) {
-      const int s1 = min(v1, s0 + kSpanVecs), lo = s0 * kPer - w.shift, n = (s1 - s0) * kPer;
-      if (marked) {
-        mark_span(a, st, w, lo, n, s1 == w.vecs, sm);
+  for (int s0 = min(row.vecs, c0 * kChunkVecs);; s0 += kSpanVecs) {
+    const int end = min(row.vecs, c1 * kChunkVecs), s1 = min(end, s0 + kSpanVecs);
+    const bool head = rank == 0 && s0 == 0, last = s1 == end, tail = last && rank == cluster - 1;
+    // bit 8 of the bitmaps is the span's first whole access, what is before or behind those its ends
+    Span span;
+    span.lo = row.head + s0 * kEach - 8;
+    span.r0 = head ? 8 - row.head : 8;
+    span.r1 = tail ? V - span.lo : (s1 - s0) * kEach + 8;
+    const int trel = w.target >= (int64_t)span.lo + span.r0 && w.target < (int64_t)span.lo + span.r1 ? (int)w.target - span.lo : -1;
+    holds |= trel >= 0;
+    int id[kIds];
+    int total = 0;
+    if (marked) {
+      mark_span(a, st, w, span, trel, id, sm);
+      __syncthreads();
+      if (w.special) {
+        total = rank_span(span.r1, w.mask != nullptr, sm);
         __syncthreads();
+        list_special(a, w, span, 0, total, id, sm);  // (complete after the dense pass's barrier)
       }
-      const int total = w.special ? rank_span(n, w.mask != nullptr, sm) : 0;
-      const int trel = w.target >= 0 && w.target >= lo && w.target < (int64_t)lo + n ? (int)w.target - lo : -1, tvec = trel < 0 ? -1 : trel / kPer;
-      // a special entry, or the target: rel its place in the span
-      auto single = [&](int rel, uint32_t slot) {
-        const int v = lo + rel;
-        const bool may = !w.mask || (__ldg(w.mask + (v >> 5)) >> (v & 31) & 1u);
-        const float z = may ? E::get1(static_cast<const T*>(w.z)[v]) : 0.f;
-        float slope = 1.f;
-        const float y = !may ? -INFINITY : slot ? adjusted(a, w, slot, z, v, slope) : z;
-        if (kOp != kGrad && rel == trel) sh.at = y;
-        if (kOp == kGrad) {
-          float d = 0.f;
-          if (may && rel == trel) {  // (p from its log-probability, which has the digits of 1 - p)
-            const float pe = expf(w.logp);
-            d = -gs * expm1f(w.logp) - (kEnt && pe > 0.f ? es * pe * (w.logp + w.ent) : 0.f);
-          } else if (may) {
-            const float x = fmaxf(fmaf(y, scale, -w.lse), -200.f), pe = ex2(x * kLog2e);
-            d = w.lse == w.lse ? -gs * pe - (kEnt ? es * pe * (x + w.ent) : 0.f) : w.lse;
-          }
-          static_cast<T*>(w.out)[v] = E::put(d * slope);
+    }
+    // d y_j = -gs p_j - es p_j (log p_j + H), without the target's gs
+    auto gradient = [&](float (&y)[kPer]) {
+      uint64_t y2[kPer / 2];
+      pairs_of(y, y2);
+      const uint64_t s2 = f2splat(scale), n2 = f2splat(-w_lse), k2 = f2splat(kLog2e), g2 = f2splat(-gs), e2 = f2splat(-es), h2 = f2splat(w_ent);
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        uint64_t d = f2fma(y2[j], s2, n2);
+        if (kEnt) d = max_f2(d, -200.f);
+        const uint64_t x = ex2_f2(f2mul(d, k2));
+        y2[j] = f2mul(x, kEnt ? f2fma(e2, f2add(d, h2), g2) : g2);
+      }
+      of_pairs(y2, y);
+    };
+    // the entries that are left in x enter the sums
+    auto sums = [&](const Vec& x) {
+      raise<kEnt>(p, E::top(x) * sl2);
+      float y[kPer];
+      uint64_t y2[kPer / 2];
+      E::widen(x, y);
+      pairs_of(y, y2);
+      const uint64_t s2 = f2splat(sl2), n2 = f2splat(-p.m);
+#pragma unroll
+      for (int j = 0; j < kPer / 2; ++j) {
+        const uint64_t d = f2fma(y2[j], s2, n2), e = ex2_f2(d);
+        p.s = f2add(p.s, e);
+        // (0 times -inf is 0 here)
+        if (kEnt) p.u = f2fma(e, E::kFloors ? d : max_f2(d, -200.f), p.u);
+      }
+    };
+    // What an allowed entry becomes (rel: its place in the span, z: its raw logit); it enters the sums.
+    auto single = [&](int rel, uint32_t slot, float z) {
+      float slope;
+      const float y = adjusted(a, w, slot, z, span.lo + rel, slope);
+      if (kOp == kGrad) {
+        float d;
+        if (rel == trel) {  // (p from its log-probability, which has the digits of 1 - p)
+          const float pe = expf(w.logp);
+          d = -gs * expm1f(w.logp) - (kEnt && pe > 0.f ? es * pe * (w.logp + w.ent) : 0.f);
         } else {
-          if (kOp == kAdjust) {
-            if (wide) static_cast<float*>(w.out)[v] = y * scale;
-            else static_cast<T*>(w.out)[v] = E::put(y * scale);
-          }
-          if (!may || rel == trel) return;
-          raise<kEnt>(p, y * sl2);
-          const float d = fmaf(y, sl2, -p.m), x = ex2(d);
-          p.s[0] += x;
-          if (kEnt) p.u[0] = fmaf(x, fmaxf(d, -200.f), p.u[0]);
+          const float x = fmaxf(fmaf(y, scale, -w.lse), -200.f), pe = ex2(x * kLog2e);
+          d = w.lse == w.lse ? -gs * pe - (kEnt ? es * pe * (x + w.ent) : 0.f) : w.lse;
         }
-      };
-      // a warp's 32 vectors, idx this lane's; edge: some may be outside the row or the span
-      auto dense = [&](const Vec& z, int idx, bool edge) {
-        const int v = idx * kPer - w.shift, at = idx - s0;
-        uint32_t take = kAll, sp = 0u, in = kAll;
-        if (edge) in = idx >= s1 ? 0u : in_row<kPer>(v, V) & kAll;
-        if (marked) {
-          const int k = edge ? min(at, kSpan / kPer - 1) : at;
-          auto bits = [&](const uint32_t* p) -> uint32_t {
-            return kPer == 16 ? reinterpret_cast<const uint16_t*>(p)[k] : reinterpret_cast<const uint8_t*>(p)[k];
-          };
-          take = bits(sm.allow);
-          if (kOp != kScore && total) sp = bits(sm.special);
-        }
-        if (edge) take &= in;
-        if (at == tvec) {
-          const uint32_t bit = 1u << (uint32_t)trel % kPer;
-          sp |= bit;
-          take &= ~bit;
-        }
-        if (kOp == kGrad) {
-          // d y_j = -gs p_j - es p_j (log p_j + H)
-          float y[kPer];
-          E::widen(z, y);
+        return d * slope;
+      }
+      if (rel == trel) {
+        sh.at = y;
+      } else {
+        raise<kEnt>(p, y * sl2);
+        const float d = fmaf(y, sl2, -p.m), x = ex2(d);
+        p.s = f2add(p.s, make_f2(x, 0.f));
+        if (kEnt) p.u = f2fma(make_f2(x, 0.f), make_f2(fmaxf(d, -200.f), 0.f), p.u);
+      }
+      return y * scale;
+    };
+    auto put = [&](int rel, float x) {
+      if (!GPO_BOUNDS(st, span.lo + rel, V, kWhereLogits)) return;
+      if (wide) static_cast<float*>(w.out)[span.lo + rel] = x;
+      else static_cast<T*>(w.out)[span.lo + rel] = E::put(x);
+    };
+    // An access of the span: its bits.
+    auto bits_at = [&](const uint32_t* p, int k) -> uint32_t {
+      const uint8_t* b = reinterpret_cast<const uint8_t*>(p) + 1;
+      return kEach == 8 ? b[k] : b[k >> 1] >> 4 * (k & 1) & 15u;
+    };
+    const int tvec = trel < 8 ? -1 : (trel - 8) / kEach;  // the target's access
+    // Two accesses of each lane, k and k + 32 of the span, entries from v on, of the accesses before `end`.  kMarked: some may be masked or special, or none of
+    // the span; kKeep: special ones are written as they were, to be read once more.
+    auto dense = [&](Vec& x, int k, int stop, auto is_marked, auto keeps) {
+      constexpr bool kMarked = decltype(is_marked)::value, kKeep = decltype(keeps)::value;
+      uint32_t take = kAll, sp = 0u;
+      if (kMarked) {
+        if (marked) take = bits_at(sm.allow, k) | bits_at(sm.allow, min(k + 32, kSpanVecs)) << kEach;
+        if (kKeep && total) sp = bits_at(sm.special, k) | bits_at(sm.special, min(k + 32, kSpanVecs)) << kEach;
+        uint32_t out = 0u;
+        if (!total && k == tvec) out = 1u << (trel - 8) % kEach;
+        if (!total && k + 32 == tvec) out = 1u << (kEach + (trel - 8) % kEach);
+        take &= ~out;
+        if (kKeep) sp |= out;
+        if (k >= stop) take = 0u;
+        else if (k + 32 >= stop) take &= (1u << kEach) - 1u;
+      }
+      const int first = span.lo + 8 + (k - lane) * kEach, from = span.lo + 8 + stop * kEach;
+      float y[kPer];
+      if (kOp == kGrad) {
+        E::widen(x, y);
+        gradient(y);
+        Vec o = E::narrow(y);
+        if (kMarked) o = E::keep(o, take, 0u);
+        if (kMarked && kKeep) o = E::choose(o, x, sp);
+        store_vec<kType, false>(w, y, o.w, first, from, stage, lane);
+        store_vec<kType, false>(w, y, o.w + 4, first + 32 * kEach, from, stage, lane);
+      } else {
+        Vec q = x;
+        if (kMarked) x = E::keep(x, take);
+        if (writes(kOp)) {
+          E::widen(x, y);
 #pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            float d = fmaf(y[j], scale, -w_lse);
-            if (kEnt) d = fmaxf(d, -200.f);
-            const float x = ex2(d * kLog2e);
-            y[j] = kEnt ? x * fmaf(-es, d + w_ent, -gs) : -gs * x;
+          for (int j = 0; j < kPer; ++j) y[j] *= scale;
+          if (!wide) {
+            Vec o = E::narrow(y);
+            if (kMarked && kKeep) o = E::choose(o, q, sp);
+            q = o;
           }
-          Vec o = E::narrow(y);
-          if (take != kAll) o = E::keep(o, take, 0u);
-          if (sp) o = E::choose(o, z, sp);  // (special ones keep theirs: `out` may be the logits, and they are read once more)
-          if (sizeof(T) == 4) E::widen(o, y);
-          store_vec<kType>(false, w, y, o, v - lane * kPer, in, min(V, s1 * kPer - w.shift), stage, lane);
-        } else {
-          Vec x = z;
-          if (take != kAll) x = E::keep(x, take);
-          if (kEnt && kOp == kScore) x = E::floor(x);
-          const float top = E::top(x) * sl2;
-          float y[kPer];
-          if (kOp == kAdjust) {
-            E::widen(x, y);
-            float o[kPer];
-            Vec q = x;
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) o[j] = y[j] * scale;
-            if (scale != 1.f && !wide) q = E::narrow(o);
-            if (sp && !wide) q = E::choose(q, z, sp);
-            if (sizeof(T) == 4) E::widen(q, o);
-            store_vec<kType>(wide, w, o, q, v - lane * kPer, in, min(V, s1 * kPer - w.shift), stage, lane);
-          } else {
-            E::widen(x, y);
-          }
-          raise<kEnt>(p, top);
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) {
-            const float d = fmaf(y[j], sl2, -p.m), e = ex2(d);
-            p.s[j & 1] += e;
-            // (0 times -inf is 0 here)
-            if (kEnt) p.u[j & 1] = fmaf(e, kOp == kScore && E::kFloors ? d : fmaxf(d, -200.f), p.u[j & 1]);
-          }
+          store_vec<kType, wide>(w, y, q.w, first, from, stage, lane);
+          store_vec<kType, wide>(w, y + kEach, q.w + 4, first + 32 * kEach, from, stage, lane);
         }
-      };
+        if (kEnt) x = E::floor(x);
+        sums(x);
+      }
+    };
+    auto pass = [&](auto keeps) {
 #pragma unroll 1
-      for (int b = s0; b < s1; b += kBatch) {
-        const int next = b + kBatch < s1 ? b + kBatch : s1;  // (of the span, or the next span's first)
-        uint32_t rest = 0u;                                  // vectors at the ends
+      for (; taken < fetched; ++taken) {
+        const int c = c0 + taken * kWarps + warp, at = c * kChunkVecs - s0;  // (accesses of the span)
+        if (at >= s1 - s0) break;
+        if (!arrived()) break;
+        const unsigned char* from = sm.ring[warp][taken % kDeep] + lane * 16;
+        const int stop = s1 - s0;
+        const bool plain = !marked && at + kChunkVecs <= stop && !(tvec >= at && tvec < at + kChunkVecs);
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-          if (full(b, i, min(s1, whole1))) dense(raw[i], b + i * kThreads + tid, false);
-          else rest |= 1u << i;
-          load_global_if(raw[i], base + next + i * kThreads, full(next, i, whole1));
+        for (int u = 0; u < kChunkVecs; u += 64) {
+          Vec x;
+          const uint4 lo4 = load_shared(from + 16 * u), hi4 = load_shared(from + 16 * (u + 32));
+          x.w[0] = lo4.x, x.w[1] = lo4.y, x.w[2] = lo4.z, x.w[3] = lo4.w;
+          x.w[4] = hi4.x, x.w[5] = hi4.y, x.w[6] = hi4.z, x.w[7] = hi4.w;
+          if (plain) dense(x, at + u + lane, stop, Bool<false>(), Bool<false>());
+          else dense(x, at + u + lane, stop, Bool<true>(), keeps);
         }
+        __syncwarp();  // (all lanes have read the chunk)
+        fetch();
+      }
+    };
+    const bool keep = kOp != kScore && !wide && w.out == w.z;
+    if (kOp == kScore || wide) pass(Bool<false>());
+    else if (keep) pass(Bool<true>());
+    else pass(Bool<false>());
+    // the entries that need more than the dense pass: special ones, the target, the row's ends
+    const T* zs = z0 + span.lo;
+    auto raw_at = [&](int rel) { return GPO_BOUNDS(st, span.lo + rel, V, kWhereLogits) ? E::get1(zs[rel]) : 0.f; };
+    __syncthreads();
+    for (int first = 0; first < total; first += kCap) {
+      if (first > 0) {
+        __syncthreads();
+        list_special(a, w, span, first, total, id, sm);
+        __syncthreads();
+      }
+      const int m = min(kCap, total - first);
 #pragma unroll 1
-        for (; rest; rest &= rest - 1) {
-          const int idx = b + (__ffs(rest) - 1) * kThreads + tid;
-          if (idx - lane < s1) dense(load_vec<kType>(w.z, idx * kPer - w.shift, V), idx, true);
-        }
+      for (int k0 = tid; k0 < m; k0 += 4 * kThreads) {
+        float z[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[k] = k0 + k * kThreads < m ? raw_at((int)sm.list[k0 + k * kThreads]) : 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k * kThreads < m) {
+            const int rel = (int)sm.list[k0 + k * kThreads];
+            const float x = single(rel, sm.count[k0 + k * kThreads], z[k]);
+            if (kOp != kScore) put(rel, x);
+          }
       }
-      if (total) {
-        for (int first = 0; first < total; first += kCap) {
-          __syncthreads();
-          list_special(a, w, lo, n, first, total, sm);
-          __syncthreads();
-          for (int k = tid; k < min(kCap, total - first); k += kThreads) single((int)sm.list[k], sm.count[k]);
-        }
+    }
+    // (ends: up to kEach - 1 before the first whole access and behind the last; then a target among no special entries)
+    const int behind = (s1 - s0) * kEach + 8;
+    int rel = -1;
+    if (tid < 8) rel = tid < 8 - span.r0 ? span.r0 + tid : -1;
+    else if (tid < 16) rel = behind + tid - 8 < span.r1 ? behind + tid - 8 : -1;
+    else if (tid == 16 && trel >= 8 && trel < behind) rel = trel;
+    if (rel >= 0 && !(total && (sm.special[rel >> 5] >> (rel & 31) & 1u))) {
+      // (rank_span has taken the special ones out of the allowed)
+      if (!marked || (sm.allow[rel >> 5] >> (rel & 31) & 1u)) {
+        const float x = single(rel, 0u, raw_at(rel));
+        if (kOp != kScore) put(rel, x);
+      } else {
+        if (kOp != kScore) put(rel, kOp == kGrad ? 0.f : -INFINITY);
+        if (kOp != kGrad && rel == trel) sh.at = -INFINITY;
       }
-      if (trel >= 0 && !(total && (sm.special[trel >> 5] >> (trel & 31) & 1u))) {
-        __syncthreads();
-        if (tid == 0) single(trel, 0u);
-      }
-      if (s1 < v1 && marked) {
-        __syncthreads();
-        if (total)
-          for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
-        __syncthreads();
-      }
+    }
+    if (last) break;
+    if (marked) {
+      __syncthreads();
+      if (total)
+        for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
+      __syncthreads();
+    }
   }
+  if (!ok) drain();
   if (kOp == kGrad) return;
-  Part x = {p.m, p.s[0] + p.s[1], p.u[0] + p.u[1]};
+  Part x = {p.m, lo_f2(p.s) + hi_f2(p.s), lo_f2(p.u) + hi_f2(p.u)};
   auto join_lanes = [&](int from) {
     for (int o = from; o > 0; o >>= 1) {
       const Part y = {__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
@@ -810,8 +938,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       st_remote(remote(&sh.cluster[rank].s, 0), x.s);
       st_remote(remote(&sh.cluster[rank].u, 0), x.u);
       // (who has the target's logit passes it on)
-      const int64_t tv = w.target < 0 ? -1 : (w.target + w.shift) / kPer;
-      if (tv >= v0 && tv < v1) st_remote(remote(&sh.cluster_at, 0), sh.at);
+      if (holds) st_remote(remote(&sh.cluster_at, 0), sh.at);
     }
     __syncwarp();
   }
@@ -834,6 +961,8 @@ template <int kType>
 cudaError_t setup_type() {
   cudaError_t e = setup_one<kType, kAdjust, false>();
   if (e == cudaSuccess) e = setup_one<kType, kAdjust, true>();
+  if (kType != GPO_DT_F32 && e == cudaSuccess) e = setup_one<kType, kType == GPO_DT_F32 ? kAdjust : kAdjust32, false>();
+  if (kType != GPO_DT_F32 && e == cudaSuccess) e = setup_one<kType, kType == GPO_DT_F32 ? kAdjust : kAdjust32, true>();
   if (e == cudaSuccess) e = setup_one<kType, kScore, false>();
   if (e == cudaSuccess) e = setup_one<kType, kScore, true>();
   if (e == cudaSuccess) e = setup_one<kType, kGrad, false>();
@@ -843,8 +972,8 @@ cudaError_t setup_type() {
 
 template <int kType, int kOp, bool kEnt>
 cudaError_t launch_one(const LaunchCtx& lc, const LogitsArgs& a, const Status& st) {
-  // a row of few gets a cluster, each of whose CTAs has a batch of its vectors or more
-  const int64_t ctas = kCtas * (int64_t)lc.num_sms, batches = (a.V / Raw<kType>::kPer + kThreads * kVecs - 1) / (kThreads * kVecs);
+  // a row of few gets a cluster, each of whose CTAs has a chunk for every warp or more
+  const int64_t ctas = kCtas * (int64_t)lc.num_sms, batches = a.V * (a.out32 ? 2 : 1) / (kWarps * kChunkVecs * Raw<kType>::kPer / 2);
   int cluster = 1;
   while (cluster < 8 && 2 * cluster * a.R <= ctas && 2 * cluster <= batches) cluster *= 2;
   cudaLaunchAttribute at;
@@ -863,6 +992,10 @@ cudaError_t launch_one(const LaunchCtx& lc, const LogitsArgs& a, const Status& s
 template <int kType>
 cudaError_t launch_type(const LaunchCtx& lc, const LogitsArgs& a, const Status& st) {
   if (a.g) return a.ge ? launch_one<kType, kGrad, true>(lc, a, st) : launch_one<kType, kGrad, false>(lc, a, st);
+  if (a.out && a.out32 && kType != GPO_DT_F32) {
+    constexpr int kOp = kType == GPO_DT_F32 ? kAdjust : kAdjust32;
+    return a.ent ? launch_one<kType, kOp, true>(lc, a, st) : launch_one<kType, kOp, false>(lc, a, st);
+  }
   if (a.out) return a.ent ? launch_one<kType, kAdjust, true>(lc, a, st) : launch_one<kType, kAdjust, false>(lc, a, st);
   return a.ent ? launch_one<kType, kScore, true>(lc, a, st) : launch_one<kType, kScore, false>(lc, a, st);
 }

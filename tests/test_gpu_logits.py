@@ -38,7 +38,8 @@ CASES = [
     (700, 5003, "f16", dict(masks=3, masked=0.4, biases=20)), (320, 9001, "f32", dict(masked=0.5, masks=2)),
     (6, 3001, "bf16", dict(penalties=False, biases=40)), (6, 3001, "bf16", dict(penalties=False, history=0, masks=2)),
     (6, 3001, "bf16", dict(history=0, penalties=False)), (2, 131072, "f32", dict(history=20000, biases=9000, masks=2)),
-    (1, 270001, "bf16", dict(history=9000, pad=1)), (5, 2000, "f16", dict(biases=2000, history=5000)),
+    (1, 270001, "bf16", dict(history=9000, pad=1)), (3, 263001, "f32", dict(history=300, pad=3, masks=2)), (2, 300007, "f16", dict(penalties=False, history=0)),
+    (4, 5, "f16", dict(pad=9, history=9)), (3, 17, "f32", dict(pad=5, biases=4, masks=2)), (64, 16390, "bf16", dict(pad=2)), (5, 2000, "f16", dict(biases=2000, history=5000)),
 ]
 
 
