@@ -20,17 +20,18 @@ namespace gpo {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kCtas = 2;                         // on one SM
-constexpr int kChunk = 2048;                     // bytes of a row that a warp fetches at a time,
-constexpr int kChunkVecs = kChunk / 16;          // accesses of 16 bytes,
-constexpr int kDeep = 3;                         // and how many of them are in flight
+constexpr int kCtas = 4;                         // on one SM
+constexpr int kChunk = 1024;                     // bytes of a row that a warp fetches at a time,
+constexpr int kChunkVecs = kChunk / 32;          // of 32 for a lane,
+constexpr int kDeep = 2;                         // and how many of them are in flight
+constexpr int kLead = 16;                        // bits of the bitmaps before a span's first whole 32 bytes
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1;  // an entry's word: flags, occurrences
 // the adjusted logits (in fp32, of 16-bit ones), only their statistics, the gradient
 enum Op { kAdjust, kAdjust32, kScore, kGrad };
 __host__ __device__ constexpr bool writes(int op) { return op == kAdjust || op == kAdjust32; }
 
-// 32 bytes of logits: two accesses of 16 bytes, 512 bytes apart.
+// 32 bytes of logits, a lane's.
 struct Vec {
   uint32_t w[8];
 };
@@ -199,7 +200,7 @@ struct Row {
   const void* z;
   void* out;
   int live;                   // has a target, or a gradient, or needs none
-  int vec;                    // the output's accesses of 16 bytes are aligned where the row's are
+  int vec;                    // the output's vectors are on boundaries of 32 bytes where the row's are
   int special;                // some entry may be special
   float scale, sl2;           // and times log2(e)
   float rep, inv, pres, freq; // repetition and 1 / it
@@ -219,13 +220,12 @@ struct Shared {
   int before[kWarps];         // special entries of each warp's words
 };
 
-constexpr int kSpan = 131072;         // entries of which it is known at one time which are special
+constexpr int kSpan = 69632;        // entries of which it is known at one time which are special
 constexpr int kWords = kSpan / 32;
 constexpr int kGroups = kWords / 4;   // groups of four words, whose special entries are counted together
-constexpr int kOwn = kGroups / kWarps;  // groups of a warp, side by side
-static_assert((kWarps & (kWarps - 1)) == 0 && kOwn % 32 == 0, "whole accesses of a warp, a join in halves");
+static_assert((kWarps & (kWarps - 1)) == 0 && kGroups % 32 == 0, "a join in halves, whole accesses of a warp");
 constexpr int kCap = 1536;            // special entries that are looked at in one round
-constexpr int kIds = 16;              // ids of the history that a thread holds
+constexpr int kIds = 4;               // ids of the history of a thread in flight
 struct Smem {
   Shared sh;
   alignas(16) uint32_t special[kWords];
@@ -259,12 +259,12 @@ __device__ __forceinline__ float adjusted(const LogitsArgs& a, const Row& w, uin
   return y;
 }
 
-// A row: `head` entries before the first 16-byte boundary, `vecs` whole accesses, then less than one.
+// A row: `head` entries before the first boundary of 32 bytes, `vecs` whole vectors, then less than one.
 template <class T>
 struct Edges {
   int head, vecs;
   __device__ __forceinline__ Edges(const T* z, int64_t V) {
-    constexpr int kPer = 16 / sizeof(T);
+    constexpr int kPer = 32 / sizeof(T);
     head = (int)min(V, (int64_t)((0 - (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T))) & (kPer - 1)));
     vecs = (int)(V - head) / kPer;
   }
@@ -317,7 +317,7 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   w.z = z;
   const size_t osz = kOp == kAdjust32 ? 4 : sizeof(T);
   w.out = kOp == kScore ? nullptr : static_cast<char*>(a.out) + r * a.out_stride * osz;
-  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) + Edges<T>(z, a.V).head * osz) & 15) == 0;
+  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) + Edges<T>(z, a.V).head * osz) & 31) == 0;
   w.scale = f32(0, a.scale, a.scale1);
   w.rep = f32(1, a.rep, a.rep1);
   w.pres = f32(2, a.pres, a.pres1);
@@ -360,31 +360,36 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   if (lane == 0) out = w;
 }
 
-// kIds ids of each thread from place `from` of the row's history on (-1 behind its end).
-__device__ __forceinline__ void load_ids(const LogitsArgs& a, const Row& w, int from, int (&id)[kIds]) {
-  const int len = (int)(w.h1 - w.h0) - from - (int)threadIdx.x;
-  // (one branch around the loads, which are then in flight together)
-  if (a.hist8) {
-    const int64_t* ids = static_cast<const int64_t*>(a.hist) + w.h0 + from + threadIdx.x;
+// Calls f(id - lo, place in the history) for the ids of the row's history from place `from` on that are in [lo + r0, lo + r1); returns
+// whether this thread met one past the vocabulary.
+template <class F>
+__device__ __forceinline__ bool each_id(const LogitsArgs& a, const Row& w, int from, int lo, int r0, int r1, F f) {
+  const int len = (int)(w.h1 - w.h0), V = (int)a.V;
+  bool bad = false;
+#pragma unroll 1
+  for (int i = from + threadIdx.x; i < len; i += kIds * kThreads) {
+    int id[kIds];
+    // (one branch around the loads, which are then in flight together)
+    if (a.hist8) {
+      const int64_t* ids = static_cast<const int64_t*>(a.hist) + w.h0 + i;
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) {
+        const int64_t x = i + k * kThreads < len ? ids[k * kThreads] : -1;
+        id[k] = x < 0 ? -1 : (int)min(x, a.V);
+      }
+    } else {
+      const int32_t* ids = static_cast<const int32_t*>(a.hist) + w.h0 + i;
+#pragma unroll
+      for (int k = 0; k < kIds; ++k) id[k] = i + k * kThreads < len ? max(ids[k * kThreads], -1) : -1;
+    }
 #pragma unroll
     for (int k = 0; k < kIds; ++k) {
-      const int64_t x = k * kThreads < len ? ids[k * kThreads] : -1;
-      id[k] = x < 0 ? -1 : (int)min(x, a.V);
+      const int rel = id[k] - lo;  // (-1 is no entry of the row: it is below r0)
+      bad |= id[k] >= V;
+      if ((uint32_t)(rel - r0) < (uint32_t)(r1 - r0)) f((uint32_t)rel, i + k * kThreads);
     }
-  } else {
-    const int32_t* ids = static_cast<const int32_t*>(a.hist) + w.h0 + from + threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < kIds; ++k) id[k] = k * kThreads < len ? ids[k * kThreads] : -1;
   }
-}
-// Calls f(id - lo, k) for those of [lo + r0, lo + r1).
-template <class F>
-__device__ __forceinline__ void each_id(const int (&id)[kIds], int lo, int r0, int r1, F f) {
-#pragma unroll
-  for (int k = 0; k < kIds; ++k) {
-    const int rel = id[k] - lo;  // (lo is -8 or more, and -1 is no entry of the row: it is below r0)
-    if ((uint32_t)(rel - r0) < (uint32_t)(r1 - r0)) f((uint32_t)rel, k);
-  }
+  return bad;
 }
 
 // A span of a row: bit j of the bitmaps is entry lo + j; [r0, r1) of them are the span's, r1 <= kSpan.
@@ -393,26 +398,17 @@ struct Span {
 };
 
 // Marks the special entries of a span in their bitmap, which was zeros, and writes that of the allowed ones where the row has a
-// mask.  id: the last ids of the history.
-__device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st, const Row& w, const Span& s, int trel, int (&id)[kIds], Smem& sm) {
+// mask.
+__device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st, const Row& w, const Span& s, Smem& sm) {
   const int V = (int)a.V;
   auto mark = [&](uint32_t rel) { atomicOr(sm.special + (rel >> 5), 1u << (rel & 31u)); };
   if (w.special) {
-    const int len = (int)(w.h1 - w.h0);
-    bool bad = false;
-    for (int from = 0; from < len; from += kIds * kThreads) {
-      load_ids(a, w, from, id);
-#pragma unroll
-      for (int k = 0; k < kIds; ++k) bad |= id[k] >= V;
-      each_id(id, s.lo, s.r0, s.r1, [&](uint32_t rel, int) { mark(rel); });
-    }
-    if (bad) report(st, GPO_ERR_SHAPE, 46, (int)w.h0);
+    if (each_id(a, w, 0, s.lo, s.r0, s.r1, [&](uint32_t rel, int) { mark(rel); })) report(st, GPO_ERR_SHAPE, 46, (int)w.h0);
     for (int64_t i = w.b0 + threadIdx.x; i < w.b1; i += kThreads) {
       const int64_t x = load_id(a.bias_ids, a.bias8, i), rel = x - s.lo;
       if (x < 0 || x >= V || (i > w.b0 && load_id(a.bias_ids, a.bias8, i - 1) >= x)) report(st, GPO_ERR_SHAPE, 47, (int)i);
       else if (rel >= s.r0 && rel < s.r1) mark((uint32_t)rel);
     }
-    if (trel >= 0 && threadIdx.x == 0) mark((uint32_t)trel);
   }
   if (w.mask) {
     const int words = (V + 31) >> 5, sh = s.lo & 31, at0 = s.lo >> 5;
@@ -424,27 +420,40 @@ __device__ __forceinline__ void mark_span(const LogitsArgs& a, const Status& st,
   }
 }
 
-// The number of special entries of the span that are allowed, which alone stay special, and of those before each group of words;
-// they leave the allowed ones.
-__device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
+// The special entries of group g, the first of which comes to place k.
+__device__ __forceinline__ void list_group(const uint4& x, int g, int k, Smem& sm) {
+  auto put = [&](uint32_t bits, int rel) {
+    for (; bits; bits &= bits - 1, ++k)
+      if (k >= 0 && k < kCap) sm.list[k] = rel + __ffs(bits) - 1;
+  };
+  put(x.x, 128 * g);
+  put(x.y, 128 * g + 32);
+  put(x.z, 128 * g + 64);
+  put(x.w, 128 * g + 96);
+}
+
+// The special entries of the span that are allowed, which alone stay special and leave the allowed ones; returns their number, with
+// the first kCap of them in the list.  Behind a barrier of the caller's; another comes before the list is read.
+__device__ __forceinline__ int rank_span(int n, bool masked, uint32_t flags, Smem& sm) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, groups = (n + 127) / 128;
+  const int own = (groups + 32 * kWarps - 1) / (32 * kWarps) * 32, end = min(groups, (warp + 1) * own);  // of a warp, side by side
+  uint4* special = reinterpret_cast<uint4*>(sm.special);
   int sum = 0;
 #pragma unroll 1
-  for (int g0 = warp * kOwn; g0 < min(groups, (warp + 1) * kOwn); g0 += 32) {
+  for (int g0 = warp * own; g0 < end; g0 += 32) {
     const int g = g0 + lane;
-    uint4& sp = reinterpret_cast<uint4*>(sm.special)[g];
     uint4& al = reinterpret_cast<uint4*>(sm.allow)[g];
-    uint4 x = sp;
-    if (masked) sp = x = make_uint4(x.x & al.x, x.y & al.y, x.z & al.z, x.w & al.w);
+    uint4 x = special[g];
+    if (masked) special[g] = x = make_uint4(x.x & al.x, x.y & al.y, x.z & al.z, x.w & al.w);
     al = masked ? make_uint4(al.x & ~x.x, al.y & ~x.y, al.z & ~x.z, al.w & ~x.w) : make_uint4(~x.x, ~x.y, ~x.z, ~x.w);
-    const int own = __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
-    int upto = own;
+    const int mine = __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w);
+    int upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
     }
-    sm.before[g] = sum + upto - own;
+    sm.before[g] = sum + upto - mine;
     sum += __shfl_sync(0xffffffffu, upto, 31);
   }
   if (lane == 0) sm.sh.before[warp] = sum;
@@ -456,27 +465,24 @@ __device__ __forceinline__ int rank_span(int n, bool masked, Smem& sm) {
     if (k < warp) before += y;
     all += y;
   }
-  for (int g = warp * kOwn + lane; g < min(groups, (warp + 1) * kOwn); g += 32) sm.before[g] += before;
+#pragma unroll 1
+  for (int g = warp * own + lane; g < end; g += 32) {
+    const int k = sm.before[g] += before;
+    list_group(special[g], g, k, sm);
+  }
+  for (int c = threadIdx.x; c < min(kCap, all); c += kThreads) sm.count[c] = flags;
   return all;
 }
 
-// The round's special entries, those of ranks [first, first + kCap), and their flags and counts.  Between barriers of the caller.
-// id: the last ids of the history.
-__device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, const Span& s, int first, int total, int (&id)[kIds], Smem& sm) {
-  for (int g = threadIdx.x; g < (s.r1 + 127) / 128; g += kThreads) {
-    const uint4 x = reinterpret_cast<const uint4*>(sm.special)[g];
-    int k = (int)sm.before[g] - first;
-    auto put = [&](uint32_t bits, int rel) {
-      for (; bits; bits &= bits - 1, ++k)
-        if (k >= 0 && k < kCap) sm.list[k] = rel + __ffs(bits) - 1;
-    };
-    put(x.x, 128 * g);
-    put(x.y, 128 * g + 32);
-    put(x.z, 128 * g + 64);
-    put(x.w, 128 * g + 96);
-  }
-  for (int c = threadIdx.x; c < min(kCap, total - first); c += kThreads) sm.count[c] = 0;
-  __syncthreads();
+// The list of a later round, of ranks [first, first + kCap).  Between barriers of the caller's.
+__device__ __forceinline__ void list_span(int n, int first, int total, uint32_t flags, Smem& sm) {
+  for (int g = threadIdx.x; g < (n + 127) / 128; g += kThreads)
+    list_group(reinterpret_cast<const uint4*>(sm.special)[g], g, (int)sm.before[g] - first, sm);
+  for (int c = threadIdx.x; c < min(kCap, total - first); c += kThreads) sm.count[c] = flags;
+}
+
+// The flags and counts of the entries in the list, whose first is of rank `first`.  Between barriers of the caller's.
+__device__ __forceinline__ void count_span(const LogitsArgs& a, const Row& w, const Span& s, int first, Smem& sm) {
   // the place of a special entry in the list, of others far above its end
   auto at = [&](uint32_t rel) {
     const uint32_t word = rel >> 5 & 3u, bit = 1u << (rel & 31u);
@@ -486,18 +492,15 @@ __device__ __forceinline__ void list_special(const LogitsArgs& a, const Row& w, 
                   (word > 2 ? __popc(x.z) : 0);
     return own & bit ? (uint32_t)k : 0xFFFFFFFFu;
   };
-  const int len = (int)(w.h1 - w.h0), generated = (int)(w.hg - w.h0) - (int)threadIdx.x;
-  constexpr int kPart = kIds * kThreads;
-  // (from the part that the thread holds back to the first)
-  for (int from = len > 0 ? (len - 1) / kPart * kPart : -1; from >= 0; from -= kPart) {
-    if (from + kPart < len || first > 0) load_ids(a, w, from, id);
-    each_id(id, s.lo, s.r0, s.r1, [&](uint32_t rel, int k) {
+  // (without biases every one of them is of the history: flags says so already, and only what was generated is looked at)
+  const int generated = (int)(w.hg - w.h0);
+  if (w.b1 > w.b0 || w.pres != 0.f || w.freq != 0.f)
+    each_id(a, w, w.b1 > w.b0 ? 0 : generated, s.lo, s.r0, s.r1, [&](uint32_t rel, int i) {
       const uint32_t to = at(rel);
       if (to >= (uint32_t)kCap) return;
-      if (from + k * kThreads >= generated) atomicAdd(sm.count + to, 1u);
+      if (i >= generated) atomicAdd(sm.count + to, 1u);
       else atomicOr(sm.count + to, kSeen);
     });
-  }
   for (int64_t i = w.b0 + threadIdx.x; i < w.b1; i += kThreads) {
     const int64_t rel = load_id(a.bias_ids, a.bias8, i) - s.lo;
     if (rel < s.r0 || rel >= s.r1) continue;
@@ -511,8 +514,10 @@ __device__ __forceinline__ uint4 load_shared(const void* p) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem_u32(p)) : "memory");
   return r;
 }
-__device__ __forceinline__ void store_global(void* p, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.global.L1::no_allocate.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+__device__ __forceinline__ void store_global(void* p, const Vec& x) {
+  asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
+               "r"(x.w[3]), "r"(x.w[4]), "r"(x.w[5]), "r"(x.w[6]), "r"(x.w[7])
+               : "memory");
 }
 // Bytes (a multiple of 16, as are the addresses) to this CTA's shared memory, counted on a barrier.
 __device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
@@ -543,24 +548,31 @@ __device__ __noinline__ void store_ragged(void* out, bool four, uint4 x, int v0,
   __syncwarp();
 }
 
-// One access of every lane to the row, by a whole warp: lane 0's first entry is v0, none from `end` on, which lies between two lanes'.
+// A vector of every lane to the row, by a whole warp: lane 0's first entry is v0, none from `end` on, which lies between two lanes'.
 // y: the same in fp32, for rows of those.
 template <int kType, bool kWide>
-__device__ __forceinline__ void store_vec(const Row& w, const float* y, const uint32_t* x, int v0, int end, uint32_t* stage, int lane) {
+__device__ __forceinline__ void store_vec(const Row& w, const float (&y)[Raw<kType>::kPer], const Vec& x, int v0, int end, uint32_t* stage, int lane) {
   using T = typename Raw<kType>::T;
-  constexpr int kEach = 16 / sizeof(T);
-  const int v = v0 + lane * kEach;
+  constexpr int kPer = Raw<kType>::kPer;
+  const int v = v0 + lane * kPer;
   if (kWide) {
 #pragma unroll
-    for (int i = 0; i < kEach; i += 4) {
-      const uint4 o = make_uint4(__float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]), __float_as_uint(y[i + 3]));
-      if (!w.vec) store_ragged(w.out, true, o, v0 + i, kEach, end, stage);
-      else if (v < end) store_global(static_cast<float*>(w.out) + v + i, o.x, o.y, o.z, o.w);
+    for (int i = 0; i < kPer; i += 8) {
+      Vec o;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o.w[k] = __float_as_uint(y[i + k]);
+      if (!w.vec) {
+        store_ragged(w.out, true, make_uint4(o.w[0], o.w[1], o.w[2], o.w[3]), v0 + i, kPer, end, stage);
+        store_ragged(w.out, true, make_uint4(o.w[4], o.w[5], o.w[6], o.w[7]), v0 + i + 4, kPer, end, stage);
+      } else if (v < end) {
+        store_global(static_cast<float*>(w.out) + v + i, o);
+      }
     }
   } else if (!w.vec) {
-    store_ragged(w.out, sizeof(T) == 4, make_uint4(x[0], x[1], x[2], x[3]), v0, kEach, end, stage);
+    store_ragged(w.out, sizeof(T) == 4, make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]), v0, kPer, end, stage);
+    store_ragged(w.out, sizeof(T) == 4, make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]), v0 + kPer / 2, kPer, end, stage);
   } else if (v < end) {
-    store_global(static_cast<T*>(w.out) + v, x[0], x[1], x[2], x[3]);
+    store_global(static_cast<T*>(w.out) + v, x);
   }
 }
 
@@ -628,8 +640,7 @@ template <int kType, int kOp, bool kEnt>
 __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, int cluster, Status st) {
   using E = Raw<kType>;
   using T = typename E::T;
-  constexpr int kPer = E::kPer, kEach = kPer / 2;            // entries of a Vec, of one access
-  constexpr int kSpanVecs = (kSpan - 16) / kEach / kChunkVecs * kChunkVecs;
+  constexpr int kPer = E::kPer, kSpanVecs = (kSpan - 3 * kLead) / kPer / kChunkVecs * kChunkVecs;
   constexpr uint32_t kAll = (1u << kPer) - 1u;
   constexpr bool wide = kOp == kAdjust32;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -645,14 +656,15 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   const int chunks = (row.vecs + kChunkVecs - 1) / kChunkVecs, share = (chunks + cluster - 1) / cluster;
   const int c0 = min(chunks, rank * share), c1 = min(chunks, c0 + share);
   uint64_t* full = sm.full[warp];
+  const char* body = reinterpret_cast<const char*>(z0 + row.head);
   int fetched = 0, taken = 0;  // chunks of this warp
   auto fetch = [&]() {
     const int c = c0 + fetched * kWarps + warp;
     if (c >= c1) return;
     if (lane == 0) {
-      const uint32_t bytes = 16u * (uint32_t)min(kChunkVecs, row.vecs - c * kChunkVecs);
+      const uint32_t bytes = 32u * (uint32_t)min(kChunkVecs, row.vecs - c * kChunkVecs);
       mbar_arrive_expect_tx(full + fetched % kDeep, bytes);
-      bulk_load(sm.ring[warp][fetched % kDeep], z0 + row.head + (int64_t)c * kChunkVecs * kEach, bytes, full + fetched % kDeep);
+      bulk_load(sm.ring[warp][fetched % kDeep], body + (int64_t)c * kChunk, bytes, full + fetched % kDeep);
     }
     ++fetched;
   };
@@ -675,7 +687,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   const Row& w = sh.row;
   bool ok = true;  // (of the whole warp)
   auto arrived = [&]() {
-    ok = ok && __all_sync(0xffffffffu, mbar_wait(full + taken % kDeep, (uint32_t)(taken / kDeep) & 1u, st, 48));
+    const uint32_t phase = (uint32_t)(taken / kDeep) & 1u;
+    if (!mbar_try_wait(full + taken % kDeep, phase)) ok = ok && mbar_wait(full + taken % kDeep, phase, st, 48);
+    ok = __all_sync(0xffffffffu, ok);
     return ok;
   };
   // every copy that was asked for lands before the shared memory goes
@@ -686,13 +700,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
     drain();
     if (kOp == kGrad) {  // zeros
       const float none[kPer] = {};
-      const uint32_t zero[4] = {0u, 0u, 0u, 0u};
-      const int body = row.head + min(row.vecs, c0 * kChunkVecs) * kEach, whole = row.head + min(row.vecs, c1 * kChunkVecs) * kEach;
-      const int first = rank == 0 ? 0 : body, end = rank == cluster - 1 ? V : whole;
+      const Vec zero = E::narrow(none);
+      const int from = row.head + min(row.vecs, c0 * kChunkVecs) * kPer, whole = row.head + min(row.vecs, c1 * kChunkVecs) * kPer;
+      const int first = rank == 0 ? 0 : from, end = rank == cluster - 1 ? V : whole;
       T* out = static_cast<T*>(w.out);
-      for (int v = first + tid; v < body; v += kThreads) out[v] = E::put(0.f);
+      for (int v = first + tid; v < from; v += kThreads) out[v] = E::put(0.f);
 #pragma unroll 1
-      for (int v = body + warp * 32 * kEach; v < whole; v += kThreads * kEach) store_vec<kType, false>(w, none, zero, v, whole, stage, lane);
+      for (int v = from + warp * 32 * kPer; v < whole; v += kThreads * kPer) store_vec<kType, false>(w, none, zero, v, whole, stage, lane);
       for (int v = whole + tid; v < end; v += kThreads) out[v] = E::put(0.f);
     } else if (rank == 0 && tid == 0) {
       if (a.logp) a.logp[r] = 0.f;
@@ -708,27 +722,27 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   if (!early)
     for (int k = 0; k < kDeep; ++k) fetch();
   bool holds = false;  // the target
+  const uint32_t flags = w.b1 > w.b0 ? 0u : kSeen;  // of every special entry
   Running p = {kLow, 0ull, 0ull};
 #pragma unroll 1
   for (int s0 = min(row.vecs, c0 * kChunkVecs);; s0 += kSpanVecs) {
     const int end = min(row.vecs, c1 * kChunkVecs), s1 = min(end, s0 + kSpanVecs);
     const bool head = rank == 0 && s0 == 0, last = s1 == end, tail = last && rank == cluster - 1;
-    // bit 8 of the bitmaps is the span's first whole access, what is before or behind those its ends
+    // bit kLead of the bitmaps is the span's first whole vector's, what is before or behind those its ends
     Span span;
-    span.lo = row.head + s0 * kEach - 8;
-    span.r0 = head ? 8 - row.head : 8;
-    span.r1 = tail ? V - span.lo : (s1 - s0) * kEach + 8;
+    span.lo = row.head + s0 * kPer - kLead;
+    span.r0 = head ? kLead - row.head : kLead;
+    span.r1 = tail ? V - span.lo : (s1 - s0) * kPer + kLead;
     const int trel = w.target >= (int64_t)span.lo + span.r0 && w.target < (int64_t)span.lo + span.r1 ? (int)w.target - span.lo : -1;
     holds |= trel >= 0;
-    int id[kIds];
     int total = 0;
     if (marked) {
-      mark_span(a, st, w, span, trel, id, sm);
+      mark_span(a, st, w, span, sm);
       __syncthreads();
       if (w.special) {
-        total = rank_span(span.r1, w.mask != nullptr, sm);
+        total = rank_span(span.r1, w.mask != nullptr, flags, sm);
         __syncthreads();
-        list_special(a, w, span, 0, total, id, sm);  // (complete after the dense pass's barrier)
+        if (total) count_span(a, w, span, 0, sm);  // (complete after the dense pass's barrier)
       }
     }
     // d y_j = -gs p_j - es p_j (log p_j + H), without the target's gs
@@ -791,29 +805,27 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       if (wide) static_cast<float*>(w.out)[span.lo + rel] = x;
       else static_cast<T*>(w.out)[span.lo + rel] = E::put(x);
     };
-    // An access of the span: its bits.
+    // the bits of the span's k-th vector
     auto bits_at = [&](const uint32_t* p, int k) -> uint32_t {
-      const uint8_t* b = reinterpret_cast<const uint8_t*>(p) + 1;
-      return kEach == 8 ? b[k] : b[k >> 1] >> 4 * (k & 1) & 15u;
+      return kPer == 16 ? reinterpret_cast<const uint16_t*>(p)[k + kLead / 16] : reinterpret_cast<const uint8_t*>(p)[k + kLead / 8];
     };
-    const int tvec = trel < 8 ? -1 : (trel - 8) / kEach;  // the target's access
-    // Two accesses of each lane, k and k + 32 of the span, entries from v on, of the accesses before `end`.  kMarked: some may be masked or special, or none of
-    // the span; kKeep: special ones are written as they were, to be read once more.
-    auto dense = [&](Vec& x, int k, int stop, auto is_marked, auto keeps) {
+    const int stop = s1 - s0, tvec = trel < kLead ? -1 : (trel - kLead) / kPer;  // the span's vectors, the target's
+    // Each lane's vector, the span's k-th.  kMarked: some entries may be masked or special, or none of the span; kKeep: special
+    // ones are written as they were, to be read once more.
+    auto dense = [&](Vec& x, int k, auto is_marked, auto keeps) {
       constexpr bool kMarked = decltype(is_marked)::value, kKeep = decltype(keeps)::value;
       uint32_t take = kAll, sp = 0u;
       if (kMarked) {
-        if (marked) take = bits_at(sm.allow, k) | bits_at(sm.allow, min(k + 32, kSpanVecs)) << kEach;
-        if (kKeep && total) sp = bits_at(sm.special, k) | bits_at(sm.special, min(k + 32, kSpanVecs)) << kEach;
-        uint32_t out = 0u;
-        if (!total && k == tvec) out = 1u << (trel - 8) % kEach;
-        if (!total && k + 32 == tvec) out = 1u << (kEach + (trel - 8) % kEach);
-        take &= ~out;
-        if (kKeep) sp |= out;
+        if (marked) take = bits_at(sm.allow, k);
+        if (kKeep && total) sp = bits_at(sm.special, k);
+        if (k == tvec) {  // (a special one, too)
+          const uint32_t bit = 1u << (trel - kLead) % kPer;
+          take &= ~bit;
+          sp |= bit;
+        }
         if (k >= stop) take = 0u;
-        else if (k + 32 >= stop) take &= (1u << kEach) - 1u;
       }
-      const int first = span.lo + 8 + (k - lane) * kEach, from = span.lo + 8 + stop * kEach;
+      const int first = span.lo + kLead + (k - lane) * kPer, from = span.lo + kLead + stop * kPer;
       float y[kPer];
       if (kOp == kGrad) {
         E::widen(x, y);
@@ -821,23 +833,19 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
         Vec o = E::narrow(y);
         if (kMarked) o = E::keep(o, take, 0u);
         if (kMarked && kKeep) o = E::choose(o, x, sp);
-        store_vec<kType, false>(w, y, o.w, first, from, stage, lane);
-        store_vec<kType, false>(w, y, o.w + 4, first + 32 * kEach, from, stage, lane);
+        store_vec<kType, false>(w, y, o, first, from, stage, lane);
       } else {
-        Vec q = x;
-        if (kMarked) x = E::keep(x, take);
         if (writes(kOp)) {
-          E::widen(x, y);
+          Vec q = x;
+          if (kMarked) q = E::keep(q, take);
+          E::widen(q, y);
 #pragma unroll
           for (int j = 0; j < kPer; ++j) y[j] *= scale;
-          if (!wide) {
-            Vec o = E::narrow(y);
-            if (kMarked && kKeep) o = E::choose(o, q, sp);
-            q = o;
-          }
-          store_vec<kType, wide>(w, y, q.w, first, from, stage, lane);
-          store_vec<kType, wide>(w, y + kEach, q.w + 4, first + 32 * kEach, from, stage, lane);
+          if (!wide) q = E::narrow(y);
+          if (!wide && kMarked && kKeep) q = E::choose(q, x, sp);
+          store_vec<kType, wide>(w, y, q, first, from, stage, lane);
         }
+        if (kMarked) x = E::keep(x, take);
         if (kEnt) x = E::floor(x);
         sums(x);
       }
@@ -845,20 +853,18 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
     auto pass = [&](auto keeps) {
 #pragma unroll 1
       for (; taken < fetched; ++taken) {
-        const int c = c0 + taken * kWarps + warp, at = c * kChunkVecs - s0;  // (accesses of the span)
-        if (at >= s1 - s0) break;
-        if (!arrived()) break;
-        const unsigned char* from = sm.ring[warp][taken % kDeep] + lane * 16;
-        const int stop = s1 - s0;
-        const bool plain = !marked && at + kChunkVecs <= stop && !(tvec >= at && tvec < at + kChunkVecs);
+        const int at = (c0 + taken * kWarps + warp) * kChunkVecs - s0;  // (the span's at-th vector)
+        if (at >= stop || !arrived()) break;
+        const unsigned char* from = sm.ring[warp][taken % kDeep] + lane * 32;
+        const bool plain = !marked && at + kChunkVecs <= stop && (uint32_t)(tvec - at) >= (uint32_t)kChunkVecs;
 #pragma unroll
-        for (int u = 0; u < kChunkVecs; u += 64) {
+        for (int u = 0; u < kChunkVecs; u += 32) {
           Vec x;
-          const uint4 lo4 = load_shared(from + 16 * u), hi4 = load_shared(from + 16 * (u + 32));
-          x.w[0] = lo4.x, x.w[1] = lo4.y, x.w[2] = lo4.z, x.w[3] = lo4.w;
-          x.w[4] = hi4.x, x.w[5] = hi4.y, x.w[6] = hi4.z, x.w[7] = hi4.w;
-          if (plain) dense(x, at + u + lane, stop, Bool<false>(), Bool<false>());
-          else dense(x, at + u + lane, stop, Bool<true>(), keeps);
+          const uint4 a4 = load_shared(from + 32 * u), b4 = load_shared(from + 32 * u + 16);
+          x.w[0] = a4.x, x.w[1] = a4.y, x.w[2] = a4.z, x.w[3] = a4.w;
+          x.w[4] = b4.x, x.w[5] = b4.y, x.w[6] = b4.z, x.w[7] = b4.w;
+          if (plain) dense(x, at + u + lane, Bool<false>(), Bool<false>());
+          else dense(x, at + u + lane, Bool<true>(), keeps);
         }
         __syncwarp();  // (all lanes have read the chunk)
         fetch();
@@ -871,11 +877,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
     // the entries that need more than the dense pass: special ones, the target, the row's ends
     const T* zs = z0 + span.lo;
     auto raw_at = [&](int rel) { return GPO_BOUNDS(st, span.lo + rel, V, kWhereLogits) ? E::get1(zs[rel]) : 0.f; };
-    __syncthreads();
+    if (total || w.target >= 0 || marked) __syncthreads();
     for (int first = 0; first < total; first += kCap) {
       if (first > 0) {
         __syncthreads();
-        list_special(a, w, span, first, total, id, sm);
+        list_span(span.r1, first, total, flags, sm);
+        __syncthreads();
+        count_span(a, w, span, first, sm);
         __syncthreads();
       }
       const int m = min(kCap, total - first);
@@ -893,12 +901,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
           }
       }
     }
-    // (ends: up to kEach - 1 before the first whole access and behind the last; then a target among no special entries)
-    const int behind = (s1 - s0) * kEach + 8;
+    // (ends: less than a vector before the first whole one and behind the last; then a target among no special entries)
+    const int behind = stop * kPer + kLead;
     int rel = -1;
-    if (tid < 8) rel = tid < 8 - span.r0 ? span.r0 + tid : -1;
-    else if (tid < 16) rel = behind + tid - 8 < span.r1 ? behind + tid - 8 : -1;
-    else if (tid == 16 && trel >= 8 && trel < behind) rel = trel;
+    if (tid < 16) rel = tid < kLead - span.r0 ? span.r0 + tid : -1;
+    else if (tid < 32) rel = behind + tid - 16 < span.r1 ? behind + tid - 16 : -1;
+    else if (tid == 32 && trel >= kLead && trel < behind) rel = trel;
     if (rel >= 0 && !(total && (sm.special[rel >> 5] >> (rel & 31) & 1u))) {
       // (rank_span has taken the special ones out of the allowed)
       if (!marked || (sm.allow[rel >> 5] >> (rel & 31) & 1u)) {
@@ -973,7 +981,7 @@ cudaError_t setup_type() {
 template <int kType, int kOp, bool kEnt>
 cudaError_t launch_one(const LaunchCtx& lc, const LogitsArgs& a, const Status& st) {
   // a row of few gets a cluster, each of whose CTAs has a chunk for every warp or more
-  const int64_t ctas = kCtas * (int64_t)lc.num_sms, batches = a.V * (a.out32 ? 2 : 1) / (kWarps * kChunkVecs * Raw<kType>::kPer / 2);
+  const int64_t ctas = kCtas * (int64_t)lc.num_sms, batches = a.V / (kWarps * kChunkVecs * Raw<kType>::kPer);
   int cluster = 1;
   while (cluster < 8 && 2 * cluster * a.R <= ctas && 2 * cluster <= batches) cluster *= 2;
   cudaLaunchAttribute at;
