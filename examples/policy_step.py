@@ -1,6 +1,6 @@
 """One GraphPO training step of a small policy model, end to end on the GPU.
 
-    python examples/policy_step.py [--steps N]
+    python examples/policy_step.py [--steps N] [--teacher WEIGHT]
 
 A batch of sampled rollouts (synthetic) gives per-edge advantages (GraphPO.__call__); the model is
 a token embedding, one residual layer and a vocabulary head tied to the embedding.  A step embeds the
@@ -8,7 +8,8 @@ tokens, runs the layer, takes the sampled next tokens' log-probabilities and ent
 head without ever holding its logits (vocab_logp), the policy loss and its gradient (token_loss),
 the entropy bonus, the gradients of hidden states and matrix (vocab_grad), the layer's own, and the
 embedding's, added to the tied matrix's (embed_grad).  The first step's old log-probabilities are the
-model's own.
+model's own.  With a teacher's weight the policy also learns from another policy's top tokens at the same places
+(vocab_distill, whose gradients are added to the others: vocab_distill_grad).
 """
 import argparse
 import os
@@ -44,8 +45,9 @@ class Policy:
         return x.t() @ da
 
 
-def train(steps=3, vocab=5000, d=256, groups=4, lr=0.5, entropy_weight=1e-3, temperature=1.0, seed=0):
-    """Runs `steps` optimiser steps on one batch; returns the losses (token_loss's, without the bonus)."""
+def train(steps=3, vocab=5000, d=256, groups=4, lr=0.5, entropy_weight=1e-3, temperature=1.0, seed=0, teacher_weight=0.0, top=16):
+    """Runs `steps` optimiser steps on one batch; returns the losses (token_loss's, without the bonus; with a teacher plus its weight
+    times the mean divergence from its `top` tokens)."""
     b = W.make_batch(W.CONFIGS["tiny"].scaled(groups=groups))
     gp = P.GraphPO(kappa=b["kappa"], w=b["w"], lambda_eff=b["lambda_eff"])
     batch = P.Batch.from_arrays(b)
@@ -59,6 +61,9 @@ def train(steps=3, vocab=5000, d=256, groups=4, lr=0.5, entropy_weight=1e-3, tem
     policy = Policy(vocab, d, seed)
     plan = gp.loss_plan(batch)
     old, losses = None, []
+    if teacher_weight > 0.0:  # its log-probabilities of its top tokens, once for all steps
+        teacher = Policy(vocab, d, seed + 1)
+        taught, ids_top = torch.log_softmax(teacher.forward(gp, ids)[2].float() @ teacher.table.float().t(), 1).topk(top, dim=1)
     for _ in range(steps):
         x, t, hidden = policy.forward(gp, ids)
         head = gp.vocab_logp(hidden, policy.table, target, scale=1.0 / temperature, entropy=True)
@@ -67,17 +72,27 @@ def train(steps=3, vocab=5000, d=256, groups=4, lr=0.5, entropy_weight=1e-3, tem
         bonus = torch.full((T,), -entropy_weight / T, device="cuda")                        # of -weight * mean entropy
         grads = gp.vocab_grad(hidden, policy.table, target, head["lse"], loss["grad_logp"], scale=1.0 / temperature,
                               entropy=head["entropy"], grad_entropy=bonus, logp=head["logp"])
+        total = loss["loss"]
+        if teacher_weight > 0.0:
+            far = gp.vocab_distill(hidden, policy.table, ids_top, taught, scale=1.0 / temperature, tail=True)
+            share = torch.full((T,), teacher_weight / T, device="cuda")                     # of weight * mean divergence
+            more = gp.vocab_distill_grad(hidden, policy.table, ids_top, far["delta"], far["rest"], far["rest_lse"], share,
+                                         scale=1.0 / temperature, accumulate=True,          # (the matrix's are added up there)
+                                         out={"d_hidden": torch.empty_like(hidden), "d_weight": grads["d_weight"]})
+            grads["d_hidden"] += more["d_hidden"]
+            total = total + teacher_weight * far["loss"].mean()
         d_layer = policy.backward(gp, ids, x, t, grads["d_hidden"], grads["d_weight"])
         policy.table -= lr * grads["d_weight"]
         policy.layer -= lr * d_layer
         gp.check()
-        losses.append(float(loss["loss"]))
+        losses.append(float(total))
     return losses
 
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser()
     ap.add_argument("--steps", type=int, default=5)
+    ap.add_argument("--teacher", type=float, default=0.0, metavar="WEIGHT")
     a = ap.parse_args()
-    for i, v in enumerate(train(steps=a.steps)):
+    for i, v in enumerate(train(steps=a.steps, teacher_weight=a.teacher)):
         print(f"step {i}: loss {v:+.6f}")

@@ -1,13 +1,27 @@
 // Logits as a sampler takes them, their log-probabilities, and the gradient of the raw ones (formulas in
 // include/graphpo.h): penalties for the tokens of a row's history, biases, a mask, a scale.
 //
-// One launch, no workspace.  A row is the work of a cluster of 1 to 8 CTAs (as many as few rows leave SMs for), which take
-// slices of it in turn: kThreads x kVecs accesses of 16 bytes, fetched one slice ahead into registers.  What makes an
-// entry special, a token of the history or a bias, is found per slice: every CTA reads the row's whole history (a few
-// thousand tokens, from L1 after the first slice) and counts those of the slice in shared memory, a word per entry and one bit in
-// a bitmap; the mask's bits of the slice are another bitmap.  So the pass over the logits looks at two bytes per 8 of them, and at
-// the counts of special ones only, of which 4096 consecutive logits have a few.  Sums of exponentials run with the
-// pass, relative to a maximum of each thread's own; threads, warps and CTAs of a row are joined in a fixed order.
+// One launch, no workspace.  A CTA takes a row (of few rows a cluster of 2 to 8 a row), four of them on an SM.
+//   fetch    Each warp fetches its own 1 KB pieces of the row by bulk copies, two at a time, in a ring of its own: no warp waits
+//            for another, and the first of them are under way before the row's arguments are known.
+//   special  What the history or a bias changes: a bitmap of the span (up to 69632 entries at a time), ranks by counting its
+//            bits, a list of them in their order with flags and occurrences.  Three barriers; the history is read once, of what was
+//            generated twice (the second time from L1).
+//   dense    One pass over all others, 32 bytes a lane: two bytes of a bitmap say which of 16 count (allowed, not special).
+//            Sums of exponentials run with the pass, relative to a maximum of each thread's own.  The entries are rounded
+//            and stored as whole vectors; of rows of other alignment through shared memory.
+//   ends     Special entries, the target, and what lies before the row's first and behind its last boundary of 32 bytes: a
+//            thread each, their logits from L2, where the pass has just been.
+// Threads, warps and CTAs of a row are joined in a fixed order, and no float is added atomically: the same bits on every run.
+//
+// What bounds it: without penalties and masks HBM and the issue of instructions together (us, calls in a row in a graph):
+// gradient of 4096 x 65536 bf16 (2870 live) 141, 5.8 TB/s of the bytes needed; log-probabilities and entropies of the same 92,
+// of which the exponentials alone take 41 of the special-function units' time and 10 instructions an entry at 2.8 of 4 a
+// cycle the rest; 256 x 131072 adjusted 27, 5.0 TB/s.  With histories of 1300 tokens, penalties and masks 190, 149; with 4000 tokens 49: the
+// bitmaps' bits spread over 16-bit lanes (2.7 instructions an entry), then the special entries (3 to 4).
+// Tried (gradient, log-probabilities, step): loads to registers in place of the rings 233, 151, 69; 3 CTAs and 2 KB pieces 190, 147,
+// 66; 2 CTAs of 512 threads 207, 175, 69; the special entries' sums before the pass, whose scattered reads come from HBM
+// then, 290, 170, 97; every warp reading the row's arguments itself 190, 153, 49.
 #define GPO_REPORT __noinline__
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -195,7 +209,7 @@ struct Raw<GPO_DT_F16> : Raw16 {
   static __device__ __forceinline__ T put(float x) { return __float2half_rn(x); }
 };
 
-// A row, read by one warp.
+// A row's arguments, read by one warp.
 struct Row {
   const void* z;
   void* out;
@@ -636,6 +650,10 @@ __device__ __forceinline__ void raise(Running& p, float top) {
   p.m = top;
 }
 
+// All CTAs of the cluster have started once the wait, behind everyone's arrival, is over: only then is there shared memory of theirs.
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 template <int kType, int kOp, bool kEnt>
 __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, int cluster, Status st) {
   using E = Raw<kType>;
@@ -649,6 +667,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, V = (int)a.V;
   uint32_t* stage = sm.stage[warp];
   const int rank = cluster > 1 ? (int)cluster_rank() : 0;
+  const bool joins = kOp != kGrad && cluster > 1;
+  if (joins) cluster_started();
   const int64_t r = blockIdx.x / cluster;
   const T* z0 = static_cast<const T*>(a.z) + r * a.z_stride;
   const Edges<T> row(z0, V);
@@ -698,6 +718,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   };
   if (!w.live) {
     drain();
+    if (joins) cluster_wait();
     if (kOp == kGrad) {  // zeros
       const float none[kPer] = {};
       const Vec zero = E::narrow(none);
@@ -938,6 +959,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   join_lanes(16);
   if (lane == 0) sh.part[warp] = x;
   __syncthreads();
+  if (joins) cluster_wait();
   if (warp == 0) {
     x = lane < kWarps ? sh.part[lane] : Part{kLow, 0.f, 0.f};
     join_lanes(kWarps / 2);

@@ -83,6 +83,11 @@ gpo_status logits_args(gpo_ctx* c, const gpo_logits* l, LogitsArgs& a) {
 bool overlap(const void* p, int64_t ps, size_t pe, const void* q, int64_t qs, size_t qe, int64_t R, int64_t V) {
   if (R == 0 || (p == q && ps == qs && pe == qe)) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  const uintptr_t step = (uintptr_t)ps * pe, off = (b > a ? b - a : a - b) % (step ? step : 1);
+  if (R > 1 && step == (uintptr_t)qs * qe) {  // (columns of one buffer, side by side)
+    const uintptr_t lower = (uintptr_t)V * (b > a ? pe : qe), upper = (uintptr_t)V * (b > a ? qe : pe);
+    if (off >= lower && step - off >= upper) return false;
+  }
   const uintptr_t a1 = a + pe * (size_t)((R - 1) * ps + V), b1 = b + qe * (size_t)((R - 1) * qs + V);
   return a < b1 && b < a1;
 }

@@ -294,6 +294,11 @@ def test_what_the_kernel_refuses(P, gp):
     with pytest.raises(P.GraphPOError):  # rows that overlap the raw ones
         buf = torch.zeros(4 * V, device="cuda")
         gp.logits_adjust(buf[:2 * V].view(2, V), out={"logits": buf[V:3 * V].view(2, V)})
+    buf = torch.randn(3, 2 * V, device="cuda")  # (side by side they do not)
+    assert torch.equal(gp.logits_adjust(buf[:, :V], out={"logits": buf[:, V:]}, scale=2.0)["logits"], 2 * buf[:, :V])
+    for a, b in ((0, V - 1), (V - 1, 0), (1, V), (V, 1)):
+        with pytest.raises(P.GraphPOError):
+            gp.logits_adjust(buf[:, a:a + V], out={"logits": buf[:, b:b + V]})
     with pytest.raises(P.GraphPOError):  # no output
         gp.logits_adjust(z, lse=False)
     gp.check()
