@@ -1003,7 +1003,7 @@ constexpr int64_t kVocabPieceBytes = (int64_t)512 << 20;  // dz of one piece of 
 constexpr int kVocabFew = 16;
 constexpr int kVocabFewCtas = 256;   // CTAs of that launch at most
 // parts of a forward row: the maxima and sums of the two column halves of every tile
-inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
+__host__ __device__ inline int64_t vocab_parts(int64_t V) { return 2 * ((V + kPairN - 1) / kPairN); }
 
 struct VocabHead {  // in the workspace, written by the kernel that lists the tokens
   int rows;         // tokens that take part
@@ -1051,11 +1051,13 @@ struct VocabArgs {
   int w_blocks;          // the matrix's rows are whole blocks of 64 columns (maps.wb)
   int dw_bulk;           // d_weight's rows take bulk stores (maps.dw)
   int debug_timeout;
-  // distillation: each token's teacher entries by id, top_n of them in rows of top_stride, and their logits in units of log 2
+  // distillation: each token's teacher entries by id in rows of top_stride, their logits in units of log 2, and the entries
+  // before every 128 columns of the vocabulary, in rows of first_stride
   const int* top_id;
-  const int* top_n;
   float* top_z;
   int64_t top_stride;
+  const uint16_t* top_first;
+  int64_t first_stride;
 };
 
 // Tensor maps of one call.  K innermost, boxes of 64 x 128: hidden rows as given (few tokens: 64 x
@@ -1125,8 +1127,9 @@ struct TeachArgs {
   int tail;                      // they are log-probabilities, and the other tokens one more outcome
   // the entries by id, in rows of `stride`: ids, places in the given order, probabilities and their logarithms; their
   // number, and the probability of the others
-  int64_t stride;
+  int64_t stride, first_stride;
   int *id, *n;
+  uint16_t* first;               // entries before every 128 columns
   int16_t* place;
   float *q, *lq, *qr;
   int* target;                   // forward 0, gradient the entry of the largest |delta|; -1: has no teacher

@@ -2,7 +2,8 @@
 // include/graphpo.h).
 //
 // Forward:  teach_sort_kernel   a warp per token puts the teacher's entries in the order of their ids (by counting the smaller
-//                               ones: k^2 / 32 comparisons a lane) with their probabilities
+//                               ones: k^2 / 32 comparisons a lane) with their probabilities, and counts those before every 128
+//                               columns of the vocabulary
 //           vocab_pair_kernel   <kLseTop>: logits tiles that stay in tensor memory; a row's entries are taken out of its
 //                               maximum and sum, which are then those of the other tokens
 //           teach_join_kernel   the parts of a row joined, divergence and p - q from them and the entries' logits
@@ -25,7 +26,7 @@ namespace {
 
 constexpr int kSortWarps = 4;
 constexpr int kNoId = 0x7fffffff;
-constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float load_value(const void* p, int dtype, int64_t i) {
   if (dtype == GPO_DT_F32) return static_cast<const float*>(p)[i];
@@ -45,7 +46,7 @@ __device__ __forceinline__ float warp_sum(float x) { return over_warp(x, [](floa
 __device__ __forceinline__ int warp_first(int x) { return (int)__reduce_min_sync(0xffffffffu, (unsigned)x); }
 
 __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t, Status st) {
-  __shared__ int s_id[kSortWarps][kTeachMax];
+  __shared__ int s_id[kSortWarps][kTeachMax], s_sorted[kSortWarps][kTeachMax];
   __shared__ float s_v[kSortWarps][kTeachMax];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   let_next_start();
@@ -109,10 +110,25 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
     if (twice) report(st, GPO_ERR_SHAPE, 52, (int)tok);
     const int64_t at = tok * t.stride + rank;
     const float lq = v[j] - m - shift;
-    t.id[at] = ids[j];
+    t.id[at] = s_sorted[warp][rank] = ids[j];
     t.place[at] = (int16_t)j;
     t.lq[at] = lq;
     t.q[at] = expf(lq);
+  }
+  __syncwarp();
+  const int parts = (int)vocab_parts(t.V);
+  for (int p = lane; p <= parts; p += 32) {  // the entries below 128 p
+    int first = 0;
+    for (int m = n; m > 0;) {
+      const int h = m >> 1;
+      if (s_sorted[warp][first + h] < 128 * p) {
+        first += h + 1;
+        m -= h + 1;
+      } else {
+        m = h;
+      }
+    }
+    t.first[tok * t.first_stride + p] = (uint16_t)first;
   }
   if (lane == 0) {
     t.n[tok] = n;

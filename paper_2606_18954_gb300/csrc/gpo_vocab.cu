@@ -576,23 +576,17 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
           if (kMode != kDzWideEnt && a.lp && tgt >= 0 && tgt < kPairN / 2) w.at = dz_at_target<has_ent(kMode)>(w, a.lp[tok]);
         }
       }
-      // the first of the teacher's entries from n0 on (looked up while the sums are still being made)
-      const int* top = nullptr;
-      int left = 0, id0 = kNoKey;  // entries from there on, the first one's id
+      // the teacher's entries among the columns: how many, from where on, the first two's ids (looked up while the sums are still
+      // being made; a search through the entries took a microsecond, as long as the MMAs of 256 columns of d)
+      int64_t top = 0;
+      int hits = 0, id0 = kNoKey, id1 = kNoKey;
       if (kMode == kLseTop && live) {
-        top = a.top_id + tok * a.top_stride;
-        left = __ldg(a.top_n + tok);
-        for (int n = left; n > 0;) {
-          const int h = n >> 1;
-          if (__ldg(top + h) < n0) {
-            top += h + 1;
-            left -= h + 1;
-            n -= h + 1;
-          } else {
-            n = h;
-          }
-        }
-        if (left > 0) id0 = __ldg(top);
+        const uint16_t* first = a.top_first + tok * a.first_stride + n0 / (kPairN / 2);
+        const int from = __ldg(first);
+        hits = __ldg(first + 1) - from;
+        top = tok * a.top_stride + from;
+        if (hits > 0) id0 = __ldg(a.top_id + top);
+        if (hits > 1) id1 = __ldg(a.top_id + top + 1);
       }
       if constexpr (kMode == kDz || kMode == kDzEnt) {
         uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
@@ -652,21 +646,23 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
               if (j >= cols) z[j] = kNone;
           }
           if constexpr (kMode == kLseTop) {  // the teacher's entries leave the sums, 32 columns at a time
+            if (__any_sync(0xffffffffu, hits > 0)) {
 #pragma unroll
-            for (int ch = 0; ch < kPairN / 2; ch += 32) {
-              while (__any_sync(0xffffffffu, id0 < n0 + ch + 32)) {
-                const int at = id0 - n0 - ch;  // (none: far above 31)
-                float tz = 0.f;
+              for (int ch = 0; ch < kPairN / 2; ch += 32) {
+                while (__any_sync(0xffffffffu, id0 < n0 + ch + 32)) {
+                  const int at = id0 - n0 - ch;  // (none: far above 31)
+                  float tz = 0.f;
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                  if (j == at) {
-                    tz = z[ch + j];
-                    z[ch + j] = kNone;
+                  for (int j = 0; j < 32; ++j)
+                    if (j == at) {
+                      tz = z[ch + j];
+                      z[ch + j] = kNone;
+                    }
+                  if (at < 32) {
+                    a.top_z[top++] = tz * a.sl2;
+                    id0 = id1;
+                    id1 = --hits > 1 ? __ldg(a.top_id + top + 1) : kNoKey;
                   }
-                if (at < 32) {
-                  a.top_z[top - a.top_id] = tz * a.sl2;
-                  ++top;
-                  id0 = --left > 0 ? __ldg(top) : kNoKey;
                 }
               }
             }

@@ -409,10 +409,10 @@ namespace {
 // The workspace of a distillation: that of the products, then the teacher's.
 struct TeachLayout {
   VocabLayout v;
-  size_t id, place, q, lq, z, n, qr, target;         // forward
+  size_t id, first, place, q, lq, z, n, qr, target;  // forward
   size_t none, dense, dense_lse;                     // gradient (and target)
   size_t total;
-  int64_t stride;
+  int64_t stride, first_stride;
 };
 
 void teach_layout(const gpo_vocab& v, int64_t k, bool grad, TeachLayout& L) {
@@ -426,10 +426,12 @@ void teach_layout(const gpo_vocab& v, int64_t k, bool grad, TeachLayout& L) {
   };
   const size_t T = (size_t)v.num_tokens;
   L.stride = up_to(k, 8);
+  L.first_stride = up_to(vocab_parts(v.vocab) + 1, 2);
   const size_t all = T * (size_t)L.stride;
   if (T > 0) L.target = take(4 * T);
   if (T > 0 && !grad) {
     L.id = take(4 * all);
+    L.first = take(2 * T * (size_t)L.first_stride);
     L.place = take(2 * all);
     L.q = take(4 * all);
     L.lq = take(4 * all);
@@ -486,6 +488,7 @@ void teach_args(const gpo_vocab& v, const gpo_teacher& t, const TeachLayout& L, 
   a.scale = (float)t.scale;
   a.tail = t.tail != 0;
   a.stride = L.stride;
+  a.first_stride = L.first_stride;
   a.target = at<int>(ws, L.target);
 }
 
@@ -529,6 +532,7 @@ gpo_status gpo_vocab_distill(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher
   TeachArgs ta;
   teach_args(*v, *t, L, workspace, ta);
   ta.id = at<int>(workspace, L.id);
+  ta.first = at<uint16_t>(workspace, L.first);
   ta.place = at<int16_t>(workspace, L.place);
   ta.q = at<float>(workspace, L.q);
   ta.lq = at<float>(workspace, L.lq);
@@ -551,7 +555,8 @@ gpo_status gpo_vocab_distill(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher
   a.logp = out->loss;  // (launch_vocab_rows: zeros of the tokens that take no part)
   a.sl2 = logit_scale(*v, 64 * kVocabSeg);
   a.top_id = ta.id;
-  a.top_n = ta.n;
+  a.top_first = ta.first;
+  a.first_stride = L.first_stride;
   a.top_z = at<float>(workspace, L.z);
   a.top_stride = L.stride;
   Stages stage(ctx, stream);
