@@ -58,8 +58,8 @@ constexpr int kVEpiWarps = 8, kLoadWarp = 0, kMmaWarp = 1, kRestWarp = 2, kIdleW
 // The split of each mode is one without spills: the loads' and the MMAs' lane would find theirs in an L1
 // that the epilogue's stores sweep, and fall behind the tensor cores.
 constexpr int kRegsLaunch = 168;
-__host__ __device__ constexpr int regs_few(int mode) { return is_wide(mode) ? 120 : 88; }
-__host__ __device__ constexpr int regs_many(int mode) { return is_wide(mode) ? 192 : 208; }
+__host__ __device__ constexpr int regs_few(int mode) { return is_wide(mode) || mode == kLseTop ? 120 : 88; }
+__host__ __device__ constexpr int regs_many(int mode) { return is_wide(mode) || mode == kLseTop ? 192 : 208; }
 static_assert(128 * regs_few(kDzWide) + 256 * regs_many(kDzWide) <= kVThreads * kRegsLaunch &&
               128 * regs_few(kLse) + 256 * regs_many(kLse) <= kVThreads * kRegsLaunch, "register split");
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
