@@ -523,21 +523,36 @@ __device__ __forceinline__ void count_span(const LogitsArgs& a, const Row& w, co
   }
 }
 
-__device__ __forceinline__ uint4 load_shared(const void* p) {
-  uint4 r;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(smem_u32(p)) : "memory");
+// A warp's ring by 32-bit addresses in shared memory (through generic pointers every chunk takes 30 instructions more).
+__device__ __forceinline__ Vec load_shared(uint32_t at) {
+  Vec r;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]) : "r"(at) : "memory");
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4 + 16];" : "=r"(r.w[4]), "=r"(r.w[5]), "=r"(r.w[6]), "=r"(r.w[7]) : "r"(at) : "memory");
   return r;
+}
+__device__ __forceinline__ bool has_arrived(uint32_t bar, uint32_t phase) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(phase)
+      : "memory");
+  return ok != 0;
 }
 __device__ __forceinline__ void store_global(void* p, const Vec& x) {
   asm volatile("st.global.L1::no_allocate.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x.w[0]), "r"(x.w[1]), "r"(x.w[2]),
                "r"(x.w[3]), "r"(x.w[4]), "r"(x.w[5]), "r"(x.w[6]), "r"(x.w[7])
                : "memory");
 }
-// Bytes (a multiple of 16, as are the addresses) to this CTA's shared memory, counted on a barrier.
-__device__ __forceinline__ void bulk_load(void* to, const void* from, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(to)), "l"(from),
-               "r"(bytes), "r"(smem_u32(bar))
-               : "memory");
+// Bytes (a multiple of 16, as are the addresses) to this CTA's shared memory, counted on a barrier that expects them.
+__device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %2;\n\t"
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+      "l"(from), "r"(bytes), "r"(bar)
+      : "memory");
 }
 
 // Four words of every lane to a row of any alignment, by a whole warp: entries of 4 or 2 bytes, lane 0's first v0, the next lane's
@@ -675,24 +690,24 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   // this CTA's share of the row's accesses, in chunks; the warps take them in turn
   const int chunks = (row.vecs + kChunkVecs - 1) / kChunkVecs, share = (chunks + cluster - 1) / cluster;
   const int c0 = min(chunks, rank * share), c1 = min(chunks, c0 + share);
-  uint64_t* full = sm.full[warp];
-  const char* body = reinterpret_cast<const char*>(z0 + row.head);
-  int fetched = 0, taken = 0;  // chunks of this warp
+  const uint32_t full = smem_u32(sm.full[warp]), ring = smem_u32(sm.ring[warp]);
+  // the chunks of this warp: the next to fetch, the vectors from it to the end of the share; how many are fetched, and done
+  const char* ahead = reinterpret_cast<const char*>(z0 + row.head) + (int64_t)(c0 + warp) * kChunk;
+  int left = min(row.vecs, c1 * kChunkVecs) - (c0 + warp) * kChunkVecs;
+  uint32_t fetched = 0, taken = 0;
   auto fetch = [&]() {
-    const int c = c0 + fetched * kWarps + warp;
-    if (c >= c1) return;
-    if (lane == 0) {
-      const uint32_t bytes = 32u * (uint32_t)min(kChunkVecs, row.vecs - c * kChunkVecs);
-      mbar_arrive_expect_tx(full + fetched % kDeep, bytes);
-      bulk_load(sm.ring[warp][fetched % kDeep], body + (int64_t)c * kChunk, bytes, full + fetched % kDeep);
-    }
+    if (left <= 0) return;
+    const uint32_t slot = fetched % kDeep;
+    if (lane == 0) bulk_load(ring + slot * kChunk, ahead, 32u * (uint32_t)min(kChunkVecs, left), full + slot * 8);
     ++fetched;
+    ahead += kWarps * kChunk;
+    left -= kWarps * kChunkVecs;
   };
   // The row's first bytes are on their way before anything else is known of it but that it is read
   // (bounded waits for them are below, for every chunk that is fetched).
   const int64_t wanted = a.target && !writes(kOp) ? load_id(a.target, a.target8, r) : 0;
   if (lane == 0) {
-    for (int k = 0; k < kDeep; ++k) mbar_init(full + k, 1);
+    for (int k = 0; k < kDeep; ++k) mbar_init(sm.full[warp] + k, 1);
     fence_mbar_init();
   }
   __syncwarp();
@@ -707,14 +722,14 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   const Row& w = sh.row;
   bool ok = true;  // (of the whole warp)
   auto arrived = [&]() {
-    const uint32_t phase = (uint32_t)(taken / kDeep) & 1u;
-    if (!mbar_try_wait(full + taken % kDeep, phase)) ok = ok && mbar_wait(full + taken % kDeep, phase, st, 48);
-    ok = __all_sync(0xffffffffu, ok);
+    const uint32_t slot = taken % kDeep, phase = taken / kDeep & 1u;
+    if (__all_sync(0xffffffffu, has_arrived(full + slot * 8, phase))) return true;
+    ok = __all_sync(0xffffffffu, mbar_wait(sm.full[warp] + slot, phase, st, 48));
     return ok;
   };
   // every copy that was asked for lands before the shared memory goes
   auto drain = [&]() {
-    for (; taken < fetched; ++taken) mbar_wait(full + taken % kDeep, (uint32_t)(taken / kDeep) & 1u, st, 48, 200000000ull, false);
+    for (; taken < fetched; ++taken) mbar_wait(sm.full[warp] + taken % kDeep, taken / kDeep & 1u, st, 48, 200000000ull, false);
   };
   if (!w.live) {
     drain();
@@ -872,19 +887,17 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       }
     };
     auto pass = [&](auto keeps) {
+      // the chunks of the span, of which those that end by `whole` have nothing special in them, but for the target's
+      const int whole = marked ? 0 : stop - kChunkVecs + 1, taught = tvec < 0 ? -1 : tvec / kChunkVecs * kChunkVecs;
+      int at = (c0 + (int)taken * kWarps + warp) * kChunkVecs - s0;  // (the span's at-th vector)
 #pragma unroll 1
-      for (; taken < fetched; ++taken) {
-        const int at = (c0 + taken * kWarps + warp) * kChunkVecs - s0;  // (the span's at-th vector)
-        if (at >= stop || !arrived()) break;
-        const unsigned char* from = sm.ring[warp][taken % kDeep] + lane * 32;
-        const bool plain = !marked && at + kChunkVecs <= stop && (uint32_t)(tvec - at) >= (uint32_t)kChunkVecs;
+      for (; at < stop && ok; at += kWarps * kChunkVecs, ++taken) {
+        if (!arrived()) break;
+        const uint32_t from = ring + taken % kDeep * kChunk + lane * 32;
 #pragma unroll
         for (int u = 0; u < kChunkVecs; u += 32) {
-          Vec x;
-          const uint4 a4 = load_shared(from + 32 * u), b4 = load_shared(from + 32 * u + 16);
-          x.w[0] = a4.x, x.w[1] = a4.y, x.w[2] = a4.z, x.w[3] = a4.w;
-          x.w[4] = b4.x, x.w[5] = b4.y, x.w[6] = b4.z, x.w[7] = b4.w;
-          if (plain) dense(x, at + u + lane, Bool<false>(), Bool<false>());
+          Vec x = load_shared(from + 32 * u);
+          if (at < whole && at != taught) dense(x, at + u + lane, Bool<false>(), Bool<false>());
           else dense(x, at + u + lane, Bool<true>(), keeps);
         }
         __syncwarp();  // (all lanes have read the chunk)
