@@ -370,8 +370,7 @@ def _matrix(t, what: str, dev: int, rows, cols, dtype) -> int:
 
 def _vector(t, what: str, dev: int, n: int, dtype=None) -> int:
     """Checks a contiguous vector of n elements on device `dev`; returns its address."""
-    shape = t.shape
-    if len(shape) != 1 or shape[0] != n or not t.is_contiguous():
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous vector of {n} elements")
     if t.get_device() != dev:
         raise ValueError(f"{what} is on {t.device}: the arrays must be on one CUDA device")
@@ -860,12 +859,18 @@ class GraphPO:
         f32 = torch.float32
         tc = _dtype_code(logits, "logits")
         ls = _matrix(logits, "logits", dev, T, K, logits.dtype)
-        if out is None:
-            out = {k: torch.empty(T, dtype=f32, device=hidden.device) for k in ("loss", "rest", "rest_lse") + (("lse",) if lse else ())}
-            out["delta"] = torch.empty(T, K, dtype=f32, device=hidden.device)
-        delta = out["delta"]
-        ds = _matrix(delta, "delta", dev, T, K, f32)
-        po = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("loss", "rest", "rest_lse", "lse")]
+        if out is None:  # (what is made here needs no check)
+            loss = torch.empty(T, dtype=f32, device=hidden.device)
+            out = {"loss": loss, "rest": torch.empty_like(loss), "rest_lse": torch.empty_like(loss)}
+            if lse:
+                out["lse"] = torch.empty_like(loss)
+            po = [t.data_ptr() for t in out.values()] + ([] if lse else [0])
+            out["delta"] = delta = torch.empty(T, K, dtype=f32, device=hidden.device)
+            ds = K
+        else:
+            delta = out["delta"]
+            ds = _matrix(delta, "delta", dev, T, K, f32)
+            po = [0 if out.get(k) is None else _vector(out[k], k, dev, T, f32) for k in ("loss", "rest", "rest_lse", "lse")]
         on = _stream_handle(dev)
         room, wp, wn = self._room((4, T, V, d, K), lambda: distill_workspace_size(
             CVocab(T, V, d, d, d, None, None, None, 0, 4, 1.0), CTeacher(K, K, K, None, None, 4, 0, 0, 1.0)), hidden.device, workspace, on)
@@ -892,17 +897,20 @@ class GraphPO:
         ds = _matrix(delta, "delta", dev, T, K, f32)
         ins = _PACK_DISTILL_IN(_vector(grad_loss, "grad_loss", dev, T, f32), delta.data_ptr(), _vector(rest, "rest", dev, T, f32),
                                _vector(rest_lse, "rest_lse", dev, T, f32), ds)
+        dh = dw = None
+        sh = sw = d
         if out is None:
             if accumulate and d_weight:
                 raise ValueError("accumulate needs the d_weight to add to in `out`")
             out = {}
             if d_hidden:
-                out["d_hidden"] = torch.empty(T, d, dtype=dt, device=hidden.device)
+                out["d_hidden"] = dh = torch.empty(T, d, dtype=dt, device=hidden.device)
             if d_weight:
-                out["d_weight"] = torch.empty(V, d, dtype=dt, device=hidden.device)
-        dh, dw = out.get("d_hidden"), out.get("d_weight")
-        sh = 0 if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
-        sw = 0 if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
+                out["d_weight"] = dw = torch.empty(V, d, dtype=dt, device=hidden.device)
+        else:
+            dh, dw = out.get("d_hidden"), out.get("d_weight")
+            sh = d if dh is None else _matrix(dh, "d_hidden", dev, T, d, dt)
+            sw = d if dw is None else _matrix(dw, "d_weight", dev, V, d, dt)
         if T == 0 and dw is None:
             return out
         on = _stream_handle(dev)
@@ -989,11 +997,10 @@ class GraphPO:
         if dev != self._device:
             self._elsewhere(dev)
         f32, i64, i32 = torch.float32, torch.int64, torch.int32
-        ptrs, values = [], []
-        for x, what in ((scale, "scale"), (repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
-            given = isinstance(x, torch.Tensor)
-            ptrs.append(_vector(x, what, dev, R, f32) if given else 0)
-            values.append(1.0 if given else x)
+        ptrs, values = [0, 0, 0, 0], [scale, repetition, presence, frequency]
+        for i, x in enumerate(values):
+            if x.__class__ is not float and isinstance(x, torch.Tensor):  # (the class alone is 0.3 us faster)
+                ptrs[i], values[i] = _vector(x, ("scale", "repetition", "presence", "frequency")[i], dev, R, f32), 1.0
         hb = bb = tb = hp = hn = sp = bp = ip = bn = bs = mp = mr = ms = mi = tp = 0
         if (history is None) != (spans is None) or (bias is None) != (bias_ids is None):
             raise ValueError("history needs spans, and bias needs bias_ids")
@@ -1020,7 +1027,7 @@ class GraphPO:
 
     @staticmethod
     def _spans(t, what: str, dev: int, rows: int, n: int, dtype) -> int:
-        if len(t.shape) != 2 or t.shape[0] != rows or t.shape[1] != n or not t.is_contiguous():
+        if t.shape != (rows, n) or not t.is_contiguous():
             raise ValueError(f"{what} must be contiguous, [{rows}, {n}]")
         if t.get_device() != dev or t.dtype is not dtype:
             raise TypeError(f"{what} must be {dtype}, on the device of the logits")
@@ -1049,20 +1056,28 @@ class GraphPO:
                                           bias_ids, bias_spans, write, lse, entropy, out)
         dev, R, V, packed = self._logits(logits, target, scale, mask, mask_row, history, spans, repetition, presence, frequency, bias,
                                          bias_ids, bias_spans)
-        f32 = torch.float32
-        if out is None:
-            out = {k: torch.empty(R, dtype=f32, device=logits.device)
-                   for k, want in (("lse", lse), ("entropy", entropy), ("logp", target is not None)) if want}
+        f32, x = torch.float32, None
+        if out is None:  # (what is made here needs no check)
+            where, out, ptrs = logits.device, {}, [0, 0, 0]
+            for i, (k, want) in enumerate((("logp", target is not None), ("lse", lse), ("entropy", entropy))):
+                if want:
+                    out[k] = t = torch.empty(R, dtype=f32, device=where)
+                    ptrs[i] = t.data_ptr()
             if write is not None:
-                out["logits"] = torch.empty(R, V, dtype=write, device=logits.device)
-        ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, R, f32) for k in ("logp", "lse", "entropy")]
-        x, stride, code = out.get("logits"), 0, 0
-        if x is not None:
+                out["logits"] = x = torch.empty(R, V, dtype=write, device=where)
+                stride = V
+        else:
+            ptrs = [0 if out.get(k) is None else _vector(out[k], k, dev, R, f32) for k in ("logp", "lse", "entropy")]
+            x = out.get("logits")
+            if x is not None:
+                stride = _matrix(x, "logits", dev, R, V, x.dtype)
+        if x is None:
+            outs = _PACK_LOGITS_OUT(0, 0, 0, *ptrs)
+        else:
             if x.dtype is not f32 and x.dtype is not logits.dtype:
                 raise TypeError(f"adjusted logits are float32 or {logits.dtype}, not {x.dtype}")
-            stride, code = _matrix(x, "logits", dev, R, V, x.dtype), _dtypes[x.dtype]
-        code = _fast["gpo_logits_adjust"](self._h, packed, _PACK_LOGITS_OUT(0 if x is None else x.data_ptr(), stride, code, *ptrs),
-                                          _stream_handle(dev))
+            outs = _PACK_LOGITS_OUT(x.data_ptr(), stride, _dtypes[x.dtype], *ptrs)
+        code = _fast["gpo_logits_adjust"](self._h, packed, outs, _stream_handle(dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
         return out
@@ -1090,9 +1105,11 @@ class GraphPO:
                       0 if grad_entropy is None else _vector(entropy, "entropy", dev, R, f32),
                       0 if grad_entropy is None else _vector(grad_entropy, "grad_entropy", dev, R, f32))
         if out is None:
-            out = {"d_logits": torch.empty(R, V, dtype=logits.dtype, device=logits.device)}
-        d = out["d_logits"]
-        stride = _matrix(d, "d_logits", dev, R, V, logits.dtype)
+            d, stride = torch.empty(R, V, dtype=logits.dtype, device=logits.device), V
+            out = {"d_logits": d}
+        else:
+            d = out["d_logits"]
+            stride = _matrix(d, "d_logits", dev, R, V, logits.dtype)
         code = _fast["gpo_logits_grad"](self._h, packed, ins, d.data_ptr(), stride, _stream_handle(dev))
         if code != GPO_OK:
             raise GraphPOError(code, self.last_error())
