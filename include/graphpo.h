@@ -517,8 +517,9 @@ gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad
  *   d_hidden_t = scale sum_v dz[t][v] weight_v    d_weight_v = scale sum_t dz[t][v] hidden_t
  *
  * The entries are kept out of the sum over the other tokens, so that rest, delta and the gradient have their
- * digits where p or q is nearly 1.  dz is rounded to the operands' type once, and the gradients after it: they have the
- * error of up to 1.5 roundings.  Products, sums and their order as for gpo_vocab_logp and gpo_vocab_grad.
+ * digits where p or q is nearly 1.  dz is rounded to the operands' type, but for the entry of the largest |delta|, which is kept as
+ * gpo_vocab_grad's target is, and the gradients after it: they have the error of about one rounding, up to 1.5 where many
+ * entries weigh the same.  Products, sums and their order as for gpo_vocab_logp and gpo_vocab_grad.
  *
  * An id below 0 is no entry (a teacher with fewer; its delta is 0); an entry whose logit is -inf is one of probability 0.  A token
  * without entries, or with tail = 0 without one above -inf, has no teacher: its outputs are 0, it has no gradient, and its

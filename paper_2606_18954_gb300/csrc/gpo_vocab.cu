@@ -10,6 +10,7 @@
 //            memory; the epilogue reduces each row's 128 columns to a maximum and a sum (and the entropy's
 //            sum), the target's logit kept apart.  Bound by the tensor cores, in long runs by the power that they may
 //            take: 2867 x 100003 x 2048 600 us, 1960 TFLOP/s; 8192 x 131072 x 2048 2.1 to 2.4 ms, 1830 to 2060
+//            (<kLseTop> of a distillation, with what is before and behind it: gpo_teach.cu)
 //   join     vocab_join_kernel, up to 256 tokens vocab_join_row_kernel: the parts of a row joined in a fixed order.
 //            Bound by HBM and latency: 26 MB in 14 us
 // Gradient, piece by piece of the vocabulary (dz of a piece takes at most 512 MiB):
