@@ -245,7 +245,7 @@ gpo_status gpo_compute_host(gpo_ctx* ctx, const gpo_batch* host, const gpo_batch
 
 /* Waits for `stream` and returns the first error the kernels of the last
  * gpo_compute (or of the gpo_compute_groups calls since the last clearing one) or loss call
- * on this context reported (GPO_OK if none).  Of the vocabulary ends' calls (gpo_vocab_*, gpo_embed*) it
+ * on this context reported (GPO_OK if none).  Of the calls on a vocabulary (gpo_vocab_*, gpo_embed*, gpo_logits_*) it
  * returns the first error of all since it last returned one, whatever has been enqueued
  * after the failing call, which disturbs no other; an error of theirs is returned once.  Replays of captured calls
  * are calls like others there. */
@@ -594,7 +594,7 @@ gpo_status gpo_vocab_distill_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_te
  * (GPO_ERR_INVALID_ARG); the call's outputs are then undefined. */
 typedef struct {
   int64_t num_rows;      /* R >= 0 */
-  int64_t vocab;         /* V >= 1 */
+  int64_t vocab;         /* V >= 1, at most 2^30 */
   int64_t logits_stride; /* elements between rows, >= vocab */
   const void* logits;    /* [R x logits_stride] raw logits, aligned to their elements */
   int32_t dtype;         /* gpo_dtype */

@@ -1004,6 +1004,8 @@ class GraphPO:
         hb = bb = tb = hp = hn = sp = bp = ip = bn = bs = mp = mr = ms = mi = tp = 0
         if (history is None) != (spans is None) or (bias is None) != (bias_ids is None):
             raise ValueError("history needs spans, and bias needs bias_ids")
+        if (bias_spans is not None and bias is None) or (mask_row is not None and mask is None):
+            raise ValueError("bias_spans needs bias, and mask_row needs mask")
         if spans is not None:
             hb, hn = _id_bytes(history, "history"), history.numel()
             hp = _vector(history, "history", dev, hn)

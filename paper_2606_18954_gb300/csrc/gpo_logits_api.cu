@@ -15,7 +15,9 @@ gpo_status logits_args(gpo_ctx* c, const gpo_logits* l, LogitsArgs& a) {
   if (!l) return set_msg(c, "logits arguments NULL"), GPO_ERR_INVALID_ARG;
   if (l->num_rows < 0 || l->vocab < 1 || l->history_len < 0 || l->bias_len < 0)
     return set_msg(c, "negative size, or vocab < 1"), GPO_ERR_INVALID_ARG;
-  if (l->num_rows > kMaxCount || l->vocab > kMaxCount) return set_msg(c, "more than 2^31 - 1024 rows or tokens"), GPO_ERR_UNSUPPORTED;
+  // (the kernel's places in a row are 32-bit, with room for a CTA's step past the end)
+  if (l->num_rows > kMaxCount || l->vocab > (int64_t)1 << 30)
+    return set_msg(c, "more than 2^31 - 1024 rows or 2^30 tokens"), GPO_ERR_UNSUPPORTED;
   if (l->logits_stride < l->vocab) return set_msg(c, "row stride < vocab"), GPO_ERR_INVALID_ARG;
   if (l->logits_stride >= kMaxMatrix || (double)l->num_rows * (double)l->logits_stride >= (double)kMaxMatrix ||
       l->history_len >= kMaxMatrix || l->bias_len >= kMaxMatrix)

@@ -283,6 +283,34 @@ def test_refusals(P, gp):
     gp.check()
 
 
+def test_replays_keep_their_errors_until_check(P, gp):
+    """Of captured calls the replays' errors are raised once each, and disturb no other replay; rows listed or not."""
+    import torch
+    from distill_ref import inputs
+    for T, V, d in ((33, 500, 64), (2100, 66000, 1000)):
+        h, w, ids, t = inputs(T, V, d, 6, torch.bfloat16, seed=2)
+        good, g = ids.clone(), torch.rand(T, device="cuda")
+
+        def step():
+            f = gp.vocab_distill(h, w, ids, t)
+            return f, gp.vocab_distill_grad(h, w, good, f["delta"], f["rest"], f["rest_lse"], g)["d_hidden"]
+        want = [x.clone() for x in (step()[0]["loss"], step()[1])]
+        graph = torch.cuda.CUDAGraph()
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            got = step()
+        for code, bad in ((SHAPE, V), (SHAPE, int(ids[3, 4]))):
+            ids[3, 2] = bad
+            graph.replay()
+            ids.copy_(good)
+            graph.replay()
+            with pytest.raises(P.GraphPOError) as e:
+                gp.check()
+            assert e.value.code == code
+            gp.check()
+            assert torch.equal(got[0]["loss"], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_a_wait_that_runs_out(P):
     """The tensor-core kernels' first wait gives up (about a millisecond): the call returns an error, the next one is right."""
     import torch

@@ -302,3 +302,38 @@ def test_what_the_kernel_refuses(P, gp):
     with pytest.raises(P.GraphPOError):  # no output
         gp.logits_adjust(z, lse=False)
     gp.check()
+
+
+def test_replays_keep_their_errors_until_check(P, gp):
+    """Of a captured call the replays' errors are raised once each, and disturb no other replay."""
+    import torch
+    z, ids = torch.randn(3, 100, device="cuda"), torch.tensor([1, 2, 3, 4], device="cuda")
+    how = dict(history=ids, spans=torch.tensor([[0, 0, 2], [1, 2, 4], [2, 2, 4]], device="cuda"), repetition=1.5, frequency=0.5)
+    step = lambda: gp.logits_adjust(z, write=torch.float32, **how)["logits"]  # noqa: E731
+    want = step().clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for _ in range(2):
+        ids[1] = 100
+        graph.replay()
+        ids[1] = 2
+        graph.replay()
+        with pytest.raises(P.GraphPOError) as e:
+            gp.check()
+        assert e.value.code == SHAPE
+        gp.check()
+        assert torch.equal(got, want)
+
+
+def test_limits(P, gp):
+    """What the library refuses by its sizes alone, before it looks at any memory."""
+    import ctypes
+    import torch
+    from paper_2606_18954_gb300 import binding as B
+    L, out = B.load(), torch.zeros(1, device="cuda")
+    for R, V, code in ((1, 2 ** 30 + 1, 5), (2 ** 31, 1, 5), (2 ** 12, 2 ** 29, 5), (1, 0, 1), (-1, 5, 1)):
+        args = B.CLogits(R, V, V, out.data_ptr(), 1, 4, 4, 4, *([None] * 4), 1.0, 1.0, 0.0, 0.0)
+        outs = B.LogitsOutputs(None, V, 1, None, out.data_ptr(), None)
+        assert L.gpo_logits_adjust(gp._h, ctypes.byref(args), ctypes.byref(outs), None) == code, (R, V)

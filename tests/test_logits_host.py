@@ -65,7 +65,8 @@ def test_the_binding_refuses(monkeypatch):
             (dict(mask=v(4, i32).view(2, 2)), ValueError), (dict(mask=v(9, torch.int64).view(3, 3)), TypeError),
             (dict(mask=v(6, i32).view(2, 3)), ValueError), (dict(mask=v(6, i32).view(2, 3), mask_row=v(3, torch.int64)), TypeError),
             (dict(mask=v(0, i32).view(0, 3), mask_row=v(3, i32)), ValueError), (dict(target=v(3)), TypeError), (dict(target=v(4, i32)), ValueError),
-            (dict(write=torch.float16), TypeError)):
+            (dict(write=torch.float16), TypeError), (dict(bias_spans=v(6, torch.int64).view(3, 2)), ValueError),
+            (dict(mask_row=v(3, i32)), ValueError)):
         with pytest.raises(error):
             gp.logits_adjust(z, **bad)
     for bad, error in ((dict(target=None), ValueError), (dict(lse=v(2)), ValueError), (dict(logp=v(3).double()), TypeError),
