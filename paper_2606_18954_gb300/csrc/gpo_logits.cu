@@ -58,14 +58,14 @@ struct Raw<GPO_DT_F32> {
   static constexpr int kPer = 8;
   static constexpr bool kFloors = false;
   // the entries of `take`, `other` in the place of the rest; those of `b` in the places `of_b`
-  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other) {
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other, uint32_t) {
     Vec x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x.w[i] = take >> i & 1u ? r.w[i] : other;
     return x;
   }
-  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return keep(r, take, 0xFF800000u); }  // -inf
-  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b) {
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t) { return keep(r, take, 0xFF800000u, 0u); }  // -inf
+  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b, uint32_t) {
     Vec x;
 #pragma unroll
     for (int i = 0; i < 8; ++i) x.w[i] = of_b >> i & 1u ? b.w[i] : a.w[i];
@@ -95,32 +95,23 @@ struct Raw<GPO_DT_F32> {
 // (two 16-bit entries per word)
 struct Raw16 {
   static constexpr int kPer = 16;
-  template <uint32_t kSel>
-  static __device__ __forceinline__ uint32_t spread(uint32_t x) {
-    uint32_t r;
-    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(x), "n"(kSel));
-    return r;
-  }
-  // Sixteen ones in the half of word i / 2 for every bit i.  A nibble's bits go to the sign bits of four bytes (i + 7 (j + 1) is
-  // different for every bit i and factor bit j, so that nothing carries), which prmt spreads.
-  static __device__ __forceinline__ Vec mask(uint32_t take) {
+  // Sixteen ones in the half of word i / 2 for every bit i: two words at a time from a table of a nibble's, whose 16 entries of 8
+  // bytes lie in all banks once (three instructions a nibble; a product and two byte permutations took six).
+  static __device__ __forceinline__ Vec mask(uint32_t take, uint32_t table) {
     Vec m;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t a = (take >> 4 * i & 15u) * 0x10204080u & 0x80808080u;
-      m.w[2 * i] = spread<0x9988>(a);
-      m.w[2 * i + 1] = spread<0xBBAA>(a);
-    }
+    for (int i = 0; i < 4; ++i)
+      asm("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(m.w[2 * i]), "=r"(m.w[2 * i + 1]) : "r"((take << 3 >> 4 * i & 0x78u) | table));
     return m;
   }
-  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other) {
-    Vec m = mask(take);
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t other, uint32_t table) {
+    Vec m = mask(take, table);
 #pragma unroll
     for (int i = 0; i < 8; ++i) m.w[i] = (r.w[i] & m.w[i]) | (other & ~m.w[i]);
     return m;
   }
-  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b) {
-    Vec m = mask(of_b);
+  static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b, uint32_t table) {
+    Vec m = mask(of_b, table);
 #pragma unroll
     for (int i = 0; i < 8; ++i) m.w[i] = (a.w[i] & ~m.w[i]) | (b.w[i] & m.w[i]);
     return m;
@@ -131,7 +122,7 @@ struct Raw<GPO_DT_BF16> : Raw16 {
   using T = __nv_bfloat16;
   using Raw16::keep;
   static constexpr bool kFloors = true;
-  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return Raw16::keep(r, take, 0xFF80FF80u); }
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t table) { return Raw16::keep(r, take, 0xFF80FF80u, table); }
   static __device__ __forceinline__ __nv_bfloat162 h2(uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); }
   // -1e33 for -inf and what is below it, which for every scale is left out of a row all the same; a NaN stays one
   static __device__ __forceinline__ Vec floor(const Vec& r) {
@@ -176,7 +167,7 @@ struct Raw<GPO_DT_F16> : Raw16 {
   using T = __half;
   using Raw16::keep;
   static constexpr bool kFloors = false;  // (fp16 has no number that is below all that counts)
-  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take) { return Raw16::keep(r, take, 0xFC00FC00u); }
+  static __device__ __forceinline__ Vec keep(const Vec& r, uint32_t take, uint32_t table) { return Raw16::keep(r, take, 0xFC00FC00u, table); }
   static __device__ __forceinline__ __half2 h2(uint32_t w) { return *reinterpret_cast<const __half2*>(&w); }
   static __device__ __forceinline__ Vec floor(const Vec& r) { return r; }
   static __device__ __forceinline__ float top(const Vec& r) {
@@ -248,6 +239,7 @@ struct Smem {
   uint32_t list[kCap];                // the round's special entries, in their order,
   uint32_t count[kCap];               // and their flags and occurrences
   uint32_t stage[kWarps][128];        // words of each warp on their way out
+  alignas(128) uint2 nibble[16];      // ones in the 16-bit lanes of a nibble's bits (Raw16::mask)
   uint64_t full[kWarps][kDeep];
   alignas(128) unsigned char ring[kWarps][kDeep][kChunk];
 };
@@ -718,7 +710,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   if (a.spans || a.bias)
     for (int g = tid; g < kGroups; g += kThreads) reinterpret_cast<uint4*>(sm.special)[g] = make_uint4(0u, 0u, 0u, 0u);
   if (blockIdx.x == 0 && tid == 32) next_tag(st);
+  if (tid >= 64 && tid < 80) {
+    auto lanes = [&](int bit) { return (tid >> bit & 1 ? 0xFFFFu : 0u) | (tid >> (bit + 1) & 1 ? 0xFFFF0000u : 0u); };
+    sm.nibble[tid - 64] = make_uint2(lanes(0), lanes(2));
+  }
   __syncthreads();
+  uint32_t nibble = smem_u32(sm.nibble);
+  asm volatile("" : "+r"(nibble));  // (so that no load from the table comes before the barrier)
   const Row& w = sh.row;
   bool ok = true;  // (of the whole warp)
   auto arrived = [&]() {
@@ -867,21 +865,21 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
         E::widen(x, y);
         gradient(y);
         Vec o = E::narrow(y);
-        if (kMarked) o = E::keep(o, take, 0u);
-        if (kMarked && kKeep) o = E::choose(o, x, sp);
+        if (kMarked) o = E::keep(o, take, 0u, nibble);
+        if (kMarked && kKeep) o = E::choose(o, x, sp, nibble);
         store_vec<kType, false>(w, y, o, first, from, stage, lane);
       } else {
         if (writes(kOp)) {
           Vec q = x;
-          if (kMarked) q = E::keep(q, take);
+          if (kMarked) q = E::keep(q, take, nibble);
           E::widen(q, y);
 #pragma unroll
           for (int j = 0; j < kPer; ++j) y[j] *= scale;
           if (!wide) q = E::narrow(y);
-          if (!wide && kMarked && kKeep) q = E::choose(q, x, sp);
+          if (!wide && kMarked && kKeep) q = E::choose(q, x, sp, nibble);
           store_vec<kType, wide>(w, y, q, first, from, stage, lane);
         }
-        if (kMarked) x = E::keep(x, take);
+        if (kMarked) x = E::keep(x, take, nibble);
         if (kEnt) x = E::floor(x);
         sums(x);
       }
