@@ -2,8 +2,10 @@
 // include/graphpo.h).  Times of 2048 tokens (1434 with a teacher) of 65536 x 2048 with up to 32 entries.
 //
 // Forward:  teach_sort_kernel   a warp per token puts the teacher's entries in the order of their ids (by counting the smaller
-//                               ones: k^2 / 32 comparisons a lane) with their probabilities, and counts those before every 128
-//                               columns of the vocabulary.  11 us, bound by latency; k^2 counts from some 200 entries on
+//                               ones: k^2 / 32 comparisons a lane, four ids of every load against up to four of the lane's own)
+//                               with their probabilities, and counts those before every 128 columns of the vocabulary.  14 us
+//                               between events, of 256 entries a token 38 (one comparison a load, and the columns one search
+//                               after another 17 and 81): the instructions of both loops
 //           vocab_pair_kernel   <kLseTop>: logits tiles that stay in tensor memory; a row's entries are taken out of its
 //                               maximum and sum, which are then those of the other tokens.  214 to 225 us, 1710 to 1800 TFLOP/s,
 //                               tensor pipe 93 % active.  Every entry among a warp's 32 rows and 32 columns is a pass over the 32
@@ -49,8 +51,30 @@ __device__ __forceinline__ float warp_sum(float x) { return over_warp(x, [](floa
 // The lowest index (below 2^31) of any lane.
 __device__ __forceinline__ int warp_first(int x) { return (int)__reduce_min_sync(0xffffffffu, (unsigned)x); }
 
+// The entries of a warp's token by their ids: calls f(j, id, rank) for every entry j that is one, kOwn of a lane at a time.
+// ids: k of them, then kNoId up to a multiple of 4.  Equal ids get equal ranks.
+template <int kOwn, class F>
+__device__ __forceinline__ void rank_entries(const int* ids, int k, F f) {
+#pragma unroll 1
+  for (int j0 = threadIdx.x & 31; j0 < k; j0 += 32 * kOwn) {
+    int id[kOwn], rank[kOwn];
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u) id[u] = j0 + 32 * u < k ? ids[j0 + 32 * u] : kNoId, rank[u] = 0;
+#pragma unroll 4
+    for (int i = 0; i < k; i += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(ids + i);
+#pragma unroll
+      for (int u = 0; u < kOwn; ++u) rank[u] += (x.x < id[u]) + (x.y < id[u]) + (x.z < id[u]) + (x.w < id[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u)
+      if (id[u] != kNoId) f(j0 + 32 * u, id[u], rank[u]);
+  }
+}
+
 __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t, Status st) {
-  __shared__ int s_id[kSortWarps][kTeachMax], s_sorted[kSortWarps][kTeachMax];
+  __shared__ __align__(16) int s_id[kSortWarps][kTeachMax];
+  __shared__ int s_sorted[kSortWarps][2 * kTeachMax];
   __shared__ float s_v[kSortWarps][kTeachMax];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   let_next_start();
@@ -70,6 +94,7 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
     m = fmaxf(m, v[j]);
     n += in;
   }
+  if (lane < (-t.k & 3)) ids[t.k + lane] = kNoId;  // (kTeachMax is a multiple of 4)
   n = __reduce_add_sync(0xffffffffu, n);
   m = warp_max(m);
   if (__any_sync(0xffffffffu, bad)) {
@@ -77,6 +102,8 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
     n = 0;
   }
   if (!t.tail && m == -INFINITY) n = 0;  // (no distribution)
+  const int step = n > 0 ? 1 << (31 - __clz(n)) : 0;  // the largest power of two that is not above n
+  for (int j = lane; j < 2 * step; j += 32) s_sorted[warp][j] = kNoId;
   __syncwarp();
   float shift = 0.f, qr = 0.f;  // log q = v - shift
   if (n > 0 && !t.tail) {
@@ -100,39 +127,39 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
     else qr = (float)(1.0 - sum);
   }
   float* delta = t.delta + tok * t.delta_stride;
-  for (int j = lane; j < t.k; j += 32) {
-    if (n == 0 || ids[j] == kNoId) {
-      delta[j] = 0.f;
-      continue;
+  for (int j = lane; j < t.k; j += 32)
+    if (n == 0 || ids[j] == kNoId) delta[j] = 0.f;
+  if (n > 0) {
+    auto put = [&](int j, int id, int rank) {
+      const int64_t at = tok * t.stride + rank;
+      const float lq = v[j] - m - shift;
+      t.id[at] = s_sorted[warp][rank] = id;
+      t.place[at] = (int16_t)j;
+      t.lq[at] = lq;
+      t.q[at] = expf(lq);
+    };
+    if (t.k <= 32) rank_entries<1>(ids, t.k, put);
+    else if (t.k <= 64) rank_entries<2>(ids, t.k, put);
+    else rank_entries<4>(ids, t.k, put);
+    __syncwarp();
+    bool twice = false;  // of equal ranks one place stays empty
+    for (int j = lane; j < n; j += 32) twice |= s_sorted[warp][j] == kNoId;
+    if (__any_sync(0xffffffffu, twice)) {
+      if (lane == 0) report(st, GPO_ERR_SHAPE, 52, (int)tok);
+      n = 0;
     }
-    int rank = 0;
-    bool twice = false;
-    for (int i = 0; i < t.k; ++i) {
-      rank += ids[i] < ids[j] || (ids[i] == ids[j] && i < j);
-      twice |= ids[i] == ids[j] && i != j;
-    }
-    if (twice) report(st, GPO_ERR_SHAPE, 52, (int)tok);
-    const int64_t at = tok * t.stride + rank;
-    const float lq = v[j] - m - shift;
-    t.id[at] = s_sorted[warp][rank] = ids[j];
-    t.place[at] = (int16_t)j;
-    t.lq[at] = lq;
-    t.q[at] = expf(lq);
   }
-  __syncwarp();
+  // The entries below 128 p, by steps of powers of two; four places a lane are looked for at a time.
   const int parts = (int)vocab_parts(t.V);
-  for (int p = lane; p <= parts; p += 32) {  // the entries below 128 p
-    int first = 0;
-    for (int m = n; m > 0;) {
-      const int h = m >> 1;
-      if (s_sorted[warp][first + h] < 128 * p) {
-        first += h + 1;
-        m -= h + 1;
-      } else {
-        m = h;
-      }
-    }
-    t.first[tok * t.first_stride + p] = (uint16_t)first;
+  for (int p = lane; p <= parts; p += 128) {
+    int first[4] = {0, 0, 0, 0};
+    for (int s = n > 0 ? step : 0; s > 0; s >>= 1)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if ((uint32_t)s_sorted[warp][first[u] + s - 1] < 128u * (uint32_t)(p + 32 * u)) first[u] += s;
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (p + 32 * u <= parts) t.first[tok * t.first_stride + p + 32 * u] = (uint16_t)first[u];
   }
   if (lane == 0) {
     t.n[tok] = n;
