@@ -10,7 +10,7 @@
 //                               maximum and sum, which are then those of the other tokens.  214 to 225 us, 1710 to 1800 TFLOP/s,
 //                               tensor pipe 93 % active.  Every entry among a warp's 32 rows and 32 columns is a pass over the 32
 //                               (100 instructions): of narrow states, whose tiles' products are short, that shows (8192 tokens of
-//                               131072 x 256 with 48 entries 560 us, log-probabilities 460)
+//                               131072 x 256 with 48 entries 547 us, log-probabilities 462)
 //           teach_join_kernel   the parts of a row joined, divergence and p - q from them and the entries' logits.  10 us
 // Gradient: outside the entries dz is g (p - q of all others together) times the softmax over the others, for either form of the
 //           loss; inside it is g (p - q).  So vocab_pair_kernel's dz of a token without a target, with the others' log-sum-exp,
