@@ -337,3 +337,26 @@ def test_limits(P, gp):
         args = B.CLogits(R, V, V, out.data_ptr(), 1, 4, 4, 4, *([None] * 4), 1.0, 1.0, 0.0, 0.0)
         outs = B.LogitsOutputs(None, V, 1, None, out.data_ptr(), None)
         assert L.gpo_logits_adjust(gp._h, ctypes.byref(args), ctypes.byref(outs), None) == code, (R, V)
+
+
+def test_offsets_past_32_bits(gp):
+    """More than 2^31 entries: the last rows are what a call on them alone gives (of 400 rows, too, each is one CTA's)."""
+    import torch
+    R, V, n = 33000, 65600, 400
+    assert R * V > 2 ** 31
+    z = torch.empty(R, V, device="cuda", dtype=torch.float16).normal_()
+    y = torch.randint(0, V, (R,), device="cuda")
+    g, s = torch.randn(R, device="cuda"), torch.rand(R, device="cuda") + 0.5
+    ids = torch.randint(0, V, (3000,), device="cuda")
+    spans = torch.tensor([[0, 1000, 3000]], device="cuda").repeat(R, 1)
+    mask = torch.randint(-2 ** 31, 2 ** 31, (R, (V + 31) // 32), device="cuda").to(torch.int32)
+    how = lambda a: dict(scale=s[a:], history=ids, spans=spans[a:], repetition=1.2, presence=0.1, frequency=0.05, mask=mask[a:])  # noqa: E731
+    tail = z[-n:].clone()
+    f = gp.logits_adjust(z, y, write=torch.float16, **how(0))
+    e = gp.logits_adjust(tail, y[-n:], write=torch.float16, **how(R - n))
+    d = gp.logits_grad(z, y, f["lse"], f["logp"], g, out={"d_logits": z}, **how(0))["d_logits"]
+    c = gp.logits_grad(tail, y[-n:], e["lse"], e["logp"], g[-n:], **how(R - n))["d_logits"]
+    gp.check()
+    for k in f:
+        assert torch.equal(f[k][-n:], e[k]), k
+    assert torch.equal(d[-n:], c)
