@@ -1057,6 +1057,7 @@ struct VocabArgs {
   float* top_z;
   int64_t top_stride;
   const uint16_t* top_first;
+  int top_seg;  // steps of 64 k that a sum takes in tensor memory
   int64_t first_stride;
 };
 

@@ -434,7 +434,7 @@ __device__ __forceinline__ bool load_tiles(const VocabMaps& maps, const VocabArg
 // Their MMAs, by one thread of the leader.
 template <int kMode, int kS>
 __device__ __forceinline__ bool mma_tiles(const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
-  constexpr int seg = segment_of<kMode>();
+  const int seg = kMode == kLseTop ? a.top_seg : segment_of<kMode>();
   const Plan plan = make_plan<kMode>(a, c.rows);
   uint32_t rest = 0;  // steps of write_rests so far
   Tile t;
@@ -547,7 +547,7 @@ __device__ __forceinline__ void dz_columns(const VocabArgs& a, const DzRow& w, c
 template <int kMode, int kS>
 __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabArgs& a, const Status& st, const Cta& c, Pipe& p) {
   constexpr bool kLogits = is_lse(kMode);
-  constexpr int seg = segment_of<kMode>();
+  const int seg = kMode == kLseTop ? a.top_seg : segment_of<kMode>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rows = c.rows;
   const Plan plan = make_plan<kMode>(a, rows);
   const int q = warp & 3, half = (warp - 4) >> 2;  // tensor memory lanes 32 q .., columns 128 half ..

@@ -553,7 +553,9 @@ gpo_status gpo_vocab_distill(gpo_ctx* ctx, const gpo_vocab* v, const gpo_teacher
   a.part_row = 1;
   a.part_col = L.v.tp;
   a.logp = out->loss;  // (launch_vocab_rows: zeros of the tokens that take no part)
-  a.sl2 = logit_scale(*v, 64 * kVocabSeg);
+  // (of few tokens shorter sums, as in their log-probabilities: there no other tokens' errors average one row's out)
+  a.top_seg = v->num_tokens <= 16 ? kVocabFewSeg : kVocabSeg;
+  a.sl2 = logit_scale(*v, 64 * a.top_seg);
   a.top_id = ta.id;
   a.top_first = ta.first;
   a.first_stride = L.first_stride;
