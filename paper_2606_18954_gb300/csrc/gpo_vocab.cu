@@ -66,7 +66,7 @@ static_assert(128 * regs_few(kDzWide) + 256 * regs_many(kDzWide) <= kVThreads * 
 constexpr int kVBox = kTile16 * 128;               // one 64 x 64 box
 constexpr int kVStage = 4 * kVBox;                 // A and B halves of one k-step, per CTA
 constexpr int kVCols = 512;                        // two accumulators of 256 columns
-// Logits: after kVocabSeg (dz: kVocabDzSeg) steps of 64 k the tensor cores' sum is taken over into registers.  Their
+// Logits: after kVocabSeg (dz: kVocabDzSeg; a teacher's of few tokens: kVocabFewSeg) steps of 64 k the tensor cores' sum is taken over into registers.  Their
 // fp32 additions drop the bits below the sum's last one, always towards zero, so that a sum of d products
 // shrinks by about d / 130 ulps: 4e-6 of a logit at d = 4096, too much for the log-probability of
 // a nearly certain token.  Shorter sums, added in registers with rounding, keep that down (the mean of what is left
