@@ -356,7 +356,7 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
     bad(GPO_ERR_SHAPE, 5);
     w.target = -1;
   }
-  w.live = writes(kOp) || w.target >= 0;
+  w.live = writes(kOp) || !a.target || w.target >= 0;  // (the gradient has targets)
   w.g = f32(11, a.g, 0.f);
   w.e = f32(12, a.ge, 0.f);
   w.ent = f32(13, a.ge, 0.f);
