@@ -247,11 +247,13 @@ __global__ void __launch_bounds__(256) teach_grad_kernel(TeachArgs t, Status st)
   if (tok >= t.T) return;
   int top = -1;  // the entry of the largest |delta|, of equal ones that of the lowest id
   float most = -1.f;
+  bool learns = !(t.rest_in[tok] == 0.f);  // (a NaN is not 0)
   for (int j = lane; j < t.k; j += 32) {
     const int64_t id = load_id(t.ids, t.id8, tok * t.ids_stride + j);
     if (id >= t.V) report(st, GPO_ERR_SHAPE, 53, (int)tok);
     if (id < 0 || id >= t.V) continue;
     const float x = fabsf(t.delta_in[tok * t.delta_stride + j]);
+    learns |= !(x == 0.f);
     if (top < 0 || x > most || (x == most && id < top)) top = (int)id, most = x;
   }
 #pragma unroll
@@ -260,9 +262,12 @@ __global__ void __launch_bounds__(256) teach_grad_kernel(TeachArgs t, Status st)
     const float x = __shfl_xor_sync(0xffffffffu, most, o);
     if (id >= 0 && (top < 0 || x > most || (x == most && id < top))) top = id, most = x;
   }
+  // Without any p - q that is not 0 every dz is 0: of a token whose teacher gives nothing a probability, rest_lse is a 0 that is
+  // none, and its hidden row may hold anything, which would reach d_weight as 0 times that.
+  learns = __any_sync(0xffffffffu, learns);
   if (lane != 0) return;
   const float lse = t.rest_lse_in[tok];
-  t.target[tok] = top;
+  t.target[tok] = learns ? top : -1;
   t.none[tok] = -1;
   t.dense[tok] = -t.g[tok] * t.rest_in[tok];
   t.dense_lse[tok] = lse == -INFINITY ? INFINITY : lse;  // (no other tokens: their p is 0)
