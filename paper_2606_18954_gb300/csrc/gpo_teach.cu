@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(1024) teach_join_kernel(TeachArgs t, VocabArgs
   for (int j = lane; j < n; j += 32)
     if (z[j] == most) first = min(first, j);
   first = warp_first(first);  // (none where they are NaN)
-  const bool some = p.s > 0.f;  // tokens other than the entries
+  const bool some = n < t.V;  // tokens other than the entries (whose sum may be NaN, or 0 where every logit of theirs is -inf)
   const float top = some ? fmaxf(p.m, most) : most, er = some ? p.s * exp2f(p.m - top) : 0.f, ef = exp2f(most - top);
   float others = 0.f, q_others = 0.f;
   for (int j = lane; j < n; j += 32) {
