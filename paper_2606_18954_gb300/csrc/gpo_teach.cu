@@ -106,25 +106,30 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
   for (int j = lane; j < 2 * step; j += 32) s_sorted[warp][j] = kNoId;
   __syncwarp();
   float shift = 0.f, qr = 0.f;  // log q = v - shift
-  if (n > 0 && !t.tail) {
-    // the largest apart: log q of a nearly certain token has its digits
+  if (n > 0) {
+    // the largest apart: log q of a nearly certain token has its digits, and 1 - q of it
     int first = kNoId;
     for (int j = lane; j < t.k; j += 32)
       if (v[j] == m) first = min(first, j);
     first = warp_first(first);
-    float others = 0.f;
-    for (int j = lane; j < t.k; j += 32)
-      if (j != first) others += expf(v[j] - m);
-    shift = log1pf(warp_sum(others));
-  } else if (n > 0) {
-    // (in 64 bits: 1 - the sum may be small)
-    double sum = 0.0;
-    for (int j = lane; j < t.k; j += 32) sum += (double)expf(v[j]);
+    if (!t.tail || m > 0.f) {
+      float others = 0.f;
+      for (int j = lane; j < t.k; j += 32)
+        if (j != first) others += expf(v[j] - m);
+      shift = log1pf(warp_sum(others));
+    } else {
+      // 1 - the sum, in 64 bits: it may be small beside the others, too.  (1 - q of the largest from exp, not expm1, was off by
+      // 6e-8, 1 % of a remainder of 1e-5)
+      double others = 0.0;
+      for (int j = lane; j < t.k; j += 32)
+        if (j != first) others += (double)expf(v[j]);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    m = 0.f;
-    if (sum > 1.0) shift = logf((float)sum);  // (probabilities rounded to fewer bits)
-    else qr = (float)(1.0 - sum);
+      for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
+      const double left = -(double)expm1f(m) - others;
+      m = 0.f;
+      if (left < 0.0) shift = log1pf((float)-left);  // (probabilities rounded to fewer bits)
+      else qr = (float)left;
+    }
   }
   float* delta = t.delta + tok * t.delta_stride;
   for (int j = lane; j < t.k; j += 32)
