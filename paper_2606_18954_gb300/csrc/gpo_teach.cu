@@ -222,8 +222,8 @@ __global__ void __launch_bounds__(1024) teach_join_kernel(TeachArgs t, VocabArgs
     q_others += q[j];
   }
   others = warp_sum(others) + er;
-  const float qr = some ? t.qr[tok] : 0.f;  // (of no tokens: what the teacher's probabilities were rounded by)
-  q_others = warp_sum(q_others) + qr;
+  const float left = t.qr[tok], qr = some ? left : 0.f;  // (of no tokens: what the teacher's probabilities were rounded by)
+  q_others = warp_sum(q_others) + left;                  // 1 - q of the largest, in either case
   const float total = others + ef, lt = top == most ? log1pf(others) : logf(total), inv = 1.f / total;
   float loss = 0.f;
   float* delta = t.delta + tok * t.delta_stride;

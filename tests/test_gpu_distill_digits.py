@@ -90,3 +90,19 @@ def test_nearly_certain_teachers(gp, left, teacher):  # noqa: F811
     tol = tol + q_err * (gap.abs() + 40) + ref["qr"] * (p_err + 8 * U * (gap.abs() + 40)) + over + 40 * U * (terms.sum(1) + ref["qr"] * gap.abs())
     err = (f["loss"].double() - ref["loss"]).abs()
     assert bool((err <= tol).all()), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T, V, d", [(5, 40, 72), (300, 200, 64)])
+def test_the_whole_vocabulary_with_a_tail(gp, T, V, d, dtype):  # noqa: F811
+    """Every token is an entry, log-probabilities rounded to few bits: q_r is 0 whatever their sum leaves, and delta p - q."""
+    import torch
+    from distill_ref import exact, inputs, near
+    teacher = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[dtype]
+    h, w, ids, t = inputs(T, V, d, V, torch.bfloat16, seed=T, tail=True, teacher=teacher)
+    ref = exact(h, w, ids, t, tail=True)
+    f = gp.vocab_distill(h, w, ids, t, tail=True, lse=True)
+    gp.check()
+    for name in ("lse", "rest_lse", "rest", "delta", "loss"):
+        near(f[name], ref[name], ref["t_" + name], name)
+    assert not f["rest"].any()
