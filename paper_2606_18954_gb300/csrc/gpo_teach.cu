@@ -215,30 +215,38 @@ __global__ void __launch_bounds__(1024) teach_join_kernel(TeachArgs t, VocabArgs
   first = warp_first(first);  // (none where they are NaN)
   const bool some = n < t.V;  // tokens other than the entries (whose sum may be NaN, or 0 where every logit of theirs is -inf)
   const float top = some ? fmaxf(p.m, most) : most, er = some ? p.s * exp2f(p.m - top) : 0.f, ef = exp2f(most - top);
-  float others = 0.f, q_others = 0.f;
+  float mine = 0.f, q_mine = 0.f;  // of the entries but the largest
   for (int j = lane; j < n; j += 32) {
     if (j == first) continue;
-    others += exp2f(z[j] - top);
-    q_others += q[j];
+    mine += exp2f(z[j] - top);
+    q_mine += q[j];
   }
-  others = warp_sum(others) + er;
+  mine = warp_sum(mine);
+  q_mine = warp_sum(q_mine);
   const float left = t.qr[tok], qr = some ? left : 0.f;  // (of no tokens: what the teacher's probabilities were rounded by)
-  q_others = warp_sum(q_others) + left;                  // 1 - q of the largest, in either case
+  const float others = mine + er, q_others = q_mine + left, qf = first < n ? q[first] : 0.f;
   const float total = others + ef, lt = top == most ? log1pf(others) : logf(total), inv = 1.f / total;
+  // p - q of the largest entry and of the others together: of numbers whose sum is above 1, 1 - q less 1 - p, whose digits p and q
+  // do not have; else p - q, whose digits 1 - p and 1 - q do not have
+  const float pf = ef * inv, pr = er * inv, p_entries = (mine + ef) * inv, q_entries = q_mine + qf;
+  const float df = pf + qf > 1.f ? q_others - others * inv : pf - qf;
+  const float dr = pr + qr > 1.f ? q_entries - p_entries : pr - qr;
   float loss = 0.f;
   float* delta = t.delta + tok * t.delta_stride;
   for (int j = lane; j < n; j += 32) {
     const float y = z[j] - top, qj = q[j];
     if (qj > 0.f) loss = fmaf(qj, lq[j] - fmaf(y, kLn2, -lt), loss);
-    // (1 - q less 1 - p of the largest, whose digits p and q may not have)
-    delta[t.place[tok * t.stride + j]] = j == first ? q_others - others * inv : fmaf(exp2f(y), inv, -qj);
+    delta[t.place[tok * t.stride + j]] = j == first ? df : fmaf(exp2f(y), inv, -qj);
   }
   loss = warp_sum(loss);
   if (lane == 0) {
     const float log_others = some ? fmaf(p.m, kLn2, logf(p.s)) : -INFINITY;
-    if (qr > 0.f) loss = fmaf(qr, logf(qr) - (fmaf(p.m - top, kLn2, logf(p.s)) - lt), loss);
+    if (qr > 0.f) {
+      const float log_q = qr > 0.5f ? log1pf(-q_entries) : logf(qr);
+      loss = fmaf(qr, log_q - (pr > 0.5f ? log1pf(-p_entries) : fmaf(p.m - top, kLn2, logf(p.s)) - lt), loss);
+    }
     t.loss[tok] = loss;
-    t.rest[tok] = er * inv - qr;
+    t.rest[tok] = dr;
     t.rest_lse[tok] = log_others;
     if (t.lse) t.lse[tok] = fmaf(top, kLn2, lt);
   }

@@ -106,3 +106,32 @@ def test_the_whole_vocabulary_with_a_tail(gp, T, V, d, dtype):  # noqa: F811
     for name in ("lse", "rest_lse", "rest", "delta", "loss"):
         near(f[name], ref[name], ref["t_" + name], name)
     assert not f["rest"].any()
+
+
+@pytest.mark.parametrize("T, V", [(64, 20000), (300, 131072)])
+def test_flat_distributions(gp, T, V):  # noqa: F811
+    """No token of either has much: p - q of the largest entry and of the others together are differences of small numbers, not
+    of what they leave of 1."""
+    import torch
+    d, k = 64, 8
+    h, w, z, _, g = _student(T, V, d, 0.25, 0.0)
+    other = z + 0.25 * torch.randn(T, V, generator=g, device="cuda", dtype=torch.float64)
+    t, ids = torch.log_softmax(other, 1).topk(k, dim=1)
+    t = t.float()
+    ref = _exact(z, ids, t)
+    f = gp.vocab_distill(h, w, ids, t, tail=True)
+    gp.check()
+    # (z and log q below 16: 1 and 8 roundings of exponents, 12 of each probability's own, sums)
+    p_err, q_err = (8 * 2 + 4 + 64 + 16) * U, 8 * U
+    tol = p_err * ref["p"] + q_err * ref["q"]
+    err = (f["delta"].double() - ref["delta"]).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
+    err = (f["rest"].double() - ref["rest"]).abs()
+    assert bool((err <= tol.sum(1)).all()), float((err / tol.sum(1)).max())
+    # log q_r and log p_r are log1p of the entries' sums
+    assert bool((ref["qr"] > 0.5).all()) and bool((ref["pr"] > 0.5).all())
+    terms = ref["q"] * (ref["lq"] - ref["lp"])
+    want = terms.sum(1) + ref["qr"] * (torch.log1p(-ref["q"].sum(1)) - torch.log1p(-ref["p"].sum(1)))
+    tol = (ref["q"] * (p_err + 8 * U * (ref["lq"].abs() + ref["lp"].abs())) + 40 * U * terms.abs()).sum(1) + 2 * tol.sum(1)
+    err = (f["loss"].double() - want).abs()
+    assert bool((err <= tol).all()), float((err / tol).max())
