@@ -525,7 +525,7 @@ gpo_status gpo_embed_grad(gpo_ctx* ctx, const gpo_embedding* e, const void* grad
  * without entries, or with tail = 0 without one above -inf, has no teacher: its outputs are 0, it has no gradient, and its
  * hidden row (NaN, say) reaches no other result.  Nor does that of a token whose grad_loss is 0.  Found on the GPU and returned by
  * gpo_sync_status: an id >= vocab, the same id twice in a row (GPO_ERR_SHAPE; the gradient does not look for the second), a
- * teacher's logit that is NaN or +inf (GPO_ERR_NONFINITE); the call's outputs are then undefined. */
+ * teacher's logit that is NaN or +inf, by itself or times its scale (GPO_ERR_NONFINITE); the call's outputs are then undefined. */
 #define GPO_MAX_TEACHER 512 /* entries of a token's teacher */
 
 typedef struct {

@@ -89,8 +89,8 @@ __global__ void __launch_bounds__(32 * kSortWarps) teach_sort_kernel(TeachArgs t
     if (id >= t.V) report(st, GPO_ERR_SHAPE, 50, (int)tok);
     ids[j] = in ? (int)id : kNoId;
     const float x = in ? load_value(t.logits, t.dtype, tok * t.logits_stride + j) : -INFINITY;
-    bad |= !(x < INFINITY);
     v[j] = x * t.scale;
+    bad |= !(v[j] < INFINITY);  // (and so x)
     m = fmaxf(m, v[j]);
     n += in;
   }

@@ -68,3 +68,20 @@ def test_entries_beside_logits_of_minus_infinity(gp):  # noqa: F811
     f = gp.vocab_distill(h, w, ids, t)
     gp.check()
     assert bool((f["loss"].abs() < 1e-6).all()) and bool((f["rest"] == 0).all())
+
+
+def test_a_teachers_logit_past_the_largest_number(P, gp):  # noqa: F811
+    """That is infinite with the scale, though not without."""
+    import torch
+    from distill_ref import inputs
+    h, w, ids, t = inputs(9, 300, 64, 4, torch.bfloat16, seed=1)
+    for value, scale in ((3e38, 2.0), (1e38, 10.0)):
+        t[4, 2] = value
+        gp.vocab_distill(h, w, ids, t, teacher_scale=scale)
+        with pytest.raises(P.GraphPOError) as e:
+            gp.check()
+        assert e.value.code == 4
+    t[4, 2] = -3e38  # (a token of probability 0)
+    f = gp.vocab_distill(h, w, ids, t, teacher_scale=2.0)
+    gp.check()
+    assert all(bool(torch.isfinite(f[k]).all()) for k in f)
