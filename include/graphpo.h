@@ -576,7 +576,8 @@ gpo_status gpo_vocab_distill_grad(gpo_ctx* ctx, const gpo_vocab* v, const gpo_te
  *   d x_v = scale du_v/dx_v (grad_logp (1[v = target] - p_v) - grad_entropy p_v (y_v - lse + entropy)), 0 where the mask has a 0
  *
  * Everything is fp32 (entries and gradients are rounded once, to their type).  The target is kept out of the sum over the other
- * tokens, so that a nearly certain token's logp has its digits, and its gradient too.  Results are the same on every run.
+ * tokens, so that a nearly certain token's logp has its digits, and its gradient too; in a row without one a largest logit that
+ * stands out is, so that the entropy has them.  Results are the same on every run.
  *
  * History: row r's is the tokens [spans[3r], spans[3r+2]) of `history`, of which those from spans[3r+1] on are generated
  * ones; rows may share tokens (the positions of a rollout, the continuations of a prefix).  An id below 0 is no token.

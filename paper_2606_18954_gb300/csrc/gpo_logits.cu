@@ -42,9 +42,12 @@ constexpr int kDeep = 2;                         // and how many of them are in 
 constexpr int kLead = 16;                        // bits of the bitmaps before a span's first whole 32 bytes
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr uint32_t kSeen = 1u << 31, kBiased = 1u << 30, kCount = kBiased - 1;  // an entry's word: flags, occurrences
-// the adjusted logits (in fp32, of 16-bit ones), only their statistics, the gradient
-enum Op { kAdjust, kAdjust32, kScore, kGrad };
+// the adjusted logits (in fp32, of 16-bit ones), only their statistics, the gradient, the statistics with entropies without targets
+enum Op { kAdjust, kAdjust32, kScore, kGrad, kScoreAll };
 __host__ __device__ constexpr bool writes(int op) { return op == kAdjust || op == kAdjust32; }
+__host__ __device__ constexpr bool scores(int op) { return op == kScore || op == kScoreAll; }
+// entropies of rows that may have no target (see raise)
+__host__ __device__ constexpr bool holds_out(int op, bool ent) { return ent && (writes(op) || op == kScoreAll); }
 
 // 32 bytes of logits, a lane's.
 struct Vec {
@@ -79,6 +82,14 @@ struct Raw<GPO_DT_F32> {
     for (int i = 1; i < 8; ++i) t = fmaxf(t, __uint_as_float(r.w[i]));
     return t;
   }
+  // leaves out the entries that are `top`; returns how many they were
+  static __device__ __forceinline__ int take_out(Vec& r, float top) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (__uint_as_float(r.w[i]) == top) r.w[i] = 0xFF800000u, ++n;
+    return n;
+  }
   static __device__ __forceinline__ void widen(const Vec& r, float (&y)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(r.w[i]);
@@ -111,6 +122,11 @@ struct Raw16 {
     for (int i = 0; i < 8; ++i) m.w[i] = (r.w[i] & m.w[i]) | (other & ~m.w[i]);
     return m;
   }
+  // (same: ones in the 16-bit lanes that leave)
+  static __device__ __forceinline__ int leave(uint32_t& w, uint32_t same, uint32_t other) {
+    w = (w & ~same) | (other & same);
+    return __popc(same);
+  }
   static __device__ __forceinline__ Vec choose(const Vec& a, const Vec& b, uint32_t of_b, uint32_t table) {
     Vec m = mask(of_b, table);
 #pragma unroll
@@ -140,6 +156,12 @@ struct Raw<GPO_DT_BF16> : Raw16 {
 #pragma unroll
     for (int i = 1; i < 8; ++i) t = __hmax2(t, h2(r.w[i]));
     return fmaxf(__low2float(t), __high2float(t));
+  }
+  static __device__ __forceinline__ int take_out(Vec& r, float top) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n += leave(r.w[i], __heq2_mask(h2(r.w[i]), __float2bfloat162_rn(top)), 0xF645F645u);
+    return n / 16;
   }
   static __device__ __forceinline__ void widen(const Vec& r, float (&y)[16]) {
 #pragma unroll
@@ -176,6 +198,12 @@ struct Raw<GPO_DT_F16> : Raw16 {
 #pragma unroll
     for (int i = 1; i < 8; ++i) t = __hmax2(t, h2(r.w[i]));
     return fmaxf(__low2float(t), __high2float(t));
+  }
+  static __device__ __forceinline__ int take_out(Vec& r, float top) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n += leave(r.w[i], __heq2_mask(h2(r.w[i]), __float2half2_rn(top)), 0xFC00FC00u);
+    return n / 16;
   }
   static __device__ __forceinline__ void widen(const Vec& r, float (&y)[16]) {
 #pragma unroll
@@ -220,8 +248,10 @@ struct Row {
 struct Shared {
   Row row;
   Part part[kWarps];
+  float held[kWarps];
   float at;                   // the target's adjusted logit
   Part cluster[8];
+  float cluster_held[8];
   float cluster_at;
   int before[kWarps];         // special entries of each warp's words
 };
@@ -323,8 +353,8 @@ __device__ __forceinline__ void read_row(const LogitsArgs& a, const Status& st, 
   const T* z = static_cast<const T*>(a.z) + r * a.z_stride;
   w.z = z;
   const size_t osz = kOp == kAdjust32 ? 4 : sizeof(T);
-  w.out = kOp == kScore ? nullptr : static_cast<char*>(a.out) + r * a.out_stride * osz;
-  w.vec = kOp == kScore || ((reinterpret_cast<uintptr_t>(w.out) + Edges<T>(z, a.V).head * osz) & 31) == 0;
+  w.out = scores(kOp) ? nullptr : static_cast<char*>(a.out) + r * a.out_stride * osz;
+  w.vec = scores(kOp) || ((reinterpret_cast<uintptr_t>(w.out) + Edges<T>(z, a.V).head * osz) & 31) == 0;
   w.scale = f32(0, a.scale, a.scale1);
   w.rep = f32(1, a.rep, a.rep1);
   w.pres = f32(2, a.pres, a.pres1);
@@ -598,15 +628,16 @@ __device__ __forceinline__ void store_vec(const Row& w, const float (&y)[Raw<kTy
   }
 }
 
-// The statistics of a row from its joined parts; zy: the target's logit in units of log 2, which is in no part.
-__device__ __forceinline__ void finish_row(const LogitsArgs& a, int64_t r, bool has, float zy, const Part& p) {
+// The statistics of a row from its joined parts; zy: the target's logit in units of log 2, which is in no part; held: how many
+// entries equal to the maximum are not (0 with a target).
+__device__ __forceinline__ void finish_row(const LogitsArgs& a, int64_t r, bool has, float zy, const Part& p, float held) {
   const bool at = has && !(zy <= kLow);  // (a NaN is one)
   const float top = at ? fmaxf(p.m, zy) : p.m;
   const float c = p.m - top, ec = exp2f(c);
   const float y = at ? zy - top : -INFINITY, ey = at ? exp2f(y) : 0.f;
-  const float others = ec * p.s, total = others + ey;
+  const float others = ec * p.s, total = others + (ey + held);
   const bool none = total == 0.f;
-  const float lt = y == 0.f ? log1pf(others) : logf(total);
+  const float lt = y == 0.f || held != 0.f ? log1pf(others) : logf(total);
   if (a.logp) a.logp[r] = !has ? 0.f : at ? fmaf(y, kLn2, -lt) : -INFINITY;
   if (a.lse) a.lse[r] = none ? -INFINITY : fmaf(top, kLn2, lt);
   if (a.ent) a.ent[r] = none ? 0.f : lt - kLn2 * (ec * (p.u + c * p.s) + (at ? ey * y : 0.f)) / total;
@@ -638,24 +669,43 @@ __device__ __forceinline__ void of_pairs(const uint64_t (&y)[kN / 2], float (&x)
   for (int j = 0; j < kN / 2; ++j) x[2 * j] = lo_f2(y[j]), x[2 * j + 1] = hi_f2(y[j]);
 }
 
-// Sums of exponentials so far, in two chains, relative to m.
+// Sums of exponentials so far, in two chains, relative to m; held: how many (0 or 1) of the entries that are m are not in them.
 struct Running {
   float m;
   uint64_t s, u;
+  float held;
 };
 template <bool kB>
 struct Bool {
   static constexpr bool value = kB;
 };
 
-template <bool kEnt>
-__device__ __forceinline__ void raise(Running& p, float top) {
-  if (!(top > p.m)) return;
+// Takes `top` as the maximum if it is larger; returns whether that entry then stays out of the sums.
+// The entropy of a row that is nearly certain of one token is a sum of small terms, of which a sum that holds the largest, 1,
+// keeps 6e-8 (an entropy of 1e-6 was off by 10 %).  A target's logit is out of the sums; in a row without one (apart) an entry more
+// than kApart above all before it stays out until a larger one comes: where others are nearer than that, the entropy is above 0.2.
+// (256 x 131072 adjusted 52 us for 50; 53 with every new maximum out.)
+constexpr float kApart = 4.f;
+template <bool kEnt, bool kHolds>
+__device__ __forceinline__ bool raise(Running& p, float top, bool apart) {
+  if (!(top > p.m)) return false;
   const float c = p.m - top;
   const uint64_t e = f2splat(ex2(c));
+  if (kHolds) p.s = f2add(p.s, make_f2(p.held, 0.f));
   if (kEnt) p.u = f2mul(e, f2fma(f2splat(c), p.s, p.u));
   p.s = f2mul(e, p.s);
   p.m = top;
+  if (kHolds) p.held = apart && c < -kApart ? 1.f : 0.f;
+  return kHolds && p.held != 0.f;
+}
+// Two parts of a row as one, of which the one with the larger maximum keeps what it holds out.
+template <bool kEnt, bool kHolds>
+__device__ __forceinline__ Part join_held(Part x, float& held, Part y, float held_y) {
+  if (kHolds) {
+    if (x.m >= y.m) y.s += held_y;
+    else x.s += held, held = held_y;
+  }
+  return join<kEnt>(x, y);
 }
 
 // All CTAs of the cluster have started once the wait, behind everyone's arrival, is over: only then is there shared memory of theirs.
@@ -668,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   using T = typename E::T;
   constexpr int kPer = E::kPer, kSpanVecs = (kSpan - 3 * kLead) / kPer / kChunkVecs * kChunkVecs;
   constexpr uint32_t kAll = (1u << kPer) - 1u;
-  constexpr bool wide = kOp == kAdjust32;
+  constexpr bool wide = kOp == kAdjust32, kHolds = holds_out(kOp, kEnt);
   extern __shared__ __align__(128) unsigned char smem[];
   Smem& sm = *reinterpret_cast<Smem*>(smem);
   Shared& sh = sm.sh;
@@ -758,7 +808,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
     for (int k = 0; k < kDeep; ++k) fetch();
   bool holds = false;  // the target
   const uint32_t flags = w.b1 > w.b0 ? 0u : kSeen;  // of every special entry
-  Running p = {kLow, 0ull, 0ull};
+  Running p = {kLow, 0ull, 0ull, 0.f};
+  const bool apart = kHolds && w.target < 0;
 #pragma unroll 1
   for (int s0 = min(row.vecs, c0 * kChunkVecs);; s0 += kSpanVecs) {
     const int end = min(row.vecs, c1 * kChunkVecs), s1 = min(end, s0 + kSpanVecs);
@@ -795,8 +846,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       of_pairs(y2, y);
     };
     // the entries that are left in x enter the sums
-    auto sums = [&](const Vec& x) {
-      raise<kEnt>(p, E::top(x) * sl2);
+    auto sums = [&](Vec& x) {
+      const float top = E::top(x);
+      if (raise<kEnt, kHolds>(p, top * sl2, apart)) p.s = f2add(p.s, make_f2((float)(E::take_out(x, top) - 1), 0.f));
       float y[kPer];
       uint64_t y2[kPer / 2];
       E::widen(x, y);
@@ -827,8 +879,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       }
       if (rel == trel) {
         sh.at = y;
-      } else {
-        raise<kEnt>(p, y * sl2);
+      } else if (!raise<kEnt, kHolds>(p, y * sl2, apart)) {
         const float d = fmaf(y, sl2, -p.m), x = ex2(d);
         p.s = f2add(p.s, make_f2(x, 0.f));
         if (kEnt) p.u = f2fma(make_f2(x, 0.f), make_f2(fmaxf(d, -200.f), 0.f), p.u);
@@ -903,8 +954,8 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
         fetch();
       }
     };
-    const bool keep = kOp != kScore && !wide && w.out == w.z;
-    if (kOp == kScore || wide) pass(Bool<false>());
+    const bool keep = !scores(kOp) && !wide && w.out == w.z;
+    if (scores(kOp) || wide) pass(Bool<false>());
     else if (keep) pass(Bool<true>());
     else pass(Bool<false>());
     // the entries that need more than the dense pass: special ones, the target, the row's ends
@@ -930,7 +981,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
           if (k0 + k * kThreads < m) {
             const int rel = (int)sm.list[k0 + k * kThreads];
             const float x = single(rel, sm.count[k0 + k * kThreads], z[k]);
-            if (kOp != kScore) put(rel, x);
+            if (!scores(kOp)) put(rel, x);
           }
       }
     }
@@ -944,9 +995,9 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
       // (rank_span has taken the special ones out of the allowed)
       if (!marked || (sm.allow[rel >> 5] >> (rel & 31) & 1u)) {
         const float x = single(rel, 0u, raw_at(rel));
-        if (kOp != kScore) put(rel, x);
+        if (!scores(kOp)) put(rel, x);
       } else {
-        if (kOp != kScore) put(rel, kOp == kGrad ? 0.f : -INFINITY);
+        if (!scores(kOp)) put(rel, kOp == kGrad ? 0.f : -INFINITY);
         if (kOp != kGrad && rel == trel) sh.at = -INFINITY;
       }
     }
@@ -961,24 +1012,30 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   if (!ok) drain();
   if (kOp == kGrad) return;
   Part x = {p.m, lo_f2(p.s) + hi_f2(p.s), lo_f2(p.u) + hi_f2(p.u)};
+  float held = p.held;
   auto join_lanes = [&](int from) {
     for (int o = from; o > 0; o >>= 1) {
       const Part y = {__shfl_xor_sync(0xffffffffu, x.m, o), __shfl_xor_sync(0xffffffffu, x.s, o),
                       __shfl_xor_sync(0xffffffffu, x.u, o)};
-      x = join<kEnt>(x, y);
+      x = join_held<kEnt, kHolds>(x, held, y, kHolds ? __shfl_xor_sync(0xffffffffu, held, o) : 0.f);
     }
   };
   join_lanes(16);
-  if (lane == 0) sh.part[warp] = x;
+  if (lane == 0) {
+    sh.part[warp] = x;
+    if (kHolds) sh.held[warp] = held;
+  }
   __syncthreads();
   if (joins) cluster_wait();
   if (warp == 0) {
     x = lane < kWarps ? sh.part[lane] : Part{kLow, 0.f, 0.f};
+    held = kHolds && lane < kWarps ? sh.held[lane] : 0.f;
     join_lanes(kWarps / 2);
     if (lane == 0 && cluster > 1) {
       st_remote(remote(&sh.cluster[rank].m, 0), x.m);
       st_remote(remote(&sh.cluster[rank].s, 0), x.s);
       st_remote(remote(&sh.cluster[rank].u, 0), x.u);
+      if (kHolds) st_remote(remote(&sh.cluster_held[rank], 0), held);
       // (who has the target's logit passes it on)
       if (holds) st_remote(remote(&sh.cluster_at, 0), sh.at);
     }
@@ -990,9 +1047,10 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(LogitsArgs a, i
   if (cluster > 1) {
     at = sh.cluster_at;
     x = sh.cluster[0];
-    for (int c = 1; c < cluster; ++c) x = join<kEnt>(x, sh.cluster[c]);
+    held = kHolds ? sh.cluster_held[0] : 0.f;
+    for (int c = 1; c < cluster; ++c) x = join_held<kEnt, kHolds>(x, held, sh.cluster[c], kHolds ? sh.cluster_held[c] : 0.f);
   }
-  finish_row(a, r, w.target >= 0, w.target >= 0 ? at * w.sl2 : 0.f, x);
+  finish_row(a, r, w.target >= 0, w.target >= 0 ? at * w.sl2 : 0.f, x, held);
 }
 
 template <int kType, int kOp, bool kEnt>
@@ -1007,6 +1065,7 @@ cudaError_t setup_type() {
   if (kType != GPO_DT_F32 && e == cudaSuccess) e = setup_one<kType, kType == GPO_DT_F32 ? kAdjust : kAdjust32, true>();
   if (e == cudaSuccess) e = setup_one<kType, kScore, false>();
   if (e == cudaSuccess) e = setup_one<kType, kScore, true>();
+  if (e == cudaSuccess) e = setup_one<kType, kScoreAll, true>();
   if (e == cudaSuccess) e = setup_one<kType, kGrad, false>();
   if (e == cudaSuccess) e = setup_one<kType, kGrad, true>();
   return e;
@@ -1039,6 +1098,7 @@ cudaError_t launch_type(const LaunchCtx& lc, const LogitsArgs& a, const Status& 
     return a.ent ? launch_one<kType, kOp, true>(lc, a, st) : launch_one<kType, kOp, false>(lc, a, st);
   }
   if (a.out) return a.ent ? launch_one<kType, kAdjust, true>(lc, a, st) : launch_one<kType, kAdjust, false>(lc, a, st);
+  if (a.ent && !a.target) return launch_one<kType, kScoreAll, true>(lc, a, st);
   return a.ent ? launch_one<kType, kScore, true>(lc, a, st) : launch_one<kType, kScore, false>(lc, a, st);
 }
 
