@@ -121,7 +121,7 @@ struct Status {
 };
 constexpr uint64_t kStoredTag = ~0ull;  // (no tag: tags have 48 bits)
 
-__device__ __forceinline__ uint64_t status_tag(const Status& st) {
+__host__ __device__ __forceinline__ uint64_t status_tag(const Status& st) {
   return st.tag == kStoredTag ? *reinterpret_cast<volatile const uint64_t*>(st.p + kStTag) : st.tag;
 }
 // Whether the error word holds an error with the tag t.
@@ -139,12 +139,22 @@ __device__ __forceinline__ void sign_status(const Status& st) {
 // its first kernel every replay gets the next one, so that the errors of the replays before, which stay for the
 // host to see, are not its own.  (An idle thread's, or at the kernel's end where it has no waits: the load took 0.8 us of
 // 16 tokens of 8000 x 512 by the thread that starts the others.)
-__device__ __forceinline__ void next_tag(const Status& st) {
-  if (st.tag == kStoredTag) ++*reinterpret_cast<volatile uint64_t*>(st.p + kStTag);
+__host__ __device__ __forceinline__ void next_tag(const Status& st) {
+  if (st.tag == kStoredTag) {
+    volatile uint64_t* tag = reinterpret_cast<volatile uint64_t*>(st.p + kStTag);
+    *tag = *tag + 1;
+  }
 }
 
-__device__ __forceinline__ bool aborted(const Status& st) {
+__host__ __device__ __forceinline__ bool aborted(const Status& st) {
   return is_error(*reinterpret_cast<volatile const uint64_t*>(st.p + kStError), status_tag(st));
+}
+// Whether a wait of so long stops for an error of the call's.  Other blocks of a replay may wait before next_tag's store is seen,
+// while the error of an earlier replay, which the host has not looked for, still has the tag in force: they stop only after a
+// millisecond, when the store, one of the first block's first steps, has long been seen.
+constexpr uint64_t kTagSeenNs = 1000000ull;
+__host__ __device__ __forceinline__ bool stops_waiting(const Status& st, uint64_t waited_ns) {
+  return (st.tag != kStoredTag || waited_ns > kTagSeenNs) && aborted(st);
 }
 
 #ifndef GPO_REPORT
@@ -256,7 +266,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
   for (uint32_t it = 1;; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((it & 255u) == 0u) {
-      if (honor_abort && aborted(st)) return false;
+      if (honor_abort && stops_waiting(st, globaltimer_ns() - t0)) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         report(st, GPO_ERR_TIMEOUT, where, 0);
         return false;
@@ -292,7 +302,7 @@ __device__ __forceinline__ bool wait_flag(const int* flag, const Status& st, int
     __nanosleep(64);
     if (ld_acquire_gpu(flag)) return true;
     if ((it & 63u) == 0u) {
-      if (aborted(st)) return false;
+      if (stops_waiting(st, globaltimer_ns() - t0)) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         report(st, GPO_ERR_TIMEOUT, where, 0);
         return false;
