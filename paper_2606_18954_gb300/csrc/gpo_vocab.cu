@@ -594,16 +594,17 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
         }
       }
       // the teacher's entries among the columns: how many, from where on, the first two's ids (looked up while the sums are still
-      // being made; a search through the entries took a microsecond, as long as the MMAs of 256 columns of d)
+      // being made; a search through the entries took a microsecond, as long as the MMAs of 256 columns of d).  Plain loads: teach_sort_kernel may
+      // still write them when this kernel starts, so that they are not constant to it
       int64_t top = 0;
       int hits = 0, id0 = kNoKey, id1 = kNoKey;
       if (kMode == kLseTop && live) {
         const uint16_t* first = a.top_first + tok * a.first_stride + n0 / (kPairN / 2);
-        const int from = __ldg(first);
-        hits = __ldg(first + 1) - from;
+        const int from = first[0];
+        hits = first[1] - from;
         top = tok * a.top_stride + from;
-        if (hits > 0) id0 = __ldg(a.top_id + top);
-        if (hits > 1) id1 = __ldg(a.top_id + top + 1);
+        if (hits > 0) id0 = a.top_id[top];
+        if (hits > 1) id1 = a.top_id[top + 1];
       }
       if constexpr (kMode == kDz || kMode == kDzEnt) {
         uint16_t* dst = a.dz + (int64_t)row * a.dz_stride + n0;
@@ -678,7 +679,7 @@ __device__ __forceinline__ bool finish_tiles(const VocabMaps& maps, const VocabA
                   if (at < 32) {
                     a.top_z[top++] = tz * a.sl2;
                     id0 = id1;
-                    id1 = --hits > 1 ? __ldg(a.top_id + top + 1) : kNoKey;
+                    id1 = --hits > 1 ? a.top_id[top + 1] : kNoKey;
                   }
                 }
               }
