@@ -4,7 +4,7 @@
 // One launch, no workspace.  A CTA takes a row (of few rows a cluster of 2 to 8 a row), four of them on an SM.
 //   fetch    Each warp fetches its own 1 KB pieces of the row by bulk copies, two at a time, in a ring of its own: no warp waits
 //            for another, and the first of them are under way before the row's arguments are known.
-//   special  What the history or a bias changes: a bitmap of the span (up to 69632 entries at a time), ranks by counting its
+//   special  What the history or a bias changes: a bitmap of the span (up to 81920 entries at a time), ranks by counting its
 //            bits, a list of them in their order with flags and occurrences.  Three barriers; the history is read once, of what was
 //            generated twice (the second time from L1).
 //   dense    One pass over all others, 32 bytes a lane: two bytes of a bitmap say which of 16 count (allowed, not special).
@@ -256,11 +256,16 @@ struct Shared {
   int before[kWarps];         // special entries of each warp's words
 };
 
-constexpr int kSpan = 69632;        // entries of which it is known at one time which are special
+// Entries of which it is known at one time which are special, and special entries that are looked at in one round: as many as four
+// CTAs on an SM have memory for (57344 bytes each; a span's bitmaps and ranks take 9 bytes for 32 entries, a round's 8 for one).  The
+// history is read anew for every span and every round (us: log-probabilities of 4096 x 65536 with histories to 1824, to 8992, of
+// 1500 x 151936 to 9500, 256 x 151936 adjusted with histories to 16384):
+// 36864 and 3072 163, 200, 203, 99; 69632 and 768 146, 195, 187, 120; 69632 and 1536 146, 178, 181, 99; these 146, 179, 164, 83.
+constexpr int kSpan = 81920;
 constexpr int kWords = kSpan / 32;
 constexpr int kGroups = kWords / 4;   // groups of four words, whose special entries are counted together
 static_assert((kWarps & (kWarps - 1)) == 0 && kGroups % 32 == 0, "a join in halves, whole accesses of a warp");
-constexpr int kCap = 1536;            // special entries that are looked at in one round
+constexpr int kCap = 1536;
 constexpr int kIds = 4;               // ids of the history of a thread in flight
 struct Smem {
   Shared sh;
@@ -274,6 +279,7 @@ struct Smem {
   uint64_t full[kWarps][kDeep];
   alignas(128) unsigned char ring[kWarps][kDeep][kChunk];
 };
+static_assert(kCtas * (sizeof(Smem) + 1024) <= 228 * 1024, "kCtas CTAs on an SM");
 
 // The bias of v among the row's (ascending).
 __device__ __forceinline__ float bias_of(const LogitsArgs& a, const Row& w, int64_t v) {
