@@ -17,11 +17,13 @@
 // What bounds it: without penalties and masks HBM and the issue of instructions together (us, calls in a row in a graph):
 // gradient of 4096 x 65536 bf16 (2870 live) 141, 5.8 TB/s of the bytes needed; log-probabilities and entropies of the same 92,
 // of which the exponentials alone take 41 of the special-function units' time and 10 instructions an entry at 2.8 of 4 a
-// cycle the rest; 256 x 131072 adjusted 27, 5.0 TB/s.  With histories of 1300 tokens, penalties and masks 187, 144; with 4000 tokens 48: the
-// bitmaps' bits spread over 16-bit lanes (2 instructions an entry), then the special entries (3 to 4).
-// Tried (gradient, log-probabilities, step): loads to registers in place of the rings 233, 151, 69; 3 CTAs and 2 KB pieces 190, 147,
-// 66; 2 CTAs of 512 threads 207, 175, 69; the special entries' sums before the pass, whose scattered reads come from HBM
-// then, 290, 170, 97; every warp reading the row's arguments itself 190, 153, 49;
+// cycle the rest; 256 x 131072 adjusted 28, 4.8 TB/s.  With histories of 1300 tokens, penalties and masks 188, 144; with 4000 tokens 52: the
+// bitmaps' bits spread over 16-bit lanes (2 instructions an entry), then the special entries (3 to 4).  Longer histories and
+// vocabularies: beside kSpan.  Where a row has many times kCap special entries the lists are read as many times: a bias for each of 131072
+// tokens takes 8.7 ms for 256 rows, 1.6 ms for one.
+// Tried when those three were 187, 144 and 48 (gradient, log-probabilities, step): loads to registers in place of the rings 233,
+// 151, 69; 3 CTAs and 2 KB pieces 190, 147, 66; 2 CTAs of 512 threads 207, 175, 69; the special entries' sums before the pass,
+// whose scattered reads come from HBM then, 290, 170, 97; every warp reading the row's arguments itself 190, 153, 49;
 // the bits spread by a product and byte permutations 188, 149, 48.
 #define GPO_REPORT __noinline__
 #include <cuda_bf16.h>

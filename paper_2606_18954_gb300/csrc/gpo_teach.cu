@@ -3,23 +3,24 @@
 //
 // Forward:  teach_sort_kernel   a warp per token puts the teacher's entries in the order of their ids (by counting the smaller
 //                               ones: k^2 / 32 comparisons a lane, four ids of every load against up to four of the lane's own)
-//                               with their probabilities, and counts those before every 128 columns of the vocabulary.  14 us
+//                               with their probabilities and a tail's remainder, and counts those before every 128 columns of the vocabulary.  14 us
 //                               between events, of 256 entries a token 38 (one comparison a load, and the columns one search
 //                               after another 17 and 81): the instructions of both loops
 //           vocab_pair_kernel   <kLseTop>: logits tiles that stay in tensor memory; a row's entries are taken out of its
 //                               maximum and sum, which are then those of the other tokens.  214 to 225 us, 1710 to 1800 TFLOP/s,
-//                               tensor pipe 93 % active.  Every entry among a warp's 32 rows and 32 columns is a pass over the 32
+//                               tensor pipe busy 86 % of the time (93 % of its SMs' active cycles).  Every entry among a warp's 32 rows and 32 columns is a pass over the 32
 //                               (100 instructions): of narrow states, whose tiles' products are short, that shows (8192 tokens of
-//                               131072 x 256 with 48 entries 547 us, log-probabilities 462)
-//           teach_join_kernel   the parts of a row joined, divergence and p - q from them and the entries' logits.  10 us
+//                               131072 x 256 with 48 entries 545 us, log-probabilities 461)
+//           teach_join_kernel   the parts of a row joined, divergence and p - q from them and the entries' logits.  12 us
 // Gradient: outside the entries dz is g (p - q of all others together) times the softmax over the others, for either form of the
 //           loss; inside it is g (p - q).  So vocab_pair_kernel's dz of a token without a target, with the others' log-sum-exp,
-//           is right for all but the entries, which teach_entries_kernel writes over it, rounded once (5 us); then the products.
-//           The largest entry (teach_grad_kernel, 4 us) takes the place that a target has there: the tokens are in the
+//           is right for all but the entries, which teach_entries_kernel writes over it, rounded once (6 us); then the products.
+//           The largest entry (teach_grad_kernel, 6 us) takes the place that a target has there: the tokens are in the
 //           order of those, and what its rounding takes is added to both products.  That brings the gradients' error from 1.4
 //           times that of their own rounding to 1.0 to 1.2.
 // Keeping the entries out of the sum over the others keeps the digits of both: where the student is nearly certain of one
-// of the teacher's tokens, 1 - p is a sum of small terms here, and so is the others' share p_r.
+// of the teacher's tokens, 1 - p is a sum of small terms here, and so is the others' share p_r.  1 - q comes from the teacher's
+// log-probability by expm1, and of two numbers p - q or 1 - q less 1 - p is taken, whichever are smaller.
 #define GPO_REPORT __noinline__
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
