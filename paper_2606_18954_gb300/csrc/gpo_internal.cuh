@@ -149,13 +149,18 @@ __host__ __device__ __forceinline__ void next_tag(const Status& st) {
 __host__ __device__ __forceinline__ bool aborted(const Status& st) {
   return is_error(*reinterpret_cast<volatile const uint64_t*>(st.p + kStError), status_tag(st));
 }
-// Whether a wait of so long stops for an error of the call's.  Other blocks of a replay may wait before next_tag's store is seen,
-// while the error of an earlier replay, which the host has not looked for, still has the tag in force: they stop only after a
-// millisecond, when the store, one of the first block's first steps, has long been seen.
+// Where replays advance their tag (1 in the files of such calls that have waits): other blocks of a replay may wait before next_tag's
+// store is seen, while the error of an earlier replay, which the host has not looked for, still has the tag in force.  They heed an
+// error only after a millisecond, when the store, one of the first block's first steps, has long been seen.
+#ifndef GPO_TAG_ADVANCES
+#define GPO_TAG_ADVANCES 0
+#endif
 constexpr uint64_t kTagSeenNs = 1000000ull;
-__host__ __device__ __forceinline__ bool stops_waiting(const Status& st, uint64_t waited_ns) {
-  return (st.tag != kStoredTag || waited_ns > kTagSeenNs) && aborted(st);
+__host__ __device__ __forceinline__ bool tag_seen(const Status& st, uint64_t waited_ns) {
+  return st.tag != kStoredTag || waited_ns > kTagSeenNs;
 }
+// (elsewhere the tag does not change while a call runs, and the timer is not read for it)
+#define GPO_STOPS_WAITING(st, waited_ns) ((!GPO_TAG_ADVANCES || ::gpo::tag_seen(st, waited_ns)) && ::gpo::aborted(st))
 
 #ifndef GPO_REPORT
 #define GPO_REPORT __forceinline__
@@ -266,7 +271,7 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, const 
   for (uint32_t it = 1;; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((it & 255u) == 0u) {
-      if (honor_abort && stops_waiting(st, globaltimer_ns() - t0)) return false;
+      if (honor_abort && GPO_STOPS_WAITING(st, globaltimer_ns() - t0)) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         report(st, GPO_ERR_TIMEOUT, where, 0);
         return false;
@@ -302,7 +307,7 @@ __device__ __forceinline__ bool wait_flag(const int* flag, const Status& st, int
     __nanosleep(64);
     if (ld_acquire_gpu(flag)) return true;
     if ((it & 63u) == 0u) {
-      if (stops_waiting(st, globaltimer_ns() - t0)) return false;
+      if (GPO_STOPS_WAITING(st, globaltimer_ns() - t0)) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         report(st, GPO_ERR_TIMEOUT, where, 0);
         return false;

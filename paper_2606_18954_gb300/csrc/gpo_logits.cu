@@ -26,6 +26,7 @@
 // whose scattered reads come from HBM then, 290, 170, 97; every warp reading the row's arguments itself 190, 153, 49;
 // the bits spread by a product and byte permutations 188, 149, 48.
 #define GPO_REPORT __noinline__
+#define GPO_TAG_ADVANCES 1
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

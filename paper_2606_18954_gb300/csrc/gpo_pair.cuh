@@ -59,7 +59,7 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity
   for (uint32_t it = 1;; ++it) {
     if (mbar_try_wait_cluster(bar, parity)) return true;
     if ((it & 255u) == 0u) {
-      if (stops_waiting(st, globaltimer_ns() - t0)) return false;
+      if (GPO_STOPS_WAITING(st, globaltimer_ns() - t0)) return false;
       if (globaltimer_ns() - t0 > limit_ns) {
         report(st, GPO_ERR_TIMEOUT, where, 0);
         return false;

@@ -29,6 +29,7 @@
 // Keeping the sum over the other tokens of the vocabulary apart from the target's term keeps the
 // digits of a nearly certain token's log-probability -log(1 + sum), which is a small number.
 #define GPO_REPORT __noinline__
+#define GPO_TAG_ADVANCES 1
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

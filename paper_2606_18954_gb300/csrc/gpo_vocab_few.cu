@@ -13,6 +13,7 @@
 // Bound by HBM: one token, 131072 x 4096, 1.074 GB read in 178 us, 6.0 TB/s; below some 30 MB by the chain of launch,
 // first loads and join: 7 tokens, 1009 x 256, 10 us.
 #define GPO_REPORT __noinline__
+#define GPO_TAG_ADVANCES 1
 #include "gpo_vocab_math.cuh"
 
 namespace gpo {
