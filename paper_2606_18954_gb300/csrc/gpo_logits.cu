@@ -262,8 +262,8 @@ struct Shared {
 // Entries of which it is known at one time which are special, and special entries that are looked at in one round: as many as four
 // CTAs on an SM have memory for (57344 bytes each; a span's bitmaps and ranks take 9 bytes for 32 entries, a round's 8 for one).  The
 // history is read anew for every span and every round (us: log-probabilities of 4096 x 65536 with histories to 1824, to 8992, of
-// 1500 x 151936 to 9500, 256 x 151936 adjusted with histories to 16384):
-// 36864 and 3072 163, 200, 203, 99; 69632 and 768 146, 195, 187, 120; 69632 and 1536 146, 178, 181, 99; these 146, 179, 164, 83.
+// 1500 x 151936 to 9500, 256 x 151936 adjusted with histories to 16384): spans of 36864 with rounds twice as long 163, 200, 203, 99;
+// 69632 and 768 146, 195, 187, 120; 69632 and 1536 146, 178, 181, 99; these 146, 178, 164, 82.
 constexpr int kSpan = 81920;
 constexpr int kWords = kSpan / 32;
 constexpr int kGroups = kWords / 4;   // groups of four words, whose special entries are counted together
